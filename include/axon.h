@@ -294,6 +294,99 @@ int axon_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_tokens, c
                         const int32_t* h_cu_seqlens, const int32_t* d_targets, float* d_loss,
                         const axon_weight* grads, int32_t n_grads, void* stream);
 
+/* ---------------------------------------------------------------- row operators
+ *
+ * Operators on the caller's tensors, without a model: rows in device memory on the
+ * current device, ``ld`` elements apart (ld >= columns, of any alignment), AXON_F32
+ * or AXON_BF16 each.  bf16 values are rounded once, from float32 results; sums,
+ * statistics and gradients of parameters are float32 or wider.  They allocate
+ * nothing and synchronize nothing: work goes to ``stream``, scratch to a
+ * caller-owned device ``workspace`` (16-byte aligned) of at least the bytes that the
+ * matching _workspace call returns, which holds nothing from one call to the next;
+ * calls that may overlap in time (other streams, graphs replayed together) need a
+ * workspace each.  They enqueue kernels only, so a caller may capture them.  Two
+ * calls on the same inputs give the same bits.  Buffers do not overlap unless a call
+ * says so. */
+
+/* Layer norm of ``rows`` >= 0 rows of 1 <= cols <= 16384 columns, the normalization
+ * of the GPT-2 definition (Technical Supplement, "A Complete Model Definition"):
+ *   y = (x - mean) / sqrt(variance + eps) * gain + bias,
+ * mean and biased variance of the row; gain and bias [cols] of param_dtype, bias may
+ * be NULL (none).  y may be x (same dtype and stride). */
+int axon_layernorm(int64_t rows, int32_t cols, const void* x, int32_t x_dtype, int64_t ldx, const void* gain,
+                   const void* bias, int32_t param_dtype, float eps, void* y, int32_t y_dtype, int64_t ldy,
+                   void* stream);
+
+/* Its backward pass, from x and the gradient dy of y (the statistics are taken from
+ * x again): dx (of x_dtype) and, overwritten, dgain and dbias (float [cols], summed
+ * over the rows in a fixed order; zero for no rows; dbias may be NULL).  dx may be x
+ * or dy (same dtype and stride). */
+int64_t axon_layernorm_backward_workspace(int64_t rows, int32_t cols);
+int axon_layernorm_backward(int64_t rows, int32_t cols, const void* x, int32_t x_dtype, int64_t ldx, const void* dy,
+                            int32_t dy_dtype, int64_t lddy, const void* gain, int32_t param_dtype, float eps, void* dx,
+                            int64_t lddx, float* dgain, float* dbias, void* workspace, int64_t workspace_bytes,
+                            void* stream);
+
+/* The operators below take the logits of ``tokens`` positions [tokens][vocab] and
+ * d_targets, device int32 [tokens], the token that each position should predict.  A
+ * position counts when its target is in [0, vocab); any other value, e.g. -1, marks
+ * one that does not (a prompt, padding, a sequence's end): none of its other inputs
+ * is used, whatever they hold, its log-probability is 0 and its gradient row zeros.
+ * dlogits [tokens][vocab] (grad_dtype, rows ldg apart) is overwritten; it may be the
+ * logits' own buffer (same dtype and stride).  Columns from vocab to the stride are
+ * neither read nor written.  tokens and vocab up to 2^30.
+ * axon_token_loss_workspace: the bytes for a call over ``seqs`` sequences (0 for the
+ * two token_logprobs calls). */
+int64_t axon_token_loss_workspace(int64_t tokens, int32_t vocab, int32_t seqs);
+
+/* d_logps[t] = logits[t][target] - logsumexp(logits[t]) (float [tokens]). */
+int axon_token_logprobs(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
+                        const int32_t* d_targets, float* d_logps, void* workspace, int64_t workspace_bytes,
+                        void* stream);
+/* The gradient at the logits of sum_t d_dlogps[t] * logps[t], for a loss of the
+ * caller's own over the log-probabilities. */
+int axon_token_logprobs_backward(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
+                                 const int32_t* d_targets, const float* d_dlogps, void* dlogits, int32_t grad_dtype,
+                                 int64_t ldg, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Preference loss over ``pairs`` >= 1 pairs of sequences packed back to back, chosen
+ * then rejected: sequence 2 i and 2 i + 1 of cu_seqlens [2 pairs + 1] (0 .. tokens;
+ * sequences may be empty; h_cu_seqlens is the host copy of d_cu_seqlens).  With s_j
+ * the sum of sequence j's log-probabilities and ref_j the same under a reference
+ * model (d_ref_logps, float [2 pairs], or NULL: zeros),
+ *   margin_i = beta ((s_2i - ref_2i) - (s_2i+1 - ref_2i+1)),
+ *   loss = mean over i of -(1 - e) log sigmoid(margin_i) - e log sigmoid(-margin_i),
+ * beta > 0, e = label_smoothing in [0, 0.5).  Writes d_loss [1], d_seq_logps
+ * [2 pairs], d_margins [pairs] (float) and the loss's gradient (dlogits; NULL: not
+ * computed). */
+int axon_preference_loss(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
+                         const int32_t* d_targets, int32_t pairs, const int32_t* d_cu_seqlens,
+                         const int32_t* h_cu_seqlens, const float* d_ref_logps, float beta, float label_smoothing,
+                         float* d_loss, float* d_seq_logps, float* d_margins, void* dlogits, int32_t grad_dtype,
+                         int64_t ldg, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Clipped policy loss with a KL term.  Position t of log-probability l has the
+ * log-probability o = d_old_logps[t] under the policy that sampled it, an advantage
+ * A = d_advantages[t] and, unless d_ref_logps is NULL, r = d_ref_logps[t] under a
+ * reference model (float [tokens] each); with q = exp(l - o),
+ *   loss = sum_t w_t (-min(q A, clip(q, 1 - clip_low, 1 + clip_high) A)
+ *                     + kl_coef (exp(r - l) - (r - l) - 1)),
+ * w_t = 1 / N over the N counted positions, or (per_sequence == 1) the mean over the
+ * sequences with counted positions of each one's mean: 1 / (sequences n_seq).  The
+ * first term's gradient is zero where the clipped value is the smaller; a position
+ * with A == 0 has no first term.  clip_low in [0, 1], clip_high >= 0, kl_coef >= 0
+ * (0 without d_ref_logps).  cu_seqlens [batch + 1] as above.  Writes d_loss [1],
+ * d_stats [3] (the w-weighted means of the first term, of exp(r - l) - (r - l) - 1
+ * (0 without d_ref_logps) and of the clipped positions), d_logps [tokens] and the
+ * gradient (dlogits; NULL: not computed).  No counted position: loss, stats and
+ * gradient 0. */
+int axon_policy_loss(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
+                     const int32_t* d_targets, int32_t batch, const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens,
+                     const float* d_old_logps, const float* d_ref_logps, const float* d_advantages, float clip_low,
+                     float clip_high, float kl_coef, int32_t per_sequence, float* d_loss, float* d_stats,
+                     float* d_logps, void* dlogits, int32_t grad_dtype, int64_t ldg, void* workspace,
+                     int64_t workspace_bytes, void* stream);
+
 /* Current length of every slot (host copy kept by the library, no device
  * access).  Writes min(n, max_batch) entries to ``lens``; returns the number of
  * active slots (the batch of the last prefill), or a negative status. */

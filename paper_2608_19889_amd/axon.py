@@ -31,7 +31,10 @@ STATUS_NAMES = {0: "AXON_OK", -1: "AXON_E_INVALID", -2: "AXON_E_SHAPE", -3: "AXO
                 -4: "AXON_E_DTYPE", -5: "AXON_E_CAPACITY", -6: "AXON_E_OOM", -7: "AXON_E_HIP"}
 
 EXPORTED = ["axon_init_model", "axon_prefill", "axon_decode_step", "axon_decode_step_noalloc", "axon_step", "axon_reset_slot", "axon_loss_and_grads",
-            "axon_slot_lengths", "axon_timing_enable", "axon_timing_records", "axon_free", "axon_last_error"]
+            "axon_slot_lengths", "axon_timing_enable", "axon_timing_records", "axon_free", "axon_last_error",
+            "axon_layernorm", "axon_layernorm_backward", "axon_layernorm_backward_workspace",
+            "axon_token_loss_workspace", "axon_token_logprobs", "axon_token_logprobs_backward",
+            "axon_preference_loss", "axon_policy_loss"]
 
 # kernel classes of the timing records
 T_GEMV, T_GEMM, T_ATTN_DECODE, T_ATTN_PREFILL, T_GEMV_GROUPED, T_ATTN_BWD = 0, 1, 2, 3, 4, 5
@@ -110,6 +113,23 @@ def lib():
         L.axon_free.restype = None
         L.axon_last_error.argtypes = []
         L.axon_last_error.restype = ctypes.c_char_p
+        p, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        i32p = ctypes.POINTER(ctypes.c_int32)
+        logits = [i64, i32, p, i32, i64, p]                  # tokens, vocab, logits, dtype, ld, targets
+        grad, work = [p, i32, i64], [p, i64, p]              # dlogits, dtype, ld; workspace, its bytes, stream
+        for name, args, res in [
+                ("axon_layernorm", [i64, i32, p, i32, i64, p, p, i32, f32, p, i32, i64, p], ctypes.c_int),
+                ("axon_layernorm_backward_workspace", [i64, i32], i64),
+                ("axon_layernorm_backward", [i64, i32, p, i32, i64, p, i32, i64, p, i32, f32, p, i64, p, p, *work],
+                 ctypes.c_int),
+                ("axon_token_loss_workspace", [i64, i32, i32], i64),
+                ("axon_token_logprobs", [*logits, p, *work], ctypes.c_int),
+                ("axon_token_logprobs_backward", [*logits, p, *grad, *work], ctypes.c_int),
+                ("axon_preference_loss", [*logits, i32, p, i32p, p, f32, f32, p, p, p, *grad, *work], ctypes.c_int),
+                ("axon_policy_loss", [*logits, i32, p, i32p, p, p, p, f32, f32, f32, i32, p, p, p, *grad, *work],
+                 ctypes.c_int)]:
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = res
         _lib = L
     return _lib
 
@@ -173,6 +193,242 @@ def _stream(stream) -> int:
     if stream is None:
         return torch.cuda.current_stream().cuda_stream
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+# ---------------------------------------------------------------- row operators
+
+_CODES = {torch.bfloat16: AXON_BF16, torch.float32: AXON_F32}
+
+
+def _code(t: torch.Tensor, name: str) -> int:
+    code = _CODES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    return code
+
+
+class _On:
+    """Makes a tensor's device and the given stream (None: the device's current
+    one) current for a call: what the call allocates belongs to that stream.  Inputs
+    made on another stream must be ready on this one; they are kept from reuse
+    until its work is done."""
+
+    def __init__(self, x: torch.Tensor, stream, *tensors):
+        if not x.is_cuda:
+            raise ValueError("the row operators take tensors on the GPU")
+        for t in tensors:
+            if t is not None and t.device != x.device:
+                raise ValueError(f"tensors on {x.device} and {t.device} in one call")
+        self.x, self.stream, self.tensors = x, stream, tensors
+
+    def __enter__(self):
+        self.device = torch.cuda.device(self.x.device)
+        self.device.__enter__()
+        if self.stream is None:
+            self.scope = None
+            return torch.cuda.current_stream().cuda_stream
+        st = self.stream if hasattr(self.stream, "cuda_stream") else torch.cuda.ExternalStream(int(self.stream))
+        for t in (self.x, *self.tensors):
+            if t is not None:
+                t.record_stream(st)
+        self.scope = torch.cuda.stream(st)
+        self.scope.__enter__()
+        return st.cuda_stream
+
+    def __exit__(self, *e):
+        if self.scope is not None:
+            self.scope.__exit__(*e)
+        self.device.__exit__(*e)
+
+
+def _rows(t: torch.Tensor, name: str, out: bool = False):
+    """(the tensor, rows, columns, row stride) of a tensor whose last dimension is
+    its columns.  An input of another layout is copied; an output is refused."""
+    if t.dim() == 0:
+        raise ValueError(f"{name} has no columns")
+    v = t
+    if t.dim() != 2:
+        try:
+            v = t.view(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
+        except RuntimeError:
+            v = None
+    if v is None or (v.shape[1] > 1 and v.stride(1) != 1) or (v.shape[0] > 1 and v.stride(0) < v.shape[1]):
+        if out:
+            raise ValueError(f"{name} must have contiguous columns and rows that do not overlap")
+        v = t.contiguous().view(-1, t.shape[-1])
+    return v, v.shape[0], v.shape[1], v.stride(0) if v.shape[0] > 1 else max(v.shape[1], 1)
+
+
+def _vector(t, n: int, dtype, name: str):
+    """``t`` as n contiguous values of ``dtype`` (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} {dtype} values, got {t.numel()} {t.dtype}")
+    return t.contiguous()
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _like(out, x: torch.Tensor, dtype, name: str) -> torch.Tensor:
+    """The caller's output buffer, or a new one of x's shape."""
+    if out is None:
+        return torch.empty(x.shape, dtype=dtype, device=x.device)
+    if out.shape != x.shape or (dtype is not None and out.dtype != dtype):
+        raise ValueError(f"{name} must be {tuple(x.shape)} {dtype}, got {tuple(out.shape)} {out.dtype}")
+    return out
+
+
+def layernorm(x: torch.Tensor, gain: torch.Tensor, bias: torch.Tensor | None = None, eps: float = 1e-5,
+              dtype: torch.dtype | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Layer norm over the last dimension of ``x`` (axon_layernorm), in ``dtype``
+    (x's by default; ``out`` may be x)."""
+    with _On(x, stream, gain, bias, out) as s:
+        y = _like(out, x, dtype if dtype is not None or out is not None else x.dtype, "out")
+        xv, rows, cols, ldx = _rows(x, "x")
+        yv, _, _, ldy = _rows(y, "out", out=True)
+        gain = _vector(gain, cols, gain.dtype, "gain")
+        bias = _vector(bias, cols, gain.dtype, "bias")
+        _check(lib().axon_layernorm(rows, cols, xv.data_ptr(), _code(x, "x"), ldx, gain.data_ptr(), _ptr(bias),
+                                    _code(gain, "gain"), eps, yv.data_ptr(), _code(y, "out"), ldy, s))
+        return y
+
+
+def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-5,
+                       dx: torch.Tensor | None = None, stream=None):
+    """(dx, dgain, dbias) of :func:`layernorm` from the gradient ``dy`` of its
+    output (axon_layernorm_backward): dx in x's dtype (``dx`` may be x or dy), dgain
+    and dbias float32."""
+    if dy.shape != x.shape:
+        raise ValueError(f"dy has shape {tuple(dy.shape)}, x {tuple(x.shape)}")
+    with _On(x, stream, dy, gain, dx) as s:
+        dx = _like(dx, x, x.dtype, "dx")
+        xv, rows, cols, ldx = _rows(x, "x")
+        dv, _, _, lddy = _rows(dy, "dy")
+        ov, _, _, lddx = _rows(dx, "dx", out=True)
+        gain = _vector(gain, cols, gain.dtype, "gain")
+        par = torch.empty((2, cols), dtype=torch.float32, device=x.device)
+        need = lib().axon_layernorm_backward_workspace(rows, cols)
+        ws = torch.empty((need,), dtype=torch.uint8, device=x.device)
+        at = par.data_ptr()
+        _check(lib().axon_layernorm_backward(rows, cols, xv.data_ptr(), _code(x, "x"), ldx, dv.data_ptr(),
+                                             _code(dy, "dy"), lddy, gain.data_ptr(), _code(gain, "gain"), eps,
+                                             ov.data_ptr(), lddx, at, at + 4 * cols, ws.data_ptr(), need, s))
+        return dx, par[0], par[1]
+
+
+def _logit_args(logits, targets):
+    z, tokens, vocab, ld = _rows(logits, "logits")
+    tg = _vector(targets, tokens, torch.int32, "targets")
+    return z, tg, (tokens, vocab, z.data_ptr(), _code(logits, "logits"), ld, tg.data_ptr())
+
+
+def _loss_workspace(tokens, vocab, seqs, device):
+    need = lib().axon_token_loss_workspace(tokens, vocab, seqs)
+    return torch.empty((need,), dtype=torch.uint8, device=device), need
+
+
+def _grad_args(dlogits, logits):
+    if dlogits is None:
+        return None, (None, AXON_F32, 0)
+    v, _, _, ld = _rows(dlogits, "dlogits", out=True)
+    return v, (v.data_ptr(), _code(dlogits, "dlogits"), ld)
+
+
+def _cu_args(cu_seqlens, cu_device, device):
+    n = len(cu_seqlens)
+    host = (ctypes.c_int32 * max(n, 1))(*cu_seqlens)
+    if cu_device is None:
+        return host, torch.tensor(cu_seqlens, dtype=torch.int32, device=device)
+    if cu_device.dtype != torch.int32 or cu_device.numel() < n or not cu_device.is_contiguous():
+        raise ValueError(f"cu_device must hold the {n} int32 values of cu_seqlens")
+    return host, cu_device
+
+
+def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, stream=None) -> torch.Tensor:
+    """log softmax(logits[t])[targets[t]] (axon_token_logprobs): logits [tokens,
+    vocab] float32 or bfloat16, targets int32 [tokens] (a value outside [0, vocab)
+    does not count and gives 0).  Returns float32 [tokens]."""
+    with _On(logits, stream, targets) as s:
+        z, tg, args = _logit_args(logits, targets)
+        out = torch.empty((args[0],), dtype=torch.float32, device=z.device)
+        ws, need = _loss_workspace(args[0], args[1], 0, z.device)
+        _check(lib().axon_token_logprobs(*args, out.data_ptr(), ws.data_ptr(), need, s))
+        return out
+
+
+def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, dlogps: torch.Tensor,
+                            dlogits: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The gradient at the logits of a loss whose gradient at
+    :func:`token_logprobs` is ``dlogps`` (float32 [tokens]).  ``dlogits``: a buffer
+    for it, of either dtype (the logits' own is allowed); by default a new one of the
+    logits' dtype."""
+    with _On(logits, stream, targets, dlogps, dlogits) as s:
+        z, tg, args = _logit_args(logits, targets)
+        dlogps = _vector(dlogps, args[0], torch.float32, "dlogps")
+        dlogits = _like(dlogits, logits, logits.dtype if dlogits is None else dlogits.dtype, "dlogits")
+        g, gargs = _grad_args(dlogits, logits)
+        ws, need = _loss_workspace(args[0], args[1], 0, z.device)
+        _check(lib().axon_token_logprobs_backward(*args, dlogps.data_ptr(), *gargs, ws.data_ptr(), need, s))
+        return dlogits
+
+
+def preference_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: list,
+                    ref_logps: torch.Tensor | None = None, beta: float = 0.1, label_smoothing: float = 0.0,
+                    dlogits: torch.Tensor | None = None, want_grad: bool = True,
+                    cu_device: torch.Tensor | None = None, stream=None):
+    """Preference loss over pairs of sequences packed back to back, chosen then
+    rejected (axon_preference_loss): cu_seqlens a host list of 2 pairs + 1 prefix sums
+    (cu_device: the same in a device int32 buffer, which saves its copy), ref_logps
+    float32 [2 pairs], each sequence's log-probability under the reference model
+    (None: zeros).  Returns (loss [1], seq_logps [2 pairs], margins [pairs],
+    dlogits or None); ``dlogits`` as in :func:`token_logprobs_backward`."""
+    pairs = (len(cu_seqlens) - 1) // 2
+    if len(cu_seqlens) != 2 * pairs + 1 or pairs < 1:
+        raise ValueError("cu_seqlens must have an odd number of entries, at least 3: sequences come in pairs")
+    with _On(logits, stream, targets, ref_logps, dlogits, cu_device) as s:
+        z, tg, args = _logit_args(logits, targets)
+        ref_logps = _vector(ref_logps, 2 * pairs, torch.float32, "ref_logps")
+        if want_grad:
+            dlogits = _like(dlogits, logits, logits.dtype if dlogits is None else dlogits.dtype, "dlogits")
+        g, gargs = _grad_args(dlogits if want_grad else None, logits)
+        host, cu = _cu_args(cu_seqlens, cu_device, z.device)
+        out = torch.empty((1 + 3 * pairs,), dtype=torch.float32, device=z.device)
+        at = out.data_ptr()
+        ws, need = _loss_workspace(args[0], args[1], 2 * pairs, z.device)
+        _check(lib().axon_preference_loss(*args, pairs, cu.data_ptr(), host, _ptr(ref_logps), beta, label_smoothing,
+                                          at, at + 4, at + 4 + 8 * pairs, *gargs, ws.data_ptr(), need, s))
+        return out[:1], out[1:1 + 2 * pairs], out[1 + 2 * pairs:], dlogits if want_grad else None
+
+
+def policy_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: list, old_logps: torch.Tensor,
+                advantages: torch.Tensor, ref_logps: torch.Tensor | None = None, clip_low: float = 0.2,
+                clip_high: float = 0.2, kl_coef: float = 0.0, per_sequence: bool = False,
+                dlogits: torch.Tensor | None = None, want_grad: bool = True,
+                cu_device: torch.Tensor | None = None, stream=None):
+    """Clipped policy loss with a KL term (axon_policy_loss): old_logps, advantages
+    and ref_logps (None: no KL term) float32 [tokens]; averaged over the counted
+    tokens, or over each sequence's and then the sequences (per_sequence).  Returns
+    (loss [1], stats [3], logps [tokens], dlogits or None)."""
+    with _On(logits, stream, targets, old_logps, advantages, ref_logps, dlogits, cu_device) as s:
+        z, tg, args = _logit_args(logits, targets)
+        old_logps = _vector(old_logps, args[0], torch.float32, "old_logps")
+        advantages = _vector(advantages, args[0], torch.float32, "advantages")
+        ref_logps = _vector(ref_logps, args[0], torch.float32, "ref_logps")
+        if want_grad:
+            dlogits = _like(dlogits, logits, logits.dtype if dlogits is None else dlogits.dtype, "dlogits")
+        g, gargs = _grad_args(dlogits if want_grad else None, logits)
+        host, cu = _cu_args(cu_seqlens, cu_device, z.device)
+        batch = len(cu_seqlens) - 1
+        out = torch.empty((4 + args[0],), dtype=torch.float32, device=z.device)
+        at = out.data_ptr()
+        ws, need = _loss_workspace(args[0], args[1], batch, z.device)
+        _check(lib().axon_policy_loss(*args, batch, cu.data_ptr(), host, old_logps.data_ptr(), _ptr(ref_logps),
+                                      advantages.data_ptr(), clip_low, clip_high, kl_coef, int(per_sequence), at,
+                                      at + 4, at + 16, *gargs, ws.data_ptr(), need, s))
+        return out[:1], out[1:4], out[4:], dlogits if want_grad else None
 
 
 class Model:

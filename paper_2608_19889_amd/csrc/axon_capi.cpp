@@ -19,6 +19,7 @@
 #include <vector>
 
 #include "axon.h"
+#include "capi.h"
 #include "kernels.h"
 
 using namespace axon;
@@ -35,6 +36,23 @@ static __device__ __align__(256) unsigned char scratch[AXON_NOALLOC_SCRATCH_BYTE
 namespace {
 
 thread_local std::string g_err;
+
+}  // namespace
+
+int axon::fail(int code, const std::string& msg) {
+  g_err = msg;
+  return code;
+}
+
+void axon::clear_error() { g_err.clear(); }
+
+int axon::check_launch(const char* what) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return fail(AXON_E_HIP, std::string(what) + ": kernel launch failed: " + hipGetErrorString(e));
+  return AXON_OK;
+}
+
+namespace {
 
 // device id -> address of that device's ``scratch`` (or the lookup's error)
 std::mutex g_scratch_mu;
@@ -79,11 +97,6 @@ hipError_t init_current_device() {
   e = gemm_init_device();
   if (e == hipSuccess) g_limits_devices.insert(dev);
   return e;
-}
-
-int fail(int code, const std::string& msg) {
-  g_err = msg;
-  return code;
 }
 
 #define HIP_TRY(expr)                                                                      \
@@ -1117,12 +1130,6 @@ void enqueue_decode(axon_model* m, int B, const int32_t* d_tokens, float* d_logi
   else if (m->bf) enqueue_decode_many<bf16>(m, B, d_tokens, d_logits, d_next, s);
   else if (B <= GEMV_F32_MAX_M) enqueue_decode_f32(m, B, d_tokens, d_logits, d_next, s);
   else enqueue_decode_many<float>(m, B, d_tokens, d_logits, d_next, s);
-}
-
-int check_launch(const char* what) {
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return fail(AXON_E_HIP, std::string(what) + ": kernel launch failed: " + hipGetErrorString(e));
-  return AXON_OK;
 }
 
 // A projection shape without a kernel (never produced by a validated model):

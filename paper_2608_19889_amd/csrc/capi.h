@@ -1,0 +1,30 @@
+// What the source files of the C ABI share.
+#pragma once
+#include <exception>
+#include <new>
+#include <string>
+
+#include "axon.h"
+
+namespace axon {
+
+// sets the calling thread's axon_last_error() and returns ``code``
+int fail(int code, const std::string& msg);
+void clear_error();
+// AXON_OK, or the last launch's error
+int check_launch(const char* what);
+
+// runs an entry point's body; no exception leaves it
+template <typename F>
+int entry(F&& body) {
+  try {
+    clear_error();
+    return body();
+  } catch (const std::bad_alloc&) {
+    return AXON_E_OOM;
+  } catch (const std::exception&) {
+    return AXON_E_INVALID;
+  }
+}
+
+}  // namespace axon

@@ -112,6 +112,58 @@ AXON_DEV bf16x8 read_tr8(const bf16* lo_p, const bf16* hi_p) {
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// Eight consecutive elements c .. c + 7 of a row of n, as float32; past the row's
+// end ``fill`` (read), or nothing (written).  The row may start at any element: the
+// wide accesses ask for no more than the element's own alignment, which global
+// memory instructions allow.
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
+AXON_DEV void load_run8(const float* row, int c, int n, float (&v)[8], float fill) {
+  if (c + 8 <= n) {
+    const f32x4 a = *(const f32x4_any*)(row + c), b = *(const f32x4_any*)(row + c + 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      v[j] = a[j];
+      v[4 + j] = b[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? row[c + j] : fill;
+  }
+}
+AXON_DEV void load_run8(const bf16* row, int c, int n, float (&v)[8], float fill) {
+  if (c + 8 <= n) {
+    const bf16x8 a = *(const bf16x8_any*)(row + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = (float)a[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? (float)row[c + j] : fill;
+  }
+}
+AXON_DEV void store_run8(float* row, int c, int n, const float (&v)[8]) {
+  if (c + 8 <= n) {
+    *(f32x4_any*)(row + c) = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4_any*)(row + c + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < n) row[c + j] = v[j];
+  }
+}
+AXON_DEV void store_run8(bf16* row, int c, int n, const float (&v)[8]) {
+  if (c + 8 <= n) {
+    bf16x8 o;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = (bf16)v[j];
+    *(bf16x8_any*)(row + c) = o;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < n) row[c + j] = (bf16)v[j];
+  }
+}
+
 // Block-wide sum for blockDim.x a multiple of 64 (<= 1024); every thread gets the result.
 AXON_DEV float block_sum(float v, float* red /* >= 16 floats of shared memory */) {
   v = wave_sum(v);

@@ -108,14 +108,61 @@ constexpr int LSE_COLS = 64;
 // [P][D]); h[t] = LayerNorm(x[t]) * g + beta (bf16)
 void launch_embed_pos_ln(const int32_t* tok, const bf16* wte, const bf16* wpe, const bf16* g, const bf16* beta,
                          float* x, bf16* h, int T, int D, int V, int P, float eps, const int32_t* cu, int nseq,
-                         const int32_t* ent_base, const int32_t* len, hipStream_t s);
+                         const int32_t* ent_base, const int32_t* len, hipStream_t s, bool h_pair = false);
 // h[i] = LayerNorm(x[r]) * g + beta with r = i, or r = cu_last[i+1]-1 (the
 // last position of sequence i) when cu_last is set
 void launch_layernorm(const float* x, const bf16* g, const bf16* beta, bf16* h, int rows, int D, float eps,
-                      const int32_t* cu_last, hipStream_t s);
+                      const int32_t* cu_last, hipStream_t s, bool h_pair = false);
+// Rows of a caller (strides ldx, ldy in elements, 1 <= cols <= LN_MAX_COLS): y =
+// LayerNorm(x) * g + b (b may be null), and its backward: dx, dg = sum over the rows
+// of dy xhat and db = sum dy (float [cols]; db may be null).  part:
+// ln_bwd_part_floats floats of scratch.  y may be x; dx may be x or dy.
+constexpr int LN_MAX_COLS = 16384;
+int64_t ln_bwd_part_floats(int64_t rows, int cols);
+template <typename TX, typename TY, typename TP>
+void launch_ln_fwd(const TX* x, int64_t ldx, const TP* g, const TP* b, float eps, TY* y, int64_t ldy, int64_t rows,
+                   int cols, hipStream_t s);
+template <typename TX, typename TD, typename TP>
+void launch_ln_bwd(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const TP* g, float eps, TX* dx, int64_t lddx,
+                   float* dg, float* db, float* part, int64_t rows, int cols, hipStream_t s);
 // dst[r][k] = src[k][perm ? perm[r] : r] (bf16): a [K][N] matrix stored
 // [in][out] transposed to [N][K], rows optionally permuted
 void launch_transpose_rows(const bf16* src, bf16* dst, int K, int N, const int32_t* perm, hipStream_t s);
+
+// ---- losses over the log-probabilities of given tokens (k_loss.hip)
+// The rows: logits z [tokens][V], rows ld elements apart, target targets[t] of row t
+// (counted when in [0, V)); dz the gradient's rows (null: none), z itself or apart from
+// it; float or bf16 each.
+struct LogitRows {
+  const void* z;
+  int z_bf16;
+  int64_t ld;
+  int64_t tokens;
+  int V;
+  const int32_t* targets;
+  void* dz;
+  int dz_bf16;
+  int64_t lddz;
+};
+struct PreferenceArgs {
+  const int32_t* cu;  // [seqs + 1]
+  int seqs;           // even
+  const float* ref;   // [seqs] or null
+  float beta, smoothing;
+  float *loss, *seq_logps, *margins;  // [1], [seqs], [seqs / 2]
+};
+struct PolicyArgs {
+  const int32_t* cu;  // [seqs + 1]: a mean per sequence first; null: over all tokens
+  int seqs;
+  const float *old, *ref, *adv;  // [tokens]; ref may be null
+  float lo, hi, kl_coef;
+  float *loss, *stats, *logps;   // [1], [3], [tokens]
+};
+size_t loss_workspace_bytes(int64_t tokens, int V, int64_t seqs);
+void launch_token_logps(const LogitRows& r, float* logps, void* ws, hipStream_t s);
+void launch_token_logps_bwd(const LogitRows& r, const float* dlogps, void* ws, hipStream_t s);
+void launch_preference_loss(const LogitRows& r, const PreferenceArgs& a, void* ws, hipStream_t s);
+void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipStream_t s);
 
 // ---- backward pass (k_train.hip)
 // loss over logits [T][ldl] (V real columns, ldl % 32 == 0) and targets
@@ -134,6 +181,10 @@ void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t
 constexpr int ROW_PARTS = 512, NORM_BWD_COLS = 8192;
 void launch_norm_bwd(const float* x, const bf16* g, const float* dy, int np, int64_t stride, int T, int D, float eps,
                      float* dx, int accumulate, bf16* dxb, float* dg, float* part, float* dgrow, hipStream_t s);
+// d0 / d1 / d2 = the column sums of part [n][C], n >= 1, in a fixed order: columns
+// below c1 go to d0, below c2 to d1, the rest to d2 (a null one is not written)
+void launch_colsum_final(const float* part, int n, int C, float* d0, int c1, float* d1, int c2, float* d2,
+                         hipStream_t s);
 // attention backward over nseq fresh sequences in slots 0.. (contiguous cache):
 // dq [T][H][hd] and each query head's share of dk / dv, dkh / dvh [T][H][hd]
 // (float), from q [T][H][hd] and o (row-pair layout) bf16, the gradient of o as
