@@ -348,7 +348,7 @@ def _cu_args(cu_seqlens, cu_device, device):
 
 
 def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, stream=None) -> torch.Tensor:
-    """log softmax(logits[t])[targets[t]] (axon_token_logprobs): logits [tokens,
+    """logits[t][targets[t]] - logsumexp(logits[t]) (axon_token_logprobs): logits [tokens,
     vocab] float32 or bfloat16, targets int32 [tokens] (a value outside [0, vocab)
     does not count and gives 0).  Returns float32 [tokens]."""
     with _On(logits, stream, targets) as s:
