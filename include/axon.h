@@ -283,16 +283,33 @@ int axon_reset_slot(axon_model* m, int32_t slot);
  *              owned by the caller and overwritten with the gradients.
  * Activations and gradients are stored in bf16 between the kernels, with
  * float32 accumulation, the residual stream and its gradient in float32.
- * Dense Llama-family models only (AXON_ARCH_LLAMA, AXON_BF16, n_experts 0,
- * sliding_window 0, contiguous cache).  The first call allocates a
+ * Dense models of either family (AXON_BF16, n_experts 0, sliding_window 0,
+ * contiguous cache); GPT-2's tied wte gradient has both its uses, the wpe rows that no
+ * sequence reaches are 0.  The first call allocates a
  * transposed copy of the weights and, for max_tokens positions, the saved
  * activations (per token and layer 12 hidden + 4 heads * head_dim + 10
- * intermediate + 4 heads bytes) and the gradient work buffers (including
+ * intermediate (GPT-2: 6) + 4 heads bytes) and the gradient work buffers (including
  * float32 and bf16 logits, 6 vocab bytes per token).  Returns AXON_OK, AXON_E_INVALID, AXON_E_CAPACITY, AXON_E_MISSING /
  * AXON_E_SHAPE / AXON_E_DTYPE (gradient map), AXON_E_OOM or AXON_E_HIP. */
 int axon_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_tokens, const int32_t* d_cu_seqlens,
                         const int32_t* h_cu_seqlens, const int32_t* d_targets, float* d_loss,
                         const axon_weight* grads, int32_t n_grads, void* stream);
+
+/* The same step (arguments, models, gradients, slots and errors as
+ * axon_loss_and_grads) with the losses of post-training in place of the mean
+ * cross-entropy; the losses and their arguments are those of axon_preference_loss
+ * and axon_policy_loss below, over the model's logits at the packed positions.
+ * Preference: 2 pairs sequences, chosen then rejected (2 pairs <= max_batch). */
+int axon_preference_loss_and_grads(axon_model* m, int32_t pairs, const int32_t* d_tokens,
+                                   const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens, const int32_t* d_targets,
+                                   const float* d_ref_logps, float beta, float label_smoothing, float* d_loss,
+                                   float* d_seq_logps, float* d_margins, const axon_weight* grads, int32_t n_grads,
+                                   void* stream);
+int axon_policy_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_tokens, const int32_t* d_cu_seqlens,
+                               const int32_t* h_cu_seqlens, const int32_t* d_targets, const float* d_old_logps,
+                               const float* d_ref_logps, const float* d_advantages, float clip_low, float clip_high,
+                               float kl_coef, int32_t per_sequence, float* d_loss, float* d_stats, float* d_logps,
+                               const axon_weight* grads, int32_t n_grads, void* stream);
 
 /* ---------------------------------------------------------------- row operators
  *

@@ -34,7 +34,8 @@ EXPORTED = ["axon_init_model", "axon_prefill", "axon_decode_step", "axon_decode_
             "axon_slot_lengths", "axon_timing_enable", "axon_timing_records", "axon_free", "axon_last_error",
             "axon_layernorm", "axon_layernorm_backward", "axon_layernorm_backward_workspace",
             "axon_token_loss_workspace", "axon_token_logprobs", "axon_token_logprobs_backward",
-            "axon_preference_loss", "axon_policy_loss"]
+            "axon_preference_loss", "axon_policy_loss", "axon_preference_loss_and_grads",
+            "axon_policy_loss_and_grads"]
 
 # kernel classes of the timing records
 T_GEMV, T_GEMM, T_ATTN_DECODE, T_ATTN_PREFILL, T_GEMV_GROUPED, T_ATTN_BWD = 0, 1, 2, 3, 4, 5
@@ -117,7 +118,11 @@ def lib():
         i32p = ctypes.POINTER(ctypes.c_int32)
         logits = [i64, i32, p, i32, i64, p]                  # tokens, vocab, logits, dtype, ld, targets
         grad, work = [p, i32, i64], [p, i64, p]              # dlogits, dtype, ld; workspace, its bytes, stream
+        step = [p, i32, p, p, i32p, p]                       # model, batch, tokens, cu_seqlens (both), targets
+        grads = [ctypes.POINTER(AxonWeight), i32, p]
         for name, args, res in [
+                ("axon_preference_loss_and_grads", [*step, p, f32, f32, p, p, p, *grads], ctypes.c_int),
+                ("axon_policy_loss_and_grads", [*step, p, p, p, f32, f32, f32, i32, p, p, p, *grads], ctypes.c_int),
                 ("axon_layernorm", [i64, i32, p, i32, i64, p, p, i32, f32, p, i32, i64, p], ctypes.c_int),
                 ("axon_layernorm_backward_workspace", [i64, i32], i64),
                 ("axon_layernorm_backward", [i64, i32, p, i32, i64, p, i32, i64, p, i32, f32, p, i64, p, p, *work],
@@ -492,6 +497,54 @@ class Model:
                                          loss.data_ptr(), arr, len(grads), ctypes.c_void_p(_stream(stream))))
         self._keep = (cu_d, tokens, targets, keep)
         return loss
+
+    def _train_args(self, tokens, cu_seqlens, targets, grads):
+        B = len(cu_seqlens) - 1
+        cu_h = (ctypes.c_int32 * (B + 1))(*[int(c) for c in cu_seqlens])
+        cu_d = torch.tensor([int(c) for c in cu_seqlens], dtype=torch.int32, device=tokens.device)
+        arr, keep = make_weights(grads)
+        return B, cu_h, cu_d, arr, keep
+
+    def preference_loss_and_grads(self, tokens: torch.Tensor, cu_seqlens: list, targets: torch.Tensor, grads: dict,
+                                  ref_logps: torch.Tensor | None = None, beta: float = 0.1,
+                                  label_smoothing: float = 0.0, stream=None):
+        """A training step with the preference loss (axon_preference_loss_and_grads):
+        pairs of sequences, chosen then rejected; tokens, targets and grads as in
+        :meth:`loss_and_grads`, the loss as :func:`preference_loss`.  Returns (loss [1],
+        seq_logps [2 pairs], margins [pairs])."""
+        B, cu_h, cu_d, arr, keep = self._train_args(tokens, cu_seqlens, targets, grads)
+        if B < 2 or B % 2:
+            raise ValueError("sequences come in pairs, chosen then rejected")
+        ref_logps = _vector(ref_logps, B, torch.float32, "ref_logps")
+        out = torch.empty((1 + B + B // 2,), dtype=torch.float32, device=tokens.device)
+        at = out.data_ptr()
+        _check(lib().axon_preference_loss_and_grads(self._h, B // 2, tokens.data_ptr(), cu_d.data_ptr(), cu_h,
+                                                    targets.data_ptr(), _ptr(ref_logps), beta, label_smoothing, at,
+                                                    at + 4, at + 4 + 4 * B, arr, len(grads),
+                                                    ctypes.c_void_p(_stream(stream))))
+        self._keep = (cu_d, tokens, targets, keep, ref_logps)
+        return out[:1], out[1:1 + B], out[1 + B:]
+
+    def policy_loss_and_grads(self, tokens: torch.Tensor, cu_seqlens: list, targets: torch.Tensor, grads: dict,
+                              old_logps: torch.Tensor, advantages: torch.Tensor,
+                              ref_logps: torch.Tensor | None = None, clip_low: float = 0.2, clip_high: float = 0.2,
+                              kl_coef: float = 0.0, per_sequence: bool = False, stream=None):
+        """A training step with the clipped policy loss (axon_policy_loss_and_grads):
+        tokens, targets and grads as in :meth:`loss_and_grads`, the loss as
+        :func:`policy_loss`.  Returns (loss [1], stats [3], logps [tokens])."""
+        B, cu_h, cu_d, arr, keep = self._train_args(tokens, cu_seqlens, targets, grads)
+        T = int(cu_seqlens[-1])
+        old_logps, advantages, ref_logps = (_vector(t, T, torch.float32, n) for t, n in (
+            (old_logps, "old_logps"), (advantages, "advantages"), (ref_logps, "ref_logps")))
+        out = torch.empty((4 + T,), dtype=torch.float32, device=tokens.device)
+        at = out.data_ptr()
+        _check(lib().axon_policy_loss_and_grads(self._h, B, tokens.data_ptr(), cu_d.data_ptr(), cu_h,
+                                                targets.data_ptr(), old_logps.data_ptr(), _ptr(ref_logps),
+                                                advantages.data_ptr(), clip_low, clip_high, kl_coef,
+                                                int(per_sequence), at, at + 4, at + 16, arr, len(grads),
+                                                ctypes.c_void_p(_stream(stream))))
+        self._keep = (cu_d, tokens, targets, keep, old_logps, advantages, ref_logps)
+        return out[:1], out[1:4], out[4:]
 
     def decode_step(self, tokens: torch.Tensor, logits: torch.Tensor | None = None,
                     next_tokens: torch.Tensor | None = None, stream=None):

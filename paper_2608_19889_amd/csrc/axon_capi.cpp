@@ -271,7 +271,9 @@ struct GraphKey {
 // activations the forward pass keeps per layer, the weights transposed and
 // tiled (the B operand of dX = dY W), and the gradient work buffers.
 struct TrainLayer {
-  float *xin, *xmid, *lse, *gu;  // layer input, residual after attention, log2-sum-exp [T][H], gate/up [T][2I]
+  // layer input, residual after attention, log2-sum-exp [T][H], gate/up [T][2I] (GPT-2:
+  // the MLP's pre-activation [T][I])
+  float *xin, *xmid, *lse, *gu;
   bf16 *h1, *h2, *q, *o, *a;     // normed inputs, rotated q, attention output, gated activation
   bf16 *wqkvT, *woT, *wguT, *wdT;
 };
@@ -283,6 +285,19 @@ struct TrainBufs {
       *dkh, *dvh;
   float2* lsep;     // log-sum-exp partials of the logits rows (EPI_LSE)
   bf16 *hf, *dlog, *dxb, *dgu, *dob, *dqkv, *headT;
+  // preference and policy losses: softmax statistics, dloss / dlp and lp of every
+  // token, one value per sequence
+  float2* stat;
+  float* coef;
+  double *lps, *seq;
+};
+
+// The loss of a training step
+struct TrainLoss {
+  enum Kind { CROSS_ENTROPY, PREFERENCE, POLICY } kind = CROSS_ENTROPY;
+  float* loss = nullptr;
+  PreferenceArgs pref{};
+  PolicyArgs pol{};
 };
 
 // Per-step work buffers of the bf16 decode step: the model's own (allocated
@@ -1929,6 +1944,8 @@ int train_setup(axon_model* m, hipStream_t s) {
   const axon_config& c = m->cfg;
   const int64_t D = c.hidden, H = c.n_heads, KV = c.n_kv_heads, hd = c.head_dim, I = c.intermediate, V = c.vocab;
   const int64_t nq = (H + 2 * KV) * hd, Hhd = H * hd;
+  const bool gpt2 = m->gpt2();
+  const int64_t Iw = gpt2 ? I : 2 * I;  // features of the first MLP projection
   tb.Tc = m->rows;
   tb.Vp = (int)((V + 31) / 32 * 32);
   const int64_t T = tb.Tc, Vp = tb.Vp, T2 = (T + 1) & ~(int64_t)1;  // T2: rows of the row-pair layout
@@ -1941,7 +1958,7 @@ int train_setup(axon_model* m, hipStream_t s) {
     if (!r) r = fa(&l.xin, T * D);
     if (!r) r = fa(&l.xmid, T * D);
     if (!r) r = fa(&l.lse, T * H);
-    if (!r) r = fa(&l.gu, T * 2 * I);
+    if (!r) r = fa(&l.gu, T * Iw);
     if (!r) r = ba(&l.h1, T2 * D);
     if (!r) r = ba(&l.h2, T2 * D);
     if (!r) r = ba(&l.q, T * Hhd);
@@ -1949,7 +1966,7 @@ int train_setup(axon_model* m, hipStream_t s) {
     if (!r) r = ba(&l.a, T2 * I);
     if (!r) r = ba(&l.wqkvT, tiled(D, nq));
     if (!r) r = ba(&l.woT, tiled(Hhd, D));
-    if (!r) r = ba(&l.wguT, tiled(D, 2 * I));
+    if (!r) r = ba(&l.wguT, tiled(D, Iw));
     if (!r) r = ba(&l.wdT, tiled(I, D));
   }
   if (!r) r = fa(&tb.xfin, T * D);
@@ -1960,17 +1977,21 @@ int train_setup(axon_model* m, hipStream_t s) {
   if (!r) r = fa(&tb.lserow, T);
   if (!r) r = fa(&tb.scal, 4);
   if (!r) r = fa(&tb.dx, T * D);
-  if (!r) r = fa(&tb.dtmp, T * std::max(D, Hhd));
-  if (!r && D > NORM_BWD_COLS) r = fa(&tb.dgrow, T * D);
+  if (!r) r = fa(&tb.dtmp, T * std::max({D, Hhd, gpt2 ? I : 0}));
+  if (!r && !gpt2 && D > NORM_BWD_COLS) r = fa(&tb.dgrow, T * D);
   if (!r) r = fa(&tb.dqf, T * Hhd);
   if (!r) r = fa(&tb.dkh, T * Hhd);
   if (!r) r = fa(&tb.dvh, T * Hhd);
   if (!r) r = fa(&tb.dsum, T * H);
-  if (!r) r = fa(&tb.colpart, ROW_PARTS * std::max(nq, D));
+  if (!r) r = fa(&tb.colpart, ROW_PARTS * std::max({nq, D, gpt2 ? std::max(3 * D, I) : 0}));
+  if (!r) r = fa((float**)&tb.stat, T * 2);
+  if (!r) r = fa(&tb.coef, T);
+  if (!r) r = fa((float**)&tb.lps, T * 2);
+  if (!r) r = fa((float**)&tb.seq, (int64_t)c.max_batch * 2);
   if (!r) r = ba(&tb.hf, T2 * D);
   if (!r) r = ba(&tb.dlog, T2 * Vp);
   if (!r) r = ba(&tb.dxb, T2 * D);
-  if (!r) r = ba(&tb.dgu, T2 * 2 * I);
+  if (!r) r = ba(&tb.dgu, T2 * Iw);
   if (!r) r = ba(&tb.dob, T * Hhd);
   if (!r) r = ba(&tb.dqkv, T2 * nq);
   if (!r) r = ba(&tb.headT, tiled(D, Vp));
@@ -1996,17 +2017,17 @@ int train_setup(axon_model* m, hipStream_t s) {
     return fail(e == hipErrorOutOfMemory ? AXON_E_OOM : AXON_E_HIP,
                 std::string("training staging allocation: ") + hipGetErrorString(e));
   }
-  auto wt = [&](const void* W, int64_t N, int64_t K, int64_t Np, bf16* dst) {
+  auto wt = [&](const void* W, int64_t N, int64_t K, int64_t Np, bf16* dst, int heads_of = 0) {
     if (Np > N) (void)hipMemsetAsync(stage, 0, (size_t)K * Np * 2, s);
-    launch_untile_transpose((const bf16*)W, N, (int)K, stage, Np, s);
+    launch_untile_transpose((const bf16*)W, N, (int)K, stage, Np, s, heads_of);
     launch_tile_weight(stage, dst, K, (int)Np, s);
   };
   for (int l = 0; l < c.n_layers; ++l) {
     const LayerW& w = m->layers[l];
     TrainLayer& t = tb.L[l];
-    wt(w.wqkv, nq, D, nq, t.wqkvT);
+    wt(w.wqkv, nq, D, nq, t.wqkvT, gpt2 ? (int)hd : 0);  // (GPT-2: as its gradient's columns)
     wt(w.wo, D, Hhd, D, t.woT);
-    wt(w.wgu, 2 * I, D, 2 * I, t.wguT);
+    wt(w.wgu, Iw, D, Iw, t.wguT);
     wt(w.wd, D, I, D, t.wdT);
   }
   wt(m->lm_head, V, D, Vp, tb.headT);
@@ -2019,12 +2040,124 @@ int train_setup(axon_model* m, hipStream_t s) {
   return AXON_OK;
 }
 
+// The head over tb.hf, the loss and its gradient at the logits (tb.dlog)
+void enqueue_train_loss(axon_model* m, int T, const int32_t* d_targets, const TrainLoss& loss, hipStream_t s) {
+  TrainBufs& tb = m->train;
+  EpiArgs le{};
+  le.lse_part = tb.lsep;
+  gemm_many<bf16>(m, m->lm_head, tb.hf, m->V(), T, m->D(), EPI_LSE, tb.logits, nullptr, tb.Vp, s, &le, nullptr, true);
+  const TrainLogits rows{tb.logits, tb.Vp,   m->V(),  T,      tb.lsep, d_targets,
+                         tb.dlog,   tb.stat, tb.coef, tb.lps, tb.seq};
+  if (loss.kind == TrainLoss::PREFERENCE) launch_preference_train(rows, loss.pref, s);
+  else if (loss.kind == TrainLoss::POLICY) launch_policy_train(rows, loss.pol, s);
+  else
+    launch_ce_loss(tb.logits, tb.Vp, m->V(), tb.lsep, d_targets, T, tb.rowloss, tb.valid, tb.lserow, loss.loss, tb.scal,
+                   tb.dlog, s);
+}
+
+// The GPT-2 family's training step (see enqueue_train): layer norms with their
+// biases, learned positions, GELU, weights and gradients stored [in][out].
+void enqueue_train_gpt2(axon_model* m, int B, int T, const int32_t* d_tokens, const int32_t* d_cu, const int32_t* h_cu,
+                        const int32_t* d_targets, const TrainLoss& loss, const std::vector<float*>& g,
+                        const std::unordered_map<std::string, size_t>& gi, hipStream_t s) {
+  const axon_config& c = m->cfg;
+  TrainBufs& tb = m->train;
+  const int D = c.hidden, H = c.n_heads, hd = c.head_dim, I = c.intermediate, V = c.vocab, L = c.n_layers;
+  const int nq = 3 * D, Vp = tb.Vp;
+  const float eps = c.rms_eps;
+  auto G = [&](const std::string& n) { return g[gi.at(n)]; };
+  // ---- forward, keeping activations (token operands in the row-pair layout)
+  launch_set_lengths(d_cu, m->d_len, B, s);
+  launch_embed_pos_ln(d_tokens, (const bf16*)m->embed, (const bf16*)m->wpe, (const bf16*)m->layers[0].gin,
+                      (const bf16*)m->layers[0].gin_b, tb.L[0].xin, tb.L[0].h1, T, D, V, c.max_positions, eps, d_cu, B,
+                      nullptr, nullptr, s, true);
+  for (int l = 0; l < L; ++l) {
+    const LayerW& w = m->layers[l];
+    TrainLayer& t = tb.L[l];
+    KVView kv = m->kv(l, false);
+    EpiArgs re = rope_epi(m, w, kv, d_cu, B, nullptr);
+    re.q_out = t.q;
+    gemm_many<bf16>(m, w.wqkv, t.h1, nq, T, D, EPI_ROPE, nullptr, nullptr, nq, s, &re, nullptr, true);
+    m->timed(3, H, B, T, s, [&] {
+      launch_attn_prefill<bf16>(t.q, kv, t.o, T, B, d_cu, h_cu, H, s, nullptr, nullptr, nullptr, nullptr, t.lse, true);
+    });
+    EpiArgs oe{}, de{};
+    oe.resid = t.xin;
+    gemm_many<bf16>(m, w.wo, t.o, D, T, D, EPI_RESID, t.xmid, nullptr, D, s, &oe, w.bo, true);
+    launch_layernorm(t.xmid, (const bf16*)w.gpost, (const bf16*)w.gpost_b, t.h2, T, D, eps, nullptr, s, true);
+    gemm_many<bf16>(m, w.wgu, t.h2, I, T, D, EPI_F32, t.gu, nullptr, I, s, nullptr, w.bfc, true);
+    launch_gelu_train(t.gu, T, I, t.a, s);
+    const bool last = l + 1 == L;
+    float* xout = last ? tb.xfin : tb.L[l + 1].xin;
+    de.resid = t.xmid;
+    gemm_many<bf16>(m, w.wd, t.a, D, T, I, EPI_RESID, xout, nullptr, D, s, &de, w.bd, true);
+    launch_layernorm(xout, (const bf16*)(last ? m->gfinal : m->layers[l + 1].gin),
+                     (const bf16*)(last ? m->gfinal_b : m->layers[l + 1].gin_b), last ? tb.hf : tb.L[l + 1].h1, T, D,
+                     eps, nullptr, s, true);
+  }
+  enqueue_train_loss(m, T, d_targets, loss, s);
+  // ---- backward.  dW of a weight stored [in K][out N]: X^T dY
+  auto dW = [&](const bf16* X, int K, const bf16* dY, int N, float* out) {
+    m->timed(1, N, K, T, s, [&] {
+      launch_wgrad(WGRAD_ROWS, X, K, K, dY, N, T, out, nullptr, nullptr, hd, H, H, m->gemm_part, m->gemm_part_floats, s);
+    });
+  };
+  // back through a projection and the layer norm before it: the gradients of that
+  // norm, of its input (tb.dx, += after the first) and of the bias added there last
+  auto dX_norm = [&](const bf16* WT, const bf16* dY, int N, const float* x, const void* gain, const std::string& ln,
+                     float* g_bias, int accumulate) {
+    const Parts dy = gemm_f32_parts(m, WT, dY, D, T, N, tb.dtmp, s);
+    LnTrain tr;
+    tr.np = dy.n;
+    tr.stride = (int64_t)T * D;
+    tr.accumulate = accumulate;
+    tr.dxb = tb.dxb;
+    launch_ln_bwd_train(x, (const bf16*)gain, dy.p, tr, T, D, eps, tb.dx, G(ln + ".weight"), G(ln + ".bias"), g_bias,
+                        tb.colpart, s);
+  };
+  const std::string tr = "transformer.";
+  auto layer = [&](int l) { return tr + "h." + std::to_string(l) + "."; };
+  float* g_embed = G(tr + "wte.weight");
+  m->timed(1, D, V, T, s, [&] {
+    launch_wgrad(WGRAD_ROWS, tb.dlog, Vp, V, tb.hf, D, T, g_embed, nullptr, nullptr, hd, H, H, m->gemm_part,
+                 m->gemm_part_floats, s);
+  });
+  dX_norm(tb.headT, tb.dlog, Vp, tb.xfin, m->gfinal, tr + "ln_f", G(layer(L - 1) + "mlp.c_proj.bias"), 0);
+  for (int l = L - 1; l >= 0; --l) {
+    const LayerW& w = m->layers[l];
+    TrainLayer& t = tb.L[l];
+    KVView kv = m->kv(l, false);
+    const std::string p = layer(l);
+    // MLP
+    dW(t.a, I, tb.dxb, D, G(p + "mlp.c_proj.weight"));
+    const Parts da = gemm_f32_parts(m, t.wdT, tb.dxb, I, T, D, tb.dtmp, s);
+    launch_gelu_bwd(t.gu, da.p, da.n, (int64_t)T * I, T, I, tb.dgu, G(p + "mlp.c_fc.bias"), tb.colpart, s);
+    dW(t.h2, D, tb.dgu, I, G(p + "mlp.c_fc.weight"));
+    dX_norm(t.wguT, tb.dgu, I, t.xmid, w.gpost, p + "ln_2", G(p + "attn.c_proj.bias"), 1);
+    // attention
+    dW(t.o, D, tb.dxb, D, G(p + "attn.c_proj.weight"));
+    const Parts dof = gemm_f32_parts(m, t.woT, tb.dxb, D, T, D, tb.dtmp, s);
+    m->timed(5, H, B, T, s, [&] {
+      launch_attn_bwd(t.q, kv, t.o, dof.p, dof.n, (int64_t)T * D, tb.dob, t.lse, tb.dsum, d_cu, h_cu, B, T, H, tb.dqf,
+                      tb.dkh, tb.dvh, s);
+    });
+    float* g_qkv = G(p + "attn.c_attn.bias");
+    launch_rope_bwd(tb.dqf, tb.dkh, tb.dvh, m->rope_cos, m->rope_sin, d_cu, B, T, H, H, hd, tb.dqkv, tb.colpart, g_qkv,
+                    g_qkv + D, g_qkv + 2 * D, s, true);
+    dW(t.h1, D, tb.dqkv, nq, G(p + "attn.c_attn.weight"));
+    dX_norm(t.wqkvT, tb.dqkv, nq, t.xin, w.gin, p + "ln_1", l > 0 ? G(layer(l - 1) + "mlp.c_proj.bias") : nullptr, 1);
+  }
+  launch_position_bwd(tb.dx, d_cu, B, D, c.max_positions, G(tr + "wpe.weight"), s);
+  launch_embed_bwd(d_tokens, tb.dx, T, D, V, g_embed, false, s);
+}
+
 // Forward over B fresh sequences keeping every activation the backward pass
 // reads, the loss, and the reverse pass into the caller's gradient buffers
 // (g: one float pointer per expected weight, in expected_weights order).
 void enqueue_train(axon_model* m, int B, int T, const int32_t* d_tokens, const int32_t* d_cu, const int32_t* h_cu,
-                   const int32_t* d_targets, float* d_loss, const std::vector<float*>& g,
+                   const int32_t* d_targets, const TrainLoss& loss, const std::vector<float*>& g,
                    const std::unordered_map<std::string, size_t>& gi, hipStream_t s) {
+  if (m->gpt2()) return enqueue_train_gpt2(m, B, T, d_tokens, d_cu, h_cu, d_targets, loss, g, gi, s);
   const axon_config& c = m->cfg;
   TrainBufs& tb = m->train;
   const int D = c.hidden, H = c.n_heads, KV = c.n_kv_heads, hd = c.head_dim, I = c.intermediate, V = c.vocab;
@@ -2055,11 +2188,7 @@ void enqueue_train(axon_model* m, int B, int T, const int32_t* d_tokens, const i
                     last ? tb.hf : tb.L[l + 1].h1, T, nullptr, s, split_for(m, D, T, I), true, true, t.xmid,
                     last ? tb.xfin : tb.L[l + 1].xin);
   }
-  EpiArgs le{};
-  le.lse_part = tb.lsep;
-  gemm_many<bf16>(m, m->lm_head, tb.hf, V, T, D, EPI_LSE, tb.logits, nullptr, Vp, s, &le, nullptr, true);
-  // ---- loss and its gradient at the logits
-  launch_ce_loss(tb.logits, Vp, V, tb.lsep, d_targets, T, tb.rowloss, tb.valid, tb.lserow, d_loss, tb.scal, tb.dlog, s);
+  enqueue_train_loss(m, T, d_targets, loss, s);
   // ---- backward
   // dW = dY^T X, [N][K] float (or its rows' own tensors), from dY [T][N] (rows
   // ldy apart) and X [T][K]
@@ -2113,20 +2242,22 @@ void enqueue_train(axon_model* m, int B, int T, const int32_t* d_tokens, const i
 
 }  // namespace
 
-extern "C" int axon_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_tokens,
-                                   const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens,
-                                   const int32_t* d_targets, float* d_loss, const axon_weight* grads,
-                                   int32_t n_grads, void* stream) {
-  g_err.clear();
-  if (!m) return fail(AXON_E_INVALID, "model is NULL");
+namespace {
+
+// A training step: argument checks shared by the losses, then the work
+int run_train(axon_model* m, int32_t batch, const int32_t* d_tokens, const int32_t* d_cu_seqlens,
+              const int32_t* h_cu_seqlens, const int32_t* d_targets, const TrainLoss& loss, const axon_weight* grads,
+              int32_t n_grads, void* stream) {
   const axon_config& c = m->cfg;
-  if (!m->bf || m->gpt2() || m->moe_model() || c.sliding_window > 0 || m->paged())
-    return fail(AXON_E_INVALID, "the backward pass covers dense Llama-family bf16 models with a contiguous cache "
-                                "and no sliding window");
+  if (!m->bf || m->moe_model() || c.sliding_window > 0 || m->paged())
+    return fail(AXON_E_INVALID, "the backward pass covers dense bf16 models (Llama family and GPT-2) with a contiguous "
+                                "cache and no sliding window");
+  if (m->gpt2() && c.n_heads * c.head_dim != c.hidden)
+    return fail(AXON_E_INVALID, "the backward pass of GPT-2 needs n_heads * head_dim == hidden");
   if (batch < 1) return fail(AXON_E_INVALID, "batch must be >= 1");
   if (batch > c.max_batch)
     return fail(AXON_E_CAPACITY, "batch " + std::to_string(batch) + " exceeds max_batch " + std::to_string(c.max_batch));
-  if (!d_tokens || !d_cu_seqlens || !h_cu_seqlens || !d_targets || !d_loss || !grads)
+  if (!d_tokens || !d_cu_seqlens || !h_cu_seqlens || !d_targets || !loss.loss || !grads)
     return fail(AXON_E_INVALID, "d_tokens, d_cu_seqlens, h_cu_seqlens, d_targets, d_loss and grads must be non-NULL");
   if (h_cu_seqlens[0] != 0) return fail(AXON_E_INVALID, "cu_seqlens[0] must be 0");
   int64_t total = 0;
@@ -2165,12 +2296,66 @@ extern "C" int axon_loss_and_grads(axon_model* m, int32_t batch, const int32_t* 
     if (!g[i]) return fail(AXON_E_MISSING, "missing gradient '" + expected[i].first + "'");
   hipStream_t s = (hipStream_t)stream;
   if (int r = train_setup(m, s)) return r;
-  enqueue_train(m, batch, (int)total, d_tokens, d_cu_seqlens, h_cu_seqlens, d_targets, d_loss, g, index, s);
+  enqueue_train(m, batch, (int)total, d_tokens, d_cu_seqlens, h_cu_seqlens, d_targets, loss, g, index, s);
   if (int r = check_launch("backward pass")) return r;
   if (int r = take_enqueue_err(m, "backward pass")) return r;
   for (int b = 0; b < c.max_batch; ++b) m->h_len[b] = b < batch ? h_cu_seqlens[b + 1] - h_cu_seqlens[b] : 0;
   m->active = batch;
   return AXON_OK;
+}
+
+}  // namespace
+
+extern "C" int axon_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_tokens,
+                                   const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens,
+                                   const int32_t* d_targets, float* d_loss, const axon_weight* grads,
+                                   int32_t n_grads, void* stream) {
+  g_err.clear();
+  if (!m) return fail(AXON_E_INVALID, "model is NULL");
+  TrainLoss loss;
+  loss.loss = d_loss;
+  return run_train(m, batch, d_tokens, d_cu_seqlens, h_cu_seqlens, d_targets, loss, grads, n_grads, stream);
+}
+
+extern "C" int axon_preference_loss_and_grads(axon_model* m, int32_t pairs, const int32_t* d_tokens,
+                                              const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens,
+                                              const int32_t* d_targets, const float* d_ref_logps, float beta,
+                                              float label_smoothing, float* d_loss, float* d_seq_logps,
+                                              float* d_margins, const axon_weight* grads, int32_t n_grads,
+                                              void* stream) {
+  return entry([&]() -> int {
+    if (!m) return fail(AXON_E_INVALID, "model is NULL");
+    if (int r = check_preference(pairs, beta, label_smoothing)) return r;
+    if (!d_seq_logps || !d_margins) return fail(AXON_E_INVALID, "d_seq_logps and d_margins must be non-NULL");
+    TrainLoss loss;
+    loss.kind = TrainLoss::PREFERENCE;
+    loss.loss = d_loss;
+    loss.pref = PreferenceArgs{d_cu_seqlens, 2 * pairs, d_ref_logps, beta, label_smoothing, d_loss, d_seq_logps,
+                               d_margins};
+    return run_train(m, 2 * pairs, d_tokens, d_cu_seqlens, h_cu_seqlens, d_targets, loss, grads, n_grads, stream);
+  });
+}
+
+extern "C" int axon_policy_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_tokens,
+                                          const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens,
+                                          const int32_t* d_targets, const float* d_old_logps,
+                                          const float* d_ref_logps, const float* d_advantages, float clip_low,
+                                          float clip_high, float kl_coef, int32_t per_sequence, float* d_loss,
+                                          float* d_stats, float* d_logps, const axon_weight* grads, int32_t n_grads,
+                                          void* stream) {
+  return entry([&]() -> int {
+    if (!m) return fail(AXON_E_INVALID, "model is NULL");
+    if (int r = check_policy(clip_low, clip_high, kl_coef, per_sequence)) return r;
+    if (!d_old_logps || !d_advantages || !d_stats || !d_logps)
+      return fail(AXON_E_INVALID, "d_old_logps, d_advantages, d_stats and d_logps must be non-NULL");
+    if (kl_coef > 0.f && !d_ref_logps) return fail(AXON_E_INVALID, "kl_coef > 0 needs d_ref_logps");
+    TrainLoss loss;
+    loss.kind = TrainLoss::POLICY;
+    loss.loss = d_loss;
+    loss.pol = PolicyArgs{per_sequence ? d_cu_seqlens : nullptr, batch, d_old_logps, d_ref_logps, d_advantages,
+                          clip_low, clip_high, kl_coef, d_loss, d_stats, d_logps};
+    return run_train(m, batch, d_tokens, d_cu_seqlens, h_cu_seqlens, d_targets, loss, grads, n_grads, stream);
+  });
 }
 
 extern "C" int axon_reset_slot(axon_model* m, int32_t slot) {

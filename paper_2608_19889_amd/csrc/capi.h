@@ -14,6 +14,10 @@ void clear_error();
 // AXON_OK, or the last launch's error
 int check_launch(const char* what);
 
+// the checks that a loss's two calls, on logits and on a model, share
+int check_preference(int32_t pairs, float beta, float label_smoothing);
+int check_policy(float clip_low, float clip_high, float kl_coef, int32_t per_sequence);
+
 // runs an entry point's body; no exception leaves it
 template <typename F>
 int entry(F&& body) {

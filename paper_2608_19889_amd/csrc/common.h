@@ -151,6 +151,12 @@ AXON_DEV void store_run8(float* row, int c, int n, const float (&v)[8]) {
       if (c + j < n) row[c + j] = v[j];
   }
 }
+AXON_DEV void store_run8(bf16* base, int64_t at, const float (&v)[8]) {  // 16-byte aligned
+  bf16x8 o;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) o[j] = (bf16)v[j];
+  *(bf16x8*)(base + at) = o;
+}
 AXON_DEV void store_run8(bf16* row, int c, int n, const float (&v)[8]) {
   if (c + 8 <= n) {
     bf16x8 o;

@@ -186,15 +186,21 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
 // every thread the same columns of each, so dg and db stay in registers until the
 // workgroup leaves one partial row [2 cols] for the column sum; up to 8192 columns
 // the next row's operands are loaded before this row's reductions.
-template <typename TX, typename TD, typename TP, int TPR, int NV>
+//
+// TRAIN, the training step's form (float rows): dy is the sum of tr.np split-K
+// partials in order; tr.accumulate: dx += instead of =; the new dx goes to tr.dxb in
+// bf16 too (row-pair layout, the next projections' operand), and its column sums,
+// the gradient of the bias that was added to the residual there, are a third
+// part of the partial row [3 cols].
+template <typename TX, typename TD, typename TP, int TPR, int NV, bool TRAIN>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
     ln_bwd_kernel(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const TP* __restrict__ g, float eps, TX* dx,
-                  int64_t lddx, float* __restrict__ part, int64_t rows, int cols, int64_t per) {
-  constexpr int RPW = TPR < 256 ? 256 / TPR : 1;
+                  int64_t lddx, float* __restrict__ part, int64_t rows, int cols, int64_t per, LnTrain tr) {
+  constexpr int RPW = TPR < 256 ? 256 / TPR : 1, SUMS = TRAIN ? 3 : 2;
   __shared__ float red[2][4][16];
   const int i = threadIdx.x % TPR;
   const int64_t r1 = min(rows, ((int64_t)blockIdx.x + 1) * per);
-  float gv[NV][8], dg[NV][8] = {}, db[NV][8] = {}, xn[NV][8], dn[NV][8];
+  float gv[NV][8], dg[NV][8] = {}, db[NV][8] = {}, dr[NV][8] = {}, xn[NV][8], dn[NV][8], an[NV][8];
 #pragma unroll
   for (int n = 0; n < NV; ++n) load_run8(g, (n * TPR + i) * 8, cols, gv[n], 0.f);
   auto load = [&](int64_t r) {
@@ -202,13 +208,27 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
     for (int n = 0; n < NV; ++n) {
       load_run8(x + r * ldx, (n * TPR + i) * 8, cols, xn[n], 0.f);
       load_run8(dy + r * lddy, (n * TPR + i) * 8, cols, dn[n], 0.f);
+      if constexpr (TRAIN) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) an[n][j] = 0.f;
+        if (tr.accumulate) load_run8(dx + r * lddx, (n * TPR + i) * 8, cols, an[n], 0.f);
+      }
     }
+    if constexpr (TRAIN)
+      for (int p = 1; p < tr.np; ++p)
+#pragma unroll
+        for (int n = 0; n < NV; ++n) {
+          float more[8];
+          load_run8(dy + p * tr.stride + r * lddy, (n * TPR + i) * 8, cols, more, 0.f);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) dn[n][j] += more[j];
+        }
   };
   int64_t r = (int64_t)blockIdx.x * per + threadIdx.x / TPR;
   constexpr bool AHEAD = NV == 1;  // the registers of two rows at once, 128 a thread at most
   if (AHEAD && r < r1) load(r);
   for (int par = 0; r < r1; r += RPW, par ^= 1) {
-    float d[NV][8], e[NV][8];
+    float d[NV][8], e[NV][8], a[NV][8];
     float s = 0.f;
     if (!AHEAD) load(r);
 #pragma unroll
@@ -217,6 +237,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
       for (int j = 0; j < 8; ++j) {
         d[n][j] = xn[n][j];
         e[n][j] = dn[n][j];
+        a[n][j] = TRAIN ? an[n][j] : 0.f;
         s += d[n][j];
       }
     if (AHEAD && r + RPW < r1) load(r + RPW);
@@ -258,28 +279,27 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         o[j] = rstd * (e[n][j] * gv[n][j] - mh - d[n][j] * k);
+        if (TRAIN) o[j] += a[n][j];
         dg[n][j] += e[n][j] * (d[n][j] * rstd);
         db[n][j] += e[n][j];
+        dr[n][j] += TRAIN && (n * TPR + i) * 8 < cols ? o[j] : 0.f;  // (TRAIN: cols a multiple of 32)
       }
       store_run8(dx + r * lddx, (n * TPR + i) * 8, cols, o);
+      if constexpr (TRAIN)
+        if ((n * TPR + i) * 8 < cols) store_run8(tr.dxb, xp_off(r, (n * TPR + i) * 8, cols), o);
     }
   }
-  float* out = part + (int64_t)blockIdx.x * 2 * cols;
-  if constexpr (RPW == 1) {
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      store_run8(out, (n * TPR + i) * 8, cols, dg[n]);
-      store_run8(out + cols, (n * TPR + i) * 8, cols, db[n]);
-    }
-  } else {  // the wavefronts' shares in order
+  float* out = part + (int64_t)blockIdx.x * SUMS * cols;
+  if constexpr (RPW > 1) {  // the wavefronts' shares in order
     static_assert(RPW == 4 && NV == 1, "one group of columns a lane");
-    __shared__ float sums[3][64][17];
+    __shared__ float sums[3][64][SUMS * 8 + 1];
     const int w = threadIdx.x / TPR;
     if (w > 0)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         sums[w - 1][i][j] = dg[0][j];
         sums[w - 1][i][8 + j] = db[0][j];
+        if (TRAIN) sums[w - 1][i][SUMS * 8 - 8 + j] = dr[0][j];
       }
     __syncthreads();
     if (w > 0) return;
@@ -288,9 +308,14 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
       for (int j = 0; j < 8; ++j) {
         dg[0][j] += sums[k][i][j];
         db[0][j] += sums[k][i][8 + j];
+        if (TRAIN) dr[0][j] += sums[k][i][SUMS * 8 - 8 + j];
       }
-    store_run8(out, i * 8, cols, dg[0]);
-    store_run8(out + cols, i * 8, cols, db[0]);
+  }
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    store_run8(out, (n * TPR + i) * 8, cols, dg[n]);
+    store_run8(out + cols, (n * TPR + i) * 8, cols, db[n]);
+    if (TRAIN) store_run8(out + 2 * cols, (n * TPR + i) * 8, cols, dr[n]);
   }
 }
 
@@ -358,10 +383,23 @@ void launch_ln_bwd(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const T
   const int64_t per = ln_bwd_per(rows, cols), n = (rows + per - 1) / per;
   ln_bwd_shape(cols, [&](auto tpr, auto nv) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-    ln_bwd_kernel<TX, TD, TP, TPR, NV>
-        <<<(unsigned)n, TPR < 256 ? 256 : TPR, 0, s>>>(x, ldx, dy, lddy, g, eps, dx, lddx, part, rows, cols, per);
+    ln_bwd_kernel<TX, TD, TP, TPR, NV, false><<<(unsigned)n, TPR < 256 ? 256 : TPR, 0, s>>>(
+        x, ldx, dy, lddy, g, eps, dx, lddx, part, rows, cols, per, LnTrain{});
   });
   launch_colsum_final(part, (int)n, 2 * cols, dg, cols, db, db ? 2 * cols : cols, nullptr, s);
+}
+
+void launch_ln_bwd_train(const float* x, const bf16* g, const float* dy, const LnTrain& tr, int T, int D, float eps,
+                         float* dx, float* dg, float* db, float* dres, float* part, hipStream_t s) {
+  if (T <= 0) return;
+  const int64_t per = ln_bwd_per(T, D), n = (T + per - 1) / per;
+  ln_bwd_shape(D, [&](auto tpr, auto nv) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+    if constexpr (NV == 1)  // D <= 8192
+      ln_bwd_kernel<float, float, bf16, TPR, NV, true><<<(unsigned)n, TPR < 256 ? 256 : TPR, 0, s>>>(
+          x, D, dy, D, g, eps, dx, D, part, T, D, per, tr);
+  });
+  launch_colsum_final(part, (int)n, 3 * D, dg, D, db, 2 * D, dres, s);
 }
 
 #define LN_INSTANCE(TX, TY, TP)                                                                                  \

@@ -148,10 +148,10 @@ AXON_DEV double softplus_f64(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v
 template <typename T>
 __global__ void __launch_bounds__(1024) preference_finish_kernel(
     const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
-    const float2* __restrict__ part, int slices, const int32_t* __restrict__ cu, int seqs,
+    const float2* part /* may be stat */, int slices, const int32_t* __restrict__ cu, int seqs,
     const float* __restrict__ ref, float beta, float smoothing, float* __restrict__ loss,
     float* __restrict__ seq_logps, float* __restrict__ margins, double* __restrict__ lps, double* __restrict__ sums,
-    float2* __restrict__ stat, float* __restrict__ coef) {
+    float2* stat, float* __restrict__ coef) {
   __shared__ double red[16];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   for (int t = tid; t < tokens; t += 1024) {
@@ -206,10 +206,10 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(
 template <typename T>
 __global__ void __launch_bounds__(1024) policy_finish_kernel(
     const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
-    const float2* __restrict__ part, int slices, const int32_t* __restrict__ cu, int seqs,
+    const float2* part /* may be stat */, int slices, const int32_t* __restrict__ cu, int seqs,
     const float* __restrict__ old, const float* __restrict__ ref, const float* __restrict__ adv, float lo, float hi,
     float kl_coef, float* __restrict__ loss, float* __restrict__ stats, float* __restrict__ logps,
-    double* __restrict__ weights, float2* __restrict__ stat, float* __restrict__ coef) {
+    double* __restrict__ weights, float2* stat, float* __restrict__ coef) {
   __shared__ double red[16];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   // the weights: counted tokens of all, or of each sequence
@@ -309,6 +309,60 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld,
     for (int k = 0; k < GRAD_RUNS; ++k)
       if (c0 + k * 2048 < V) store_run8(out, c0 + k * 2048, V, v[k]);
   }
+}
+
+// ---------------------------------------------------------------- within a training step
+
+// (m, S) of a row from the np (largest, sum) partials of its 64-column pieces, a
+// workgroup a row; rows that do not count are skipped
+__global__ void __launch_bounds__(256) piece_merge_kernel(const float2* __restrict__ pieces, int np, int V,
+                                                          const int32_t* __restrict__ targets,
+                                                          float2* __restrict__ stat) {
+  __shared__ float red[2][4];
+  const int t = blockIdx.x, tg = targets[t];
+  if (tg < 0 || tg >= V) return;
+  float m = -INFINITY, s = 0.f;
+  for (int i = threadIdx.x; i < np; i += 256) {
+    const float2 p = pieces[(int64_t)t * np + i];
+    join_part(m, s, p.x, p.y);
+  }
+  const float wm = wave_max(m);
+  s = wave_sum(s * __expf(m - (wm == -INFINITY ? 0.f : wm)));
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = wm;
+    red[1][threadIdx.x >> 6] = s;
+  }
+  __syncthreads();
+  if (threadIdx.x) return;
+  m = red[0][0];
+  s = red[1][0];
+#pragma unroll
+  for (int w = 1; w < 4; ++w) join_part(m, s, red[0][w], red[1][w]);
+  stat[t] = float2{m, s};
+}
+
+// The gradient as the training step's GEMM operand: bf16 in the row-pair layout,
+// columns V .. ldl - 1 zero.  8 columns per thread (ldl % 32 == 0), every load
+// unconditional (the padding columns hold whatever the buffer held and are not used);
+// 8 lanes fill one 128-byte line of a row pair.
+__global__ void __launch_bounds__(256) logit_grad_pair_kernel(const float* __restrict__ z, int ldl, int V, int T,
+                                                              const int32_t* __restrict__ targets,
+                                                              const float2* __restrict__ stat,
+                                                              const float* __restrict__ coef, bf16* __restrict__ dlog) {
+  const int tid = threadIdx.x;
+  const int t = blockIdx.y * 2 + ((tid >> 2) & 1);
+  const int v0 = (blockIdx.x * 32 + (tid >> 3)) * 32 + (tid & 3) * 8;
+  if (t >= T || v0 >= ldl) return;
+  float v[8];
+  load_run8(z + (int64_t)t * ldl, v0, ldl, v, 0.f);
+  const float w = coef[t];
+  const float2 st = stat[t];
+  const int tg = targets[t];
+  const float f = -w / st.y;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    v[j] = w == 0.f || v0 + j >= V ? 0.f : __expf(v[j] - st.x) * f + (v0 + j == tg ? w : 0.f);
+  store_run8(dlog, xp_off(t, v0, ldl), v);
 }
 
 // ---------------------------------------------------------------- launchers
@@ -433,6 +487,35 @@ void launch_preference_loss(const LogitRows& r, const PreferenceArgs& a, void* w
 void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipStream_t s) {
   if (r.z_bf16) policy<bf16>(r, a, ws, s);
   else policy<float>(r, a, ws, s);
+}
+
+namespace {
+
+void train_stat(const TrainLogits& r, hipStream_t s) {
+  piece_merge_kernel<<<r.T, 256, 0, s>>>(r.lse_part, (r.V + LSE_COLS - 1) / LSE_COLS, r.V, r.targets, r.stat);
+}
+
+void train_grad(const TrainLogits& r, hipStream_t s) {
+  logit_grad_pair_kernel<<<dim3((r.ldl / 32 + 31) / 32, (r.T + 1) / 2), 256, 0, s>>>(r.z, r.ldl, r.V, r.T, r.targets,
+                                                                                     r.stat, r.coef, r.dlog);
+}
+
+}  // namespace
+
+void launch_preference_train(const TrainLogits& r, const PreferenceArgs& a, hipStream_t s) {
+  train_stat(r, s);
+  preference_finish_kernel<float><<<1, 1024, 0, s>>>(r.z, r.ldl, r.V, r.targets, r.T, r.stat, 1, a.cu, a.seqs, a.ref,
+                                                     a.beta, a.smoothing, a.loss, a.seq_logps, a.margins, r.lps, r.seq,
+                                                     r.stat, r.coef);
+  train_grad(r, s);
+}
+
+void launch_policy_train(const TrainLogits& r, const PolicyArgs& a, hipStream_t s) {
+  train_stat(r, s);
+  policy_finish_kernel<float><<<1, 1024, 0, s>>>(r.z, r.ldl, r.V, r.targets, r.T, r.stat, 1, a.cu, a.seqs, a.old, a.ref,
+                                                 a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats, a.logps, r.seq, r.stat,
+                                                 r.coef);
+  train_grad(r, s);
 }
 
 }  // namespace axon

@@ -117,15 +117,20 @@ __global__ void __launch_bounds__(256) ce_grad_kernel(const float* __restrict__ 
 // ---------------------------------------------------------------- layouts
 
 // dst[k][n] = W[n][k] from the fragment-tiled W [N][K]; dst rows are Np
-// apart (the caller zeroes columns N .. Np-1)
+// apart (the caller zeroes columns N .. Np-1).  hd > 0: row n = 8 g + j of a head
+// holds its original row 4 g + j (j < 4) or hd / 2 + 4 g + j - 4, dst's column
 __global__ void __launch_bounds__(256) untile_transpose_kernel(const bf16* __restrict__ W, int64_t N, int K,
-                                                               bf16* __restrict__ dst, int64_t Np) {
+                                                               bf16* __restrict__ dst, int64_t Np, int hd) {
   const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;  // (n, k-chunk)
   const int kc = K / 8;
   if (q >= N * kc) return;
-  const int64_t n = q / kc;
+  int64_t n = q / kc;
   const int c = (int)(q % kc);
   const bf16x8 v = *(const bf16x8*)(W + wt_chunk(n, c, K));
+  if (hd > 0) {
+    const int r = (int)(n % hd), g = r >> 3, j = r & 7;
+    n += (j < 4 ? 4 * g + j : hd / 2 + 4 * g + j - 4) - r;
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) dst[(int64_t)(c * 8 + j) * Np + n] = v[j];
 }
@@ -621,7 +626,8 @@ __global__ void __launch_bounds__(256, HD == 64 ? 2 : 1) attn_bwd_dkv_kernel(con
 // query head; a kv head's are summed in head order.  A thread owns one 8-row
 // group (16-byte loads and stores) over ``rows`` tokens, so that with bpart the
 // bias gradient's column sums [workgroup][nq] (original row order) stay in
-// registers.  One thread per rotation pair, with the share sum and a float32 copy
+// registers.  plain: the heads' original row order (GPT-2, whose weight gradient
+// has the projection's outputs as its columns).  One thread per rotation pair, with the share sum and a float32 copy
 // of dqkv for the bias as passes of their own, took 46 us on 4096 x 3072; this
 // kernel 27 us (125 MB).
 __global__ void __launch_bounds__(128) rope_bwd_kernel(const float* __restrict__ dq, const float* __restrict__ dkh,
@@ -629,7 +635,7 @@ __global__ void __launch_bounds__(128) rope_bwd_kernel(const float* __restrict__
                                                        const float* __restrict__ sin_t,
                                                        const int32_t* __restrict__ cu, int nseq, int T, int H,
                                                        int KVh, int hd, bf16* __restrict__ dqkv,
-                                                       float* __restrict__ bpart, int rows) {
+                                                       float* __restrict__ bpart, int rows, bool plain) {
   const int half = hd / 2, NH = H + 2 * KVh, nq = NH * hd, group = H / KVh;
   const int item = blockIdx.x * 128 + threadIdx.x;
   if (item >= nq / 8) return;
@@ -655,8 +661,14 @@ __global__ void __launch_bounds__(128) rope_bwd_kernel(const float* __restrict__
       y2 = y2 * c - y1 * sn;
       y1 = x1;
     }
-    *(bf16x8*)(dqkv + xp_off(t, (int64_t)item * 8, nq)) =
-        bf16x8{(bf16)y1[0], (bf16)y1[1], (bf16)y1[2], (bf16)y1[3], (bf16)y2[0], (bf16)y2[1], (bf16)y2[2], (bf16)y2[3]};
+    const bf16x4 b1 = {(bf16)y1[0], (bf16)y1[1], (bf16)y1[2], (bf16)y1[3]};
+    const bf16x4 b2 = {(bf16)y2[0], (bf16)y2[1], (bf16)y2[2], (bf16)y2[3]};
+    if (plain) {
+      *(bf16x4*)(dqkv + xp_off(t, hh * hd + i0, nq)) = b1;
+      *(bf16x4*)(dqkv + xp_off(t, hh * hd + half + i0, nq)) = b2;
+    } else {
+      *(bf16x8*)(dqkv + xp_off(t, (int64_t)item * 8, nq)) = __builtin_shufflevector(b1, b2, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
     s1 += y1;
     s2 += y2;
   }
@@ -683,6 +695,69 @@ __global__ void __launch_bounds__(256) embed_bwd_kernel(const int32_t* __restric
   for (int d = threadIdx.x; d < D; d += 256) atomicAdd(dE + (int64_t)id * D + d, dx[(int64_t)t * D + d]);
 }
 
+// ---------------------------------------------------------------- GPT-2: GELU and learned positions
+
+// a = gelu(z), 8 features a thread
+__global__ void __launch_bounds__(256) gelu_train_kernel(const float* __restrict__ z, int T, int I,
+                                                         bf16* __restrict__ a) {
+  const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int ic = I / 8;
+  if (q >= (int64_t)T * ic) return;
+  const int64_t t = q / ic;
+  const int c = (int)(q % ic) * 8;
+  float v[8];
+  load_run8(z + t * I, c, I, v, 0.f);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = gelu_tanh_f(v[j]);
+  store_run8(a, xp_off(t, c, I), v);
+}
+
+// dz = da gelu'(z), with u = sqrt(2/pi) (z + 0.044715 z^3), h = tanh(u): gelu' = (1 + h)
+// / 2 + z (1 - h^2) u' / 2.  A thread owns 8 features over ``rows`` tokens, so that the
+// bias gradient's column sums [workgroup][I] stay in registers.
+__global__ void __launch_bounds__(128) gelu_bwd_kernel(const float* __restrict__ z, const float* __restrict__ da,
+                                                       int np, int64_t stride, int T, int I, bf16* __restrict__ dz,
+                                                       float* __restrict__ part, int rows) {
+  const int c = (blockIdx.x * 128 + threadIdx.x) * 8;
+  if (c >= I) return;
+  const int t0 = blockIdx.y * rows, t1 = min(T, t0 + rows);
+  float sum[8] = {};
+  for (int t = t0; t < t1; ++t) {
+    float v[8], d[8];
+    load_run8(z + (int64_t)t * I, c, I, v, 0.f);
+    load_run8(da + (int64_t)t * I, c, I, d, 0.f);
+    for (int p = 1; p < np; ++p) {
+      float more[8];
+      load_run8(da + p * stride + (int64_t)t * I, c, I, more, 0.f);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[j] += more[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = v[j], k = 0.7978845608028654f;
+      const float h = 1.f - 2.f / (__expf(2.f * k * (x + 0.044715f * x * x * x)) + 1.f);
+      d[j] *= 0.5f * (1.f + h) + 0.5f * x * (1.f - h * h) * (k * (1.f + 0.134145f * x * x));
+      sum[j] += d[j];
+    }
+    store_run8(dz, xp_off(t, c, I), d);
+  }
+  store_run8(part + (int64_t)blockIdx.y * I, c, I, sum);
+}
+
+// dP[p] = sum over the sequences longer than p, in order, of dx[cu[e] + p]
+__global__ void __launch_bounds__(256) position_bwd_kernel(const float* __restrict__ dx, const int32_t* __restrict__ cu,
+                                                           int nseq, int D, float* __restrict__ dP) {
+  const int p = blockIdx.x;
+  for (int d = threadIdx.x * 4; d < D; d += 1024) {
+    f32x4 s = {};
+    for (int e = 0; e < nseq; ++e) {
+      const int t = cu[e] + p;
+      if (t < cu[e + 1]) s += *(const f32x4*)(dx + (int64_t)t * D + d);
+    }
+    *(f32x4*)(dP + (int64_t)p * D + d) = s;
+  }
+}
+
 // ---------------------------------------------------------------- launchers
 
 void launch_ce_loss(const float* logits, int ldl, int V, const float2* lse_part, const int32_t* targets, int T,
@@ -694,9 +769,9 @@ void launch_ce_loss(const float* logits, int ldl, int V, const float2* lse_part,
                                                                        dlog);
 }
 
-void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t Np, hipStream_t s) {
+void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t Np, hipStream_t s, int hd) {
   const int64_t n = N * (K / 8);
-  if (n > 0) untile_transpose_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(W, N, K, dst, Np);
+  if (n > 0) untile_transpose_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(W, N, K, dst, Np, hd);
 }
 
 // rows per workgroup of the row kernels that leave one partial per workgroup:
@@ -748,11 +823,11 @@ void launch_attn_bwd(const bf16* q, KVView kv, const bf16* o, const float* dof, 
 
 void launch_rope_bwd(const float* dq, const float* dkh, const float* dvh, const float* cos_t, const float* sin_t,
                      const int32_t* cu, int nseq, int T, int H, int KVh, int hd, bf16* dqkv, float* bpart, float* dbq,
-                     float* dbk, float* dbv, hipStream_t s) {
+                     float* dbk, float* dbv, hipStream_t s, bool plain) {
   if (T <= 0) return;
   const int nq = (H + 2 * KVh) * hd, rows = row_chunk(T), n = (T + rows - 1) / rows;
   rope_bwd_kernel<<<dim3((nq / 8 + 127) / 128, n), 128, 0, s>>>(dq, dkh, dvh, cos_t, sin_t, cu, nseq, T, H, KVh, hd,
-                                                               dqkv, dbq ? bpart : nullptr, rows);
+                                                               dqkv, dbq ? bpart : nullptr, rows, plain);
   if (dbq) launch_colsum_final(bpart, n, nq, dbq, H * hd, dbk, (H + KVh) * hd, dbv, s);
 }
 
@@ -760,6 +835,23 @@ void launch_embed_bwd(const int32_t* tok, const float* dx, int T, int D, int V, 
   const int64_t n4 = (int64_t)V * D / 4;
   if (clear) zero_f32_kernel<<<(unsigned)((n4 + 255) / 256), 256, 0, s>>>(dE, n4);
   if (T > 0) embed_bwd_kernel<<<T, 256, 0, s>>>(tok, dx, D, V, dE);
+}
+
+void launch_gelu_train(const float* z, int T, int I, bf16* a, hipStream_t s) {
+  const int64_t n = (int64_t)T * (I / 8);
+  if (n > 0) gelu_train_kernel<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(z, T, I, a);
+}
+
+void launch_gelu_bwd(const float* z, const float* da, int np, int64_t stride, int T, int I, bf16* dz, float* dbias,
+                     float* part, hipStream_t s) {
+  if (T <= 0) return;
+  const int rows = row_chunk(T), n = (T + rows - 1) / rows;
+  gelu_bwd_kernel<<<dim3((I / 8 + 127) / 128, n), 128, 0, s>>>(z, da, np, stride, T, I, dz, part, rows);
+  launch_colsum_final(part, n, I, dbias, I, nullptr, I, nullptr, s);
+}
+
+void launch_position_bwd(const float* dx, const int32_t* cu, int nseq, int D, int P, float* dP, hipStream_t s) {
+  position_bwd_kernel<<<P, 256, 0, s>>>(dx, cu, nseq, D, dP);
 }
 
 }  // namespace axon

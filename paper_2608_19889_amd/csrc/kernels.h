@@ -125,6 +125,18 @@ void launch_ln_fwd(const TX* x, int64_t ldx, const TP* g, const TP* b, float eps
 template <typename TX, typename TD, typename TP>
 void launch_ln_bwd(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const TP* g, float eps, TX* dx, int64_t lddx,
                    float* dg, float* db, float* part, int64_t rows, int cols, hipStream_t s);
+// The training step's form: x and dy [T][D] float, dy the sum of tr.np partials
+// tr.stride apart; dx [T][D] (tr.accumulate: += instead of =), its bf16 copy tr.dxb
+// (row-pair layout) and, beside dg and db, dres = the column sums of the new dx (null:
+// not written).  D % 32 == 0, D <= 8192; part: ROW_PARTS x 3 D floats.
+struct LnTrain {
+  int np = 1;
+  int64_t stride = 0;
+  int accumulate = 0;
+  bf16* dxb = nullptr;
+};
+void launch_ln_bwd_train(const float* x, const bf16* g, const float* dy, const LnTrain& tr, int T, int D, float eps,
+                         float* dx, float* dg, float* db, float* dres, float* part, hipStream_t s);
 // dst[r][k] = src[k][perm ? perm[r] : r] (bf16): a [K][N] matrix stored
 // [in][out] transposed to [N][K], rows optionally permuted
 void launch_transpose_rows(const bf16* src, bf16* dst, int K, int N, const int32_t* perm, hipStream_t s);
@@ -163,6 +175,21 @@ void launch_token_logps(const LogitRows& r, float* logps, void* ws, hipStream_t 
 void launch_token_logps_bwd(const LogitRows& r, const float* dlogps, void* ws, hipStream_t s);
 void launch_preference_loss(const LogitRows& r, const PreferenceArgs& a, void* ws, hipStream_t s);
 void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipStream_t s);
+// The same within a training step, as launch_ce_loss: logits [T][ldl] of V real columns
+// (ldl % 32 == 0) and their projection's EPI_LSE partials; dlog [T][ldl] bf16 = the
+// gradient (zero padding, row-pair layout).
+struct TrainLogits {
+  const float* z;
+  int ldl, V, T;
+  const float2* lse_part;
+  const int32_t* targets;
+  bf16* dlog;
+  float2* stat;  // scratch: [T] each, seq one per sequence
+  float* coef;
+  double *lps, *seq;
+};
+void launch_preference_train(const TrainLogits& r, const PreferenceArgs& a, hipStream_t s);
+void launch_policy_train(const TrainLogits& r, const PolicyArgs& a, hipStream_t s);
 
 // ---- backward pass (k_train.hip)
 // loss over logits [T][ldl] (V real columns, ldl % 32 == 0) and targets
@@ -171,8 +198,9 @@ void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipSt
 // (zero padding, row-pair layout); rowloss / valid / lse [T] and scal [1] scratch
 void launch_ce_loss(const float* logits, int ldl, int V, const float2* lse_part, const int32_t* targets, int T,
                     float* rowloss, float* valid, float* lse, float* loss, float* scal, bf16* dlog, hipStream_t s);
-// dst [K][Np] (row-major) = W^T for the fragment-tiled W [N][K]
-void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t Np, hipStream_t s);
+// dst [K][Np] (row-major) = W^T for the fragment-tiled W [N][K]; hd > 0: W's rows are
+// heads of hd in the rotation-pair order, dst's columns in the original one
+void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t Np, hipStream_t s, int hd = 0);
 // The row kernels below that reduce over tokens leave at most ROW_PARTS partial
 // rows.  RMSNorm backward: dx (accumulate ? += : =), its bf16 copy dxb (row-pair
 // layout) and the gain's gradient dg [D], from dy as np partials [T][D] ``stride``
@@ -195,10 +223,20 @@ void launch_attn_bwd(const bf16* q, KVView kv, const bf16* o, const float* dof, 
                      float* dq, float* dkh, float* dvh, hipStream_t s);
 // back through RoPE into the fused QKV row order (bf16, row-pair layout), the
 // heads' shares of dk / dv summed; with dbq the bias gradients dbq / dbk / dbv too
-// (bpart: ROW_PARTS x nq floats)
+// (bpart: ROW_PARTS x nq floats); plain: dqkv in the original row order of the heads
 void launch_rope_bwd(const float* dq, const float* dkh, const float* dvh, const float* cos_t, const float* sin_t,
                      const int32_t* cu, int nseq, int T, int H, int KVh, int hd, bf16* dqkv, float* bpart, float* dbq,
-                     float* dbk, float* dbv, hipStream_t s);
+                     float* dbk, float* dbv, hipStream_t s, bool plain = false);
+// GELU (tanh form) of GPT-2's MLP in a training step: a [T][I] = gelu(z), and from the
+// gradient of a as np float partials ``stride`` apart dz = da gelu'(z) and the bias
+// gradient dbias [I] = its column sums (part: ROW_PARTS x I floats).  z float rows; a
+// and dz bf16 in the row-pair layout (I % 32 == 0).
+void launch_gelu_train(const float* z, int T, int I, bf16* a, hipStream_t s);
+void launch_gelu_bwd(const float* z, const float* da, int np, int64_t stride, int T, int I, bf16* dz, float* dbias,
+                     float* part, hipStream_t s);
+// dP [P][D] = the sum over the sequences of dx's row at each position (learned
+// positions; zero where no sequence reaches), D % 4 == 0
+void launch_position_bwd(const float* dx, const int32_t* cu, int nseq, int D, int P, float* dP, hipStream_t s);
 // dE [V][D] += the tokens' rows of dx [T][D]; clear: dE = 0 first (D % 4 == 0)
 void launch_embed_bwd(const int32_t* tok, const float* dx, int T, int D, int V, float* dE, bool clear, hipStream_t s);
 
