@@ -112,64 +112,67 @@ AXON_DEV bf16x8 read_tr8(const bf16* lo_p, const bf16* hi_p) {
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// Eight consecutive elements c .. c + 7 of a row of n, as float32; past the row's
-// end ``fill`` (read), or nothing (written).  The row may start at any element: the
-// wide accesses ask for no more than the element's own alignment, which global
-// memory instructions allow.
+// Eight consecutive elements of a row as they are stored (one or two 16-byte
+// registers' worth).  A row may start at any element: the wide accesses ask for no more
+// than the element's own alignment, which global memory instructions allow (rows off
+// by 4 bytes or more cost nothing; by 2 bytes, 10-20%).
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef bf16x8 bf16x8_any __attribute__((aligned(2)));
-AXON_DEV void load_run8(const float* row, int c, int n, float (&v)[8], float fill) {
-  if (c + 8 <= n) {
-    const f32x4 a = *(const f32x4_any*)(row + c), b = *(const f32x4_any*)(row + c + 4);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = a[j];
-      v[4 + j] = b[j];
-    }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? row[c + j] : fill;
+template <typename T>
+struct Run8;
+template <>
+struct Run8<float> {
+  f32x4 lo, hi;
+  AXON_DEV float operator[](int j) const { return j < 4 ? lo[j & 3] : hi[j & 3]; }
+  AXON_DEV void load(const float* p) {
+    lo = *(const f32x4_any*)p;
+    hi = *(const f32x4_any*)(p + 4);
   }
-}
-AXON_DEV void load_run8(const bf16* row, int c, int n, float (&v)[8], float fill) {
-  if (c + 8 <= n) {
-    const bf16x8 a = *(const bf16x8_any*)(row + c);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = (float)a[j];
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? (float)row[c + j] : fill;
+  AXON_DEV void fill(float x) { lo = hi = f32x4{x, x, x, x}; }
+  static AXON_DEV void store(float* p, const float (&v)[8]) {
+    *(f32x4_any*)p = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4_any*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
   }
-}
-AXON_DEV void store_run8(float* row, int c, int n, const float (&v)[8]) {
-  if (c + 8 <= n) {
-    *(f32x4_any*)(row + c) = f32x4{v[0], v[1], v[2], v[3]};
-    *(f32x4_any*)(row + c + 4) = f32x4{v[4], v[5], v[6], v[7]};
-  } else {
+};
+template <>
+struct Run8<bf16> {
+  bf16x8 v;
+  AXON_DEV float operator[](int j) const { return (float)v[j]; }
+  AXON_DEV void load(const bf16* p) { v = *(const bf16x8_any*)p; }
+  AXON_DEV void fill(float x) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < n) row[c + j] = v[j];
+    for (int j = 0; j < 8; ++j) v[j] = (bf16)x;
   }
-}
-AXON_DEV void store_run8(bf16* base, int64_t at, const float (&v)[8]) {  // 16-byte aligned
-  bf16x8 o;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) o[j] = (bf16)v[j];
-  *(bf16x8*)(base + at) = o;
-}
-AXON_DEV void store_run8(bf16* row, int c, int n, const float (&v)[8]) {
-  if (c + 8 <= n) {
+  static AXON_DEV void store(bf16* p, const float (&v)[8]) {
     bf16x8 o;
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = (bf16)v[j];
-    *(bf16x8_any*)(row + c) = o;
+    *(bf16x8_any*)p = o;
+  }
+};
+// columns c .. c + 7 of a row of n as float32, ``fill`` past its end
+template <typename T>
+AXON_DEV void load_run8(const T* row, int c, int n, float (&v)[8], float fill) {
+  if (c + 8 <= n) {
+    Run8<T> r;
+    r.load(row + c);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = r[j];
   } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (c + j < n) row[c + j] = (bf16)v[j];
+    for (int j = 0; j < 8; ++j) v[j] = c + j < n ? to_f32(row[c + j]) : fill;
   }
 }
-
+template <typename T>
+AXON_DEV void store_run8(T* row, int c, int n, const float (&v)[8]) {
+  if (c + 8 <= n) {
+    Run8<T>::store(row + c, v);
+  } else if (c < n) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c + j < n) row[c + j] = from_f32<T>(v[j]);
+  }
+}
 // Block-wide sum for blockDim.x a multiple of 64 (<= 1024); every thread gets the result.
 AXON_DEV float block_sum(float v, float* red /* >= 16 floats of shared memory */) {
   v = wave_sum(v);

@@ -117,258 +117,432 @@ void launch_layernorm(const float* x, const bf16* g, const bf16* beta, bf16* h, 
 // TPR threads share a row (a wavefront's 64, or a workgroup's 256 to 1024) and keep
 // it in registers as NV groups of 8 consecutive columns each: group v of thread i
 // starts at column (v * TPR + i) * 8, so a row is read once, 16 bytes a lane and
-// load.  Rows may start at any element (their stride and width are free): the wide
-// loads ask for the element's alignment only, and the group that runs past the
-// row's end is read and written one element at a time.
+// load.  Rows may start at any element (their stride and width are free); of a width
+// that is no multiple of 8 (ODD) the last few columns go to one thread each.  Every
+// load is unconditional: threads past the row's end read its last columns again, which
+// then count nothing.  (A load under a branch whose other arm fills the same registers
+// is waited for there: nothing stays in flight.  Backward of 16384 x 8184 took 225 us
+// that way, of 8192 columns 158.)
+//
+// A row's sums cost one exchange between its wavefronts: each takes the mean of its
+// own columns first and its sums around that, and the joined ones follow from the
+// wavefronts' (n_w columns, mean m_w, sum of squares Q_w around m_w):
+//   mean = sum n_w m_w / n,  Q = sum Q_w + n_w (m_w - mean)^2,
+// so nothing is lost to a common offset of the row, as a sum of x^2 would lose it.
 
-// sum over the TPR threads of a row, in every one of them; red: 16 floats per use
-// that no earlier use still reads
-template <int TPR>
-AXON_DEV float row_sum(float v, float* red) {
-  v = wave_sum(v);
-  if constexpr (TPR == 64) return v;
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float s = 0.f;
+// what a thread holds of a row, and which of it counts
+template <typename T, int NV, bool ODD>
+struct RowRegs {
+  Run8<T> g[NV];
+  T t;  // ODD: one of the last cols % 8 columns
+};
+template <int TPR, int NV, bool ODD>
+struct RowCols {
+  int i, cols, whole;  // thread of the row; columns; those in groups of 8
+  AXON_DEV explicit RowCols(int cols) : i(threadIdx.x % TPR), cols(cols), whole(ODD ? cols & ~7 : cols) {}
+  AXON_DEV int at(int n) const { return (n * TPR + i) * 8; }
+  AXON_DEV bool on(int n) const { return at(n) < whole; }
+  AXON_DEV int tail() const { return whole + i; }
+  AXON_DEV bool tail_on() const { return tail() < cols; }
+  template <typename T>
+  AXON_DEV void load(RowRegs<T, NV, ODD>& r, const T* row) const {
 #pragma unroll
-  for (int i = 0; i < TPR / 64; ++i) s += red[i];
+    for (int n = 0; n < NV; ++n)
+      if (!ODD || whole > 0) r.g[n].load(row + min(at(n), whole - 8));
+      else r.g[n].fill(0.f);  // (a row of fewer than 8 columns)
+    if constexpr (ODD) r.t = row[min(tail(), cols - 1)];
+  }
+  // zero in what does not count, for factors that are kept
+  template <typename T>
+  AXON_DEV void mask(RowRegs<T, NV, ODD>& r) const {
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if (!on(n)) r.g[n].fill(0.f);
+    if constexpr (ODD)
+      if (!tail_on()) r.t = from_f32<T>(0.f);
+  }
+  template <typename T>
+  AXON_DEV void store(T* row, const float (&v)[NV][8], float t) const {
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if (on(n)) Run8<T>::store(row + at(n), v[n]);
+    if constexpr (ODD)
+      if (tail_on()) row[tail()] = from_f32<T>(t);
+  }
+};
+
+// a wavefront's sums over its columns of a row, h and hd for the backward pass only:
+// mean, sum (x - mean)^2, sum h, sum h (x - mean)
+struct __align__(16) RowSums {
+  float mean, q, h, hd;
+};
+// what depends on the row's width alone, and the exchange.  Lane l joins what
+// wavefront l % NW left: one 16-byte LDS read and log2 NW register moves a sum.
+template <int TPR, int NV, bool ODD>
+struct RowShape {
+  static constexpr int NW = TPR / 64;
+  float own;    // columns of this wavefront, at least 1
+  float other;  // columns of wavefront lane % NW
+  float all;    // columns of the row
+  AXON_DEV explicit RowShape(int cols) {
+    const int whole = ODD ? cols & ~7 : cols;
+    auto count = [&](int wave) {
+      int c = wave == 0 ? cols - whole : 0;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) c += min(512, max(0, whole - (v * TPR + wave * 64) * 8));
+      return (float)c;
+    };
+    own = fmaxf(count((threadIdx.x >> 6) % NW), 1.f);
+    other = count(threadIdx.x % NW);
+    all = (float)cols;
+  }
+  // over the lanes that differ in lane % NW; every lane the same result (see wave_sum)
+  static AXON_DEV float over_waves(float v) {
+    if constexpr (NW > 1) v += dpp_move<0xB1>(v);
+    if constexpr (NW > 2) v += dpp_move<0x4E>(v);
+    if constexpr (NW > 4) v += dpp_move<0x141>(v);
+    if constexpr (NW > 8) v += dpp_move<0x140>(v);
+    return v;
+  }
+  // the whole row's sums, around its mean, in every thread.  red: a slot per wavefront
+  // that no wavefront may still read from an earlier call
+  template <bool BWD>
+  AXON_DEV RowSums join(RowSums w, RowSums* red) const {
+    if constexpr (NW == 1) return w;
+    if ((threadIdx.x & 63) == 0) red[(threadIdx.x >> 6) % NW] = w;
+    __syncthreads();
+    const RowSums p = red[threadIdx.x % NW];
+    RowSums r{};
+    r.mean = over_waves(other * p.mean) / all;
+    const float d = p.mean - r.mean;
+    r.q = over_waves(p.q + other * d * d);
+    if (BWD) {
+      r.h = over_waves(p.h);
+      r.hd = over_waves(p.hd + d * p.h);
+    }
+    return r;
+  }
+};
+
+// sums of a thread's columns: x, and around a mean (x - mean)^2
+template <int TPR, int NV, bool ODD>
+AXON_DEV float sum_cols(const RowCols<TPR, NV, ODD>& rc, const float (&v)[NV][8], float t) {
+  float s = ODD && rc.tail_on() ? t : 0.f;
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    float g = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g += v[n][j];
+    s += rc.on(n) ? g : 0.f;
+  }
+  return s;
+}
+template <int TPR, int NV, bool ODD>
+AXON_DEV float square_cols(const RowCols<TPR, NV, ODD>& rc, const float (&v)[NV][8], float t, float mean) {
+  float s = ODD && rc.tail_on() ? (t - mean) * (t - mean) : 0.f;
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    float g = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g += (v[n][j] - mean) * (v[n][j] - mean);
+    s += rc.on(n) ? g : 0.f;
+  }
   return s;
 }
 
-// y = (x - mean) rstd g + b, one row per TPR threads.  The mean first, then the
-// variance around it, both from registers: no cancellation, one read of x.
-template <typename TX, typename TY, typename TP, int TPR, int NV>
+// y = (x - mean) rstd g + b, one row per TPR threads.  HBM bound.  The workgroups
+// stay for several rows: g and b are loaded once, and the next row's loads are under
+// way while this one is reduced.
+template <typename TX, typename TY, typename TP, int TPR, int NV, bool ODD>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
     ln_fwd_kernel(const TX* x, int64_t ldx, const TP* __restrict__ g, const TP* __restrict__ b, float eps, TY* y,
                   int64_t ldy, int64_t rows, int cols) {
   constexpr int RPW = TPR < 256 ? 256 / TPR : 1;  // rows of a workgroup
-  __shared__ float red[2][16];
-  const int i = threadIdx.x % TPR;
+  __shared__ RowSums red[2][16];
+  const RowCols<TPR, NV, ODD> rc(cols);
+  const RowShape<TPR, NV, ODD> shape(cols);
+  RowRegs<TP, NV, ODD> gv, bv;
+  RowRegs<TX, NV, ODD> next;
+  rc.load(gv, g);
+  rc.load(bv, b ? b : g);
   // wave-uniform trip count: with TPR > 64 the whole workgroup shares the row
-  for (int64_t r = (int64_t)blockIdx.x * RPW + threadIdx.x / TPR; r < rows; r += (int64_t)gridDim.x * RPW) {
-    float v[NV][8];
-    float s = 0.f;
-#pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      load_run8(x + r * ldx, (n * TPR + i) * 8, cols, v[n], 0.f);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s += v[n][j];
-    }
-    const float mean = row_sum<TPR>(s, red[0]) / (float)cols;
-    float q = 0.f;
+  const int64_t step = (int64_t)gridDim.x * RPW;
+  int64_t r = (int64_t)blockIdx.x * RPW + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  if (r < rows) rc.load(next, x + r * ldx);
+  for (int par = 0; r < rows; r += step, par ^= 1) {
+    float v[NV][8], t = 0.f;
 #pragma unroll
     for (int n = 0; n < NV; ++n)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float d = v[n][j] - mean;
-        v[n][j] = d;
-        q += (n * TPR + i) * 8 + j < cols ? d * d : 0.f;
-      }
-    const float rstd = 1.f / sqrtf(row_sum<TPR>(q, red[1]) / (float)cols + eps);
+      for (int j = 0; j < 8; ++j) v[n][j] = next.g[n][j];
+    if constexpr (ODD) t = to_f32(next.t);
+    if (r + step < rows) rc.load(next, x + (r + step) * ldx);
+    RowSums w{};
+    w.mean = wave_sum(sum_cols(rc, v, t)) / shape.own;
+    w.q = wave_sum(square_cols(rc, v, t, w.mean));
+    w = shape.template join<false>(w, red[par]);
+    const float rstd = rsqrtf(w.q / shape.all + eps);
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      const int c = (n * TPR + i) * 8;
-      if (c >= cols) continue;
-      float gv[8], bv[8] = {};
-      load_run8(g, c, cols, gv, 0.f);
-      if (b) load_run8(b, c, cols, bv, 0.f);
+    for (int n = 0; n < NV; ++n)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[n][j] = v[n][j] * rstd * gv[j] + bv[j];
-      store_run8(y + r * ldy, c, cols, v[n]);
-    }
+      for (int j = 0; j < 8; ++j) v[n][j] = (v[n][j] - w.mean) * rstd * gv.g[n][j] + (b ? bv.g[n][j] : 0.f);
+    if constexpr (ODD) t = (t - w.mean) * rstd * to_f32(gv.t) + (b ? to_f32(bv.t) : 0.f);
+    rc.store(y + r * ldy, v, t);
   }
 }
 
 // Backward of y = (x - mean) rstd g + b.  With h = dy g and d = x - mean:
 //   dx = rstd h - rstd mean(h) - d rstd^3 mean(h d),  dg = sum dy d rstd,  db = sum dy
 // (sums over the rows).  The statistics are taken from x again, which is read
-// anyway.  HBM bound.  A workgroup takes ``per`` rows in turn, TPR threads a row,
+// anyway.  HBM bound.  A workgroup takes every n-th row, TPR threads a row,
 // every thread the same columns of each, so dg and db stay in registers until the
-// workgroup leaves one partial row [2 cols] for the column sum; up to 8192 columns
-// the next row's operands are loaded before this row's reductions.
+// workgroup leaves one partial row [2 cols] for the column sum.  The next row's
+// operands are loaded before this row's reductions where registers allow it.
 //
 // TRAIN, the training step's form (float rows): dy is the sum of tr.np split-K
 // partials in order; tr.accumulate: dx += instead of =; the new dx goes to tr.dxb in
 // bf16 too (row-pair layout, the next projections' operand), and its column sums,
 // the gradient of the bias that was added to the residual there, are a third
 // part of the partial row [3 cols].
-template <typename TX, typename TD, typename TP, int TPR, int NV, bool TRAIN>
+constexpr bool ln_ahead(int tpr, int nv) { return nv == 1 || (tpr > 64 && tpr < 1024); }
+
+template <typename TX, typename TD, typename TP, int TPR, int NV, bool ODD, bool TRAIN>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
     ln_bwd_kernel(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const TP* __restrict__ g, float eps, TX* dx,
-                  int64_t lddx, float* __restrict__ part, int64_t rows, int cols, int64_t per, LnTrain tr) {
+                  int64_t lddx, float* __restrict__ part, int64_t rows, int cols, LnTrain tr) {
   constexpr int RPW = TPR < 256 ? 256 / TPR : 1, SUMS = TRAIN ? 3 : 2;
-  __shared__ float red[2][4][16];
-  const int i = threadIdx.x % TPR;
-  const int64_t r1 = min(rows, ((int64_t)blockIdx.x + 1) * per);
-  float gv[NV][8], dg[NV][8] = {}, db[NV][8] = {}, dr[NV][8] = {}, xn[NV][8], dn[NV][8], an[NV][8];
-#pragma unroll
-  for (int n = 0; n < NV; ++n) load_run8(g, (n * TPR + i) * 8, cols, gv[n], 0.f);
+  constexpr bool AHEAD = ln_ahead(TPR, NV);
+  __shared__ RowSums red[2][16];
+  const RowCols<TPR, NV, ODD> rc(cols);
+  const RowShape<TPR, NV, ODD> shape(cols);
+  RowRegs<TP, NV, ODD> gv;
+  RowRegs<TX, NV, ODD> xn, an;
+  RowRegs<TD, NV, ODD> dn;
+  float dg[NV][8] = {}, db[NV][8] = {}, dr[NV][8] = {}, more[NV][8], dgt = 0.f, dbt = 0.f;
+  rc.load(gv, g);
+  rc.mask(gv);
+  const int64_t step = (int64_t)gridDim.x * RPW;  // neighbouring rows at one time, over the chip
   auto load = [&](int64_t r) {
+    rc.load(xn, x + r * ldx);
+    rc.load(dn, dy + r * lddy);
+    if constexpr (TRAIN) {
+      if (tr.accumulate) rc.load(an, (const TX*)dx + r * lddx);
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      load_run8(x + r * ldx, (n * TPR + i) * 8, cols, xn[n], 0.f);
-      load_run8(dy + r * lddy, (n * TPR + i) * 8, cols, dn[n], 0.f);
-      if constexpr (TRAIN) {
+      for (int n = 0; n < NV; ++n)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) an[n][j] = 0.f;
-        if (tr.accumulate) load_run8(dx + r * lddx, (n * TPR + i) * 8, cols, an[n], 0.f);
+        for (int j = 0; j < 8; ++j) more[n][j] = 0.f;
+      for (int p = 1; p < tr.np; ++p) {
+        RowRegs<TD, NV, ODD> q;
+        rc.load(q, dy + p * tr.stride + r * lddy);
+#pragma unroll
+        for (int n = 0; n < NV; ++n)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) more[n][j] += q.g[n][j];
       }
     }
-    if constexpr (TRAIN)
-      for (int p = 1; p < tr.np; ++p)
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          float more[8];
-          load_run8(dy + p * tr.stride + r * lddy, (n * TPR + i) * 8, cols, more, 0.f);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) dn[n][j] += more[j];
-        }
   };
-  int64_t r = (int64_t)blockIdx.x * per + threadIdx.x / TPR;
-  constexpr bool AHEAD = NV == 1;  // the registers of two rows at once, 128 a thread at most
-  if (AHEAD && r < r1) load(r);
-  for (int par = 0; r < r1; r += RPW, par ^= 1) {
-    float d[NV][8], e[NV][8], a[NV][8];
-    float s = 0.f;
+  int64_t r = (int64_t)blockIdx.x * RPW + __builtin_amdgcn_readfirstlane(threadIdx.x / TPR);
+  if (AHEAD && r < rows) load(r);
+  for (int par = 0; r < rows; r += step, par ^= 1) {
+    float d[NV][8], e[NV][8], a[NV][8], dt = 0.f, et = 0.f;
     if (!AHEAD) load(r);
 #pragma unroll
     for (int n = 0; n < NV; ++n)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        d[n][j] = xn[n][j];
-        e[n][j] = dn[n][j];
-        a[n][j] = TRAIN ? an[n][j] : 0.f;
-        s += d[n][j];
+        d[n][j] = xn.g[n][j];
+        e[n][j] = dn.g[n][j] + (TRAIN ? more[n][j] : 0.f);
+        a[n][j] = TRAIN && tr.accumulate ? an.g[n][j] : 0.f;
       }
-    if (AHEAD && r + RPW < r1) load(r + RPW);
-    const float mean = row_sum<TPR>(s, red[par][0]) / (float)cols;
-    float q = 0.f, sh = 0.f, shd = 0.f;
+    if constexpr (ODD) {
+      dt = to_f32(xn.t);
+      et = to_f32(dn.t);
+    }
+    if (AHEAD && r + step < rows) load(r + step);
+    RowSums w{};
+    w.mean = wave_sum(sum_cols(rc, d, dt)) / shape.own;
+    w.q = wave_sum(square_cols(rc, d, dt, w.mean));
 #pragma unroll
     for (int n = 0; n < NV; ++n)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {  // past the row: g = dy = 0
-        d[n][j] -= mean;
-        const float h = e[n][j] * gv[n][j];
-        q += (n * TPR + i) * 8 + j < cols ? d[n][j] * d[n][j] : 0.f;
-        sh += h;
-        shd += h * d[n][j];
+      for (int j = 0; j < 8; ++j) {  // past the row: g = 0
+        const float h = e[n][j] * gv.g[n][j];
+        w.h += h;
+        w.hd += h * (d[n][j] - w.mean);
       }
-    q = wave_sum(q);
-    sh = wave_sum(sh);
-    shd = wave_sum(shd);
-    if constexpr (TPR > 64) {
-      if ((threadIdx.x & 63) == 0) {
-        red[par][1][threadIdx.x >> 6] = q;
-        red[par][2][threadIdx.x >> 6] = sh;
-        red[par][3][threadIdx.x >> 6] = shd;
-      }
-      __syncthreads();
-      q = sh = shd = 0.f;
-#pragma unroll
-      for (int w = 0; w < TPR / 64; ++w) {
-        q += red[par][1][w];
-        sh += red[par][2][w];
-        shd += red[par][3][w];
-      }
+    if constexpr (ODD) {
+      const float h = et * to_f32(gv.t);
+      w.h += h;
+      w.hd += h * (dt - w.mean);
     }
-    const float rstd = 1.f / sqrtf(q / (float)cols + eps);
-    const float mh = sh / (float)cols, k = rstd * rstd * (shd / (float)cols);
+    w.h = wave_sum(w.h);
+    w.hd = wave_sum(w.hd);
+    w = shape.template join<true>(w, red[par]);
+    const float per_col = 1.f / shape.all;
+    const float rstd = rsqrtf(w.q * per_col + eps);
+    const float mh = w.h * per_col, k = rstd * rstd * (w.hd * per_col);
 #pragma unroll
-    for (int n = 0; n < NV; ++n) {
-      float o[8];
+    for (int n = 0; n < NV; ++n)
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        o[j] = rstd * (e[n][j] * gv[n][j] - mh - d[n][j] * k);
-        if (TRAIN) o[j] += a[n][j];
-        dg[n][j] += e[n][j] * (d[n][j] * rstd);
+        const float c = d[n][j] - w.mean;
+        d[n][j] = rstd * (e[n][j] * gv.g[n][j] - mh - c * k);
+        if (TRAIN) d[n][j] += a[n][j];
+        dg[n][j] += e[n][j] * (c * rstd);
         db[n][j] += e[n][j];
-        dr[n][j] += TRAIN && (n * TPR + i) * 8 < cols ? o[j] : 0.f;  // (TRAIN: cols a multiple of 32)
+        if (TRAIN) dr[n][j] += d[n][j];
       }
-      store_run8(dx + r * lddx, (n * TPR + i) * 8, cols, o);
-      if constexpr (TRAIN)
-        if ((n * TPR + i) * 8 < cols) store_run8(tr.dxb, xp_off(r, (n * TPR + i) * 8, cols), o);
+    if constexpr (ODD) {
+      const float c = dt - w.mean;
+      dt = rstd * (et * to_f32(gv.t) - mh - c * k);
+      dgt += et * (c * rstd);
+      dbt += et;
     }
+    rc.store(dx + r * lddx, d, dt);
+    if constexpr (TRAIN)
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        if (rc.on(n)) Run8<bf16>::store(tr.dxb + xp_off(r, rc.at(n), cols), d[n]);
   }
   float* out = part + (int64_t)blockIdx.x * SUMS * cols;
-  if constexpr (RPW > 1) {  // the wavefronts' shares in order
-    static_assert(RPW == 4 && NV == 1, "one group of columns a lane");
-    __shared__ float sums[3][64][SUMS * 8 + 1];
-    const int w = threadIdx.x / TPR;
-    if (w > 0)
+  if constexpr (RPW > 1) {  // the wavefronts' shares in order, a group of columns at a time
+    __shared__ float sums[RPW - 1][64][SUMS * 8 + 3];
+    const int w = threadIdx.x / TPR, i = rc.i;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sums[w - 1][i][j] = dg[0][j];
-        sums[w - 1][i][8 + j] = db[0][j];
-        if (TRAIN) sums[w - 1][i][SUMS * 8 - 8 + j] = dr[0][j];
+    for (int n = 0; n < NV; ++n) {
+      if (n > 0) __syncthreads();
+      if (w > 0) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          sums[w - 1][i][j] = dg[n][j];
+          sums[w - 1][i][8 + j] = db[n][j];
+          if (TRAIN) sums[w - 1][i][SUMS * 8 - 8 + j] = dr[n][j];
+        }
+        sums[w - 1][i][SUMS * 8] = dgt;
+        sums[w - 1][i][SUMS * 8 + 1] = dbt;
       }
-    __syncthreads();
+      __syncthreads();
+      if (w == 0)
+        for (int k = 0; k < RPW - 1; ++k) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            dg[n][j] += sums[k][i][j];
+            db[n][j] += sums[k][i][8 + j];
+            if (TRAIN) dr[n][j] += sums[k][i][SUMS * 8 - 8 + j];
+          }
+          if (n == 0) {
+            dgt += sums[k][i][SUMS * 8];
+            dbt += sums[k][i][SUMS * 8 + 1];
+          }
+        }
+    }
     if (w > 0) return;
-    for (int k = 0; k < 3; ++k)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        dg[0][j] += sums[k][i][j];
-        db[0][j] += sums[k][i][8 + j];
-        if (TRAIN) dr[0][j] += sums[k][i][SUMS * 8 - 8 + j];
-      }
   }
+  rc.store(out, dg, dgt);
+  rc.store(out + cols, db, dbt);
+  if (TRAIN) rc.store(out + 2 * cols, dr, 0.f);
+}
+
+// Column c of part [n][C] summed in a fixed order: 64 interleaved groups of rows, then
+// the groups in order, 16 columns a workgroup, so that a narrow layer norm's few
+// columns still make a hundred workgroups.  Columns below c1 go to d0, below c2 to d1,
+// the rest to d2; a null one is not written.
+__global__ void __launch_bounds__(1024) ln_colsum_kernel(const float* __restrict__ part, int n, int C,
+                                                         float* __restrict__ d0, int c1, float* __restrict__ d1, int c2,
+                                                         float* __restrict__ d2) {
+  __shared__ float sums[64][17];
+  const int lane = threadIdx.x & 15, grp = threadIdx.x >> 4, c = blockIdx.x * 16 + lane;
+  float s = 0.f;
+  if (c < C)
+    for (int i0 = grp; i0 < n; i0 += 64 * 8) {
+      float v[8];
 #pragma unroll
-  for (int n = 0; n < NV; ++n) {
-    store_run8(out, (n * TPR + i) * 8, cols, dg[n]);
-    store_run8(out + cols, (n * TPR + i) * 8, cols, db[n]);
-    if (TRAIN) store_run8(out + 2 * cols, (n * TPR + i) * 8, cols, dr[n]);
-  }
+      for (int q = 0; q < 8; ++q) v[q] = i0 + q * 64 < n ? part[(int64_t)(i0 + q * 64) * C + c] : 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) s += v[q];
+    }
+  sums[grp][lane] = s;
+  __syncthreads();
+  if (grp > 0 || c >= C) return;
+  s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 64; ++i) s += sums[i][lane];
+  if (c < c1) d0[c] = s;
+  else if (c < c2) d1[c - c1] = s;
+  else if (d2) d2[c - c2] = s;
 }
 
 namespace {
 
-// calls f(integral_constant TPR, integral_constant NV) for rows of ``cols``
+void ln_colsum(const float* part, int n, int C, float* d0, int c1, float* d1, int c2, float* d2, hipStream_t s) {
+  ln_colsum_kernel<<<(C + 15) / 16, 1024, 0, s>>>(part, n, C, d0, c1, d1, c2, d2);
+}
+
+// f(threads of a row, groups of 8 columns a thread, most workgroups) for rows of
+// ``cols``, each a compile-time constant
 template <int V>
 struct Int {
   static constexpr int value = V;
 };
 
+// Threads by what a wavefront can hold without spilling; workgroups by what still
+// fills the chip (each holds g and b, and in the backward pass leaves a partial row, so
+// not more).  bf16, TB/s: forward 65536 x 384 5.3, 32768 x 768 5.7 (TPR 256: 3.9), 16384 x
+// 4096 5.9, 16384 x 8192 6.0; backward 4.8, 4.8 (TPR 256: 1.7), 5.4, 5.5.  float32
+// rows with bf16 outputs of 8192 x 1600: 6.2 and 4.8.
 template <typename F>
 void ln_fwd_shape(int cols, F&& f) {
-  if (cols <= 512) f(Int<64>{}, Int<1>{});
-  else if (cols <= 1024) f(Int<64>{}, Int<2>{});
-  else if (cols <= 2048) f(Int<256>{}, Int<1>{});
-  else if (cols <= 4096) f(Int<256>{}, Int<2>{});
-  else if (cols <= 8192) f(Int<512>{}, Int<2>{});
-  else f(Int<1024>{}, Int<2>{});
+  if (cols <= 512) f(Int<64>{}, Int<1>{}, 2048);
+  else if (cols <= 1024) f(Int<64>{}, Int<2>{}, 3072);
+  else if (cols <= 2048) f(Int<64>{}, Int<4>{}, 512);
+  else if (cols <= 4096) f(Int<256>{}, Int<2>{}, 16384);
+  else if (cols <= 8192) f(Int<512>{}, Int<2>{}, 16384);
+  else f(Int<1024>{}, Int<2>{}, 16384);
 }
 
 template <typename F>
 void ln_bwd_shape(int cols, F&& f) {
-  if (cols <= 512) f(Int<64>{}, Int<1>{});
-  else if (cols <= 2048) f(Int<256>{}, Int<1>{});
-  else if (cols <= 4096) f(Int<512>{}, Int<1>{});
-  else if (cols <= 8192) f(Int<1024>{}, Int<1>{});
-  else f(Int<1024>{}, Int<2>{});
+  if (cols <= 512) f(Int<64>{}, Int<1>{}, 1024);
+  else if (cols <= 1024) f(Int<64>{}, Int<2>{}, 1024);
+  else if (cols <= 2048) f(Int<64>{}, Int<4>{}, 256);
+  else if (cols <= 4096) f(Int<256>{}, Int<2>{}, 256);
+  else if (cols <= 8192) f(Int<512>{}, Int<2>{}, 256);
+  else f(Int<1024>{}, Int<2>{}, 256);
+}
+// the training step's form keeps a third sum of the columns: one group a thread
+template <typename F>
+void ln_train_shape(int cols, F&& f) {
+  if (cols <= 512) f(Int<64>{}, Int<1>{}, ROW_PARTS);
+  else if (cols <= 2048) f(Int<256>{}, Int<1>{}, ROW_PARTS);
+  else if (cols <= 4096) f(Int<512>{}, Int<1>{}, ROW_PARTS);
+  else f(Int<1024>{}, Int<1>{}, ROW_PARTS);
 }
 
-// rows of a workgroup of the backward kernel and the workgroups that leaves
-int64_t ln_bwd_per(int64_t rows, int cols) {
-  const int64_t step = cols <= 512 ? 4 : 1;  // rows a workgroup takes at once
-  const int64_t per = (rows + ROW_PARTS - 1) / ROW_PARTS;
-  return std::max(step, (per + step - 1) / step * step);
+// workgroups for ``rows`` at ``tpr`` threads each, at most ``most``: as many rows for each
+unsigned ln_wgs(int64_t rows, int tpr, int most) {
+  const int at_once = tpr < 256 ? 256 / tpr : 1;
+  const int64_t turns = (rows + at_once - 1) / at_once, each = (turns + most - 1) / most;
+  return (unsigned)((turns + each - 1) / each);
 }
 
 }  // namespace
 
 int64_t ln_bwd_part_floats(int64_t rows, int cols) {
-  const int64_t per = ln_bwd_per(rows, cols);
-  return (rows + per - 1) / per * 2 * cols;
+  int64_t n = 0;
+  ln_bwd_shape(cols, [&](auto tpr, auto, int most) { n = ln_wgs(rows, decltype(tpr)::value, most); });
+  return n * 2 * cols;
 }
 
 template <typename TX, typename TY, typename TP>
 void launch_ln_fwd(const TX* x, int64_t ldx, const TP* g, const TP* b, float eps, TY* y, int64_t ldy, int64_t rows,
                    int cols, hipStream_t s) {
   if (rows <= 0) return;
-  ln_fwd_shape(cols, [&](auto tpr, auto nv) {
-    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, RPW = TPR < 256 ? 256 / TPR : 1;
-    const int64_t wgs = std::min<int64_t>((rows + RPW - 1) / RPW, 1 << 20);
-    ln_fwd_kernel<TX, TY, TP, TPR, NV>
-        <<<(unsigned)wgs, TPR < 256 ? 256 : TPR, 0, s>>>(x, ldx, g, b, eps, y, ldy, rows, cols);
+  ln_fwd_shape(cols, [&](auto tpr, auto nv, int most) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+    auto go = [&](auto kern) {
+      kern<<<ln_wgs(rows, TPR, most), TPR < 256 ? 256 : TPR, 0, s>>>(x, ldx, g, b, eps, y, ldy, rows, cols);
+    };
+    cols % 8 ? go(ln_fwd_kernel<TX, TY, TP, TPR, NV, true>) : go(ln_fwd_kernel<TX, TY, TP, TPR, NV, false>);
   });
 }
 
@@ -380,26 +554,27 @@ void launch_ln_bwd(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const T
     if (db) launch_zero_i32((int32_t*)db, cols, s);
     return;
   }
-  const int64_t per = ln_bwd_per(rows, cols), n = (rows + per - 1) / per;
-  ln_bwd_shape(cols, [&](auto tpr, auto nv) {
+  ln_bwd_shape(cols, [&](auto tpr, auto nv, int most) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-    ln_bwd_kernel<TX, TD, TP, TPR, NV, false><<<(unsigned)n, TPR < 256 ? 256 : TPR, 0, s>>>(
-        x, ldx, dy, lddy, g, eps, dx, lddx, part, rows, cols, per, LnTrain{});
+    const unsigned n = ln_wgs(rows, TPR, most);
+    auto go = [&](auto kern) {
+      kern<<<n, TPR < 256 ? 256 : TPR, 0, s>>>(x, ldx, dy, lddy, g, eps, dx, lddx, part, rows, cols, LnTrain{});
+    };
+    cols % 8 ? go(ln_bwd_kernel<TX, TD, TP, TPR, NV, true, false>) : go(ln_bwd_kernel<TX, TD, TP, TPR, NV, false, false>);
+    ln_colsum(part, (int)n, 2 * cols, dg, cols, db, db ? 2 * cols : cols, nullptr, s);
   });
-  launch_colsum_final(part, (int)n, 2 * cols, dg, cols, db, db ? 2 * cols : cols, nullptr, s);
 }
 
 void launch_ln_bwd_train(const float* x, const bf16* g, const float* dy, const LnTrain& tr, int T, int D, float eps,
                          float* dx, float* dg, float* db, float* dres, float* part, hipStream_t s) {
   if (T <= 0) return;
-  const int64_t per = ln_bwd_per(T, D), n = (T + per - 1) / per;
-  ln_bwd_shape(D, [&](auto tpr, auto nv) {
+  ln_train_shape(D, [&](auto tpr, auto nv, int most) {
     constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
-    if constexpr (NV == 1)  // D <= 8192
-      ln_bwd_kernel<float, float, bf16, TPR, NV, true><<<(unsigned)n, TPR < 256 ? 256 : TPR, 0, s>>>(
-          x, D, dy, D, g, eps, dx, D, part, T, D, per, tr);
+    const unsigned n = ln_wgs(T, TPR, most);
+    ln_bwd_kernel<float, float, bf16, TPR, NV, false, true><<<n, TPR < 256 ? 256 : TPR, 0, s>>>(x, D, dy, D, g, eps, dx, D,
+                                                                                        part, T, D, tr);
+    ln_colsum(part, (int)n, 3 * D, dg, D, db, 2 * D, dres, s);
   });
-  launch_colsum_final(part, (int)n, 3 * D, dg, D, db, 2 * D, dres, s);
 }
 
 #define LN_INSTANCE(TX, TY, TP)                                                                                  \

@@ -37,6 +37,53 @@ AXON_DEV void join_part(float& m, float& s, float m2, float s2) {
   m = top;
 }
 
+// exp(v - m) for many v and one m as 2^(v log2 e - m log2 e): one fused multiply-add
+// and the hardware exponential.  m log2 e is rounded, which scales every result by
+// the same 2^d; ``fix`` = 2^-d undoes it once, on the sum.  Where m log2 e may
+// overflow (``low``: a row or slice of nothing but the type's lowest values, or
+// -infinity), the difference is taken first.
+struct ExpFrom {
+  static constexpr float L = 1.4426950408889634f;
+  float m, base, fix;
+  bool low;
+  AXON_DEV explicit ExpFrom(float top) {
+    m = top == -INFINITY ? 0.f : top;  // -inf - (-inf) is not a number
+    low = m < -2e38f;
+    base = low ? 0.f : m * L;
+    fix = low ? 1.f : 1.f - fmaf(m, L, -base) * 0.6931471805599453f;
+  }
+  template <int N>
+  AXON_DEV void operator()(float (&v)[N]) const {
+    if (!low) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = __builtin_amdgcn_exp2f(fmaf(v[j], L, -base));
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = __builtin_amdgcn_exp2f((v[j] - m) * L);
+    }
+  }
+};
+
+// N groups of 8 logits into a thread's (m, s)
+template <int N>
+AXON_DEV void take_runs(float& m, float& s, float (&v)[N][8]) {
+  float top = m;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = fmaxf(top, v[k][j]);
+  const ExpFrom e(top);
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    e(v[k]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += v[k][j];
+  }
+  s = s * __expf(m - (top == -INFINITY ? 0.f : top)) + sum * e.fix;
+  m = top;
+}
+
 // One slice (of ``slices``, ``cols`` wide) of one row a workgroup: its maximum and
 // sum of exponentials.  Rows that do not count are skipped.
 template <typename T>
@@ -59,18 +106,7 @@ __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __res
       float v[PART_RUNS][8];
 #pragma unroll
       for (int k = 0; k < PART_RUNS; ++k) load_run8(row, c + k * PART_THREADS * 8, c1, v[k], -INFINITY);
-      float top = m;
-#pragma unroll
-      for (int k = 0; k < PART_RUNS; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, v[k][j]);
-      const float a = top == -INFINITY ? 0.f : top;
-      s *= __expf(m - a);
-#pragma unroll
-      for (int k = 0; k < PART_RUNS; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) s += __expf(v[k][j] - a);
-      m = top;
+      take_runs(m, s, v);
     }
     // over the workgroup: the common maximum first, then the sums scaled to it
     const float wm = wave_max(m);
@@ -273,6 +309,17 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
   }
 }
 
+// 8 logits to their gradients f exp(v - m), f = -c / S, and c more at the target, the
+// ``at``-th of them if it is one
+AXON_DEV void grad_run(float (&v)[8], const ExpFrom& e, float f, float c, int at) {
+  e(v);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] *= f;
+  if ((unsigned)at < 8u)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += j == at ? c : 0.f;
+}
+
 // dz of one slice of a row a workgroup.  z and dz may be one buffer: a thread reads
 // what it then writes.
 template <typename T, typename TO>
@@ -296,14 +343,12 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld,
     } else {
       const float2 st = stat[t];
       const int tg = targets[t];
-      const float f = -w / st.y;
+      const ExpFrom e(st.x);
+      const float f = -w / st.y * e.fix;
 #pragma unroll
       for (int k = 0; k < GRAD_RUNS; ++k) load_run8(row, c0 + k * 2048, V, v[k], 0.f);
 #pragma unroll
-      for (int k = 0; k < GRAD_RUNS; ++k)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          v[k][j] = __expf(v[k][j] - st.x) * f + (c0 + k * 2048 + j == tg ? w : 0.f);
+      for (int k = 0; k < GRAD_RUNS; ++k) grad_run(v[k], e, f, w, tg - (c0 + k * 2048));
     }
 #pragma unroll
     for (int k = 0; k < GRAD_RUNS; ++k)
@@ -362,7 +407,7 @@ __global__ void __launch_bounds__(256) logit_grad_pair_kernel(const float* __res
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     v[j] = w == 0.f || v0 + j >= V ? 0.f : __expf(v[j] - st.x) * f + (v0 + j == tg ? w : 0.f);
-  store_run8(dlog, xp_off(t, v0, ldl), v);
+  Run8<bf16>::store(dlog + xp_off(t, v0, ldl), v);
 }
 
 // ---------------------------------------------------------------- launchers

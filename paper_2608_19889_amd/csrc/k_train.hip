@@ -709,7 +709,7 @@ __global__ void __launch_bounds__(256) gelu_train_kernel(const float* __restrict
   load_run8(z + t * I, c, I, v, 0.f);
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = gelu_tanh_f(v[j]);
-  store_run8(a, xp_off(t, c, I), v);
+  Run8<bf16>::store(a + xp_off(t, c, I), v);
 }
 
 // dz = da gelu'(z), with u = sqrt(2/pi) (z + 0.044715 z^3), h = tanh(u): gelu' = (1 + h)
@@ -739,7 +739,7 @@ __global__ void __launch_bounds__(128) gelu_bwd_kernel(const float* __restrict__
       d[j] *= 0.5f * (1.f + h) + 0.5f * x * (1.f - h * h) * (k * (1.f + 0.134145f * x * x));
       sum[j] += d[j];
     }
-    store_run8(dz, xp_off(t, c, I), d);
+    Run8<bf16>::store(dz + xp_off(t, c, I), d);
   }
   store_run8(part + (int64_t)blockIdx.y * I, c, I, sum);
 }
