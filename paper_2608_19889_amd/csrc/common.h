@@ -112,6 +112,17 @@ AXON_DEV bf16x8 read_tr8(const bf16* lo_p, const bf16* hi_p) {
   return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
+// The value, no longer known to the compiler: what it derived from it before is derived
+// again rather than kept in registers.
+typedef __attribute__((__vector_size__(4 * sizeof(int)))) int i32x4;
+template <typename V>
+AXON_DEV void forget(V& v) {
+  static_assert(sizeof(V) == 16, "a 16-byte register");
+  i32x4 w = __builtin_bit_cast(i32x4, v);
+  asm volatile("" : "+v"(w));
+  v = __builtin_bit_cast(V, w);
+}
+
 // Eight consecutive elements of a row as they are stored (one or two 16-byte
 // registers' worth).  A row may start at any element: the wide accesses ask for no more
 // than the element's own alignment, which global memory instructions allow (rows off
@@ -129,6 +140,10 @@ struct Run8<float> {
     hi = *(const f32x4_any*)(p + 4);
   }
   AXON_DEV void fill(float x) { lo = hi = f32x4{x, x, x, x}; }
+  AXON_DEV void reread() {
+    forget(lo);
+    forget(hi);
+  }
   static AXON_DEV void store(float* p, const float (&v)[8]) {
     *(f32x4_any*)p = f32x4{v[0], v[1], v[2], v[3]};
     *(f32x4_any*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
@@ -139,6 +154,7 @@ struct Run8<bf16> {
   bf16x8 v;
   AXON_DEV float operator[](int j) const { return (float)v[j]; }
   AXON_DEV void load(const bf16* p) { v = *(const bf16x8_any*)p; }
+  AXON_DEV void reread() { forget(v); }
   AXON_DEV void fill(float x) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = (bf16)x;

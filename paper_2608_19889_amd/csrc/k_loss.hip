@@ -7,9 +7,8 @@
 // nothing of the row is read and its gradient is zero.  A loss is a function of the
 // lp, so its gradient is dz_v = c ([v = y] - p_v) with c = dloss / dlp and p_v =
 // exp(z_v - m) / S.  Everything but the passes over the logits is a few operations
-// per token, done in float64 by one workgroup (a ratio of probabilities shows every
-// digit of their logarithms, and a sequence's sum of them cancels against the
-// reference's).
+// per token, done by one workgroup, the sums in float64 (a sequence's cancels against
+// the reference's).
 //
 //   logit_part_kernel   reads the rows: (m, S) of every slice of a row
 //   *_finish_kernel     merges a row's slices; loss, statistics, c of every token
@@ -37,36 +36,28 @@ AXON_DEV void join_part(float& m, float& s, float m2, float s2) {
   m = top;
 }
 
-// exp(v - m) for many v and one m as 2^(v log2 e - m log2 e): one fused multiply-add
-// and the hardware exponential.  m log2 e is rounded, which scales every result by
-// the same 2^d; ``fix`` = 2^-d undoes it once, on the sum.  Where m log2 e may
-// overflow (``low``: a row or slice of nothing but the type's lowest values, or
-// -infinity), the difference is taken first.
+// exp(v - m) for many v <= m as 2^(v log2 e - m log2 e): one fused multiply-add and the
+// hardware exponential.  m log2 e is rounded, which scales every result by the same
+// 2^d; ``fix`` = 2^-d undoes it once, on the sum.  Where m log2 e might overflow (rows
+// or slices of nothing but the type's lowest values), neighbouring values lie so far
+// apart that only v = m gives more than 0: then any power of two serves as the factor,
+// and the product is exact.
 struct ExpFrom {
   static constexpr float L = 1.4426950408889634f;
-  float m, base, fix;
-  bool low;
+  float m, scale, base, fix;
   AXON_DEV explicit ExpFrom(float top) {
     m = top == -INFINITY ? 0.f : top;  // -inf - (-inf) is not a number
-    low = m < -2e38f;
-    base = low ? 0.f : m * L;
+    const bool low = m < -2e38f;
+    scale = low ? 0.0625f : L;
+    base = m * scale;
     fix = low ? 1.f : 1.f - fmaf(m, L, -base) * 0.6931471805599453f;
   }
-  template <int N>
-  AXON_DEV void operator()(float (&v)[N]) const {
-    if (!low) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = __builtin_amdgcn_exp2f(fmaf(v[j], L, -base));
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = __builtin_amdgcn_exp2f((v[j] - m) * L);
-    }
-  }
+  AXON_DEV float operator()(float v) const { return __builtin_amdgcn_exp2f(fmaf(v, scale, -base)); }
 };
 
 // N groups of 8 logits into a thread's (m, s)
 template <int N>
-AXON_DEV void take_runs(float& m, float& s, float (&v)[N][8]) {
+AXON_DEV void take_runs(float& m, float& s, const float (&v)[N][8]) {
   float top = m;
 #pragma unroll
   for (int k = 0; k < N; ++k)
@@ -75,13 +66,44 @@ AXON_DEV void take_runs(float& m, float& s, float (&v)[N][8]) {
   const ExpFrom e(top);
   float sum = 0.f;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    e(v[k]);
+  for (int k = 0; k < N; ++k)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sum += v[k][j];
-  }
+    for (int j = 0; j < 8; ++j) sum += e(v[k][j]);
   s = s * __expf(m - (top == -INFINITY ? 0.f : top)) + sum * e.fix;
   m = top;
+}
+
+// N groups of 8 of the columns c, c + stride, .. of [0, n), n >= 8, into a thread's (m, s).
+// CUT: groups at the end, read whole at its last columns and counted where they are
+// still to come.  (Every load is unconditional: one under a branch whose other arm fills
+// the same registers is waited for at once.)
+template <int N, bool CUT, typename T>
+AXON_DEV void read_runs(const T* row, int c, int stride, int n, float& m, float& s) {
+  Run8<T> r[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) r[k].load(row + (CUT ? min(c + k * stride, n - 8) : c + k * stride));
+  float v[N][8];
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[k][j] = !CUT || min(c + k * stride, n - 8) + j >= c + k * stride ? r[k][j] : -INFINITY;
+  take_runs(m, s, v);
+}
+
+// (m, s) over a workgroup of PART_THREADS, in every thread
+AXON_DEV void join_block(float& m, float& s, float (*red)[PART_THREADS / 64]) {
+  const float wm = wave_max(m);
+  s = wave_sum(s * __expf(m - (wm == -INFINITY ? 0.f : wm)));
+  __syncthreads();  // the last values have been read
+  if ((threadIdx.x & 63) == 0) {
+    red[0][threadIdx.x >> 6] = wm;
+    red[1][threadIdx.x >> 6] = s;
+  }
+  __syncthreads();
+  m = red[0][0];
+  s = red[1][0];
+#pragma unroll
+  for (int w = 1; w < PART_THREADS / 64; ++w) join_part(m, s, red[0][w], red[1][w]);
 }
 
 // One slice (of ``slices``, ``cols`` wide) of one row a workgroup: its maximum and
@@ -91,38 +113,30 @@ __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __res
                                                                   const int32_t* __restrict__ targets, int64_t items,
                                                                   int slices, int cols, float2* __restrict__ part,
                                                                   float* __restrict__ logps) {
+  constexpr int STRIDE = PART_THREADS * 8, BLOCK = STRIDE * PART_RUNS;
   __shared__ float red[2][PART_THREADS / 64];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t t = it / slices;
-    const int c0 = (int)(it % slices) * cols, c1 = min(V, c0 + cols);
+    const int c0 = (int)(it % slices) * cols, n = min(V - c0, cols);
     const int tg = targets[t];
     if (tg < 0 || tg >= V) {  // uniform over the workgroup
       if (logps && threadIdx.x == 0) logps[t] = 0.f;
       continue;
     }
-    const T* row = z + t * ld;
+    const T* row = z + t * ld + c0;
     float m = -INFINITY, s = 0.f;
-    for (int c = c0 + threadIdx.x * 8; c < c1; c += PART_THREADS * 8 * PART_RUNS) {
-      float v[PART_RUNS][8];
-#pragma unroll
-      for (int k = 0; k < PART_RUNS; ++k) load_run8(row, c + k * PART_THREADS * 8, c1, v[k], -INFINITY);
-      take_runs(m, s, v);
+    if (n >= 8) {
+      int c = 0;
+      for (; c + BLOCK <= n; c += BLOCK) read_runs<PART_RUNS, false>(row, c + threadIdx.x * 8, STRIDE, n, m, s);
+      for (; c < n; c += STRIDE) read_runs<1, true>(row, c + threadIdx.x * 8, STRIDE, n, m, s);
+    } else if (threadIdx.x < n) {
+      m = to_f32(row[threadIdx.x]);
+      s = m == -INFINITY ? 0.f : m - m + 1.f;  // (an infinite or NaN logit: NaN)
     }
-    // over the workgroup: the common maximum first, then the sums scaled to it
-    const float wm = wave_max(m);
-    s = wave_sum(s * __expf(m - (wm == -INFINITY ? 0.f : wm)));
-    __syncthreads();  // the last item's values have been read
-    if ((threadIdx.x & 63) == 0) {
-      red[0][threadIdx.x >> 6] = wm;
-      red[1][threadIdx.x >> 6] = s;
-    }
-    __syncthreads();
+    join_block(m, s, red);
     if (threadIdx.x == 0) {
-      float M = red[0][0], S = red[1][0];
-#pragma unroll
-      for (int w = 1; w < PART_THREADS / 64; ++w) join_part(M, S, red[0][w], red[1][w]);
-      if (part) part[it] = float2{M, S};
-      if (logps) logps[t] = (float)((double)to_f32(row[tg]) - (double)M - log((double)S));
+      if (part) part[it] = float2{m, s};
+      if (logps) logps[t] = (float)((double)to_f32(z[t * ld + tg]) - (double)m - log((double)s));
     }
   }
 }
@@ -190,16 +204,43 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(
     float2* stat, float* __restrict__ coef) {
   __shared__ double red[16];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  for (int t = tid; t < tokens; t += 1024) {
-    const int tg = targets[t];
-    float2 st = {0.f, 1.f};
-    lps[t] = tg >= 0 && tg < V ? merge_row(z, ld, part, slices, t, tg, st) : 0.0;
-    stat[t] = st;
+  constexpr int U = 4;  // tokens of a thread whose loads are under way together
+  for (int t0 = tid; t0 < tokens; t0 += 1024 * U) {
+    int tg[U];
+    float zt[U];
+    float2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      tg[u] = -1;
+      if (t0 + u * 1024 < tokens) tg[u] = targets[t0 + u * 1024];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * 1024;
+      zt[u] = 0.f;
+      st[u] = float2{0.f, 1.f};
+      if (tg[u] < 0 || tg[u] >= V) continue;
+      zt[u] = to_f32(z[t * ld + tg[u]]);
+      st[u] = part[t * slices];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = t0 + u * 1024;
+      if (t >= tokens) continue;
+      double lp = 0.0;
+      if (tg[u] >= 0 && tg[u] < V) {
+        for (int i = 1; i < slices; ++i) join_part(st[u].x, st[u].y, part[t * slices + i].x, part[t * slices + i].y);
+        lp = (double)zt[u] - (double)st[u].x - log((double)st[u].y);
+      }
+      lps[t] = lp;
+      stat[t] = st[u];
+    }
   }
   __syncthreads();
   for (int j = wave; j < seqs; j += 16) {
     const int t1 = min(tokens, cu[j + 1]);
     double s = 0.0;
+#pragma unroll 4
     for (int t = max(0, cu[j]) + lane; t < t1; t += 64) s += lps[t];
     s = wave_sum_f64(s);
     if (lane == 0) {
@@ -234,21 +275,51 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(
   }
 }
 
-// Tokens with ratio q = exp(lp - old) and advantage A: -min(q A, clip(q, 1 - lo, 1 +
-// hi) A) + k (exp(g) - g - 1), g = ref - lp, weighted by w: 1 / counted tokens or
-// (per sequence) 1 / (sequences with counted tokens x the sequence's counted tokens).
-// dloss / dlp = w (-(not clipped) q A + k (1 - exp(g))).  stats: the weighted means of
-// the clipped term, of exp(g) - g - 1 and of the clipped tokens.
-template <typename T>
-__global__ void __launch_bounds__(1024) policy_finish_kernel(
-    const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
-    const float2* part /* may be stat */, int slices, const int32_t* __restrict__ cu, int seqs,
-    const float* __restrict__ old, const float* __restrict__ ref, const float* __restrict__ adv, float lo, float hi,
-    float kl_coef, float* __restrict__ loss, float* __restrict__ stats, float* __restrict__ logps,
-    double* __restrict__ weights, float2* stat, float* __restrict__ coef) {
-  __shared__ double red[16];
+struct PolicyTerms {
+  float lp, c;  // log-probability; dloss / dlp of weight 1
+  float surrogate, kl;
+  bool clipped;
+};
+// one token (see policy_finish_kernel), from its logit and its row's (m, S), in float32:
+// float64 exponentials of a batch's tokens took one workgroup longer than everything
+// else here.  The log-probability's three terms and the other policy's are added with
+// their rounding errors kept, so the ratio is off by the last digits of S and of two
+// logarithms.
+AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A, bool has_ref, float ref, float lo,
+                                  float hi, float kl_coef) {
+  auto sum = [](float a, float b, float& low) {  // a + b, its rounding error added to low
+    const float r = a + b, bb = r - a;
+    low += (a - (r - bb)) + (b - bb);
+    return r;
+  };
+  PolicyTerms p;
+  float low = 0.f;
+  const float lp = sum(sum(z, -m, low), -logf(s), low);
+  p.lp = fabsf(lp) < INFINITY ? lp + low : lp;  // (an infinite sum's error is not a number)
+  float el = low;
+  const float d = sum(lp, -old, el), e = expf(d);
+  const float q = fabsf(d) < 100.f ? e * (1.f + el) : e;  // (beyond, 0 or infinity, and el may be a whole term)
+  const float held = fminf(fmaxf(q, 1.f - lo), 1.f + hi);
+  // A = 0: no term, also where the ratio overflows
+  const float free_term = A == 0.f ? 0.f : q * A, held_term = A == 0.f ? 0.f : held * A;
+  p.clipped = free_term > held_term;
+  p.surrogate = -(p.clipped ? held_term : free_term);
+  p.c = p.clipped ? 0.f : -free_term;
+  p.kl = 0.f;
+  if (has_ref) {
+    float er = -low;
+    const float g = sum(ref, -lp, er), x = fabsf(g) < INFINITY ? g + er : g, dkl = -expm1f(x);
+    p.kl = -dkl - x;
+    p.c += kl_coef * dkl;
+  }
+  return p;
+}
+
+// counted tokens of each sequence into weights[seqs] (cu), and in every thread the
+// number of sequences that have some, or (no cu) of all counted tokens.  1024 threads.
+AXON_DEV double policy_counts(const int32_t* targets, int tokens, int V, const int32_t* cu, int seqs, double* weights,
+                              double* red) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  // the weights: counted tokens of all, or of each sequence
   double n = 0.0;
   if (cu) {
     for (int j = wave; j < seqs; j += 16) {
@@ -262,39 +333,73 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
   } else {
     for (int t = tid; t < tokens; t += 1024) n += targets[t] >= 0 && targets[t] < V ? 1.0 : 0.0;
   }
-  n = block_sum_f64(n, red);  // and the sequences' counts are visible
+  return block_sum_f64(n, red);  // (its barriers make the sequences' counts visible)
+}
+
+// Tokens with ratio q = exp(lp - old) and advantage A: -min(q A, clip(q, 1 - lo, 1 +
+// hi) A) + k (exp(g) - g - 1), g = ref - lp, weighted by w: 1 / counted tokens or
+// (per sequence) 1 / (sequences with counted tokens x the sequence's counted tokens).
+// dloss / dlp = w (-(not clipped) q A + k (1 - exp(g))).  stats: the weighted means of
+// the clipped term, of exp(g) - g - 1 and of the clipped tokens.  chosen: the targets'
+// logits, where the rows have had their gradient before (it may have replaced z).
+template <typename T>
+__global__ void __launch_bounds__(1024) policy_finish_kernel(
+    const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
+    const float2* part /* may be stat */, int slices, const int32_t* __restrict__ cu, int seqs,
+    const float* __restrict__ old, const float* __restrict__ ref, const float* __restrict__ adv, float lo, float hi,
+    float kl_coef, float* __restrict__ loss, float* __restrict__ stats, float* __restrict__ logps,
+    double* __restrict__ weights, float2* stat, float* __restrict__ coef, const float* __restrict__ chosen) {
+  __shared__ double red[16];
+  const int tid = threadIdx.x;
+  const double n = chosen ? 0.0 : policy_counts(targets, tokens, V, cu, seqs, weights, red);
   double sum_l = 0.0, sum_s = 0.0, sum_k = 0.0, sum_c = 0.0;
-  for (int t = tid; t < tokens; t += 1024) {
-    const int tg = targets[t];
-    const bool ok = tg >= 0 && tg < V;
-    float2 st = {0.f, 1.f};
-    double lp = 0.0, c = 0.0;
-    if (ok) {
-      lp = merge_row(z, ld, part, slices, t, tg, st);
-      const double w = 1.0 / (cu ? n * weights[seq_of_token(cu, seqs, t)] : n);
-      const double A = (double)adv[t], q = exp(lp - (double)old[t]);
-      const double held = fmin(fmax(q, 1.0 - (double)lo), 1.0 + (double)hi);
-      // A = 0: no term, also where the ratio overflows
-      const double free_term = A == 0.0 ? 0.0 : q * A, held_term = A == 0.0 ? 0.0 : held * A;
-      const bool clipped = free_term > held_term;
-      const double surrogate = -(clipped ? held_term : free_term);
-      double kl = 0.0, dkl = 0.0;
-      if (ref) {
-        const double g = (double)ref[t] - lp;
-        dkl = -expm1(g);
-        kl = -dkl - g;
-      }
-      const double k = (double)kl_coef;
-      c = w * ((clipped ? 0.0 : -free_term) + (ref ? k * dkl : 0.0));
-      sum_l += w * (surrogate + (ref ? k * kl : 0.0));
-      sum_s += w * surrogate;
-      sum_k += w * kl;
-      sum_c += clipped ? w : 0.0;
+  constexpr int U = 4;  // tokens of a thread whose loads are under way together
+  for (int t0 = tid; t0 < tokens; t0 += 1024 * U) {
+    int tg[U];
+    float zt[U], o[U], a[U], rf[U];
+    float2 st[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * 1024;
+      tg[u] = -1;
+      if (t < tokens) tg[u] = targets[t];
     }
-    logps[t] = (float)lp;
-    if (coef) {
-      stat[t] = st;
-      coef[t] = (float)c;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * 1024;
+      st[u] = float2{0.f, 1.f};
+      zt[u] = o[u] = a[u] = rf[u] = 0.f;
+      if (tg[u] < 0 || tg[u] >= V) continue;
+      zt[u] = chosen ? chosen[t] : to_f32(z[t * ld + tg[u]]);
+      st[u] = part[(int64_t)t * slices];
+      o[u] = old[t];
+      a[u] = adv[t];
+      if (ref) rf[u] = ref[t];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int t = t0 + u * 1024;
+      if (t >= tokens) continue;
+      PolicyTerms p{};
+      double w = 0.0;
+      if (tg[u] >= 0 && tg[u] < V) {
+        for (int i = 1; i < slices; ++i) {
+          const float2 q = part[(int64_t)t * slices + i];
+          join_part(st[u].x, st[u].y, q.x, q.y);
+        }
+        const int j = cu ? seq_of_token(cu, seqs, t) : 0;
+        w = chosen ? weights[j] : 1.0 / (cu ? n * weights[j] : n);
+        p = policy_token(zt[u], st[u].x, st[u].y, o[u], a[u], ref != nullptr, rf[u], lo, hi, kl_coef);
+        sum_l += w * (double)(p.surrogate + (ref ? kl_coef * p.kl : 0.f));
+        sum_s += w * (double)p.surrogate;
+        sum_k += w * (double)p.kl;
+        sum_c += p.clipped ? w : 0.0;
+      }
+      logps[t] = p.lp;
+      if (coef) {
+        stat[t] = st[u];
+        coef[t] = (float)w * p.c;
+      }
     }
   }
   sum_l = block_sum_f64(sum_l, red);
@@ -309,81 +414,235 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
   }
 }
 
+// joins (op) over the lanes that differ in lane % NW; every lane the same result (see
+// wave_sum)
+template <int NW, typename F>
+AXON_DEV float over_waves(float v, F&& op) {
+  if constexpr (NW > 1) v = op(v, dpp_move<0xB1>(v));
+  if constexpr (NW > 2) v = op(v, dpp_move<0x4E>(v));
+  if constexpr (NW > 4) v = op(v, dpp_move<0x141>(v));
+  if constexpr (NW > 8) v = op(v, dpp_move<0x140>(v));
+  return v;
+}
+
 // 8 logits to their gradients f exp(v - m), f = -c / S, and c more at the target, the
 // ``at``-th of them if it is one
 AXON_DEV void grad_run(float (&v)[8], const ExpFrom& e, float f, float c, int at) {
-  e(v);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] *= f;
+  for (int j = 0; j < 8; ++j) v[j] = e(v[j]) * f;
   if ((unsigned)at < 8u)
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += j == at ? c : 0.f;
 }
 
-// dz of one slice of a row a workgroup.  z and dz may be one buffer: a thread reads
-// what it then writes.
+// dz of one slice of a row a workgroup.  z and dz may be one buffer: a thread writes
+// what it has read, and what it reads beyond that (groups at the row's end) counts
+// nothing.
 template <typename T, typename TO>
 __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld, int V,
                                                          const int32_t* __restrict__ targets, int64_t items, int slices,
                                                          const float2* __restrict__ stat,
                                                          const float* __restrict__ coef, TO* dz, int64_t lddz) {
-  constexpr int COLS = 256 * 8 * GRAD_RUNS;
+  constexpr int STRIDE = 256 * 8, COLS = STRIDE * GRAD_RUNS;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t t = it / slices;
-    const int c0 = (int)(it % slices) * COLS + threadIdx.x * 8;
+    const int first = (int)(it % slices) * COLS, c0 = first + threadIdx.x * 8;
     const float w = coef[t];
     const T* row = z + t * ld;
     TO* out = dz + t * lddz;
-    float v[GRAD_RUNS][8];
-    if (w == 0.f) {
+    const float2 st = stat[t];
+    const int tg = targets[t];
+    const ExpFrom e(st.x);
+    const float f = -w / st.y * e.fix;
+    if (first + COLS <= V) {
+      float v[GRAD_RUNS][8] = {};
+      if (w != 0.f) {
+        Run8<T> r[GRAD_RUNS];
 #pragma unroll
-      for (int k = 0; k < GRAD_RUNS; ++k)
+        for (int k = 0; k < GRAD_RUNS; ++k) r[k].load(row + c0 + k * STRIDE);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[k][j] = 0.f;
-    } else {
-      const float2 st = stat[t];
-      const int tg = targets[t];
-      const ExpFrom e(st.x);
-      const float f = -w / st.y * e.fix;
+        for (int k = 0; k < GRAD_RUNS; ++k) {
 #pragma unroll
-      for (int k = 0; k < GRAD_RUNS; ++k) load_run8(row, c0 + k * 2048, V, v[k], 0.f);
+          for (int j = 0; j < 8; ++j) v[k][j] = r[k][j];
+          grad_run(v[k], e, f, w, tg - (c0 + k * STRIDE));
+        }
+      }
 #pragma unroll
-      for (int k = 0; k < GRAD_RUNS; ++k) grad_run(v[k], e, f, w, tg - (c0 + k * 2048));
+      for (int k = 0; k < GRAD_RUNS; ++k) Run8<TO>::store(out + c0 + k * STRIDE, v[k]);
+    } else {  // the row's last slice
+      for (int c = c0; c < V; c += STRIDE) {
+        float v[8] = {};
+        if (w != 0.f) {
+          load_run8(row, c, V, v, 0.f);
+          grad_run(v, e, f, w, tg - c);
+        }
+        store_run8(out, c, V, v);
+      }
     }
-#pragma unroll
-    for (int k = 0; k < GRAD_RUNS; ++k)
-      if (c0 + k * 2048 < V) store_run8(out, c0 + k * 2048, V, v[k]);
   }
+}
+
+// ---------------------------------------------------------------- whole rows, read once
+//
+// Where a row's coefficient depends on that row alone (a caller's own dlogps, the
+// policy loss) and there are rows enough for every CU, a workgroup keeps its row in
+// registers from the statistics to the gradient: the logits are read once.  RUNS
+// groups of 8 logits a thread, THREADS x RUNS x 8 columns; what a row has beyond them is
+// read a second time.  HBM bound: 2 V values a row against 3.
+
+// the weights, one launch before the rows: w[0] = 1 / counted tokens, or w[j] = 1 /
+// (sequences with counted tokens x those of sequence j)
+__global__ void __launch_bounds__(1024) policy_weights_kernel(const int32_t* __restrict__ targets, int tokens, int V,
+                                                              const int32_t* __restrict__ cu, int seqs,
+                                                              double* __restrict__ w) {
+  __shared__ double red[16];
+  const double n = policy_counts(targets, tokens, V, cu, seqs, w, red);
+  if (!cu) {
+    if (threadIdx.x == 0) w[0] = 1.0 / n;
+    return;
+  }
+  for (int j = threadIdx.x; j < seqs; j += 1024) w[j] = 1.0 / (w[j] * n);
+}
+
+struct RowCoef {
+  const float* dlogps;  // a caller's own, or the policy loss:
+  const int32_t* cu;
+  int seqs;
+  const float *old, *ref, *adv;
+  float lo, hi, kl_coef;
+  const double* weights;
+  float2* stat;   // out (policy), for the loss itself: (m, S) of each token
+  float* chosen;  // and its target's logit
+};
+
+// p + b bytes, b unsigned 32-bit: one register of address beside a uniform p
+template <typename T>
+AXON_DEV const T* at_byte(const T* p, unsigned b) {
+  return (const T*)((const char*)p + b);
+}
+template <typename T>
+AXON_DEV T* at_byte(T* p, unsigned b) {
+  return (T*)((char*)p + b);
+}
+
+template <typename T, typename TO, int THREADS, int RUNS>
+__global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t ld, int V,
+                                                            const int32_t* __restrict__ targets, int64_t first,
+                                                            RowCoef rc, TO* dz, int64_t lddz) {
+  constexpr int NW = THREADS / 64, STRIDE = THREADS * 8, HELD = STRIDE * RUNS;
+  __shared__ float2 parts[16];
+  __shared__ float2 chosen;  // c, and the target's logit
+  const int i = threadIdx.x, whole = V & ~7;
+  const int full = min(whole / STRIDE, RUNS);                // groups that every thread has,
+  const bool more = full * STRIDE + i * 8 < min(whole, HELD);  // and whether it has one after them
+  const int groups = full + (full * STRIDE < min(whole, HELD) ? 1 : 0);
+  auto zeros = [&](TO* out) {
+    const float zero[8] = {};
+    for (int c = i * 8; c < whole; c += STRIDE) Run8<TO>::store(out + c, zero);
+    if (whole + i < V) out[whole + i] = from_f32<TO>(0.f);
+  };
+  const int64_t t = first + blockIdx.x;
+  const T* row = z + t * ld;
+  TO* out = dz + t * lddz;
+  const int tg = targets[t];
+  if (tg < 0 || tg >= V) {  // uniform over the workgroup
+    zeros(out);
+    return;
+  }
+  // every load unconditional (past the row's groups its last one again), so that
+  // each is waited for by itself and the sums run under the loads behind them
+  Run8<T> r[RUNS];
+#pragma unroll
+  for (int k = 0; k < RUNS; ++k) r[k].load(at_byte(row, min(k * STRIDE + i * 8, whole - 8) * (unsigned)sizeof(T)));
+  // the columns past the groups of 8, one a thread
+  const float last = whole + i < V ? to_f32(row[whole + i]) : -INFINITY;
+  float m = -INFINITY, s = 0.f;
+#pragma unroll
+  for (int k = 0; k < RUNS; ++k) {
+    if (k < groups) {  // (uniform)
+      float v[1][8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[0][j] = k < full || more ? r[k][j] : -INFINITY;
+      take_runs(m, s, v);
+    }
+    r[k].reread();  // (kept in float32 until the gradient, bf16 logits would take twice the registers)
+  }
+  for (int c = HELD + i * 8; c < whole; c += STRIDE) {  // not held
+    Run8<T> q;
+    q.load(row + c);
+    float v[1][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[0][j] = q[j];
+    take_runs(m, s, v);
+  }
+  join_part(m, s, last, last == -INFINITY ? 0.f : last - last + 1.f);  // (infinity or NaN: NaN)
+  const float top = m;
+  // over the wavefronts: lane l joins what wavefront l % NW left
+  const float wm = wave_max(top);
+  s = wave_sum(s * __expf(top - (wm == -INFINITY ? 0.f : wm)));
+  if ((i & 63) == 0) parts[i >> 6] = float2{wm, s};
+  __syncthreads();
+  const float2 p = parts[i % NW];
+  m = over_waves<NW>(p.x, [](float a, float b) { return fmaxf(a, b); });
+  s = over_waves<NW>(p.y * __expf(p.x - (m == -INFINITY ? 0.f : m)), [](float a, float b) { return a + b; });
+  if (i == 0) {
+    const float zt = to_f32(row[tg]);
+    if (rc.dlogps) {
+      chosen = float2{rc.dlogps[t], zt};
+    } else {
+      const float w = (float)rc.weights[rc.cu ? seq_of_token(rc.cu, rc.seqs, (int)t) : 0];
+      const PolicyTerms p = policy_token(zt, m, s, rc.old[t], rc.adv[t], rc.ref != nullptr, rc.ref ? rc.ref[t] : 0.f,
+                                         rc.lo, rc.hi, rc.kl_coef);
+      chosen = float2{w * p.c, zt};
+      rc.stat[t] = float2{m, s};
+      rc.chosen[t] = zt;
+    }
+  }
+  __syncthreads();
+  const float w = chosen.x, zt = chosen.y;
+  const ExpFrom e(m);
+  // a coefficient of 0 (clipped): zeros, whatever the row holds
+  if (w == 0.f) {
+    zeros(out);
+    return;
+  }
+  const float f = -w / s * e.fix;
+  auto grad = [&](const Run8<T>& q, TO* to) {
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = e(q[j]) * f;
+    Run8<TO>::store(to, v);
+  };
+#pragma unroll
+  for (int k = 0; k < RUNS; ++k)
+    if (k < full || (k == full && more)) grad(r[k], at_byte(out, (k * STRIDE + i * 8) * (unsigned)sizeof(TO)));
+  for (int c = HELD + i * 8; c < whole; c += STRIDE) {
+    Run8<T> q;
+    q.load(row + c);
+    grad(q, out + c);
+  }
+  if (whole + i < V) out[whole + i] = from_f32<TO>(e(last) * f);
+  // the target's own column, by the thread that has just written it
+  if (i == (tg < whole ? (tg >> 3) % THREADS : tg - whole)) out[tg] = from_f32<TO>(e(zt) * f + w);
 }
 
 // ---------------------------------------------------------------- within a training step
 
 // (m, S) of a row from the np (largest, sum) partials of its 64-column pieces, a
 // workgroup a row; rows that do not count are skipped
-__global__ void __launch_bounds__(256) piece_merge_kernel(const float2* __restrict__ pieces, int np, int V,
+__global__ void __launch_bounds__(PART_THREADS) piece_merge_kernel(const float2* __restrict__ pieces, int np, int V,
                                                           const int32_t* __restrict__ targets,
                                                           float2* __restrict__ stat) {
-  __shared__ float red[2][4];
+  __shared__ float red[2][PART_THREADS / 64];
   const int t = blockIdx.x, tg = targets[t];
   if (tg < 0 || tg >= V) return;
   float m = -INFINITY, s = 0.f;
-  for (int i = threadIdx.x; i < np; i += 256) {
+  for (int i = threadIdx.x; i < np; i += PART_THREADS) {
     const float2 p = pieces[(int64_t)t * np + i];
     join_part(m, s, p.x, p.y);
   }
-  const float wm = wave_max(m);
-  s = wave_sum(s * __expf(m - (wm == -INFINITY ? 0.f : wm)));
-  if ((threadIdx.x & 63) == 0) {
-    red[0][threadIdx.x >> 6] = wm;
-    red[1][threadIdx.x >> 6] = s;
-  }
-  __syncthreads();
-  if (threadIdx.x) return;
-  m = red[0][0];
-  s = red[1][0];
-#pragma unroll
-  for (int w = 1; w < 4; ++w) join_part(m, s, red[0][w], red[1][w]);
-  stat[t] = float2{m, s};
+  join_block(m, s, red);
+  if (threadIdx.x == 0) stat[t] = float2{m, s};
 }
 
 // The gradient as the training step's GEMM operand: bf16 in the row-pair layout,
@@ -416,12 +675,14 @@ namespace {
 
 constexpr int64_t MAX_WGS = 1 << 20;  // more items than this: the workgroups loop
 
+constexpr int64_t ROW_TOKENS = 1024;
+
 // Slices of a row for the statistics pass: whole rows once there are enough of
-// them to fill the chip (8 workgroups on each of the 256 CUs), else as many slices
+// them for two rounds of 8 workgroups on each of the 256 CUs, else as many slices
 // as give that, of at least one group of 8 per thread
 void part_shape(int64_t tokens, int V, int& slices, int& cols) {
   const int most = (V + PART_THREADS * 8 - 1) / (PART_THREADS * 8);
-  const int want = (int)std::min<int64_t>(most, std::max<int64_t>(1, 2048 / std::max<int64_t>(tokens, 1)));
+  const int want = (int)std::min<int64_t>(most, std::max<int64_t>(1, 4096 / std::max<int64_t>(tokens, 1)));
   const int runs = (most + want - 1) / want;
   cols = runs * PART_THREADS * 8;
   slices = (V + cols - 1) / cols;
@@ -479,11 +740,38 @@ void run_grad(const LogitRows& r, const LossWs& w, hipStream_t s) {
                                                     (float*)r.dz, r.lddz);
 }
 
+// rows enough to give each CU several, and long enough for the registers to matter
+bool whole_rows(const LogitRows& r) { return r.dz && r.tokens >= ROW_TOKENS && r.V >= 2048; }
+
+template <typename T, typename TO>
+void run_rows(const LogitRows& r, const RowCoef& rc, hipStream_t s) {
+  auto go = [&](auto kern, int threads) {
+    for (int64_t first = 0; first < r.tokens; first += MAX_WGS)  // a launch holds at most 2^32 threads
+      kern<<<(unsigned)std::min(r.tokens - first, MAX_WGS), threads, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, first,
+                                                                            rc, (TO*)r.dz, r.lddz);
+  };
+  constexpr int R = sizeof(T) == 2 ? 16 : 8;  // 64 registers of logits a thread
+  if (r.V <= 256 * 8 * 4) go(logit_row_kernel<T, TO, 256, 4>, 256);
+  else if (r.V <= 256 * 8 * R) go(logit_row_kernel<T, TO, 256, R>, 256);
+  else if (r.V <= 512 * 8 * R) go(logit_row_kernel<T, TO, 512, R>, 512);
+  else if (r.V <= 1024 * 8 * R) go(logit_row_kernel<T, TO, 1024, R>, 1024);
+  else go(logit_row_kernel<T, TO, 1024, sizeof(T) == 2 ? 20 : 12>, 1024);
+}
+template <typename T>
+void run_rows(const LogitRows& r, const RowCoef& rc, hipStream_t s) {
+  r.dz_bf16 ? run_rows<T, bf16>(r, rc, s) : run_rows<T, float>(r, rc, s);
+}
+
 template <typename T>
 void logprobs(const LogitRows& r, float* logps, const float* dlogps, void* wsp, hipStream_t s) {
   if (r.tokens <= 0) return;
   LossWs w;
   carve(r.tokens, r.V, 0, (char*)wsp, &w);
+  if (whole_rows(r)) {
+    RowCoef rc{};
+    rc.dlogps = dlogps;
+    return run_rows<T>(r, rc, s);
+  }
   const int slices = run_parts<T>(r, w.part, logps, s);
   if (logps && slices == 1) return;
   logps_finish_kernel<T><<<(unsigned)((r.tokens + 255) / 256), 256, 0, s>>>(
@@ -506,10 +794,18 @@ template <typename T>
 void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, a.seqs, (char*)wsp, &w);
+  if (whole_rows(r)) {
+    policy_weights_kernel<<<1, 1024, 0, s>>>(r.targets, (int)r.tokens, r.V, a.cu, a.seqs, w.seq);
+    run_rows<T>(r, RowCoef{nullptr, a.cu, a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, w.seq, w.stat, w.coef}, s);
+    policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.stat, 1, a.cu,
+                                               a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
+                                               a.logps, w.seq, nullptr, nullptr, w.coef);
+    return;
+  }
   const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, s) : 1;
   policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices, a.cu,
                                              a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
-                                             a.logps, w.seq, w.stat, r.dz ? w.coef : nullptr);
+                                             a.logps, w.seq, w.stat, r.dz ? w.coef : nullptr, nullptr);
   if (r.dz && r.tokens > 0) run_grad<T>(r, w, s);
 }
 
@@ -537,7 +833,7 @@ void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipSt
 namespace {
 
 void train_stat(const TrainLogits& r, hipStream_t s) {
-  piece_merge_kernel<<<r.T, 256, 0, s>>>(r.lse_part, (r.V + LSE_COLS - 1) / LSE_COLS, r.V, r.targets, r.stat);
+  piece_merge_kernel<<<r.T, PART_THREADS, 0, s>>>(r.lse_part, (r.V + LSE_COLS - 1) / LSE_COLS, r.V, r.targets, r.stat);
 }
 
 void train_grad(const TrainLogits& r, hipStream_t s) {
@@ -559,7 +855,7 @@ void launch_policy_train(const TrainLogits& r, const PolicyArgs& a, hipStream_t 
   train_stat(r, s);
   policy_finish_kernel<float><<<1, 1024, 0, s>>>(r.z, r.ldl, r.V, r.targets, r.T, r.stat, 1, a.cu, a.seqs, a.old, a.ref,
                                                  a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats, a.logps, r.seq, r.stat,
-                                                 r.coef);
+                                                 r.coef, nullptr);
   train_grad(r, s);
 }
 

@@ -136,10 +136,17 @@ CASES = [([2, 1], 1, 1, F), ([1, 1], 2, 2, B), ([5, 0, 0, 3], 7, 9, B), ([9, 4],
          ([20, 13], 2048, 2048, B), ([20, 13], 2049, 2056, B), ([3, 4, 5, 6], 8191, 8192, B), ([7, 7], 8193, 8193, F),
          ([11, 30], 50257, 50257, B), ([11, 30], 50257, 50272, F), ([100, 87, 33, 160], 32000, 32000, B),
          ([600, 400, 90, 300], 5003, 5003, F), ([1100, 1200], 4100, 4100, B)]
-IDS = ["%dx%d-%s" % (sum(c[0]), c[1], "f32" if c[3] == F else "bf16") for c in CASES]
+# rows enough to be read once (1024): each width that a workgroup holds in registers
+# (4 groups of 8 a thread, then 64 registers of 256, 512 and 1024 threads), and rows
+# longer than the registers of any
+LONG = [([600, 0, 425], 2050, 2050, F), ([1024], 8192, 8192, B), ([700, 330], 8197, 8200, F),
+        ([500, 1, 530], 16385, 16385, F), ([1030], 32771, 32771, B), ([515, 515], 40003, 40003, F),
+        ([1025], 65544, 65544, B), ([300, 730], 70001, 70001, F), ([1026], 131072, 131072, B),
+        ([1027], 140003, 140005, B)]
+name = lambda c: "%dx%d-%s" % (sum(c[0]), c[1], "f32" if c[3] == F else "bf16")  # noqa: E731
 
 
-@pytest.mark.parametrize("case", CASES, ids=IDS)
+@pytest.mark.parametrize("case", CASES + LONG, ids=name)
 def test_log_probabilities_and_their_gradient(case):
     lens, V, ld, dtype = case
     z, tg, cu = make(lens, V, dtype, 1, ld)
@@ -161,7 +168,7 @@ def test_log_probabilities_and_their_gradient(case):
 
 
 @pytest.mark.parametrize("smoothing", [0.0, 0.2])
-@pytest.mark.parametrize("case", CASES, ids=IDS)
+@pytest.mark.parametrize("case", CASES, ids=name)
 def test_preference_loss(case, smoothing):
     lens, V, ld, dtype = case
     z, tg, cu = make(lens, V, dtype, 2, ld)
@@ -183,7 +190,7 @@ def test_preference_loss(case, smoothing):
 
 
 @pytest.mark.parametrize("per", [False, True])
-@pytest.mark.parametrize("case", CASES, ids=IDS)
+@pytest.mark.parametrize("case", CASES + LONG, ids=name)
 def test_policy_loss(case, per):
     lens, V, ld, dtype = case
     z, tg, cu = make(lens, V, dtype, 4, ld)
@@ -240,17 +247,20 @@ def test_nothing_counts():
 
 
 @pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
-def test_masked_vocabulary(dtype):
+@pytest.mark.parametrize("lens", [[9, 6], [900, 300]], ids=["few", "many"])
+def test_masked_vocabulary(lens, dtype):
     """Tokens ruled out by -infinity or the type's lowest value have probability and
-    gradient 0, also where whole slices of a row hold nothing else."""
-    z, tg, cu = make([9, 6], 9001, dtype, 6, counted=1.0)
+    gradient 0, also where whole slices of a row hold nothing else; rows of nothing but
+    the lowest value are uniform."""
+    n = sum(lens)
+    z, tg, cu = make(lens, 9001, dtype, 6, counted=1.0)
     for i, low in enumerate((-INF, torch.finfo(dtype).min)):
         z[:, 3000:] = low
         z[:, ::2] = low
         tg = torch.where(tg >= 0, tg % 1500 * 2 + 1, tg).int()
         r = Rows(z, tg)
         check(ops.token_logprobs(z, tg), r.lp, r.E * U + U * r.lp.abs(), "logps")
-        c = torch.ones(15, device="cuda")
+        c = torch.ones(n, device="cuda")
         g = ops.token_logprobs_backward(z, tg, c)
         assert not g[:, 3000:].any() and not g[:, ::2].any()
         check(g, r.grad(c.double()), r.grad_bound(c.double(), c.double() * 0, HALF[dtype]), "dlogits")
@@ -258,17 +268,23 @@ def test_masked_vocabulary(dtype):
     z[0, 1] = -INF
     tg[0] = 1
     assert float(ops.token_logprobs(z, tg)[0]) == -INF
-    g = ops.token_logprobs_backward(z, tg, torch.ones(15, device="cuda"))
+    g = ops.token_logprobs_backward(z, tg, torch.ones(n, device="cuda"))
     assert float(g[0, 1]) == 1 and bool(torch.isfinite(g).all())
+    z[2] = torch.finfo(dtype).min
+    tg[2] = 5
+    assert abs(float(ops.token_logprobs(z, tg)[2]) + math.log(9001)) < 1e-5
+    g = ops.token_logprobs_backward(z, tg, torch.ones(n, device="cuda"))[2].double()
+    assert abs(float(g[5]) - 1) < 2.0 ** -8 and abs(float(g[7]) * 9001 + 1) < 2.0 ** -7
 
 
-def test_not_a_number_stays_in_its_row():
-    z, tg, _ = make([40], 3000, F, 7, counted=1.0)
+@pytest.mark.parametrize("n", [40, 1100])
+def test_not_a_number_stays_in_its_row(n):
+    z, tg, _ = make([n], 3000, F, 7, counted=1.0)
     z[3, 77] = float("nan")
     z[8, 2999] = INF
     got = ops.token_logprobs(z, tg)
     assert got[3].isnan() and got[8].isnan() and int((~torch.isfinite(got)).sum()) == 2
-    g = ops.token_logprobs_backward(z, tg, torch.ones(40, device="cuda"))
+    g = ops.token_logprobs_backward(z, tg, torch.ones(n, device="cuda"))
     bad = ~torch.isfinite(g).all(-1)
     assert bad.nonzero().flatten().tolist() == [3, 8]
 
@@ -289,10 +305,10 @@ def test_ratio_that_overflows():
 def test_gradient_in_the_logits_buffer():
     """dlogits in place of the logits gives the same bits; what lies between the rows
     keeps its own."""
-    for dtype in (F, B):
-        z, tg, cu = make([30, 50], 10007, dtype, 9, 10012)
+    for dtype, lens in ((F, [30, 50]), (B, [30, 50]), (F, [700, 600]), (B, [700, 600])):
+        z, tg, cu = make(lens, 10007, dtype, 9, 10012)
         r = Rows(z, tg)
-        ref = torch.randn(80, device="cuda") + r.lp.float()
+        ref = torch.randn(sum(lens), device="cuda") + r.lp.float()
         want = ops.policy_loss(z, tg, cu, ref, ref, ref, kl_coef=0.1)
         base = z._base
         between = base[:, 10007:].clone()
