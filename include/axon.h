@@ -352,8 +352,8 @@ int axon_layernorm_backward(int64_t rows, int32_t cols, const void* x, int32_t x
  * dlogits [tokens][vocab] (grad_dtype, rows ldg apart) is overwritten; it may be the
  * logits' own buffer (same dtype and stride).  Columns from vocab to the stride are
  * neither read nor written.  tokens and vocab up to 2^30.
- * axon_token_loss_workspace: the bytes for a call over ``seqs`` sequences (0 for the
- * two token_logprobs calls). */
+ * axon_token_loss_workspace: the bytes for a call over ``seqs`` sequences (0 for
+ * axon_token_logprobs). */
 int64_t axon_token_loss_workspace(int64_t tokens, int32_t vocab, int32_t seqs);
 
 /* d_logps[t] = logits[t][target] - logsumexp(logits[t]) (float [tokens]). */
@@ -361,10 +361,10 @@ int axon_token_logprobs(int64_t tokens, int32_t vocab, const void* logits, int32
                         const int32_t* d_targets, float* d_logps, void* workspace, int64_t workspace_bytes,
                         void* stream);
 /* The gradient at the logits of sum_t d_dlogps[t] * logps[t], for a loss of the
- * caller's own over the log-probabilities. */
+ * caller's own over the log-probabilities.  No workspace. */
 int axon_token_logprobs_backward(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
                                  const int32_t* d_targets, const float* d_dlogps, void* dlogits, int32_t grad_dtype,
-                                 int64_t ldg, void* workspace, int64_t workspace_bytes, void* stream);
+                                 int64_t ldg, void* stream);
 
 /* Preference loss over ``pairs`` >= 1 pairs of sequences packed back to back, chosen
  * then rejected: sequence 2 i and 2 i + 1 of cu_seqlens [2 pairs + 1] (0 .. tokens;

@@ -7,6 +7,7 @@ stream; there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import torch
@@ -129,7 +130,7 @@ def lib():
                  ctypes.c_int),
                 ("axon_token_loss_workspace", [i64, i32, i32], i64),
                 ("axon_token_logprobs", [*logits, p, *work], ctypes.c_int),
-                ("axon_token_logprobs_backward", [*logits, p, *grad, *work], ctypes.c_int),
+                ("axon_token_logprobs_backward", [*logits, p, *grad, p], ctypes.c_int),
                 ("axon_preference_loss", [*logits, i32, p, i32p, p, f32, f32, p, p, p, *grad, *work], ctypes.c_int),
                 ("axon_policy_loss", [*logits, i32, p, i32p, p, p, p, f32, f32, f32, i32, p, p, p, *grad, *work],
                  ctypes.c_int)]:
@@ -212,56 +213,65 @@ def _code(t: torch.Tensor, name: str) -> int:
     return code
 
 
-class _On:
-    """Makes a tensor's device and the given stream (None: the device's current
-    one) current for a call: what the call allocates belongs to that stream.  Inputs
-    made on another stream must be ready on this one; they are kept from reuse
-    until its work is done."""
+def _row_operator(f):
+    """Runs f on its tensors' device and on ``stream`` (None: that device's current
+    one), so that what it allocates belongs there.  Inputs made on another stream must
+    be ready on this one; they are kept from reuse until its work is done."""
+    @functools.wraps(f)
+    def call(*args, stream=None, **kw):
+        device = None
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor):
+                if device is None:
+                    device = t.device
+                    if device.type != "cuda":
+                        raise ValueError(f"{f.__name__} takes tensors on the GPU, got one on {device}")
+                elif t.device != device:
+                    raise ValueError(f"{f.__name__}: tensors on {device} and {t.device} in one call")
+        if device is None:
+            raise ValueError(f"{f.__name__} takes tensors on the GPU")
+        if stream is None and device.index == torch.cuda.current_device():
+            return f(*args, **kw)
+        with torch.cuda.device(device):
+            if stream is None:
+                return f(*args, **kw)
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream))
+            for t in (*args, *kw.values()):
+                if isinstance(t, torch.Tensor):
+                    t.record_stream(stream)
+            with torch.cuda.stream(stream):
+                return f(*args, **kw)
+    return call
 
-    def __init__(self, x: torch.Tensor, stream, *tensors):
-        if not x.is_cuda:
-            raise ValueError("the row operators take tensors on the GPU")
-        for t in tensors:
-            if t is not None and t.device != x.device:
-                raise ValueError(f"tensors on {x.device} and {t.device} in one call")
-        self.x, self.stream, self.tensors = x, stream, tensors
 
-    def __enter__(self):
-        self.device = torch.cuda.device(self.x.device)
-        self.device.__enter__()
-        if self.stream is None:
-            self.scope = None
-            return torch.cuda.current_stream().cuda_stream
-        st = self.stream if hasattr(self.stream, "cuda_stream") else torch.cuda.ExternalStream(int(self.stream))
-        for t in (self.x, *self.tensors):
-            if t is not None:
-                t.record_stream(st)
-        self.scope = torch.cuda.stream(st)
-        self.scope.__enter__()
-        return st.cuda_stream
-
-    def __exit__(self, *e):
-        if self.scope is not None:
-            self.scope.__exit__(*e)
-        self.device.__exit__(*e)
+def _current(t: torch.Tensor) -> int:
+    """The current stream of t's device, as the C ABI takes it."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device())
 
 
 def _rows(t: torch.Tensor, name: str, out: bool = False):
     """(the tensor, rows, columns, row stride) of a tensor whose last dimension is
     its columns.  An input of another layout is copied; an output is refused."""
-    if t.dim() == 0:
-        raise ValueError(f"{name} has no columns")
     v = t
     if t.dim() != 2:
+        if t.dim() == 0:
+            raise ValueError(f"{name} has no columns")
         try:
             v = t.view(-1, t.shape[-1]) if t.shape[-1] else t.reshape(0, 0)
         except RuntimeError:
             v = None
-    if v is None or (v.shape[1] > 1 and v.stride(1) != 1) or (v.shape[0] > 1 and v.stride(0) < v.shape[1]):
-        if out:
-            raise ValueError(f"{name} must have contiguous columns and rows that do not overlap")
-        v = t.contiguous().view(-1, t.shape[-1])
-    return v, v.shape[0], v.shape[1], v.stride(0) if v.shape[0] > 1 else max(v.shape[1], 1)
+    if v is not None:
+        rows, cols = v.shape
+        ld, one = v.stride()
+        if rows < 2:
+            ld = max(cols, 1)
+        if (one == 1 or cols < 2) and ld >= cols:
+            return v, rows, cols, ld
+    if out:
+        raise ValueError(f"{name} must have contiguous columns and rows that do not overlap")
+    v = t.contiguous().view(-1, t.shape[-1])
+    return v, v.shape[0], v.shape[1], max(v.shape[1], 1)
 
 
 def _vector(t, n: int, dtype, name: str):
@@ -278,50 +288,51 @@ def _ptr(t):
 
 
 def _like(out, x: torch.Tensor, dtype, name: str) -> torch.Tensor:
-    """The caller's output buffer, or a new one of x's shape."""
+    """The caller's output buffer (of any dtype when dtype is None), or a new one of
+    x's shape."""
     if out is None:
-        return torch.empty(x.shape, dtype=dtype, device=x.device)
+        return torch.empty_like(x, dtype=dtype, memory_format=torch.contiguous_format)
     if out.shape != x.shape or (dtype is not None and out.dtype != dtype):
-        raise ValueError(f"{name} must be {tuple(x.shape)} {dtype}, got {tuple(out.shape)} {out.dtype}")
+        raise ValueError(f"{name} must be {tuple(x.shape)} {dtype or ''}, got {tuple(out.shape)} {out.dtype}")
     return out
 
 
+@_row_operator
 def layernorm(x: torch.Tensor, gain: torch.Tensor, bias: torch.Tensor | None = None, eps: float = 1e-5,
-              dtype: torch.dtype | None = None, out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+              dtype: torch.dtype | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """Layer norm over the last dimension of ``x`` (axon_layernorm), in ``dtype``
     (x's by default; ``out`` may be x)."""
-    with _On(x, stream, gain, bias, out) as s:
-        y = _like(out, x, dtype if dtype is not None or out is not None else x.dtype, "out")
-        xv, rows, cols, ldx = _rows(x, "x")
-        yv, _, _, ldy = _rows(y, "out", out=True)
-        gain = _vector(gain, cols, gain.dtype, "gain")
-        bias = _vector(bias, cols, gain.dtype, "bias")
-        _check(lib().axon_layernorm(rows, cols, xv.data_ptr(), _code(x, "x"), ldx, gain.data_ptr(), _ptr(bias),
-                                    _code(gain, "gain"), eps, yv.data_ptr(), _code(y, "out"), ldy, s))
-        return y
+    y = _like(out, x, x.dtype if dtype is None and out is None else dtype, "out")
+    xv, rows, cols, ldx = _rows(x, "x")
+    yv, _, _, ldy = _rows(y, "out", out=True)
+    gain = _vector(gain, cols, gain.dtype, "gain")
+    bias = _vector(bias, cols, gain.dtype, "bias")
+    _check(lib().axon_layernorm(rows, cols, xv.data_ptr(), _code(x, "x"), ldx, gain.data_ptr(), _ptr(bias),
+                                _code(gain, "gain"), eps, yv.data_ptr(), _code(y, "out"), ldy, _current(x)))
+    return y
 
 
+@_row_operator
 def layernorm_backward(dy: torch.Tensor, x: torch.Tensor, gain: torch.Tensor, eps: float = 1e-5,
-                       dx: torch.Tensor | None = None, stream=None):
+                       dx: torch.Tensor | None = None):
     """(dx, dgain, dbias) of :func:`layernorm` from the gradient ``dy`` of its
     output (axon_layernorm_backward): dx in x's dtype (``dx`` may be x or dy), dgain
     and dbias float32."""
     if dy.shape != x.shape:
         raise ValueError(f"dy has shape {tuple(dy.shape)}, x {tuple(x.shape)}")
-    with _On(x, stream, dy, gain, dx) as s:
-        dx = _like(dx, x, x.dtype, "dx")
-        xv, rows, cols, ldx = _rows(x, "x")
-        dv, _, _, lddy = _rows(dy, "dy")
-        ov, _, _, lddx = _rows(dx, "dx", out=True)
-        gain = _vector(gain, cols, gain.dtype, "gain")
-        par = torch.empty((2, cols), dtype=torch.float32, device=x.device)
-        need = lib().axon_layernorm_backward_workspace(rows, cols)
-        ws = torch.empty((need,), dtype=torch.uint8, device=x.device)
-        at = par.data_ptr()
-        _check(lib().axon_layernorm_backward(rows, cols, xv.data_ptr(), _code(x, "x"), ldx, dv.data_ptr(),
-                                             _code(dy, "dy"), lddy, gain.data_ptr(), _code(gain, "gain"), eps,
-                                             ov.data_ptr(), lddx, at, at + 4 * cols, ws.data_ptr(), need, s))
-        return dx, par[0], par[1]
+    dx = _like(dx, x, x.dtype, "dx")
+    xv, rows, cols, ldx = _rows(x, "x")
+    dv, _, _, lddy = _rows(dy, "dy")
+    ov, _, _, lddx = _rows(dx, "dx", out=True)
+    gain = _vector(gain, cols, gain.dtype, "gain")
+    dgain = torch.empty(cols, dtype=torch.float32, device=x.device)
+    dbias = torch.empty_like(dgain)
+    need = lib().axon_layernorm_backward_workspace(rows, cols)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check(lib().axon_layernorm_backward(rows, cols, xv.data_ptr(), _code(x, "x"), ldx, dv.data_ptr(), _code(dy, "dy"),
+                                         lddy, gain.data_ptr(), _code(gain, "gain"), eps, ov.data_ptr(), lddx,
+                                         dgain.data_ptr(), dbias.data_ptr(), ws.data_ptr(), need, _current(x)))
+    return dx, dgain, dbias
 
 
 def _logit_args(logits, targets):
@@ -330,60 +341,61 @@ def _logit_args(logits, targets):
     return z, tg, (tokens, vocab, z.data_ptr(), _code(logits, "logits"), ld, tg.data_ptr())
 
 
-def _loss_workspace(tokens, vocab, seqs, device):
+def _loss_workspace(tokens, vocab, seqs, like):
     need = lib().axon_token_loss_workspace(tokens, vocab, seqs)
-    return torch.empty((need,), dtype=torch.uint8, device=device), need
+    return torch.empty(need, dtype=torch.uint8, device=like.device), need
 
 
-def _grad_args(dlogits, logits):
-    if dlogits is None:
-        return None, (None, AXON_F32, 0)
-    v, _, _, ld = _rows(dlogits, "dlogits", out=True)
-    return v, (v.data_ptr(), _code(dlogits, "dlogits"), ld)
+def _grad(dlogits, logits, wanted=True):
+    """(the gradient's tensor, a view that keeps its rows, their C arguments)"""
+    if not wanted:
+        return None, None, (None, AXON_F32, 0)
+    g = _like(dlogits, logits, logits.dtype if dlogits is None else None, "dlogits")
+    v, _, _, ld = _rows(g, "dlogits", out=True)
+    return g, v, (v.data_ptr(), _code(g, "dlogits"), ld)
 
 
-def _cu_args(cu_seqlens, cu_device, device):
+def _cu_args(cu_seqlens, cu_device, like):
     n = len(cu_seqlens)
     host = (ctypes.c_int32 * max(n, 1))(*cu_seqlens)
     if cu_device is None:
-        return host, torch.tensor(cu_seqlens, dtype=torch.int32, device=device)
+        return host, torch.tensor(cu_seqlens, dtype=torch.int32, device=like.device)
     if cu_device.dtype != torch.int32 or cu_device.numel() < n or not cu_device.is_contiguous():
         raise ValueError(f"cu_device must hold the {n} int32 values of cu_seqlens")
     return host, cu_device
 
 
-def token_logprobs(logits: torch.Tensor, targets: torch.Tensor, stream=None) -> torch.Tensor:
+@_row_operator
+def token_logprobs(logits: torch.Tensor, targets: torch.Tensor) -> torch.Tensor:
     """logits[t][targets[t]] - logsumexp(logits[t]) (axon_token_logprobs): logits [tokens,
     vocab] float32 or bfloat16, targets int32 [tokens] (a value outside [0, vocab)
     does not count and gives 0).  Returns float32 [tokens]."""
-    with _On(logits, stream, targets) as s:
-        z, tg, args = _logit_args(logits, targets)
-        out = torch.empty((args[0],), dtype=torch.float32, device=z.device)
-        ws, need = _loss_workspace(args[0], args[1], 0, z.device)
-        _check(lib().axon_token_logprobs(*args, out.data_ptr(), ws.data_ptr(), need, s))
-        return out
+    z, tg, args = _logit_args(logits, targets)
+    out = torch.empty(args[0], dtype=torch.float32, device=z.device)
+    ws, need = _loss_workspace(args[0], args[1], 0, z)
+    _check(lib().axon_token_logprobs(*args, out.data_ptr(), ws.data_ptr(), need, _current(z)))
+    return out
 
 
+@_row_operator
 def token_logprobs_backward(logits: torch.Tensor, targets: torch.Tensor, dlogps: torch.Tensor,
-                            dlogits: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+                            dlogits: torch.Tensor | None = None) -> torch.Tensor:
     """The gradient at the logits of a loss whose gradient at
     :func:`token_logprobs` is ``dlogps`` (float32 [tokens]).  ``dlogits``: a buffer
     for it, of either dtype (the logits' own is allowed); by default a new one of the
     logits' dtype."""
-    with _On(logits, stream, targets, dlogps, dlogits) as s:
-        z, tg, args = _logit_args(logits, targets)
-        dlogps = _vector(dlogps, args[0], torch.float32, "dlogps")
-        dlogits = _like(dlogits, logits, logits.dtype if dlogits is None else dlogits.dtype, "dlogits")
-        g, gargs = _grad_args(dlogits, logits)
-        ws, need = _loss_workspace(args[0], args[1], 0, z.device)
-        _check(lib().axon_token_logprobs_backward(*args, dlogps.data_ptr(), *gargs, ws.data_ptr(), need, s))
-        return dlogits
+    z, tg, args = _logit_args(logits, targets)
+    dlogps = _vector(dlogps, args[0], torch.float32, "dlogps")
+    g, gv, gargs = _grad(dlogits, logits)
+    _check(lib().axon_token_logprobs_backward(*args, dlogps.data_ptr(), *gargs, _current(z)))
+    return g
 
 
+@_row_operator
 def preference_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: list,
                     ref_logps: torch.Tensor | None = None, beta: float = 0.1, label_smoothing: float = 0.0,
                     dlogits: torch.Tensor | None = None, want_grad: bool = True,
-                    cu_device: torch.Tensor | None = None, stream=None):
+                    cu_device: torch.Tensor | None = None):
     """Preference loss over pairs of sequences packed back to back, chosen then
     rejected (axon_preference_loss): cu_seqlens a host list of 2 pairs + 1 prefix sums
     (cu_device: the same in a device int32 buffer, which saves its copy), ref_logps
@@ -393,47 +405,44 @@ def preference_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: lis
     pairs = (len(cu_seqlens) - 1) // 2
     if len(cu_seqlens) != 2 * pairs + 1 or pairs < 1:
         raise ValueError("cu_seqlens must have an odd number of entries, at least 3: sequences come in pairs")
-    with _On(logits, stream, targets, ref_logps, dlogits, cu_device) as s:
-        z, tg, args = _logit_args(logits, targets)
-        ref_logps = _vector(ref_logps, 2 * pairs, torch.float32, "ref_logps")
-        if want_grad:
-            dlogits = _like(dlogits, logits, logits.dtype if dlogits is None else dlogits.dtype, "dlogits")
-        g, gargs = _grad_args(dlogits if want_grad else None, logits)
-        host, cu = _cu_args(cu_seqlens, cu_device, z.device)
-        out = torch.empty((1 + 3 * pairs,), dtype=torch.float32, device=z.device)
-        at = out.data_ptr()
-        ws, need = _loss_workspace(args[0], args[1], 2 * pairs, z.device)
-        _check(lib().axon_preference_loss(*args, pairs, cu.data_ptr(), host, _ptr(ref_logps), beta, label_smoothing,
-                                          at, at + 4, at + 4 + 8 * pairs, *gargs, ws.data_ptr(), need, s))
-        return out[:1], out[1:1 + 2 * pairs], out[1 + 2 * pairs:], dlogits if want_grad else None
+    z, tg, args = _logit_args(logits, targets)
+    ref_logps = _vector(ref_logps, 2 * pairs, torch.float32, "ref_logps")
+    g, gv, gargs = _grad(dlogits, logits, want_grad)
+    host, cu = _cu_args(cu_seqlens, cu_device, z)
+    out = torch.empty(1 + 3 * pairs, dtype=torch.float32, device=z.device)
+    at = out.data_ptr()
+    ws, need = _loss_workspace(args[0], args[1], 2 * pairs, z)
+    _check(lib().axon_preference_loss(*args, pairs, cu.data_ptr(), host, _ptr(ref_logps), beta, label_smoothing, at,
+                                      at + 4, at + 4 + 8 * pairs, *gargs, ws.data_ptr(), need, _current(z)))
+    loss, seq, margins = out.split_with_sizes((1, 2 * pairs, pairs))
+    return loss, seq, margins, g
 
 
+@_row_operator
 def policy_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: list, old_logps: torch.Tensor,
                 advantages: torch.Tensor, ref_logps: torch.Tensor | None = None, clip_low: float = 0.2,
                 clip_high: float = 0.2, kl_coef: float = 0.0, per_sequence: bool = False,
                 dlogits: torch.Tensor | None = None, want_grad: bool = True,
-                cu_device: torch.Tensor | None = None, stream=None):
+                cu_device: torch.Tensor | None = None):
     """Clipped policy loss with a KL term (axon_policy_loss): old_logps, advantages
     and ref_logps (None: no KL term) float32 [tokens]; averaged over the counted
     tokens, or over each sequence's and then the sequences (per_sequence).  Returns
     (loss [1], stats [3], logps [tokens], dlogits or None)."""
-    with _On(logits, stream, targets, old_logps, advantages, ref_logps, dlogits, cu_device) as s:
-        z, tg, args = _logit_args(logits, targets)
-        old_logps = _vector(old_logps, args[0], torch.float32, "old_logps")
-        advantages = _vector(advantages, args[0], torch.float32, "advantages")
-        ref_logps = _vector(ref_logps, args[0], torch.float32, "ref_logps")
-        if want_grad:
-            dlogits = _like(dlogits, logits, logits.dtype if dlogits is None else dlogits.dtype, "dlogits")
-        g, gargs = _grad_args(dlogits if want_grad else None, logits)
-        host, cu = _cu_args(cu_seqlens, cu_device, z.device)
-        batch = len(cu_seqlens) - 1
-        out = torch.empty((4 + args[0],), dtype=torch.float32, device=z.device)
-        at = out.data_ptr()
-        ws, need = _loss_workspace(args[0], args[1], batch, z.device)
-        _check(lib().axon_policy_loss(*args, batch, cu.data_ptr(), host, old_logps.data_ptr(), _ptr(ref_logps),
-                                      advantages.data_ptr(), clip_low, clip_high, kl_coef, int(per_sequence), at,
-                                      at + 4, at + 16, *gargs, ws.data_ptr(), need, s))
-        return out[:1], out[1:4], out[4:], dlogits if want_grad else None
+    z, tg, args = _logit_args(logits, targets)
+    tokens, batch = args[0], len(cu_seqlens) - 1
+    old_logps = _vector(old_logps, tokens, torch.float32, "old_logps")
+    advantages = _vector(advantages, tokens, torch.float32, "advantages")
+    ref_logps = _vector(ref_logps, tokens, torch.float32, "ref_logps")
+    g, gv, gargs = _grad(dlogits, logits, want_grad)
+    host, cu = _cu_args(cu_seqlens, cu_device, z)
+    out = torch.empty(4 + tokens, dtype=torch.float32, device=z.device)
+    at = out.data_ptr()
+    ws, need = _loss_workspace(tokens, args[1], batch, z)
+    _check(lib().axon_policy_loss(*args, batch, cu.data_ptr(), host, old_logps.data_ptr(), _ptr(ref_logps),
+                                  advantages.data_ptr(), clip_low, clip_high, kl_coef, int(per_sequence), at, at + 4,
+                                  at + 16, *gargs, ws.data_ptr(), need, _current(z)))
+    loss, stats, logps = out.split_with_sizes((1, 3, tokens))
+    return loss, stats, logps, g
 
 
 class Model:

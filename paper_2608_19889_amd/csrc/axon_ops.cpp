@@ -179,16 +179,14 @@ extern "C" int axon_token_logprobs(int64_t tokens, int32_t vocab, const void* lo
 
 extern "C" int axon_token_logprobs_backward(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype,
                                             int64_t ld, const int32_t* d_targets, const float* d_dlogps, void* dlogits,
-                                            int32_t grad_dtype, int64_t ldg, void* workspace, int64_t workspace_bytes,
-                                            void* stream) {
+                                            int32_t grad_dtype, int64_t ldg, void* stream) {
   return entry([&]() -> int {
     if (int r = check_logits(tokens, vocab, logits, dtype, ld, d_targets)) return r;
     if (int r = check_grad(dlogits, grad_dtype, ldg, tokens, vocab, logits, dtype, ld)) return r;
     if (tokens == 0) return AXON_OK;
     if (int r = check_array("d_dlogps", d_dlogps, 4)) return r;
-    if (int r = check_workspace(workspace, workspace_bytes, axon_token_loss_workspace(tokens, vocab, 0))) return r;
     launch_token_logps_bwd(rows_of(logits, dtype, ld, tokens, vocab, d_targets, dlogits, grad_dtype, ldg), d_dlogps,
-                           workspace, (hipStream_t)stream);
+                           (hipStream_t)stream);
     return check_launch("token log-probabilities backward");
   });
 }

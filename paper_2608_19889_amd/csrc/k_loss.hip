@@ -11,11 +11,12 @@
 // the reference's).
 //
 //   logit_part_kernel   reads the rows: (m, S) of every slice of a row
-//   *_finish_kernel     merges a row's slices; loss, statistics, c of every token
+//   *_finish_kernel     joins a row's slices; loss, statistics, c of every token
 //   logit_grad_kernel   reads the rows again and writes the gradient
+//   logit_row_kernel    all of it in one pass, where c depends on the row alone
 //
-// All three are HBM bound (V 4 or 2 bytes a row against a few exponentials).  No
-// atomics: every sum has one order.
+// All are HBM bound (V 4 or 2 bytes a row against a few exponentials).  No atomics:
+// every sum has one order.
 #include <algorithm>
 
 #include "common.h"
@@ -35,6 +36,14 @@ AXON_DEV void join_part(float& m, float& s, float m2, float s2) {
   s = s * __expf(m - a) + s2 * __expf(m2 - a);
   m = top;
 }
+
+// the sum of a single logit, as its own maximum
+AXON_DEV float one_exp(float v) { return v == -INFINITY ? 0.f : v - v + 1.f; }  // (infinity or NaN: NaN)
+
+// 1 where a row's wide accesses would be off by 2 bytes (they take 20% longer than any
+// multiple of 4): its first logit goes alone then, the groups of 8 start after it
+AXON_DEV int odd_head(const float*) { return 0; }
+AXON_DEV int odd_head(const bf16* row) { return (int)((uintptr_t)row >> 1 & 1); }
 
 // exp(v - m) for many v <= m as 2^(v log2 e - m log2 e): one fused multiply-add and the
 // hardware exponential.  m log2 e is rounded, which scales every result by the same
@@ -117,21 +126,23 @@ __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __res
   __shared__ float red[2][PART_THREADS / 64];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t t = it / slices;
-    const int c0 = (int)(it % slices) * cols, n = min(V - c0, cols);
     const int tg = targets[t];
     if (tg < 0 || tg >= V) {  // uniform over the workgroup
       if (logps && threadIdx.x == 0) logps[t] = 0.f;
       continue;
     }
-    const T* row = z + t * ld + c0;
+    const T* row = z + t * ld;
+    const int h = odd_head(row), c0 = (int)(it % slices) * cols, n = min(V - h - c0, cols);
     float m = -INFINITY, s = 0.f;
+    if (h && c0 == 0 && threadIdx.x == 0) join_part(m, s, to_f32(row[0]), one_exp(to_f32(row[0])));
+    row += h + c0;
     if (n >= 8) {
       int c = 0;
       for (; c + BLOCK <= n; c += BLOCK) read_runs<PART_RUNS, false>(row, c + threadIdx.x * 8, STRIDE, n, m, s);
       for (; c < n; c += STRIDE) read_runs<1, true>(row, c + threadIdx.x * 8, STRIDE, n, m, s);
-    } else if (threadIdx.x < n) {
-      m = to_f32(row[threadIdx.x]);
-      s = m == -INFINITY ? 0.f : m - m + 1.f;  // (an infinite or NaN logit: NaN)
+    } else if ((int)threadIdx.x < n) {
+      const float v = to_f32(row[threadIdx.x]);
+      join_part(m, s, v, one_exp(v));
     }
     join_block(m, s, red);
     if (threadIdx.x == 0) {
@@ -141,34 +152,26 @@ __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __res
   }
 }
 
-// (m, S) of row t from its slices, and its target's log-probability
-template <typename T>
-AXON_DEV double merge_row(const T* z, int64_t ld, const float2* part, int slices, int64_t t, int tg, float2& st) {
-  const float2* p = part + t * slices;
-  float m = p[0].x, s = p[0].y;
-  for (int i = 1; i < slices; ++i) join_part(m, s, p[i].x, p[i].y);
-  st = float2{m, s};
-  return (double)to_f32(z[t * ld + tg]) - (double)m - log((double)s);
-}
-
+// log-probabilities from the rows' slices
 template <typename T>
 __global__ void __launch_bounds__(256) logps_finish_kernel(const T* __restrict__ z, int64_t ld, int V,
                                                            const int32_t* __restrict__ targets, int64_t tokens,
                                                            const float2* __restrict__ part, int slices,
-                                                           float* __restrict__ logps,
-                                                           const float* __restrict__ dlogps, float2* __restrict__ stat,
-                                                           float* __restrict__ coef) {
+                                                           float* __restrict__ logps) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (t >= tokens) return;
   const int tg = targets[t];
-  const bool ok = tg >= 0 && tg < V;
-  float2 st = {0.f, 1.f};
-  const double lp = ok ? merge_row(z, ld, part, slices, t, tg, st) : 0.0;
-  if (logps) logps[t] = (float)lp;
-  if (coef) {
-    stat[t] = st;
-    coef[t] = ok ? dlogps[t] : 0.f;
+  float m = -INFINITY, s = 0.f;
+  if (tg < 0 || tg >= V) {
+    logps[t] = 0.f;
+    return;
   }
+#pragma unroll 4
+  for (int i = 0; i < slices; ++i) {
+    const float2 p = part[t * slices + i];
+    join_part(m, s, p.x, p.y);
+  }
+  logps[t] = (float)((double)to_f32(z[t * ld + tg]) - (double)m - log((double)s));
 }
 
 AXON_DEV double wave_sum_f64(double v) {
@@ -448,13 +451,15 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld,
     const int64_t t = it / slices;
     const int first = (int)(it % slices) * COLS, c0 = first + threadIdx.x * 8;
     const float w = coef[t];
-    const T* row = z + t * ld;
-    TO* out = dz + t * lddz;
     const float2 st = stat[t];
-    const int tg = targets[t];
     const ExpFrom e(st.x);
     const float f = -w / st.y * e.fix;
-    if (first + COLS <= V) {
+    const T* row = z + t * ld;
+    const int h = odd_head(row), n = V - h, tg = targets[t] - h;
+    row += h;
+    TO* out = dz + t * lddz + h;
+    if (h && c0 == 0) out[-1] = from_f32<TO>(w == 0.f ? 0.f : e(to_f32(row[-1])) * f + (tg == -1 ? w : 0.f));
+    if (first + COLS <= n) {
       float v[GRAD_RUNS][8] = {};
       if (w != 0.f) {
         Run8<T> r[GRAD_RUNS];
@@ -470,13 +475,13 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld,
 #pragma unroll
       for (int k = 0; k < GRAD_RUNS; ++k) Run8<TO>::store(out + c0 + k * STRIDE, v[k]);
     } else {  // the row's last slice
-      for (int c = c0; c < V; c += STRIDE) {
+      for (int c = c0; c < n; c += STRIDE) {
         float v[8] = {};
         if (w != 0.f) {
-          load_run8(row, c, V, v, 0.f);
+          load_run8(row, c, n, v, 0.f);
           grad_run(v, e, f, w, tg - c);
         }
-        store_run8(out, c, V, v);
+        store_run8(out, c, n, v);
       }
     }
   }
@@ -485,10 +490,12 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld,
 // ---------------------------------------------------------------- whole rows, read once
 //
 // Where a row's coefficient depends on that row alone (a caller's own dlogps, the
-// policy loss) and there are rows enough for every CU, a workgroup keeps its row in
-// registers from the statistics to the gradient: the logits are read once.  RUNS
-// groups of 8 logits a thread, THREADS x RUNS x 8 columns; what a row has beyond them is
-// read a second time.  HBM bound: 2 V values a row against 3.
+// policy loss), a workgroup keeps its row in registers from the statistics to the
+// gradient: the logits are read once.  RUNS groups of 8 logits a thread, THREADS x RUNS x
+// 8 columns; what a row has beyond them is read a second time (soon enough to come from
+// the L2).  HBM bound: 2 V values a row against 3.  4096 x 128256: bf16 390 us (5.4 TB/s
+// of the 2 V; in two passes with a kernel for the coefficients between them 592), float32
+// 811 (1153); 64 rows 17 us (34), one row 15 (14).
 
 // the weights, one launch before the rows: w[0] = 1 / counted tokens, or w[j] = 1 /
 // (sequences with counted tokens x those of sequence j)
@@ -531,31 +538,41 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
                                                             RowCoef rc, TO* dz, int64_t lddz) {
   constexpr int NW = THREADS / 64, STRIDE = THREADS * 8, HELD = STRIDE * RUNS;
   __shared__ float2 parts[16];
-  __shared__ float2 chosen;  // c, and the target's logit
-  const int i = threadIdx.x, whole = V & ~7;
-  const int full = min(whole / STRIDE, RUNS);                // groups that every thread has,
-  const bool more = full * STRIDE + i * 8 < min(whole, HELD);  // and whether it has one after them
-  const int groups = full + (full * STRIDE < min(whole, HELD) ? 1 : 0);
-  auto zeros = [&](TO* out) {
-    const float zero[8] = {};
-    for (int c = i * 8; c < whole; c += STRIDE) Run8<TO>::store(out + c, zero);
-    if (whole + i < V) out[whole + i] = from_f32<TO>(0.f);
-  };
+  __shared__ float coef;
+  const int i = threadIdx.x;
   const int64_t t = first + blockIdx.x;
   const T* row = z + t * ld;
-  TO* out = dz + t * lddz;
-  const int tg = targets[t];
-  if (tg < 0 || tg >= V) {  // uniform over the workgroup
-    zeros(out);
+  const int h = odd_head(row), whole = V - h & ~7;
+  row += h;
+  TO* out = dz + t * lddz + h;
+  const int tg = targets[t] - h;
+  const bool counts = tg + h >= 0 && tg + h < V;
+  // groups that every thread has, and whether this one has another after them
+  const int full = min(whole / STRIDE, RUNS), groups = min((whole + STRIDE - 1) / STRIDE, RUNS);
+  const bool more = full < groups && full * STRIDE + i * 8 < whole;
+  // the columns beside the groups of 8, one a thread: the last few, and the head
+  const bool single = i < V - h - whole || (i == 7 && h);
+  const int at = i < V - h - whole ? whole + i : -1;
+  auto zeros = [&] {
+    const float zero[8] = {};
+    for (int c = i * 8; c < whole; c += STRIDE) Run8<TO>::store(out + c, zero);
+    if (single) out[at] = from_f32<TO>(0.f);
+  };
+  if (!counts) {  // uniform over the workgroup
+    zeros();
     return;
   }
+  const bool policy = rc.dlogps == nullptr;
+  const float zt = to_f32(row[tg]), given = policy ? rc.old[t] : rc.dlogps[t];
+  const float adv = policy ? rc.adv[t] : 0.f, ref = policy && rc.ref ? rc.ref[t] : 0.f;
+  const float weight = policy ? (float)rc.weights[rc.cu ? seq_of_token(rc.cu, rc.seqs, (int)t) : 0] : 1.f;
   // every load unconditional (past the row's groups its last one again), so that
   // each is waited for by itself and the sums run under the loads behind them
   Run8<T> r[RUNS];
+  if (whole > 0)
 #pragma unroll
-  for (int k = 0; k < RUNS; ++k) r[k].load(at_byte(row, min(k * STRIDE + i * 8, whole - 8) * (unsigned)sizeof(T)));
-  // the columns past the groups of 8, one a thread
-  const float last = whole + i < V ? to_f32(row[whole + i]) : -INFINITY;
+    for (int k = 0; k < RUNS; ++k) r[k].load(at_byte(row, min(k * STRIDE + i * 8, whole - 8) * (unsigned)sizeof(T)));
+  const float alone = single ? to_f32(row[at]) : -INFINITY;
   float m = -INFINITY, s = 0.f;
 #pragma unroll
   for (int k = 0; k < RUNS; ++k) {
@@ -575,37 +592,31 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
     for (int j = 0; j < 8; ++j) v[0][j] = q[j];
     take_runs(m, s, v);
   }
-  join_part(m, s, last, last == -INFINITY ? 0.f : last - last + 1.f);  // (infinity or NaN: NaN)
-  const float top = m;
+  join_part(m, s, alone, one_exp(alone));
   // over the wavefronts: lane l joins what wavefront l % NW left
-  const float wm = wave_max(top);
-  s = wave_sum(s * __expf(top - (wm == -INFINITY ? 0.f : wm)));
+  const float wm = wave_max(m);
+  s = wave_sum(s * __expf(m - (wm == -INFINITY ? 0.f : wm)));
   if ((i & 63) == 0) parts[i >> 6] = float2{wm, s};
   __syncthreads();
   const float2 p = parts[i % NW];
   m = over_waves<NW>(p.x, [](float a, float b) { return fmaxf(a, b); });
   s = over_waves<NW>(p.y * __expf(p.x - (m == -INFINITY ? 0.f : m)), [](float a, float b) { return a + b; });
-  if (i == 0) {
-    const float zt = to_f32(row[tg]);
-    if (rc.dlogps) {
-      chosen = float2{rc.dlogps[t], zt};
-    } else {
-      const float w = (float)rc.weights[rc.cu ? seq_of_token(rc.cu, rc.seqs, (int)t) : 0];
-      const PolicyTerms p = policy_token(zt, m, s, rc.old[t], rc.adv[t], rc.ref != nullptr, rc.ref ? rc.ref[t] : 0.f,
-                                         rc.lo, rc.hi, rc.kl_coef);
-      chosen = float2{w * p.c, zt};
+  float w = given;
+  if (policy) {
+    if (i == 0) {
+      coef = weight * policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef).c;
       rc.stat[t] = float2{m, s};
       rc.chosen[t] = zt;
     }
+    __syncthreads();
+    w = coef;
   }
-  __syncthreads();
-  const float w = chosen.x, zt = chosen.y;
-  const ExpFrom e(m);
   // a coefficient of 0 (clipped): zeros, whatever the row holds
   if (w == 0.f) {
-    zeros(out);
+    zeros();
     return;
   }
+  const ExpFrom e(m);
   const float f = -w / s * e.fix;
   auto grad = [&](const Run8<T>& q, TO* to) {
     float v[8];
@@ -621,9 +632,10 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
     q.load(row + c);
     grad(q, out + c);
   }
-  if (whole + i < V) out[whole + i] = from_f32<TO>(e(last) * f);
+  if (single) out[at] = from_f32<TO>(e(alone) * f);
   // the target's own column, by the thread that has just written it
-  if (i == (tg < whole ? (tg >> 3) % THREADS : tg - whole)) out[tg] = from_f32<TO>(e(zt) * f + w);
+  const int owner = tg < 0 ? 7 : tg < whole ? (tg >> 3) % THREADS : tg - whole;
+  if (i == owner) out[tg] = from_f32<TO>(e(zt) * f + w);
 }
 
 // ---------------------------------------------------------------- within a training step
@@ -675,14 +687,14 @@ namespace {
 
 constexpr int64_t MAX_WGS = 1 << 20;  // more items than this: the workgroups loop
 
-constexpr int64_t ROW_TOKENS = 1024;
-
 // Slices of a row for the statistics pass: whole rows once there are enough of
-// them for two rounds of 8 workgroups on each of the 256 CUs, else as many slices
-// as give that, of at least one group of 8 per thread
+// them for two rounds of 8 workgroups on each of the 256 CUs, else as many slices as
+// give that, of at least one group of 8 per thread, and at most 16 (they are joined by
+// one thread)
 void part_shape(int64_t tokens, int V, int& slices, int& cols) {
   const int most = (V + PART_THREADS * 8 - 1) / (PART_THREADS * 8);
-  const int want = (int)std::min<int64_t>(most, std::max<int64_t>(1, 4096 / std::max<int64_t>(tokens, 1)));
+  const int64_t fill = std::max<int64_t>(1, 4096 / std::max<int64_t>(tokens, 1));
+  const int want = (int)std::min<int64_t>({most, 16, fill});
   const int runs = (most + want - 1) / want;
   cols = runs * PART_THREADS * 8;
   slices = (V + cols - 1) / cols;
@@ -740,9 +752,6 @@ void run_grad(const LogitRows& r, const LossWs& w, hipStream_t s) {
                                                     (float*)r.dz, r.lddz);
 }
 
-// rows enough to give each CU several, and long enough for the registers to matter
-bool whole_rows(const LogitRows& r) { return r.dz && r.tokens >= ROW_TOKENS && r.V >= 2048; }
-
 template <typename T, typename TO>
 void run_rows(const LogitRows& r, const RowCoef& rc, hipStream_t s) {
   auto go = [&](auto kern, int threads) {
@@ -763,20 +772,20 @@ void run_rows(const LogitRows& r, const RowCoef& rc, hipStream_t s) {
 }
 
 template <typename T>
-void logprobs(const LogitRows& r, float* logps, const float* dlogps, void* wsp, hipStream_t s) {
-  if (r.tokens <= 0) return;
+void logprobs(const LogitRows& r, float* logps, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, 0, (char*)wsp, &w);
-  if (whole_rows(r)) {
-    RowCoef rc{};
-    rc.dlogps = dlogps;
-    return run_rows<T>(r, rc, s);
-  }
   const int slices = run_parts<T>(r, w.part, logps, s);
-  if (logps && slices == 1) return;
-  logps_finish_kernel<T><<<(unsigned)((r.tokens + 255) / 256), 256, 0, s>>>(
-      (const T*)r.z, r.ld, r.V, r.targets, r.tokens, w.part, slices, logps, dlogps, w.stat, dlogps ? w.coef : nullptr);
-  if (dlogps) run_grad<T>(r, w, s);
+  if (slices > 1)
+    logps_finish_kernel<T><<<(unsigned)((r.tokens + 255) / 256), 256, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets,
+                                                                             r.tokens, w.part, slices, logps);
+}
+
+template <typename T>
+void logprobs_bwd(const LogitRows& r, const float* dlogps, hipStream_t s) {
+  RowCoef rc{};
+  rc.dlogps = dlogps;
+  run_rows<T>(r, rc, s);
 }
 
 template <typename T>
@@ -794,7 +803,7 @@ template <typename T>
 void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, a.seqs, (char*)wsp, &w);
-  if (whole_rows(r)) {
+  if (r.dz && r.tokens > 0) {
     policy_weights_kernel<<<1, 1024, 0, s>>>(r.targets, (int)r.tokens, r.V, a.cu, a.seqs, w.seq);
     run_rows<T>(r, RowCoef{nullptr, a.cu, a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, w.seq, w.stat, w.coef}, s);
     policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.stat, 1, a.cu,
@@ -802,11 +811,11 @@ void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
                                                a.logps, w.seq, nullptr, nullptr, w.coef);
     return;
   }
+  // the loss alone
   const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, s) : 1;
   policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices, a.cu,
                                              a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
-                                             a.logps, w.seq, w.stat, r.dz ? w.coef : nullptr, nullptr);
-  if (r.dz && r.tokens > 0) run_grad<T>(r, w, s);
+                                             a.logps, w.seq, nullptr, nullptr, nullptr);
 }
 
 }  // namespace
@@ -814,12 +823,12 @@ void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
 size_t loss_workspace_bytes(int64_t tokens, int V, int64_t seqs) { return carve(tokens, V, seqs, nullptr, nullptr); }
 
 void launch_token_logps(const LogitRows& r, float* logps, void* ws, hipStream_t s) {
-  if (r.z_bf16) logprobs<bf16>(r, logps, nullptr, ws, s);
-  else logprobs<float>(r, logps, nullptr, ws, s);
+  if (r.z_bf16) logprobs<bf16>(r, logps, ws, s);
+  else logprobs<float>(r, logps, ws, s);
 }
-void launch_token_logps_bwd(const LogitRows& r, const float* dlogps, void* ws, hipStream_t s) {
-  if (r.z_bf16) logprobs<bf16>(r, nullptr, dlogps, ws, s);
-  else logprobs<float>(r, nullptr, dlogps, ws, s);
+void launch_token_logps_bwd(const LogitRows& r, const float* dlogps, hipStream_t s) {
+  if (r.z_bf16) logprobs_bwd<bf16>(r, dlogps, s);
+  else logprobs_bwd<float>(r, dlogps, s);
 }
 void launch_preference_loss(const LogitRows& r, const PreferenceArgs& a, void* ws, hipStream_t s) {
   if (r.z_bf16) preference<bf16>(r, a, ws, s);

@@ -172,7 +172,7 @@ struct PolicyArgs {
 };
 size_t loss_workspace_bytes(int64_t tokens, int V, int64_t seqs);
 void launch_token_logps(const LogitRows& r, float* logps, void* ws, hipStream_t s);
-void launch_token_logps_bwd(const LogitRows& r, const float* dlogps, void* ws, hipStream_t s);
+void launch_token_logps_bwd(const LogitRows& r, const float* dlogps, hipStream_t s);
 void launch_preference_loss(const LogitRows& r, const PreferenceArgs& a, void* ws, hipStream_t s);
 void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipStream_t s);
 // The same within a training step, as launch_ce_loss: logits [T][ldl] of V real columns

@@ -131,14 +131,13 @@ def ref_policy(r, cu, old, adv, ref, lo, hi, kl, per):
 
 # lengths, vocabulary, row stride, type: one token; a vocabulary of one; sequences
 # without a position; each edge of a slice (2048), of a gradient slice (8192); rows
-# of odd length at any alignment; many slices a row, and whole rows (above 1024 tokens)
+# of odd length at any alignment; many slices a row, and whole rows
 CASES = [([2, 1], 1, 1, F), ([1, 1], 2, 2, B), ([5, 0, 0, 3], 7, 9, B), ([9, 4], 50, 50, F), ([20, 13], 2047, 2047, F),
          ([20, 13], 2048, 2048, B), ([20, 13], 2049, 2056, B), ([3, 4, 5, 6], 8191, 8192, B), ([7, 7], 8193, 8193, F),
          ([11, 30], 50257, 50257, B), ([11, 30], 50257, 50272, F), ([100, 87, 33, 160], 32000, 32000, B),
          ([600, 400, 90, 300], 5003, 5003, F), ([1100, 1200], 4100, 4100, B)]
-# rows enough to be read once (1024): each width that a workgroup holds in registers
-# (4 groups of 8 a thread, then 64 registers of 256, 512 and 1024 threads), and rows
-# longer than the registers of any
+# each width that a workgroup holds in registers (4 groups of 8 a thread, then 64
+# registers of 256, 512 and 1024 threads, then more), and rows longer than that
 LONG = [([600, 0, 425], 2050, 2050, F), ([1024], 8192, 8192, B), ([700, 330], 8197, 8200, F),
         ([500, 1, 530], 16385, 16385, F), ([1030], 32771, 32771, B), ([515, 515], 40003, 40003, F),
         ([1025], 65544, 65544, B), ([300, 730], 70001, 70001, F), ([1026], 131072, 131072, B),
@@ -213,6 +212,37 @@ def test_policy_loss(case, per):
         check(got[1], stats, dstats + tol, "stats")
         check(got[2], r.lp, r.E * U + U * r.lp.abs(), "logps")
         check(got[3], r.grad(c), r.grad_bound(c, dc + 4 * U * c.abs(), HALF[dtype]), "dlogits")
+
+
+def test_what_the_binding_refuses():
+    z, tg, cu = make([4, 5], 30, F, 50)
+    f = torch.zeros(9, device="cuda")
+    for text, call in (
+            ("int32", lambda: ops.token_logprobs(z, tg.long())),
+            ("targets must hold 9", lambda: ops.token_logprobs(z, tg[:8])),
+            ("bfloat16 or float32", lambda: ops.token_logprobs(z.half(), tg)),
+            ("tensors on", lambda: ops.token_logprobs(z, tg.cpu())),
+            ("dlogps", lambda: ops.token_logprobs_backward(z, tg, f.double())),
+            ("dlogits must", lambda: ops.token_logprobs_backward(z, tg, f, dlogits=torch.empty(9, 31, device="cuda"))),
+            ("contiguous columns", lambda: ops.token_logprobs_backward(
+                z, tg, f, dlogits=torch.empty(30, 9, device="cuda").t())),
+            ("pairs", lambda: ops.preference_loss(z, tg, [0, 9])),
+            ("pairs", lambda: ops.preference_loss(z, tg, [0, 2, 4, 9])),
+            ("ref_logps", lambda: ops.preference_loss(z, tg, cu, f)),
+            ("cu_device", lambda: ops.preference_loss(z, tg, cu, cu_device=tg[:2])),
+            ("old_logps", lambda: ops.policy_loss(z, tg, cu, f[:3], f))):
+        with pytest.raises(ValueError, match=text):
+            call()
+    from paper_2608_19889_amd import AxonError
+    with pytest.raises(AxonError, match="end at 8"):
+        ops.preference_loss(z, tg, [0, 4, 8])
+    with pytest.raises(AxonError, match="logits' buffer"):
+        wide = torch.empty(9, 64, device="cuda")
+        ops.token_logprobs_backward(wide[:, :30], tg, f, dlogits=wide.view(18, 32)[:9, :30])
+    # layouts that the kernels do not take are copied: a transposed input, a broadcast row
+    want = ops.token_logprobs(z, tg)
+    assert torch.equal(ops.token_logprobs(z.t().contiguous().t(), tg), want)
+    assert torch.equal(ops.token_logprobs(z[:1].expand(9, 30), tg), ops.token_logprobs(z[:1].repeat(9, 1), tg))
 
 
 def test_nothing_counts():

@@ -25,7 +25,7 @@ ROWS = dict(tokens=6, vocab=50, z=P, dtype=F, ld=50, targets=P)
 GRAD = dict(dz=2 * P, gdtype=F, ldg=50)
 WORK = dict(ws=P, ws_bytes=BIG, stream=None)
 LP = dict(ROWS, logps=P, **WORK)
-LPB = dict(ROWS, dlogps=P, **GRAD, **WORK)
+LPB = dict(ROWS, dlogps=P, **GRAD, stream=None)
 PREF = dict(ROWS, pairs=1, d_cu=P, h_cu=cu(0, 2, 6), ref=P, beta=0.1, e=0.1, loss=P, seq=P, margins=P, **GRAD, **WORK)
 POL = dict(ROWS, batch=2, d_cu=P, h_cu=cu(0, 2, 6), old=P, ref=P, adv=P, lo=0.2, hi=0.2, kl=0.1, per=0, loss=P, stats=P,
            logps=P, **GRAD, **WORK)
@@ -114,9 +114,8 @@ def test_workspaces_grow_with_the_call_and_are_zero_for_what_is_refused():
 
 def test_binding_refuses_what_it_cannot_hand_over():
     x = torch.zeros(4, 8)
-    with pytest.raises(ValueError, match="on the GPU"):
-        ops.layernorm(x, torch.ones(8))
-    with pytest.raises(ValueError, match="pairs"):
-        ops.preference_loss(x, torch.zeros(4, dtype=torch.int32), [0, 2, 3, 4])
-    with pytest.raises(ValueError, match="shape"):
-        ops.layernorm_backward(x, x[:2], torch.ones(8))
+    for call in (lambda: ops.layernorm(x, torch.ones(8)), lambda: ops.token_logprobs(x, x[0]),
+                 lambda: ops.layernorm_backward(x, x, gain=x[0]),
+                 lambda: ops.policy_loss(x, x[0], [0, 4], x[0], x[0], stream=0)):
+        with pytest.raises(ValueError, match="on the GPU"):
+            call()
