@@ -2084,16 +2084,16 @@ void enqueue_train_gpt2(axon_model* m, int B, int T, const int32_t* d_tokens, co
     EpiArgs oe{}, de{};
     oe.resid = t.xin;
     gemm_many<bf16>(m, w.wo, t.o, D, T, D, EPI_RESID, t.xmid, nullptr, D, s, &oe, w.bo, true);
-    launch_layernorm(t.xmid, (const bf16*)w.gpost, (const bf16*)w.gpost_b, t.h2, T, D, eps, nullptr, s, true);
+    launch_ln_fwd_pair(t.xmid, (const bf16*)w.gpost, (const bf16*)w.gpost_b, eps, t.h2, T, D, s);
     gemm_many<bf16>(m, w.wgu, t.h2, I, T, D, EPI_F32, t.gu, nullptr, I, s, nullptr, w.bfc, true);
     launch_gelu_train(t.gu, T, I, t.a, s);
     const bool last = l + 1 == L;
     float* xout = last ? tb.xfin : tb.L[l + 1].xin;
     de.resid = t.xmid;
     gemm_many<bf16>(m, w.wd, t.a, D, T, I, EPI_RESID, xout, nullptr, D, s, &de, w.bd, true);
-    launch_layernorm(xout, (const bf16*)(last ? m->gfinal : m->layers[l + 1].gin),
-                     (const bf16*)(last ? m->gfinal_b : m->layers[l + 1].gin_b), last ? tb.hf : tb.L[l + 1].h1, T, D,
-                     eps, nullptr, s, true);
+    launch_ln_fwd_pair(xout, (const bf16*)(last ? m->gfinal : m->layers[l + 1].gin),
+                       (const bf16*)(last ? m->gfinal_b : m->layers[l + 1].gin_b), eps,
+                       last ? tb.hf : tb.L[l + 1].h1, T, D, s);
   }
   enqueue_train_loss(m, T, d_targets, loss, s);
   // ---- backward.  dW of a weight stored [in K][out N]: X^T dY

@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(256) embed_pos_ln_kernel(const int32_t* __rest
 
 __global__ void __launch_bounds__(256) layernorm_kernel(const float* __restrict__ x, const bf16* __restrict__ g,
                                                         const bf16* __restrict__ beta, bf16* __restrict__ h, int D,
-                                                        float eps, const int32_t* __restrict__ cu_last, bool pair) {
+                                                        float eps, const int32_t* __restrict__ cu_last) {
   __shared__ float red[16];
   const int i_out = blockIdx.x;
   const int r = cu_last ? cu_last[i_out + 1] - 1 : i_out;
@@ -96,7 +96,7 @@ __global__ void __launch_bounds__(256) layernorm_kernel(const float* __restrict_
     const int i = threadIdx.x * 4 + j * 1024;
     if (i < D) v[j] = *(const f32x4*)(x + (int64_t)r * D + i);
   }
-  ln_store(v, D, eps, g, beta, h, i_out, pair, red);
+  ln_store(v, D, eps, g, beta, h, i_out, false, red);
 }
 
 void launch_embed_pos_ln(const int32_t* tok, const bf16* wte, const bf16* wpe, const bf16* g, const bf16* beta,
@@ -107,9 +107,9 @@ void launch_embed_pos_ln(const int32_t* tok, const bf16* wte, const bf16* wpe, c
 }
 
 void launch_layernorm(const float* x, const bf16* g, const bf16* beta, bf16* h, int rows, int D, float eps,
-                      const int32_t* cu_last, hipStream_t s, bool h_pair) {
+                      const int32_t* cu_last, hipStream_t s) {
   if (rows <= 0) return;
-  layernorm_kernel<<<rows, 256, 0, s>>>(x, g, beta, h, D, eps, cu_last, h_pair);
+  layernorm_kernel<<<rows, 256, 0, s>>>(x, g, beta, h, D, eps, cu_last);
 }
 
 // ---------------------------------------------------------------- rows of any width, forward and backward
@@ -252,8 +252,8 @@ AXON_DEV float square_cols(const RowCols<TPR, NV, ODD>& rc, const float (&v)[NV]
 
 // y = (x - mean) rstd g + b, one row per TPR threads.  HBM bound.  The workgroups
 // stay for several rows: g and b are loaded once, and the next row's loads are under
-// way while this one is reduced.
-template <typename TX, typename TY, typename TP, int TPR, int NV, bool ODD>
+// way while this one is reduced.  PAIR: y in the row-pair layout (cols % 32 == 0).
+template <typename TX, typename TY, typename TP, int TPR, int NV, bool ODD, bool PAIR = false>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
     ln_fwd_kernel(const TX* x, int64_t ldx, const TP* __restrict__ g, const TP* __restrict__ b, float eps, TY* y,
                   int64_t ldy, int64_t rows, int cols) {
@@ -287,7 +287,13 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[n][j] = (v[n][j] - w.mean) * rstd * gv.g[n][j] + (b ? bv.g[n][j] : 0.f);
     if constexpr (ODD) t = (t - w.mean) * rstd * to_f32(gv.t) + (b ? to_f32(bv.t) : 0.f);
-    rc.store(y + r * ldy, v, t);
+    if constexpr (PAIR) {
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        if (rc.on(n)) Run8<TY>::store(y + xp_off(r, rc.at(n), cols), v[n]);
+    } else {
+      rc.store(y + r * ldy, v, t);
+    }
   }
 }
 
@@ -543,6 +549,15 @@ void launch_ln_fwd(const TX* x, int64_t ldx, const TP* g, const TP* b, float eps
       kern<<<ln_wgs(rows, TPR, most), TPR < 256 ? 256 : TPR, 0, s>>>(x, ldx, g, b, eps, y, ldy, rows, cols);
     };
     cols % 8 ? go(ln_fwd_kernel<TX, TY, TP, TPR, NV, true>) : go(ln_fwd_kernel<TX, TY, TP, TPR, NV, false>);
+  });
+}
+
+void launch_ln_fwd_pair(const float* x, const bf16* g, const bf16* b, float eps, bf16* y, int T, int D, hipStream_t s) {
+  if (T <= 0) return;
+  ln_fwd_shape(D, [&](auto tpr, auto nv, int most) {
+    constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value;
+    ln_fwd_kernel<float, bf16, bf16, TPR, NV, false, true>
+        <<<ln_wgs(T, TPR, most), TPR < 256 ? 256 : TPR, 0, s>>>(x, D, g, b, eps, y, D, T, D);
   });
 }
 

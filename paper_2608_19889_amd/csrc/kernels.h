@@ -112,7 +112,7 @@ void launch_embed_pos_ln(const int32_t* tok, const bf16* wte, const bf16* wpe, c
 // h[i] = LayerNorm(x[r]) * g + beta with r = i, or r = cu_last[i+1]-1 (the
 // last position of sequence i) when cu_last is set
 void launch_layernorm(const float* x, const bf16* g, const bf16* beta, bf16* h, int rows, int D, float eps,
-                      const int32_t* cu_last, hipStream_t s, bool h_pair = false);
+                      const int32_t* cu_last, hipStream_t s);
 // Rows of a caller (strides ldx, ldy in elements, 1 <= cols <= LN_MAX_COLS): y =
 // LayerNorm(x) * g + b (b may be null), and its backward: dx, dg = sum over the rows
 // of dy xhat and db = sum dy (float [cols]; db may be null).  part:
@@ -125,7 +125,8 @@ void launch_ln_fwd(const TX* x, int64_t ldx, const TP* g, const TP* b, float eps
 template <typename TX, typename TD, typename TP>
 void launch_ln_bwd(const TX* x, int64_t ldx, const TD* dy, int64_t lddy, const TP* g, float eps, TX* dx, int64_t lddx,
                    float* dg, float* db, float* part, int64_t rows, int cols, hipStream_t s);
-// The training step's form: x and dy [T][D] float, dy the sum of tr.np partials
+// The training step's forms.  Forward: y [T][D] bf16 in the row-pair layout (D % 32 ==
+// 0).  Backward: x and dy [T][D] float, dy the sum of tr.np partials
 // tr.stride apart; dx [T][D] (tr.accumulate: += instead of =), its bf16 copy tr.dxb
 // (row-pair layout) and, beside dg and db, dres = the column sums of the new dx (null:
 // not written).  D % 32 == 0, D <= 8192; part: ROW_PARTS x 3 D floats.
@@ -135,6 +136,7 @@ struct LnTrain {
   int accumulate = 0;
   bf16* dxb = nullptr;
 };
+void launch_ln_fwd_pair(const float* x, const bf16* g, const bf16* b, float eps, bf16* y, int T, int D, hipStream_t s);
 void launch_ln_bwd_train(const float* x, const bf16* g, const float* dy, const LnTrain& tr, int T, int D, float eps,
                          float* dx, float* dg, float* db, float* dres, float* part, hipStream_t s);
 // dst[r][k] = src[k][perm ? perm[r] : r] (bf16): a [K][N] matrix stored
