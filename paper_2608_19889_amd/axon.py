@@ -202,6 +202,9 @@ def _stream(stream) -> int:
 
 
 # ---------------------------------------------------------------- row operators
+#
+# Each takes stream=, the torch stream (or its raw handle) to run on; None: the current
+# one of its tensors' device.
 
 _CODES = {torch.bfloat16: AXON_BF16, torch.float32: AXON_F32}
 
@@ -213,6 +216,14 @@ def _code(t: torch.Tensor, name: str) -> int:
     return code
 
 
+def _tensors(values):
+    for v in values:
+        if isinstance(v, torch.Tensor):
+            yield v
+        elif isinstance(v, dict):
+            yield from _tensors(v.values())
+
+
 def _row_operator(f):
     """Runs f on its tensors' device and on ``stream`` (None: that device's current
     one), so that what it allocates belongs there.  Inputs made on another stream must
@@ -220,14 +231,13 @@ def _row_operator(f):
     @functools.wraps(f)
     def call(*args, stream=None, **kw):
         device = None
-        for t in (*args, *kw.values()):
-            if isinstance(t, torch.Tensor):
-                if device is None:
-                    device = t.device
-                    if device.type != "cuda":
-                        raise ValueError(f"{f.__name__} takes tensors on the GPU, got one on {device}")
-                elif t.device != device:
-                    raise ValueError(f"{f.__name__}: tensors on {device} and {t.device} in one call")
+        for t in _tensors((*args, *kw.values())):
+            if device is None:
+                device = t.device
+                if device.type != "cuda":
+                    raise ValueError(f"{f.__name__} takes tensors on the GPU, got one on {device}")
+            elif t.device != device:
+                raise ValueError(f"{f.__name__}: tensors on {device} and {t.device} in one call")
         if device is None:
             raise ValueError(f"{f.__name__} takes tensors on the GPU")
         if stream is None and device.index == torch.cuda.current_device():
@@ -237,9 +247,10 @@ def _row_operator(f):
                 return f(*args, **kw)
             if not hasattr(stream, "cuda_stream"):
                 stream = torch.cuda.ExternalStream(int(stream))
-            for t in (*args, *kw.values()):
-                if isinstance(t, torch.Tensor):
-                    t.record_stream(stream)
+            if stream.device != device:
+                raise ValueError(f"{f.__name__}: tensors on {device}, the stream on {stream.device}")
+            for t in _tensors((*args, *kw.values())):
+                t.record_stream(stream)
             with torch.cuda.stream(stream):
                 return f(*args, **kw)
     return call
@@ -508,51 +519,57 @@ class Model:
         return loss
 
     def _train_args(self, tokens, cu_seqlens, targets, grads):
+        """The C arguments up to the targets, those of the gradients, and what has to
+        live until the step has run."""
         B = len(cu_seqlens) - 1
-        cu_h = (ctypes.c_int32 * (B + 1))(*[int(c) for c in cu_seqlens])
-        cu_d = torch.tensor([int(c) for c in cu_seqlens], dtype=torch.int32, device=tokens.device)
+        T = int(cu_seqlens[-1])
+        tokens, targets = _vector(tokens, T, torch.int32, "tokens"), _vector(targets, T, torch.int32, "targets")
+        for name, g in grads.items():
+            if not g.is_contiguous():
+                raise ValueError(f"the gradient buffer of {name} is not contiguous")
+        host, cu = _cu_args([int(c) for c in cu_seqlens], None, tokens)
         arr, keep = make_weights(grads)
-        return B, cu_h, cu_d, arr, keep
+        return (tokens.data_ptr(), cu.data_ptr(), host, targets.data_ptr()), \
+            (arr, len(grads), _current(tokens)), (cu, tokens, targets, keep)
 
+    @_row_operator
     def preference_loss_and_grads(self, tokens: torch.Tensor, cu_seqlens: list, targets: torch.Tensor, grads: dict,
                                   ref_logps: torch.Tensor | None = None, beta: float = 0.1,
-                                  label_smoothing: float = 0.0, stream=None):
+                                  label_smoothing: float = 0.0):
         """A training step with the preference loss (axon_preference_loss_and_grads):
         pairs of sequences, chosen then rejected; tokens, targets and grads as in
         :meth:`loss_and_grads`, the loss as :func:`preference_loss`.  Returns (loss [1],
         seq_logps [2 pairs], margins [pairs])."""
-        B, cu_h, cu_d, arr, keep = self._train_args(tokens, cu_seqlens, targets, grads)
+        B = len(cu_seqlens) - 1
         if B < 2 or B % 2:
             raise ValueError("sequences come in pairs, chosen then rejected")
+        args, gargs, keep = self._train_args(tokens, cu_seqlens, targets, grads)
         ref_logps = _vector(ref_logps, B, torch.float32, "ref_logps")
         out = torch.empty((1 + B + B // 2,), dtype=torch.float32, device=tokens.device)
         at = out.data_ptr()
-        _check(lib().axon_preference_loss_and_grads(self._h, B // 2, tokens.data_ptr(), cu_d.data_ptr(), cu_h,
-                                                    targets.data_ptr(), _ptr(ref_logps), beta, label_smoothing, at,
-                                                    at + 4, at + 4 + 4 * B, arr, len(grads),
-                                                    ctypes.c_void_p(_stream(stream))))
-        self._keep = (cu_d, tokens, targets, keep, ref_logps)
+        _check(lib().axon_preference_loss_and_grads(self._h, B // 2, *args, _ptr(ref_logps), beta, label_smoothing, at,
+                                                    at + 4, at + 4 + 4 * B, *gargs))
+        self._keep = (keep, ref_logps)
         return out[:1], out[1:1 + B], out[1 + B:]
 
+    @_row_operator
     def policy_loss_and_grads(self, tokens: torch.Tensor, cu_seqlens: list, targets: torch.Tensor, grads: dict,
                               old_logps: torch.Tensor, advantages: torch.Tensor,
                               ref_logps: torch.Tensor | None = None, clip_low: float = 0.2, clip_high: float = 0.2,
-                              kl_coef: float = 0.0, per_sequence: bool = False, stream=None):
+                              kl_coef: float = 0.0, per_sequence: bool = False):
         """A training step with the clipped policy loss (axon_policy_loss_and_grads):
         tokens, targets and grads as in :meth:`loss_and_grads`, the loss as
         :func:`policy_loss`.  Returns (loss [1], stats [3], logps [tokens])."""
-        B, cu_h, cu_d, arr, keep = self._train_args(tokens, cu_seqlens, targets, grads)
+        args, gargs, keep = self._train_args(tokens, cu_seqlens, targets, grads)
         T = int(cu_seqlens[-1])
         old_logps, advantages, ref_logps = (_vector(t, T, torch.float32, n) for t, n in (
             (old_logps, "old_logps"), (advantages, "advantages"), (ref_logps, "ref_logps")))
         out = torch.empty((4 + T,), dtype=torch.float32, device=tokens.device)
         at = out.data_ptr()
-        _check(lib().axon_policy_loss_and_grads(self._h, B, tokens.data_ptr(), cu_d.data_ptr(), cu_h,
-                                                targets.data_ptr(), old_logps.data_ptr(), _ptr(ref_logps),
-                                                advantages.data_ptr(), clip_low, clip_high, kl_coef,
-                                                int(per_sequence), at, at + 4, at + 16, arr, len(grads),
-                                                ctypes.c_void_p(_stream(stream))))
-        self._keep = (cu_d, tokens, targets, keep, old_logps, advantages, ref_logps)
+        _check(lib().axon_policy_loss_and_grads(self._h, len(cu_seqlens) - 1, *args, old_logps.data_ptr(),
+                                                _ptr(ref_logps), advantages.data_ptr(), clip_low, clip_high, kl_coef,
+                                                int(per_sequence), at, at + 4, at + 16, *gargs))
+        self._keep = (keep, old_logps, advantages, ref_logps)
         return out[:1], out[1:4], out[4:]
 
     def decode_step(self, tokens: torch.Tensor, logits: torch.Tensor | None = None,

@@ -1,6 +1,5 @@
 // What the source files of the C ABI share.
 #pragma once
-#include <exception>
 #include <new>
 #include <string>
 
@@ -25,9 +24,9 @@ int entry(F&& body) {
     clear_error();
     return body();
   } catch (const std::bad_alloc&) {
-    return AXON_E_OOM;
-  } catch (const std::exception&) {
-    return AXON_E_INVALID;
+    return fail(AXON_E_OOM, "out of memory");  // (short enough to need none)
+  } catch (...) {
+    return fail(AXON_E_INVALID, "host failure");
   }
 }
 

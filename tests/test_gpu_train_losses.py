@@ -234,6 +234,27 @@ def test_replayed_capture_of_a_step(family):
     m.close()
 
 
+@pytest.mark.parametrize("family", ["llama", "gpt2"])
+def test_step_on_another_stream(family):
+    """The bits of the same step on the current stream, whose own work goes on."""
+    shape, lens = FAMILIES[family]
+    w, seqs, tg, m, flat, cu, targets, grads = setup(shape, lens, 93)
+    old = torch.full((len(tg),), -6.5, device="cuda")
+    adv = torch.randn(len(tg), device="cuda")
+    want = [t.clone() for t in m.policy_loss_and_grads(flat, cu, targets, grads, old, adv)]
+    pref = [t.clone() for t in m.preference_loss_and_grads(flat, cu, targets, grads)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        got = m.policy_loss_and_grads(flat, cu, targets, grads, old, adv, stream=stream)
+        more = m.preference_loss_and_grads(flat, cu, targets, grads, stream=stream)
+        junk = [torch.full((1 << 16,), 7.0, device="cuda") for _ in range(8)]
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want + pref, (*got, *more)))
+        assert all(bool((j == 7).all()) for j in junk)
+    m.close()
+
+
 def test_refusals_of_a_step():
     shape, lens = FAMILIES["gpt2"]
     w, seqs, tg, m, flat, cu, targets, grads = setup(shape, lens, 99)
@@ -246,6 +267,22 @@ def test_refusals_of_a_step():
         m.preference_loss_and_grads(flat, cu, targets, grads, beta=-1.0)
     with pytest.raises(ValueError, match="old_logps"):
         m.policy_loss_and_grads(flat, cu, targets, grads, f[:3], f)
+    with pytest.raises(ValueError, match="tensors on"):
+        m.policy_loss_and_grads(flat, cu, targets, grads, f.cpu(), f)
+    with pytest.raises(ValueError, match="tensors on"):
+        m.policy_loss_and_grads(flat, cu, targets, {**grads, "transformer.ln_f.bias": f.cpu()}, f, f)
+    with pytest.raises(ValueError, match="targets must hold"):
+        m.policy_loss_and_grads(flat, cu, targets.long(), grads, f, f)
+    with pytest.raises(ValueError, match="not contiguous"):
+        wide = torch.empty(grads["transformer.wpe.weight"].shape[::-1], device="cuda").t()
+        m.policy_loss_and_grads(flat, cu, targets, {**grads, "transformer.wpe.weight": wide}, f, f)
+
+    class Elsewhere:  # a stream of another device
+        cuda_stream, device = 0, torch.device("cuda", 1)
+    with pytest.raises(ValueError, match="the stream on"):
+        m.policy_loss_and_grads(flat, cu, targets, grads, f, f, stream=Elsewhere())
+    with pytest.raises(ValueError, match="the stream on"):
+        ops.layernorm(f.view(1, -1), f, stream=Elsewhere())
     bad = dict(grads)
     del bad["transformer.wpe.weight"]
     with pytest.raises(ax.AxonError, match="missing gradient"):

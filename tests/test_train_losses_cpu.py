@@ -48,3 +48,24 @@ def test_refusals_of_the_training_losses():
         assert rc == ax.AXON_E_INVALID and text in ax.last_error()
         rc = L.axon_policy_loss_and_grads(None, 1, P, P, cu, P, P, None, P, 0.2, 0.2, 0.0, 0, P, P, P, None, 0, None)
         assert rc == ax.AXON_E_INVALID and text in ax.last_error()
+
+
+class NoModel:
+    _h = None
+    _train_args = ax.Model._train_args
+
+
+def test_binding_refuses_what_a_step_cannot_take():
+    """Host tensors and mixed devices never reach the library as pointers."""
+    i, f = torch.zeros(4, dtype=torch.int32), torch.zeros(4)
+    with pytest.raises(ValueError, match="on the GPU"):
+        ax.Model.policy_loss_and_grads(NoModel(), i, [0, 2, 4], i, {"w": f}, f, f)
+    with pytest.raises(ValueError, match="on the GPU"):
+        ax.Model.preference_loss_and_grads(NoModel(), i, [0, 2, 4], i, {"w": f})
+    meta = torch.zeros(4, dtype=torch.int32, device="meta")
+    with pytest.raises(ValueError, match="on the GPU"):
+        ax.Model.preference_loss_and_grads(NoModel(), meta, [0, 2, 4], i, {"w": f})
+    for tokens, targets, grads, text in [(i.long(), i, {}, "tokens must hold 4"), (i, i[:3], {}, "targets must hold 4"),
+                                         (i, i, {"w": torch.zeros(3, 2).t()}, "buffer of w is not contiguous")]:
+        with pytest.raises(ValueError, match=text):
+            NoModel()._train_args(tokens, [0, 2, 4], targets, grads)
