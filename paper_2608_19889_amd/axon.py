@@ -230,18 +230,24 @@ def _row_operator(f):
     be ready on this one; they are kept from reuse until its work is done."""
     @functools.wraps(f)
     def call(*args, stream=None, **kw):
-        device = None
-        for t in _tensors((*args, *kw.values())):
-            if device is None:
-                device = t.device
-                if device.type != "cuda":
-                    raise ValueError(f"{f.__name__} takes tensors on the GPU, got one on {device}")
-            elif t.device != device:
-                raise ValueError(f"{f.__name__}: tensors on {device} and {t.device} in one call")
-        if device is None:
+        first = None
+        for t in (*args, *kw.values()):
+            if isinstance(t, torch.Tensor):
+                if first is None:
+                    first, at = t, t.get_device()
+                    if at < 0:
+                        raise ValueError(f"{f.__name__} takes tensors on the GPU, got one on {t.device}")
+                elif t.get_device() != at:
+                    raise ValueError(f"{f.__name__}: tensors on {first.device} and {t.device} in one call")
+            elif isinstance(t, dict):
+                for g in t.values():
+                    if first is None or g.get_device() != at:
+                        raise ValueError(f"{f.__name__}: a gradient buffer on {g.device}")
+        if first is None:
             raise ValueError(f"{f.__name__} takes tensors on the GPU")
-        if stream is None and device.index == torch.cuda.current_device():
+        if stream is None and at == torch.cuda.current_device():
             return f(*args, **kw)
+        device = first.device
         with torch.cuda.device(device):
             if stream is None:
                 return f(*args, **kw)

@@ -13,7 +13,8 @@
 //   logit_part_kernel   reads the rows: (m, S) of every slice of a row
 //   *_finish_kernel     joins a row's slices; loss, statistics, c of every token
 //   logit_grad_kernel   reads the rows again and writes the gradient
-//   logit_row_kernel    all of it in one pass, where c depends on the row alone
+//   logit_row_kernel    all of it in one pass, where c depends on the row alone; then
+//   policy_sum_kernel   adds up the loss's terms
 //
 // All are HBM bound (V 4 or 2 bytes a row against a few exponentials).  No atomics:
 // every sum has one order.
@@ -115,20 +116,30 @@ AXON_DEV void join_block(float& m, float& s, float (*red)[PART_THREADS / 64]) {
   for (int w = 1; w < PART_THREADS / 64; ++w) join_part(m, s, red[0][w], red[1][w]);
 }
 
+// A token's log-probability, for whichever is asked for; 0 where it does not count
+template <typename T>
+AXON_DEV void put_logp(bool counts, const T* chosen, float m, float s, float* logp, double* lp) {
+  if (!logp && !lp) return;
+  const double v = counts ? (double)to_f32(*chosen) - (double)m - log((double)s) : 0.0;
+  if (logp) *logp = (float)v;
+  if (lp) *lp = v;
+}
+
 // One slice (of ``slices``, ``cols`` wide) of one row a workgroup: its maximum and
-// sum of exponentials.  Rows that do not count are skipped.
+// sum of exponentials, and, of whole rows, the target's log-probability.  Rows that do
+// not count are skipped.
 template <typename T>
 __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __restrict__ z, int64_t ld, int V,
                                                                   const int32_t* __restrict__ targets, int64_t items,
                                                                   int slices, int cols, float2* __restrict__ part,
-                                                                  float* __restrict__ logps) {
+                                                                  float* __restrict__ logps, double* __restrict__ lps) {
   constexpr int STRIDE = PART_THREADS * 8, BLOCK = STRIDE * PART_RUNS;
   __shared__ float red[2][PART_THREADS / 64];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t t = it / slices;
     const int tg = targets[t];
     if (tg < 0 || tg >= V) {  // uniform over the workgroup
-      if (logps && threadIdx.x == 0) logps[t] = 0.f;
+      if (threadIdx.x == 0) put_logp(false, z, 0.f, 1.f, logps ? logps + t : nullptr, lps ? lps + t : nullptr);
       continue;
     }
     const T* row = z + t * ld;
@@ -147,9 +158,21 @@ __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __res
     join_block(m, s, red);
     if (threadIdx.x == 0) {
       if (part) part[it] = float2{m, s};
-      if (logps) logps[t] = (float)((double)to_f32(z[t * ld + tg]) - (double)m - log((double)s));
+      put_logp(true, z + t * ld + tg, m, s, logps ? logps + t : nullptr, lps ? lps + t : nullptr);
     }
   }
+}
+
+// (m, s) of token t from its slices, at most 16, all under way together
+AXON_DEV float2 join_slices(const float2* part, int64_t t, int slices) {
+  float2 p[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) p[i] = part[t * slices + min(i, slices - 1)];
+  float m = p[0].x, s = p[0].y;
+#pragma unroll
+  for (int i = 1; i < 16; ++i)
+    if (i < slices) join_part(m, s, p[i].x, p[i].y);
+  return float2{m, s};
 }
 
 // log-probabilities from the rows' slices
@@ -161,17 +184,9 @@ __global__ void __launch_bounds__(256) logps_finish_kernel(const T* __restrict__
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (t >= tokens) return;
   const int tg = targets[t];
-  float m = -INFINITY, s = 0.f;
-  if (tg < 0 || tg >= V) {
-    logps[t] = 0.f;
-    return;
-  }
-#pragma unroll 4
-  for (int i = 0; i < slices; ++i) {
-    const float2 p = part[t * slices + i];
-    join_part(m, s, p.x, p.y);
-  }
-  logps[t] = (float)((double)to_f32(z[t * ld + tg]) - (double)m - log((double)s));
+  const bool counts = tg >= 0 && tg < V;
+  const float2 st = counts ? join_slices(part, t, slices) : float2{0.f, 1.f};
+  put_logp(counts, z + t * ld + tg, st.x, st.y, logps + t, nullptr);
 }
 
 AXON_DEV double wave_sum_f64(double v) {
@@ -180,16 +195,38 @@ AXON_DEV double wave_sum_f64(double v) {
   return v;
 }
 
-// sum over a workgroup of 1024 threads, in every thread
-AXON_DEV double block_sum_f64(double v, double* red /* 16 */) {
-  v = wave_sum_f64(v);
+// N sums over a workgroup of 1024 threads, in every thread
+template <int N>
+AXON_DEV void block_sums_f64(double (&v)[N], double (*red)[16]) {
+#pragma unroll
+  for (int k = 0; k < N; ++k) v[k] = wave_sum_f64(v[k]);
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if ((threadIdx.x & 63) == 0) red[k][threadIdx.x >> 6] = v[k];
   __syncthreads();
-  double s = 0.0;
-  for (int i = 0; i < 16; ++i) s += red[i];
-  return s;
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    v[k] = 0.0;
+    for (int i = 0; i < 16; ++i) v[k] += red[k][i];
+  }
 }
+
+// The sequence of a token, for a workgroup of 1024 threads that look up many: the
+// boundaries of up to CU_HELD sequences are kept in LDS (a search in memory waits for
+// every step).  A barrier between hold() and of().
+constexpr int CU_HELD = 1024;
+struct SeqLookup {
+  const int32_t* cu;
+  int seqs;
+  AXON_DEV void hold(int32_t* held) const {
+    if (cu && seqs <= CU_HELD)
+      for (int i = threadIdx.x; i < seqs; i += 1024) held[i] = cu[i];
+  }
+  AXON_DEV int of(const int32_t* held, int t) const {
+    return seqs <= CU_HELD ? seq_of_token(held, seqs, t) : seq_of_token(cu, seqs, t);
+  }
+};
 
 // log(1 + exp(v)) without overflow
 AXON_DEV double softplus_f64(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v))); }
@@ -197,53 +234,33 @@ AXON_DEV double softplus_f64(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v
 // Pairs (chosen 2i, rejected 2i + 1): s_j the sum of sequence j's lp, u_i = beta
 // ((s_2i - ref_2i) - (s_2i+1 - ref_2i+1)), loss = mean of (1 - e) softplus(-u) + e
 // softplus(u); dloss / ds_2i = beta / pairs (e sigmoid(u) - (1 - e) sigmoid(-u)).
-// One workgroup: tokens, then sequences, then pairs.
+// One workgroup: tokens (slices > 1: else the rows' pass has left lps and stat), then
+// sequences, then pairs.
 template <typename T>
 __global__ void __launch_bounds__(1024) preference_finish_kernel(
     const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
-    const float2* part /* may be stat */, int slices, const int32_t* __restrict__ cu, int seqs,
+    const float2* __restrict__ part, int slices, const int32_t* __restrict__ cu, int seqs,
     const float* __restrict__ ref, float beta, float smoothing, float* __restrict__ loss,
     float* __restrict__ seq_logps, float* __restrict__ margins, double* __restrict__ lps, double* __restrict__ sums,
-    float2* stat, float* __restrict__ coef) {
-  __shared__ double red[16];
+    float2* __restrict__ stat, float* __restrict__ coef) {
+  __shared__ double red[1][16];
+  __shared__ int32_t held[CU_HELD];
+  const SeqLookup seq{cu, seqs};
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  constexpr int U = 4;  // tokens of a thread whose loads are under way together
-  for (int t0 = tid; t0 < tokens; t0 += 1024 * U) {
-    int tg[U];
-    float zt[U];
-    float2 st[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      tg[u] = -1;
-      if (t0 + u * 1024 < tokens) tg[u] = targets[t0 + u * 1024];
+  seq.hold(held);
+  if (slices > 1)
+    for (int64_t t = tid; t < tokens; t += 1024) {
+      const int tg = targets[t];
+      const bool counts = tg >= 0 && tg < V;
+      const float2 st = counts ? join_slices(part, t, slices) : float2{0.f, 1.f};
+      put_logp(counts, z + t * ld + tg, st.x, st.y, nullptr, lps + t);
+      stat[t] = st;
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * 1024;
-      zt[u] = 0.f;
-      st[u] = float2{0.f, 1.f};
-      if (tg[u] < 0 || tg[u] >= V) continue;
-      zt[u] = to_f32(z[t * ld + tg[u]]);
-      st[u] = part[t * slices];
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t t = t0 + u * 1024;
-      if (t >= tokens) continue;
-      double lp = 0.0;
-      if (tg[u] >= 0 && tg[u] < V) {
-        for (int i = 1; i < slices; ++i) join_part(st[u].x, st[u].y, part[t * slices + i].x, part[t * slices + i].y);
-        lp = (double)zt[u] - (double)st[u].x - log((double)st[u].y);
-      }
-      lps[t] = lp;
-      stat[t] = st[u];
-    }
-  }
   __syncthreads();
   for (int j = wave; j < seqs; j += 16) {
     const int t1 = min(tokens, cu[j + 1]);
     double s = 0.0;
-#pragma unroll 4
+#pragma unroll 8
     for (int t = max(0, cu[j]) + lane; t < t1; t += 64) s += lps[t];
     s = wave_sum_f64(s);
     if (lane == 0) {
@@ -268,13 +285,15 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(
     sums[2 * i] = d;
     sums[2 * i + 1] = -d;
   }
-  total = block_sum_f64(total, red);
-  if (tid == 0) loss[0] = pairs > 0 ? (float)(total / pairs) : 0.f;
-  __syncthreads();
+  double one[1] = {total};
+  block_sums_f64(one, red);  // (its barriers make the sequences' coefficients visible)
+  if (tid == 0) loss[0] = pairs > 0 ? (float)(one[0] / pairs) : 0.f;
   if (!coef) return;
+#pragma unroll 4
   for (int t = tid; t < tokens; t += 1024) {
     const int tg = targets[t];
-    coef[t] = tg >= 0 && tg < V ? (float)sums[seq_of_token(cu, seqs, t)] : 0.f;
+    const double d = sums[seq.of(held, t)];
+    coef[t] = tg >= 0 && tg < V ? (float)d : 0.f;
   }
 }
 
@@ -284,8 +303,8 @@ struct PolicyTerms {
   bool clipped;
 };
 // one token (see policy_finish_kernel), from its logit and its row's (m, S), in float32:
-// float64 exponentials of a batch's tokens took one workgroup longer than everything
-// else here.  The log-probability's three terms and the other policy's are added with
+// where one workgroup does a batch's tokens, float64 exponentials took longer than
+// everything else there.  The log-probability's three terms and the other policy's are added with
 // their rounding errors kept, so the ratio is off by the last digits of S and of two
 // logarithms.
 AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A, bool has_ref, float ref, float lo,
@@ -321,41 +340,63 @@ AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A,
 // counted tokens of each sequence into weights[seqs] (cu), and in every thread the
 // number of sequences that have some, or (no cu) of all counted tokens.  1024 threads.
 AXON_DEV double policy_counts(const int32_t* targets, int tokens, int V, const int32_t* cu, int seqs, double* weights,
-                              double* red) {
+                              double (*red)[16]) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  double n = 0.0;
+  // of the tokens t, t + step, .. below t1, 8 loads at a time
+  auto counted = [&](int t, int step, int t1) {
+    int own = 0;
+    for (; t < t1; t += 8 * step) {
+      int tg[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) tg[u] = targets[min((int64_t)t + (int64_t)u * step, (int64_t)t1 - 1)];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) own += (int64_t)t + (int64_t)u * step < t1 && tg[u] >= 0 && tg[u] < V;
+      if (t > t1 - 8 * step) break;  // (t + 8 step may pass 2^31)
+    }
+    return (double)own;
+  };
+  double n[1] = {};
   if (cu) {
     for (int j = wave; j < seqs; j += 16) {
-      const int t1 = min(tokens, cu[j + 1]);
-      int own = 0;
-      for (int t = max(0, cu[j]) + lane; t < t1; t += 64) own += targets[t] >= 0 && targets[t] < V;
-      const double c = wave_sum_f64((double)own);
+      const double c = wave_sum_f64(counted(max(0, cu[j]) + lane, 64, min(tokens, cu[j + 1])));
       if (lane == 0) weights[j] = c;
-      n += lane == 0 && c > 0.0 ? 1.0 : 0.0;
+      n[0] += lane == 0 && c > 0.0 ? 1.0 : 0.0;
     }
   } else {
-    for (int t = tid; t < tokens; t += 1024) n += targets[t] >= 0 && targets[t] < V ? 1.0 : 0.0;
+    n[0] = counted(tid, 1024, tokens);
   }
-  return block_sum_f64(n, red);  // (its barriers make the sequences' counts visible)
+  block_sums_f64(n, red);  // (its barriers make the sequences' counts visible)
+  return n[0];
 }
 
 // Tokens with ratio q = exp(lp - old) and advantage A: -min(q A, clip(q, 1 - lo, 1 +
 // hi) A) + k (exp(g) - g - 1), g = ref - lp, weighted by w: 1 / counted tokens or
 // (per sequence) 1 / (sequences with counted tokens x the sequence's counted tokens).
 // dloss / dlp = w (-(not clipped) q A + k (1 - exp(g))).  stats: the weighted means of
-// the clipped term, of exp(g) - g - 1 and of the clipped tokens.  chosen: the targets'
-// logits, where the rows have had their gradient before (it may have replaced z).
+// the clipped term, of exp(g) - g - 1 and of the clipped tokens.
+AXON_DEV void policy_results(double (&sum)[4], double (*red)[16], float* loss, float* stats) {
+  block_sums_f64(sum, red);
+  if (threadIdx.x > 0) return;
+  loss[0] = (float)sum[0];
+  stats[0] = (float)sum[1];
+  stats[1] = (float)sum[2];
+  stats[2] = (float)sum[3];
+}
+
 template <typename T>
 __global__ void __launch_bounds__(1024) policy_finish_kernel(
     const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
     const float2* part /* may be stat */, int slices, const int32_t* __restrict__ cu, int seqs,
     const float* __restrict__ old, const float* __restrict__ ref, const float* __restrict__ adv, float lo, float hi,
     float kl_coef, float* __restrict__ loss, float* __restrict__ stats, float* __restrict__ logps,
-    double* __restrict__ weights, float2* stat, float* __restrict__ coef, const float* __restrict__ chosen) {
-  __shared__ double red[16];
+    double* __restrict__ weights, float2* stat, float* __restrict__ coef) {
+  __shared__ double red[4][16];
+  __shared__ int32_t held[CU_HELD];
+  const SeqLookup seq{cu, seqs};
   const int tid = threadIdx.x;
-  const double n = chosen ? 0.0 : policy_counts(targets, tokens, V, cu, seqs, weights, red);
-  double sum_l = 0.0, sum_s = 0.0, sum_k = 0.0, sum_c = 0.0;
+  seq.hold(held);
+  const double n = policy_counts(targets, tokens, V, cu, seqs, weights, red);
+  double sum[4] = {};
   constexpr int U = 4;  // tokens of a thread whose loads are under way together
   for (int t0 = tid; t0 < tokens; t0 += 1024 * U) {
     int tg[U];
@@ -373,8 +414,8 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
       st[u] = float2{0.f, 1.f};
       zt[u] = o[u] = a[u] = rf[u] = 0.f;
       if (tg[u] < 0 || tg[u] >= V) continue;
-      zt[u] = chosen ? chosen[t] : to_f32(z[t * ld + tg[u]]);
-      st[u] = part[(int64_t)t * slices];
+      zt[u] = to_f32(z[t * ld + tg[u]]);
+      if (slices == 1) st[u] = part[t];
       o[u] = old[t];
       a[u] = adv[t];
       if (ref) rf[u] = ref[t];
@@ -386,17 +427,13 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
       PolicyTerms p{};
       double w = 0.0;
       if (tg[u] >= 0 && tg[u] < V) {
-        for (int i = 1; i < slices; ++i) {
-          const float2 q = part[(int64_t)t * slices + i];
-          join_part(st[u].x, st[u].y, q.x, q.y);
-        }
-        const int j = cu ? seq_of_token(cu, seqs, t) : 0;
-        w = chosen ? weights[j] : 1.0 / (cu ? n * weights[j] : n);
+        if (slices > 1) st[u] = join_slices(part, t, slices);
+        w = 1.0 / (cu ? n * weights[seq.of(held, t)] : n);
         p = policy_token(zt[u], st[u].x, st[u].y, o[u], a[u], ref != nullptr, rf[u], lo, hi, kl_coef);
-        sum_l += w * (double)(p.surrogate + (ref ? kl_coef * p.kl : 0.f));
-        sum_s += w * (double)p.surrogate;
-        sum_k += w * (double)p.kl;
-        sum_c += p.clipped ? w : 0.0;
+        sum[0] += w * (double)(p.surrogate + (ref ? kl_coef * p.kl : 0.f));
+        sum[1] += w * (double)p.surrogate;
+        sum[2] += w * (double)p.kl;
+        sum[3] += p.clipped ? w : 0.0;
       }
       logps[t] = p.lp;
       if (coef) {
@@ -405,16 +442,26 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
       }
     }
   }
-  sum_l = block_sum_f64(sum_l, red);
-  sum_s = block_sum_f64(sum_s, red);
-  sum_k = block_sum_f64(sum_k, red);
-  sum_c = block_sum_f64(sum_c, red);
-  if (tid == 0) {
-    loss[0] = (float)sum_l;
-    stats[0] = (float)sum_s;
-    stats[1] = (float)sum_k;
-    stats[2] = (float)sum_c;
+  policy_results(sum, red, loss, stats);
+}
+
+// the same sums from the terms that the rows' own pass left (see RowCoef)
+__global__ void __launch_bounds__(1024) policy_sum_kernel(int tokens, const float2* __restrict__ terms,
+                                                          const float* __restrict__ clipped,
+                                                          const double* __restrict__ w, float kl_coef, bool has_ref,
+                                                          float* __restrict__ loss, float* __restrict__ stats) {
+  __shared__ double red[4][16];
+  double sum[4] = {};
+#pragma unroll 4
+  for (int t = threadIdx.x; t < tokens; t += 1024) {
+    const float2 p = terms[t];
+    const double v = w[t];
+    sum[0] += v * (double)(p.x + (has_ref ? kl_coef * p.y : 0.f));
+    sum[1] += v * (double)p.x;
+    sum[2] += v * (double)p.y;
+    sum[3] += v * (double)clipped[t];
   }
+  policy_results(sum, red, loss, stats);
 }
 
 // joins (op) over the lanes that differ in lane % NW; every lane the same result (see
@@ -497,12 +544,12 @@ __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld,
 // of the 2 V; in two passes with a kernel for the coefficients between them 592), float32
 // 811 (1153); 64 rows 17 us (34), one row 15 (14).
 
-// the weights, one launch before the rows: w[0] = 1 / counted tokens, or w[j] = 1 /
+// the weights of more than FEW tokens, one launch before the rows: w[0] = 1 / counted tokens, or w[j] = 1 /
 // (sequences with counted tokens x those of sequence j)
 __global__ void __launch_bounds__(1024) policy_weights_kernel(const int32_t* __restrict__ targets, int tokens, int V,
                                                               const int32_t* __restrict__ cu, int seqs,
                                                               double* __restrict__ w) {
-  __shared__ double red[16];
+  __shared__ double red[1][16];
   const double n = policy_counts(targets, tokens, V, cu, seqs, w, red);
   if (!cu) {
     if (threadIdx.x == 0) w[0] = 1.0 / n;
@@ -517,10 +564,56 @@ struct RowCoef {
   int seqs;
   const float *old, *ref, *adv;
   float lo, hi, kl_coef;
-  const double* weights;
-  float2* stat;   // out (policy), for the loss itself: (m, S) of each token
-  float* chosen;  // and its target's logit
+  const double* weights;  // null: each workgroup counts for itself (at most FEW tokens)
+  int tokens;
+  // out (policy), for the loss: of each token its log-probability, (clipped term, KL
+  // term), whether it is clipped, and its weight; zeros where it does not count
+  float* logps;
+  float2* terms;
+  float* clipped;
+  double* w;
 };
+
+constexpr int FEW = 256;  // tokens that a workgroup counts by itself, one a thread
+
+// bits [a, b) of mask, 64 a word
+AXON_DEV int bits_in(const uint64_t* mask, int a, int b) {
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < FEW / 64; ++k) {
+    const int lo = min(max(a - k * 64, 0), 64), hi = min(max(b - k * 64, 0), 64);
+    const uint64_t below_hi = hi == 64 ? ~0ull : (1ull << hi) - 1, below_lo = lo == 64 ? ~0ull : (1ull << lo) - 1;
+    n += __popcll(mask[k] & below_hi & ~below_lo);
+  }
+  return n;
+}
+
+// token t's weight where there are at most FEW tokens (policy_weights_kernel's values):
+// the counted ones as a bit mask; with cu, a token counts its sequence if it is
+// the first of it that counts.  A launch less: 47 rows of 50257 float32 logits 20.7 ->
+// 17.1 us a call; of 4096 rows of 128256 that launch is 5 us of 338.
+template <int THREADS>
+AXON_DEV double few_tokens_weight(const int32_t* targets, int V, const RowCoef& rc, int t) {
+  static_assert(THREADS >= FEW, "a thread for every token");
+  __shared__ uint64_t mask[FEW / 64];
+  __shared__ int firsts[FEW / 64];
+  const int i = threadIdx.x, wave = i >> 6;
+  const int tg = i < rc.tokens && i < FEW ? targets[i] : -1;
+  const bool counts = tg >= 0 && tg < V;
+  const uint64_t mine = __ballot(counts);
+  if (wave < FEW / 64 && (i & 63) == 0) mask[wave] = mine;
+  __syncthreads();
+  if (!rc.cu) return 1.0 / (double)bits_in(mask, 0, FEW);
+  const bool first = counts && bits_in(mask, rc.cu[seq_of_token(rc.cu, rc.seqs, i)], i) == 0;
+  const uint64_t heads = __ballot(first);
+  if (wave < FEW / 64 && (i & 63) == 0) firsts[wave] = __popcll(heads);
+  __syncthreads();
+  int n = 0;
+#pragma unroll
+  for (int k = 0; k < FEW / 64; ++k) n += firsts[k];
+  const int j = seq_of_token(rc.cu, rc.seqs, t);
+  return 1.0 / ((double)bits_in(mask, rc.cu[j], rc.cu[j + 1]) * (double)n);
+}
 
 // p + b bytes, b unsigned 32-bit: one register of address beside a uniform p
 template <typename T>
@@ -558,14 +651,22 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
     for (int c = i * 8; c < whole; c += STRIDE) Run8<TO>::store(out + c, zero);
     if (single) out[at] = from_f32<TO>(0.f);
   };
+  const bool policy = rc.dlogps == nullptr;
   if (!counts) {  // uniform over the workgroup
     zeros();
+    if (policy && i == 0) {
+      rc.logps[t] = rc.clipped[t] = 0.f;
+      rc.terms[t] = float2{0.f, 0.f};
+      rc.w[t] = 0.0;
+    }
     return;
   }
-  const bool policy = rc.dlogps == nullptr;
   const float zt = to_f32(row[tg]), given = policy ? rc.old[t] : rc.dlogps[t];
   const float adv = policy ? rc.adv[t] : 0.f, ref = policy && rc.ref ? rc.ref[t] : 0.f;
-  const float weight = policy ? (float)rc.weights[rc.cu ? seq_of_token(rc.cu, rc.seqs, (int)t) : 0] : 1.f;
+  double weight = 1.0;
+  if (policy)
+    weight = rc.weights ? rc.weights[rc.cu ? seq_of_token(rc.cu, rc.seqs, (int)t) : 0]
+                        : few_tokens_weight<THREADS>(targets, V, rc, (int)t);
   // every load unconditional (past the row's groups its last one again), so that
   // each is waited for by itself and the sums run under the loads behind them
   Run8<T> r[RUNS];
@@ -604,9 +705,12 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
   float w = given;
   if (policy) {
     if (i == 0) {
-      coef = weight * policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef).c;
-      rc.stat[t] = float2{m, s};
-      rc.chosen[t] = zt;
+      const PolicyTerms p = policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef);
+      coef = (float)weight * p.c;
+      rc.logps[t] = p.lp;
+      rc.terms[t] = float2{p.surrogate, p.kl};
+      rc.clipped[t] = p.clipped ? 1.f : 0.f;
+      rc.w[t] = weight;
     }
     __syncthreads();
     w = coef;
@@ -640,21 +744,27 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
 
 // ---------------------------------------------------------------- within a training step
 
-// (m, S) of a row from the np (largest, sum) partials of its 64-column pieces, a
-// workgroup a row; rows that do not count are skipped
+// (m, S) of a row from the np (largest, sum) partials of its 64-column pieces, and
+// (lps) its target's log-probability, a workgroup a row; rows that do not count are skipped
 __global__ void __launch_bounds__(PART_THREADS) piece_merge_kernel(const float2* __restrict__ pieces, int np, int V,
-                                                          const int32_t* __restrict__ targets,
-                                                          float2* __restrict__ stat) {
+                                                                   const int32_t* __restrict__ targets,
+                                                                   float2* __restrict__ stat,
+                                                                   const float* __restrict__ z, int ldl,
+                                                                   double* __restrict__ lps) {
   __shared__ float red[2][PART_THREADS / 64];
   const int t = blockIdx.x, tg = targets[t];
-  if (tg < 0 || tg >= V) return;
+  const bool counts = tg >= 0 && tg < V;
   float m = -INFINITY, s = 0.f;
-  for (int i = threadIdx.x; i < np; i += PART_THREADS) {
-    const float2 p = pieces[(int64_t)t * np + i];
-    join_part(m, s, p.x, p.y);
+  if (counts) {
+    for (int i = threadIdx.x; i < np; i += PART_THREADS) {
+      const float2 p = pieces[(int64_t)t * np + i];
+      join_part(m, s, p.x, p.y);
+    }
+    join_block(m, s, red);
   }
-  join_block(m, s, red);
-  if (threadIdx.x == 0) stat[t] = float2{m, s};
+  if (threadIdx.x > 0) return;
+  if (counts) stat[t] = float2{m, s};
+  put_logp(counts, z + (int64_t)t * ldl + tg, m, s, nullptr, lps ? lps + t : nullptr);
 }
 
 // The gradient as the training step's GEMM operand: bf16 in the row-pair layout,
@@ -705,9 +815,9 @@ size_t up(size_t n) { return (n + 255) / 256 * 256; }
 // the workspace of a call
 struct LossWs {
   float2* part;
-  float2* stat;
-  float* coef;
-  double* lps;   // preference: [tokens]
+  float2* stat;  // (policy: RowCoef's terms)
+  float* coef;   // (policy: its clipped)
+  double* lps;   // preference: log-probabilities; policy: weights
   double* seq;   // [seqs]
 };
 size_t carve(int64_t tokens, int V, int64_t seqs, char* base, LossWs* ws) {
@@ -730,12 +840,13 @@ size_t carve(int64_t tokens, int V, int64_t seqs, char* base, LossWs* ws) {
 }
 
 template <typename T>
-int run_parts(const LogitRows& r, float2* part, float* logps, hipStream_t s) {
+int run_parts(const LogitRows& r, float2* part, float* logps, double* lps, hipStream_t s) {
   int slices, cols;
   part_shape(r.tokens, r.V, slices, cols);
   const int64_t items = r.tokens * slices;
   logit_part_kernel<T><<<(unsigned)std::min(items, MAX_WGS), PART_THREADS, 0, s>>>(
-      (const T*)r.z, r.ld, r.V, r.targets, items, slices, cols, part, slices == 1 ? logps : nullptr);
+      (const T*)r.z, r.ld, r.V, r.targets, items, slices, cols, part, slices == 1 ? logps : nullptr,
+      slices == 1 ? lps : nullptr);
   return slices;
 }
 
@@ -775,7 +886,7 @@ template <typename T>
 void logprobs(const LogitRows& r, float* logps, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, 0, (char*)wsp, &w);
-  const int slices = run_parts<T>(r, w.part, logps, s);
+  const int slices = run_parts<T>(r, w.part, logps, nullptr, s);
   if (slices > 1)
     logps_finish_kernel<T><<<(unsigned)((r.tokens + 255) / 256), 256, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets,
                                                                              r.tokens, w.part, slices, logps);
@@ -792,7 +903,8 @@ template <typename T>
 void preference(const LogitRows& r, const PreferenceArgs& a, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, a.seqs, (char*)wsp, &w);
-  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, s) : 1;
+  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, w.lps, s) : 1;
+  if (slices == 1) w.stat = w.part;
   preference_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices,
                                                  a.cu, a.seqs, a.ref, a.beta, a.smoothing, a.loss, a.seq_logps,
                                                  a.margins, w.lps, w.seq, w.stat, r.dz ? w.coef : nullptr);
@@ -804,18 +916,21 @@ void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, a.seqs, (char*)wsp, &w);
   if (r.dz && r.tokens > 0) {
-    policy_weights_kernel<<<1, 1024, 0, s>>>(r.targets, (int)r.tokens, r.V, a.cu, a.seqs, w.seq);
-    run_rows<T>(r, RowCoef{nullptr, a.cu, a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, w.seq, w.stat, w.coef}, s);
-    policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.stat, 1, a.cu,
-                                               a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
-                                               a.logps, w.seq, nullptr, nullptr, w.coef);
+    const bool few = r.tokens <= FEW;
+    if (!few) policy_weights_kernel<<<1, 1024, 0, s>>>(r.targets, (int)r.tokens, r.V, a.cu, a.seqs, w.seq);
+    run_rows<T>(r,
+                RowCoef{nullptr, a.cu, a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, few ? nullptr : w.seq,
+                        (int)r.tokens, a.logps, w.stat, w.coef, w.lps},
+                s);
+    policy_sum_kernel<<<1, 1024, 0, s>>>((int)r.tokens, w.stat, w.coef, w.lps, a.kl_coef, a.ref != nullptr, a.loss,
+                                         a.stats);
     return;
   }
   // the loss alone
-  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, s) : 1;
+  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, nullptr, s) : 1;
   policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices, a.cu,
                                              a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
-                                             a.logps, w.seq, nullptr, nullptr, nullptr);
+                                             a.logps, w.seq, nullptr, nullptr);
 }
 
 }  // namespace
@@ -841,8 +956,9 @@ void launch_policy_loss(const LogitRows& r, const PolicyArgs& a, void* ws, hipSt
 
 namespace {
 
-void train_stat(const TrainLogits& r, hipStream_t s) {
-  piece_merge_kernel<<<r.T, PART_THREADS, 0, s>>>(r.lse_part, (r.V + LSE_COLS - 1) / LSE_COLS, r.V, r.targets, r.stat);
+void train_stat(const TrainLogits& r, double* lps, hipStream_t s) {
+  piece_merge_kernel<<<r.T, PART_THREADS, 0, s>>>(r.lse_part, (r.V + LSE_COLS - 1) / LSE_COLS, r.V, r.targets, r.stat,
+                                                  r.z, r.ldl, lps);
 }
 
 void train_grad(const TrainLogits& r, hipStream_t s) {
@@ -853,7 +969,7 @@ void train_grad(const TrainLogits& r, hipStream_t s) {
 }  // namespace
 
 void launch_preference_train(const TrainLogits& r, const PreferenceArgs& a, hipStream_t s) {
-  train_stat(r, s);
+  train_stat(r, r.lps, s);
   preference_finish_kernel<float><<<1, 1024, 0, s>>>(r.z, r.ldl, r.V, r.targets, r.T, r.stat, 1, a.cu, a.seqs, a.ref,
                                                      a.beta, a.smoothing, a.loss, a.seq_logps, a.margins, r.lps, r.seq,
                                                      r.stat, r.coef);
@@ -861,10 +977,10 @@ void launch_preference_train(const TrainLogits& r, const PreferenceArgs& a, hipS
 }
 
 void launch_policy_train(const TrainLogits& r, const PolicyArgs& a, hipStream_t s) {
-  train_stat(r, s);
+  train_stat(r, nullptr, s);
   policy_finish_kernel<float><<<1, 1024, 0, s>>>(r.z, r.ldl, r.V, r.targets, r.T, r.stat, 1, a.cu, a.seqs, a.old, a.ref,
                                                  a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats, a.logps, r.seq, r.stat,
-                                                 r.coef, nullptr);
+                                                 r.coef);
   train_grad(r, s);
 }
 

@@ -214,6 +214,19 @@ def test_policy_loss(case, per):
         check(got[3], r.grad(c), r.grad_bound(c, dc + 4 * U * c.abs(), HALF[dtype]), "dlogits")
 
 
+# more sequences than a workgroup keeps the boundaries of (1024); as many tokens as a
+# workgroup counts by itself (256) and one more; few tokens in many sequences
+MANY = [([1, 0, 2] * 400, 130, 130, F), ([64, 0, 0, 192], 301, 301, B), ([200, 0, 0, 57], 300, 300, F),
+        ([1, 0, 0, 0] * 80, 41, 41, B), ([0, 65, 0, 1] * 3 + [0, 0], 9000, 9000, F)]
+
+
+@pytest.mark.parametrize("case", MANY, ids=name)
+def test_many_sequences(case):
+    test_preference_loss(case, 0.1)
+    test_policy_loss(case, False)
+    test_policy_loss(case, True)
+
+
 def test_what_the_binding_refuses():
     z, tg, cu = make([4, 5], 30, F, 50)
     f = torch.zeros(9, device="cuda")

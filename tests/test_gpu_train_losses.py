@@ -269,7 +269,7 @@ def test_refusals_of_a_step():
         m.policy_loss_and_grads(flat, cu, targets, grads, f[:3], f)
     with pytest.raises(ValueError, match="tensors on"):
         m.policy_loss_and_grads(flat, cu, targets, grads, f.cpu(), f)
-    with pytest.raises(ValueError, match="tensors on"):
+    with pytest.raises(ValueError, match="gradient buffer on cpu"):
         m.policy_loss_and_grads(flat, cu, targets, {**grads, "transformer.ln_f.bias": f.cpu()}, f, f)
     with pytest.raises(ValueError, match="targets must hold"):
         m.policy_loss_and_grads(flat, cu, targets.long(), grads, f, f)
