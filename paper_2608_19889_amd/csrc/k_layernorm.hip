@@ -499,7 +499,7 @@ struct Int {
 template <typename F>
 void ln_fwd_shape(int cols, F&& f) {
   if (cols <= 512) f(Int<64>{}, Int<1>{}, 2048);
-  else if (cols <= 1024) f(Int<64>{}, Int<2>{}, 3072);
+  else if (cols <= 1024) f(Int<64>{}, Int<2>{}, 4096);
   else if (cols <= 2048) f(Int<64>{}, Int<4>{}, 512);
   else if (cols <= 4096) f(Int<256>{}, Int<2>{}, 16384);
   else if (cols <= 8192) f(Int<512>{}, Int<2>{}, 16384);
