@@ -255,6 +255,77 @@ def test_step_on_another_stream(family):
     m.close()
 
 
+@pytest.mark.parametrize("family", ["llama", "gpt2"])
+def test_steps_that_count_nothing(family):
+    """Every gradient is overwritten with zeros; what the positions' other inputs hold
+    is not used; a preference loss of equal margins is log 2."""
+    shape, lens = FAMILIES[family]
+    w, seqs, tg, m, flat, cu, targets, grads = setup(shape, lens, 102)
+    none = torch.where(targets % 2 == 0, -1, shape["vocab_size"]).to(torch.int32)
+    nan = torch.full((len(tg),), float("nan"), device="cuda")
+    for per in (False, True):
+        loss, stats, logps = m.policy_loss_and_grads(flat, cu, none, grads, nan, nan, nan, kl_coef=0.1,
+                                                     per_sequence=per)
+        assert not loss.any() and not stats.any() and not logps.any()
+        assert all(not g.any() for g in grads.values())
+    for g in grads.values():
+        g.fill_(float("nan"))
+    loss, seq, margins = m.preference_loss_and_grads(flat, cu, none, grads)
+    assert abs(float(loss) - math.log(2)) <= 2.0 ** -23 and not seq.any() and not margins.any()
+    assert all(not g.any() for g in grads.values())
+    m.close()
+
+
+@pytest.mark.parametrize("family", ["llama", "gpt2"])
+def test_step_of_one_token(family):
+    """One sequence of one token.  Its attention has one key, so the gradients of q and k
+    are zero but for the rounding of what is stored, and are left out here."""
+    shape, _ = FAMILIES[family]
+    w, seqs, tg, m, flat, cu, targets, grads = setup(shape, [1], 105)
+    targets.fill_(17)
+    want, ref = ag.loss_and_grads(shape, w, seqs, ag.cross_entropy(np.array([17])))
+    loss = m.loss_and_grads(flat, cu, targets, grads)
+    assert abs(float(loss) - want) <= 6 * 3e-3
+    assert all(bool(torch.isfinite(g).all()) for g in grads.values())
+    for name, r in ref.items():
+        if not any(k in name for k in ("q_proj", "k_proj", "c_attn")):
+            check_weighted(name, grads[name].cpu().double().numpy(), r)
+    # A = 1 and a ratio of 1: the cross-entropy's gradient, up to elements of the logits'
+    # whose bf16 rounding falls the other way (2^-8)
+    first = {k: g.clone() for k, g in grads.items()}
+    old = -loss.clone()
+    loss, stats, logps = m.policy_loss_and_grads(flat, cu, targets, grads, old, torch.ones_like(old))
+    assert abs(float(loss) + 1) <= 1e-4 and abs(float(logps) - float(old)) <= 1e-4
+    for name, g in grads.items():
+        assert float((g - first[name]).norm()) <= 1e-2 * float(first[name].norm()) + 1e-6, name
+    m.close()
+
+
+@pytest.mark.parametrize("family", ["llama", "gpt2"])
+def test_decode_goes_on_after_a_step(family):
+    """A step leaves its sequences in the cache, as a prompt would."""
+    shape, lens = FAMILIES[family]
+    w = model_weights(shape, seed=108)
+    ids = prompts(len(lens), max(lens), shape["vocab_size"], seed=109).numpy()
+    seqs = [ids[i, :n] for i, n in enumerate(lens)]
+    m, fresh = (gpu_model(shape, w, max_batch=len(lens), max_seq=max(lens) + 3) for _ in range(2))
+    flat, cu = pack(seqs)
+    targets = torch.as_tensor(np.concatenate(_targets(seqs, shape["vocab_size"], seed=110)), dtype=torch.int32).cuda()
+    grads = {k: torch.empty(tuple(v.shape), dtype=torch.float32, device="cuda") for k, v in w.items()}
+    m.policy_loss_and_grads(flat, cu, targets, grads, torch.zeros(len(flat), device="cuda"),
+                            torch.zeros(len(flat), device="cuda"))
+    _, nxt = fresh.prefill(flat, cu)
+    a, b = (torch.empty(len(lens), shape["vocab_size"], device="cuda") for _ in range(2))
+    for _ in range(3):
+        m.decode_step(nxt, logits=a)
+        _, more = fresh.decode_step(nxt, logits=b)
+        # each within 6 x 3e-3 of the exact ones
+        assert float((a - b).abs().max()) <= 2 * 6 * 3e-3
+        nxt = more.clone()
+    m.close()
+    fresh.close()
+
+
 def test_refusals_of_a_step():
     shape, lens = FAMILIES["gpt2"]
     w, seqs, tg, m, flat, cu, targets, grads = setup(shape, lens, 99)
