@@ -12,6 +12,7 @@
 //
 //   logit_part_kernel   reads the rows: (m, S) of every slice of a row
 //   *_finish_kernel     joins a row's slices; loss, statistics, c of every token
+//                       (preference_few_kernel: with the gradient, for few tokens)
 //   logit_grad_kernel   reads the rows again and writes the gradient
 //   logit_row_kernel    all of it in one pass, where c depends on the row alone; then
 //   policy_sum_kernel   adds up the loss's terms
@@ -28,6 +29,7 @@ namespace axon {
 constexpr int PART_THREADS = 256;
 constexpr int PART_RUNS = 4;  // groups of 8 logits a thread holds at once
 constexpr int GRAD_RUNS = 4;
+constexpr int FEW = 256;  // tokens that every workgroup goes through by itself, one a thread
 
 // (m, s) joined with (m2, s2), both the sum of exp(value - maximum); a side that has
 // seen nothing is (-inf, 0)
@@ -127,12 +129,13 @@ AXON_DEV void put_logp(bool counts, const T* chosen, float m, float s, float* lo
 
 // One slice (of ``slices``, ``cols`` wide) of one row a workgroup: its maximum and
 // sum of exponentials, and, of whole rows, the target's log-probability.  Rows that do
-// not count are skipped.
+// not count are skipped.  chosen: the targets' logits too.
 template <typename T>
-__global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __restrict__ z, int64_t ld, int V,
+__global__ void __launch_bounds__(PART_THREADS, 8) logit_part_kernel(const T* __restrict__ z, int64_t ld, int V,
                                                                   const int32_t* __restrict__ targets, int64_t items,
                                                                   int slices, int cols, float2* __restrict__ part,
-                                                                  float* __restrict__ logps, double* __restrict__ lps) {
+                                                                  float* __restrict__ logps, double* __restrict__ lps,
+                                                                  float* __restrict__ chosen) {
   constexpr int STRIDE = PART_THREADS * 8, BLOCK = STRIDE * PART_RUNS;
   __shared__ float red[2][PART_THREADS / 64];
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
@@ -158,6 +161,7 @@ __global__ void __launch_bounds__(PART_THREADS) logit_part_kernel(const T* __res
     join_block(m, s, red);
     if (threadIdx.x == 0) {
       if (part) part[it] = float2{m, s};
+      if (chosen && c0 == 0) chosen[t] = to_f32(z[t * ld + tg]);
       put_logp(true, z + t * ld + tg, m, s, logps ? logps + t : nullptr, lps ? lps + t : nullptr);
     }
   }
@@ -195,8 +199,8 @@ AXON_DEV double wave_sum_f64(double v) {
   return v;
 }
 
-// N sums over a workgroup of 1024 threads, in every thread
-template <int N>
+// N sums over a workgroup of THREADS, in every thread
+template <int THREADS = 1024, int N>
 AXON_DEV void block_sums_f64(double (&v)[N], double (*red)[16]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) v[k] = wave_sum_f64(v[k]);
@@ -208,7 +212,7 @@ AXON_DEV void block_sums_f64(double (&v)[N], double (*red)[16]) {
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     v[k] = 0.0;
-    for (int i = 0; i < 16; ++i) v[k] += red[k][i];
+    for (int i = 0; i < THREADS / 64; ++i) v[k] += red[k][i];
   }
 }
 
@@ -234,19 +238,58 @@ AXON_DEV double softplus_f64(double v) { return fmax(v, 0.0) + log1p(exp(-fabs(v
 // Pairs (chosen 2i, rejected 2i + 1): s_j the sum of sequence j's lp, u_i = beta
 // ((s_2i - ref_2i) - (s_2i+1 - ref_2i+1)), loss = mean of (1 - e) softplus(-u) + e
 // softplus(u); dloss / ds_2i = beta / pairs (e sigmoid(u) - (1 - e) sigmoid(-u)).
-// One workgroup: tokens (slices > 1: else the rows' pass has left lps and stat), then
-// sequences, then pairs.
+// One workgroup, from the tokens' lps: sums [seqs] in, dloss / ds out; the
+// results only where ``write``.
+struct PairOut {
+  float *loss, *seq_logps, *margins;
+};
+template <int THREADS>
+AXON_DEV void pair_coefs(const double* lps, int tokens, const int32_t* cu, int seqs, const float* ref, float beta,
+                         float smoothing, double* sums, double (*red)[16], bool write, PairOut out) {
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  for (int j = wave; j < seqs; j += THREADS / 64) {
+    const int t1 = min(tokens, cu[j + 1]);
+    double s = 0.0;
+#pragma unroll 8
+    for (int t = max(0, cu[j]) + lane; t < t1; t += 64) s += lps[t];
+    s = wave_sum_f64(s);
+    if (lane == 0) {
+      sums[j] = s;
+      if (write) out.seq_logps[j] = (float)s;
+    }
+  }
+  __syncthreads();
+  const int pairs = seqs / 2;
+  double total[1] = {};
+  for (int i = tid; i < pairs; i += THREADS) {
+    double r0 = sums[2 * i], r1 = sums[2 * i + 1];
+    if (ref) {
+      r0 -= (double)ref[2 * i];
+      r1 -= (double)ref[2 * i + 1];
+    }
+    const double u = (double)beta * (r0 - r1), e = (double)smoothing;
+    if (write) out.margins[i] = (float)u;
+    total[0] += (1.0 - e) * softplus_f64(-u) + e * softplus_f64(u);
+    const double yes = 1.0 / (1.0 + exp(-u)), no = 1.0 / (1.0 + exp(u));
+    const double d = (double)beta / pairs * (e * yes - (1.0 - e) * no);
+    sums[2 * i] = d;
+    sums[2 * i + 1] = -d;
+  }
+  block_sums_f64<THREADS>(total, red);  // (its barriers make the sequences' coefficients visible)
+  if (write && tid == 0) out.loss[0] = pairs > 0 ? (float)(total[0] / pairs) : 0.f;
+}
+
+// slices > 1: the tokens' lps and stat first (else the rows' pass has left them)
 template <typename T>
 __global__ void __launch_bounds__(1024) preference_finish_kernel(
     const T* __restrict__ z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens,
     const float2* __restrict__ part, int slices, const int32_t* __restrict__ cu, int seqs,
-    const float* __restrict__ ref, float beta, float smoothing, float* __restrict__ loss,
-    float* __restrict__ seq_logps, float* __restrict__ margins, double* __restrict__ lps, double* __restrict__ sums,
-    float2* __restrict__ stat, float* __restrict__ coef) {
+    const float* __restrict__ ref, float beta, float smoothing, PairOut out, double* __restrict__ lps,
+    double* __restrict__ sums, float2* __restrict__ stat, float* __restrict__ coef) {
   __shared__ double red[1][16];
   __shared__ int32_t held[CU_HELD];
   const SeqLookup seq{cu, seqs};
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int tid = threadIdx.x;
   seq.hold(held);
   if (slices > 1)
     for (int64_t t = tid; t < tokens; t += 1024) {
@@ -257,37 +300,7 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(
       stat[t] = st;
     }
   __syncthreads();
-  for (int j = wave; j < seqs; j += 16) {
-    const int t1 = min(tokens, cu[j + 1]);
-    double s = 0.0;
-#pragma unroll 8
-    for (int t = max(0, cu[j]) + lane; t < t1; t += 64) s += lps[t];
-    s = wave_sum_f64(s);
-    if (lane == 0) {
-      sums[j] = s;
-      seq_logps[j] = (float)s;
-    }
-  }
-  __syncthreads();
-  const int pairs = seqs / 2;
-  double total = 0.0;
-  for (int i = tid; i < pairs; i += 1024) {
-    double r0 = sums[2 * i], r1 = sums[2 * i + 1];
-    if (ref) {
-      r0 -= (double)ref[2 * i];
-      r1 -= (double)ref[2 * i + 1];
-    }
-    const double u = (double)beta * (r0 - r1), e = (double)smoothing;
-    margins[i] = (float)u;
-    total += (1.0 - e) * softplus_f64(-u) + e * softplus_f64(u);
-    const double yes = 1.0 / (1.0 + exp(-u)), no = 1.0 / (1.0 + exp(u));
-    const double d = (double)beta / pairs * (e * yes - (1.0 - e) * no);
-    sums[2 * i] = d;
-    sums[2 * i + 1] = -d;
-  }
-  double one[1] = {total};
-  block_sums_f64(one, red);  // (its barriers make the sequences' coefficients visible)
-  if (tid == 0) loss[0] = pairs > 0 ? (float)(one[0] / pairs) : 0.f;
+  pair_coefs<1024>(lps, tokens, cu, seqs, ref, beta, smoothing, sums, red, true, out);
   if (!coef) return;
 #pragma unroll 4
   for (int t = tid; t < tokens; t += 1024) {
@@ -485,53 +498,85 @@ AXON_DEV void grad_run(float (&v)[8], const ExpFrom& e, float f, float c, int at
     for (int j = 0; j < 8; ++j) v[j] += j == at ? c : 0.f;
 }
 
-// dz of one slice of a row a workgroup.  z and dz may be one buffer: a thread writes
-// what it has read, and what it reads beyond that (groups at the row's end) counts
-// nothing.
+// dz of one slice of a row, by a workgroup of 256.  z and dz may be one buffer: a thread
+// writes what it has read, and what it reads beyond that (groups at the row's end)
+// counts nothing.
+constexpr int GRAD_COLS = 256 * 8 * GRAD_RUNS;
+template <typename T, typename TO>
+AXON_DEV void grad_slice(const T* row, int V, int tg, int first, float w, float2 st, TO* out) {
+  constexpr int STRIDE = 256 * 8;
+  const int c0 = first + threadIdx.x * 8;
+  const ExpFrom e(st.x);
+  const float f = -w / st.y * e.fix;
+  const int h = odd_head(row), n = V - h;
+  tg -= h;
+  row += h;
+  out += h;
+  if (h && c0 == 0) out[-1] = from_f32<TO>(w == 0.f ? 0.f : e(to_f32(row[-1])) * f + (tg == -1 ? w : 0.f));
+  if (first + GRAD_COLS <= n) {
+    float v[GRAD_RUNS][8] = {};
+    if (w != 0.f) {
+      Run8<T> r[GRAD_RUNS];
+#pragma unroll
+      for (int k = 0; k < GRAD_RUNS; ++k) r[k].load(row + c0 + k * STRIDE);
+#pragma unroll
+      for (int k = 0; k < GRAD_RUNS; ++k) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[k][j] = r[k][j];
+        grad_run(v[k], e, f, w, tg - (c0 + k * STRIDE));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < GRAD_RUNS; ++k) Run8<TO>::store(out + c0 + k * STRIDE, v[k]);
+  } else {  // the row's last slice
+    for (int c = c0; c < n; c += STRIDE) {
+      float v[8] = {};
+      if (w != 0.f) {
+        load_run8(row, c, n, v, 0.f);
+        grad_run(v, e, f, w, tg - c);
+      }
+      store_run8(out, c, n, v);
+    }
+  }
+}
+
 template <typename T, typename TO>
 __global__ void __launch_bounds__(256) logit_grad_kernel(const T* z, int64_t ld, int V,
                                                          const int32_t* __restrict__ targets, int64_t items, int slices,
                                                          const float2* __restrict__ stat,
                                                          const float* __restrict__ coef, TO* dz, int64_t lddz) {
-  constexpr int STRIDE = 256 * 8, COLS = STRIDE * GRAD_RUNS;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t t = it / slices;
-    const int first = (int)(it % slices) * COLS, c0 = first + threadIdx.x * 8;
-    const float w = coef[t];
-    const float2 st = stat[t];
-    const ExpFrom e(st.x);
-    const float f = -w / st.y * e.fix;
-    const T* row = z + t * ld;
-    const int h = odd_head(row), n = V - h, tg = targets[t] - h;
-    row += h;
-    TO* out = dz + t * lddz + h;
-    if (h && c0 == 0) out[-1] = from_f32<TO>(w == 0.f ? 0.f : e(to_f32(row[-1])) * f + (tg == -1 ? w : 0.f));
-    if (first + COLS <= n) {
-      float v[GRAD_RUNS][8] = {};
-      if (w != 0.f) {
-        Run8<T> r[GRAD_RUNS];
-#pragma unroll
-        for (int k = 0; k < GRAD_RUNS; ++k) r[k].load(row + c0 + k * STRIDE);
-#pragma unroll
-        for (int k = 0; k < GRAD_RUNS; ++k) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[k][j] = r[k][j];
-          grad_run(v[k], e, f, w, tg - (c0 + k * STRIDE));
-        }
-      }
-#pragma unroll
-      for (int k = 0; k < GRAD_RUNS; ++k) Run8<TO>::store(out + c0 + k * STRIDE, v[k]);
-    } else {  // the row's last slice
-      for (int c = c0; c < n; c += STRIDE) {
-        float v[8] = {};
-        if (w != 0.f) {
-          load_run8(row, c, n, v, 0.f);
-          grad_run(v, e, f, w, tg - c);
-        }
-        store_run8(out, c, n, v);
-      }
-    }
+    grad_slice(z + t * ld, V, targets[t], (int)(it % slices) * GRAD_COLS, coef[t], stat[t], dz + t * lddz);
   }
+}
+
+// The preference loss and its gradient from the slices of at most FEW tokens in at most
+// FEW sequences: every workgroup works the coefficients out for itself, the first
+// writes the results, and a launch less is made.  chosen: the targets' logits, which dz
+// may be about to replace.
+template <typename T, typename TO>
+__global__ void __launch_bounds__(256) preference_few_kernel(
+    const T* z, int64_t ld, int V, const int32_t* __restrict__ targets, int tokens, const float2* __restrict__ part,
+    int slices, const float* __restrict__ chosen, const double* __restrict__ lps, const int32_t* __restrict__ cu,
+    int seqs, const float* __restrict__ ref, float beta, float smoothing, PairOut out, int grad_slices, TO* dz,
+    int64_t lddz) {
+  __shared__ double red[1][16], lp[FEW], sums[FEW];
+  __shared__ float2 own;
+  const int i = threadIdx.x, t = blockIdx.x / grad_slices;
+  if (i < tokens) {
+    const int tg = targets[i];
+    const bool counts = tg >= 0 && tg < V;
+    const float2 st = counts ? join_slices(part, i, slices) : float2{0.f, 1.f};
+    if (slices > 1) put_logp(counts, chosen + i, st.x, st.y, nullptr, lp + i);
+    else lp[i] = lps[i];
+    if (i == t) own = st;
+  }
+  __syncthreads();
+  pair_coefs<256>(lp, tokens, cu, seqs, ref, beta, smoothing, sums, red, blockIdx.x == 0, out);
+  const int tg = targets[t];
+  const float w = tg >= 0 && tg < V ? (float)sums[seq_of_token(cu, seqs, t)] : 0.f;
+  grad_slice(z + (int64_t)t * ld, V, tg, (int)(blockIdx.x % grad_slices) * GRAD_COLS, w, own, dz + t * lddz);
 }
 
 // ---------------------------------------------------------------- whole rows, read once
@@ -573,8 +618,6 @@ struct RowCoef {
   float* clipped;
   double* w;
 };
-
-constexpr int FEW = 256;  // tokens that a workgroup counts by itself, one a thread
 
 // bits [a, b) of mask, 64 a word
 AXON_DEV int bits_in(const uint64_t* mask, int a, int b) {
@@ -840,19 +883,19 @@ size_t carve(int64_t tokens, int V, int64_t seqs, char* base, LossWs* ws) {
 }
 
 template <typename T>
-int run_parts(const LogitRows& r, float2* part, float* logps, double* lps, hipStream_t s) {
+int run_parts(const LogitRows& r, float2* part, float* logps, double* lps, float* chosen, hipStream_t s) {
   int slices, cols;
   part_shape(r.tokens, r.V, slices, cols);
   const int64_t items = r.tokens * slices;
   logit_part_kernel<T><<<(unsigned)std::min(items, MAX_WGS), PART_THREADS, 0, s>>>(
       (const T*)r.z, r.ld, r.V, r.targets, items, slices, cols, part, slices == 1 ? logps : nullptr,
-      slices == 1 ? lps : nullptr);
+      slices == 1 ? lps : nullptr, chosen);
   return slices;
 }
 
 template <typename T>
 void run_grad(const LogitRows& r, const LossWs& w, hipStream_t s) {
-  const int slices = (r.V + 2048 * GRAD_RUNS - 1) / (2048 * GRAD_RUNS);
+  const int slices = (r.V + GRAD_COLS - 1) / GRAD_COLS;
   const int64_t items = r.tokens * slices;
   const unsigned wgs = (unsigned)std::min(items, MAX_WGS);
   if (r.dz_bf16)
@@ -886,7 +929,7 @@ template <typename T>
 void logprobs(const LogitRows& r, float* logps, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, 0, (char*)wsp, &w);
-  const int slices = run_parts<T>(r, w.part, logps, nullptr, s);
+  const int slices = run_parts<T>(r, w.part, logps, nullptr, nullptr, s);
   if (slices > 1)
     logps_finish_kernel<T><<<(unsigned)((r.tokens + 255) / 256), 256, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets,
                                                                              r.tokens, w.part, slices, logps);
@@ -899,15 +942,36 @@ void logprobs_bwd(const LogitRows& r, const float* dlogps, hipStream_t s) {
   run_rows<T>(r, rc, s);
 }
 
+// Every workgroup its own coefficients while there are few of both: us a call that way
+// and with a launch between, 61 x 32000 bf16 15.0 and 16.4, 61 x 128256 float32 (976
+// workgroups) 21.6 and 23.7, 128 x 128256 (2048) 42.9 and 41.7, 250 x 32000 bf16 (1000)
+// 23.7 and 21.7, 250 x 128256 (4000) 55 and 41.
+bool few_pairs(const LogitRows& r, int seqs) {
+  return r.dz && r.tokens > 0 && r.tokens <= FEW / 2 && seqs <= FEW &&
+         r.tokens * ((r.V + GRAD_COLS - 1) / GRAD_COLS) <= 1024;
+}
+
 template <typename T>
 void preference(const LogitRows& r, const PreferenceArgs& a, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, a.seqs, (char*)wsp, &w);
-  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, w.lps, s) : 1;
+  const bool few = few_pairs(r, a.seqs);
+  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, w.lps, few ? w.coef : nullptr, s) : 1;
+  const PairOut out{a.loss, a.seq_logps, a.margins};
+  if (few) {
+    const int g = (r.V + GRAD_COLS - 1) / GRAD_COLS;
+    auto go = [&](auto kern, auto* dz) {
+      kern<<<(unsigned)r.tokens * g, 256, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices,
+                                                  w.coef, w.lps, a.cu, a.seqs, a.ref, a.beta, a.smoothing, out, g, dz,
+                                                  r.lddz);
+    };
+    r.dz_bf16 ? go(preference_few_kernel<T, bf16>, (bf16*)r.dz) : go(preference_few_kernel<T, float>, (float*)r.dz);
+    return;
+  }
   if (slices == 1) w.stat = w.part;
   preference_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices,
-                                                 a.cu, a.seqs, a.ref, a.beta, a.smoothing, a.loss, a.seq_logps,
-                                                 a.margins, w.lps, w.seq, w.stat, r.dz ? w.coef : nullptr);
+                                                 a.cu, a.seqs, a.ref, a.beta, a.smoothing, out, w.lps, w.seq, w.stat,
+                                                 r.dz ? w.coef : nullptr);
   if (r.dz && r.tokens > 0) run_grad<T>(r, w, s);
 }
 
@@ -927,7 +991,7 @@ void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
     return;
   }
   // the loss alone
-  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, nullptr, s) : 1;
+  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, nullptr, nullptr, s) : 1;
   policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices, a.cu,
                                              a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
                                              a.logps, w.seq, nullptr, nullptr);
@@ -971,8 +1035,8 @@ void train_grad(const TrainLogits& r, hipStream_t s) {
 void launch_preference_train(const TrainLogits& r, const PreferenceArgs& a, hipStream_t s) {
   train_stat(r, r.lps, s);
   preference_finish_kernel<float><<<1, 1024, 0, s>>>(r.z, r.ldl, r.V, r.targets, r.T, r.stat, 1, a.cu, a.seqs, a.ref,
-                                                     a.beta, a.smoothing, a.loss, a.seq_logps, a.margins, r.lps, r.seq,
-                                                     r.stat, r.coef);
+                                                     a.beta, a.smoothing, PairOut{a.loss, a.seq_logps, a.margins},
+                                                     r.lps, r.seq, r.stat, r.coef);
   train_grad(r, s);
 }
 

@@ -21,12 +21,13 @@ void row_partials(const std::string& k, dim3 grid, void** args) {
   };
   if (is("ln_bwd_kernel")) say(8, grid.x * (is("Lb1EEEvPKT_") ? 3 : 2) * n(10));
   else if (is("gelu_bwd_kernel")) say(7, grid.y * n(5));
-  else if (is("logit_part_kernel")) say(7, *(const int64_t*)args[4] * 2), say(9, *(const int64_t*)args[4] * 2);
+  else if (is("logit_part_kernel")) say(7, *(const int64_t*)args[4] * 2), say(9, *(const int64_t*)args[4] * 2), say(10, *(const int64_t*)args[4] / n(5));
   else if (is("logit_grad_kernel")) say(6, *(const int64_t*)args[4] / n(5) * 2), say(7, *(const int64_t*)args[4] / n(5));
   else if (is("piece_merge_kernel")) say(4, (int64_t)grid.x * 2), say(7, (int64_t)grid.x * 2);
   else if (is("policy_weights_kernel")) say(5, (*(void**)args[3] ? n(4) : 1) * 2);
   else if (is("preference_finish_kernel"))
-    say(5, n(4) * n(6) * 2), say(15, n(4) * 2), say(16, n(8) * 2), say(17, n(4) * 2), say(18, n(4));
+    say(5, n(4) * n(6) * 2), say(13, n(4) * 2), say(14, n(8) * 2), say(15, n(4) * 2), say(16, n(4));
+  else if (is("preference_few_kernel")) say(5, n(4) * n(6) * 2), say(7, n(4)), say(8, n(4) * 2);
   else if (is("policy_finish_kernel"))
     say(5, n(4) * n(6) * 2), say(18, (*(void**)args[7] ? n(8) : 1) * 2), say(19, n(4) * 2), say(20, n(4));
   else if (is("policy_sum_kernel")) say(1, n(0) * 2), say(2, n(0)), say(3, n(0) * 2);

@@ -217,7 +217,10 @@ def test_policy_loss(case, per):
 # more sequences than a workgroup keeps the boundaries of (1024); as many tokens as a
 # workgroup counts by itself (256) and one more; few tokens in many sequences
 MANY = [([1, 0, 2] * 400, 130, 130, F), ([64, 0, 0, 192], 301, 301, B), ([200, 0, 0, 57], 300, 300, F),
-        ([1, 0, 0, 0] * 80, 41, 41, B), ([0, 65, 0, 1] * 3 + [0, 0], 9000, 9000, F)]
+        ([1, 0, 0, 0] * 80, 41, 41, B), ([0, 65, 0, 1] * 3 + [0, 0], 9000, 9000, F),
+        # pairs whose workgroups work out the coefficients, up to 128 tokens and 256 sequences, and past it
+        ([1, 0] * 128, 2500, 2501, B), ([1, 0] * 127 + [0, 0, 1, 0], 2049, 2049, F), ([50, 78], 65536, 65536, B),
+        ([50, 78], 65537, 65537, B), ([100, 28], 1003, 1003, F)]
 
 
 @pytest.mark.parametrize("case", MANY, ids=name)
@@ -358,6 +361,21 @@ def test_gradient_in_the_logits_buffer():
         got = ops.policy_loss(z, tg, cu, ref, ref, ref, kl_coef=0.1, dlogits=z)
         assert got[3] is z and all(torch.equal(a, b) for a, b in zip(got, want))
         assert torch.equal(base[:, 10007:].view(torch.int16), between.view(torch.int16))
+
+
+@pytest.mark.parametrize("ld", [10007, 10012])
+@pytest.mark.parametrize("lens", [[30, 50], [100, 0, 60, 40], [700, 600]], ids=["few", "some", "many"])
+@pytest.mark.parametrize("dtype", [F, B], ids=["f32", "bf16"])
+def test_other_gradients_in_the_logits_buffer(dtype, lens, ld):
+    z, tg, cu = make(lens, 10007, dtype, 12, ld)
+    c = torch.randn(sum(lens), device="cuda")
+    for call in (lambda out: ops.preference_loss(z, tg, cu, dlogits=out),
+                 lambda out: (ops.token_logprobs_backward(z, tg, c, dlogits=out),)):
+        keep = z.clone()
+        want = call(torch.empty_like(z))
+        got = call(z)
+        assert got[-1] is z and all(torch.equal(a, b) for a, b in zip(got, want))
+        z.copy_(keep)
 
 
 def test_gradients_against_differences():
