@@ -202,9 +202,6 @@ def _stream(stream) -> int:
 
 
 # ---------------------------------------------------------------- row operators
-#
-# Each takes stream=, the torch stream (or its raw handle) to run on; None: the current
-# one of its tensors' device.
 
 _CODES = {torch.bfloat16: AXON_BF16, torch.float32: AXON_F32}
 
@@ -259,6 +256,7 @@ def _row_operator(f):
                 t.record_stream(stream)
             with torch.cuda.stream(stream):
                 return f(*args, **kw)
+    call.__doc__ = (f.__doc__ or "") + "\n\n``stream``: the torch stream (or its raw handle) to run on; None: the current one."
     return call
 
 
@@ -415,10 +413,10 @@ def preference_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: lis
                     cu_device: torch.Tensor | None = None):
     """Preference loss over pairs of sequences packed back to back, chosen then
     rejected (axon_preference_loss): cu_seqlens a host list of 2 pairs + 1 prefix sums
-    (cu_device: the same in a device int32 buffer, which saves its copy), ref_logps
-    float32 [2 pairs], each sequence's log-probability under the reference model
-    (None: zeros).  Returns (loss [1], seq_logps [2 pairs], margins [pairs],
-    dlogits or None); ``dlogits`` as in :func:`token_logprobs_backward`."""
+    (cu_device: the same in a device int32 buffer, which saves its copy; a captured
+    call needs it), ref_logps float32 [2 pairs], each sequence's log-probability under
+    the reference model (None: zeros).  Returns (loss [1], seq_logps [2 pairs],
+    margins [pairs], dlogits or None); ``dlogits`` as in :func:`token_logprobs_backward`."""
     pairs = (len(cu_seqlens) - 1) // 2
     if len(cu_seqlens) != 2 * pairs + 1 or pairs < 1:
         raise ValueError("cu_seqlens must have an odd number of entries, at least 3: sequences come in pairs")
