@@ -589,8 +589,8 @@ __global__ void __launch_bounds__(256) preference_few_kernel(
 // of the 2 V; in two passes with a kernel for the coefficients between them 592), float32
 // 811 (1153); 64 rows 17 us (34), one row 15 (14).
 
-// the weights of more than FEW tokens, one launch before the rows: w[0] = 1 / counted tokens, or w[j] = 1 /
-// (sequences with counted tokens x those of sequence j)
+// the weights of more than FEW tokens, one launch before the rows: w[0] = 1 / counted
+// tokens, or w[j] = 1 / (sequences with counted tokens x those of sequence j)
 __global__ void __launch_bounds__(1024) policy_weights_kernel(const int32_t* __restrict__ targets, int tokens, int V,
                                                               const int32_t* __restrict__ cu, int seqs,
                                                               double* __restrict__ w) {
@@ -658,6 +658,34 @@ AXON_DEV double few_tokens_weight(const int32_t* targets, int V, const RowCoef& 
   return 1.0 / ((double)bits_in(mask, rc.cu[j], rc.cu[j + 1]) * (double)n);
 }
 
+AXON_DEV void put_terms(const RowCoef& rc, int64_t t, const PolicyTerms& p, double weight) {
+  rc.logps[t] = p.lp;
+  rc.terms[t] = float2{p.surrogate, p.kl};
+  rc.clipped[t] = p.clipped ? 1.f : 0.f;
+  rc.w[t] = weight;
+}
+
+// the same from the (m, S) of whole rows, a thread a token: the loss alone of more than
+// 2048 tokens, 131072 x 32000 bf16 1.41 ms a call, 4096 x 128256 192 us (1.76 and 202 with
+// policy_finish_kernel, which is two launches less).
+template <typename T>
+__global__ void __launch_bounds__(256) policy_terms_kernel(const T* __restrict__ z, int64_t ld, int V,
+                                                           const int32_t* __restrict__ targets,
+                                                           const float2* __restrict__ stat, RowCoef rc) {
+  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (t >= rc.tokens) return;
+  const int tg = targets[t];
+  PolicyTerms p{};
+  double weight = 0.0;
+  if (tg >= 0 && tg < V) {
+    const float2 st = stat[t];
+    weight = rc.weights[rc.cu ? seq_of_token(rc.cu, rc.seqs, (int)t) : 0];
+    p = policy_token(to_f32(z[t * ld + tg]), st.x, st.y, rc.old[t], rc.adv[t], rc.ref != nullptr,
+                     rc.ref ? rc.ref[t] : 0.f, rc.lo, rc.hi, rc.kl_coef);
+  }
+  put_terms(rc, t, p, weight);
+}
+
 // p + b bytes, b unsigned 32-bit: one register of address beside a uniform p
 template <typename T>
 AXON_DEV const T* at_byte(const T* p, unsigned b) {
@@ -697,11 +725,7 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
   const bool policy = rc.dlogps == nullptr;
   if (!counts) {  // uniform over the workgroup
     zeros();
-    if (policy && i == 0) {
-      rc.logps[t] = rc.clipped[t] = 0.f;
-      rc.terms[t] = float2{0.f, 0.f};
-      rc.w[t] = 0.0;
-    }
+    if (policy && i == 0) put_terms(rc, t, PolicyTerms{}, 0.0);
     return;
   }
   const float zt = to_f32(row[tg]), given = policy ? rc.old[t] : rc.dlogps[t];
@@ -750,10 +774,7 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
     if (i == 0) {
       const PolicyTerms p = policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef);
       coef = (float)weight * p.c;
-      rc.logps[t] = p.lp;
-      rc.terms[t] = float2{p.surrogate, p.kl};
-      rc.clipped[t] = p.clipped ? 1.f : 0.f;
-      rc.w[t] = weight;
+      put_terms(rc, t, p, weight);
     }
     __syncthreads();
     w = coef;
@@ -979,22 +1000,23 @@ template <typename T>
 void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
   LossWs w;
   carve(r.tokens, r.V, a.seqs, (char*)wsp, &w);
-  if (r.dz && r.tokens > 0) {
-    const bool few = r.tokens <= FEW;
-    if (!few) policy_weights_kernel<<<1, 1024, 0, s>>>(r.targets, (int)r.tokens, r.V, a.cu, a.seqs, w.seq);
-    run_rows<T>(r,
-                RowCoef{nullptr, a.cu, a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, few ? nullptr : w.seq,
-                        (int)r.tokens, a.logps, w.stat, w.coef, w.lps},
-                s);
-    policy_sum_kernel<<<1, 1024, 0, s>>>((int)r.tokens, w.stat, w.coef, w.lps, a.kl_coef, a.ref != nullptr, a.loss,
-                                         a.stats);
+  const bool grad = r.dz && r.tokens > 0, few = grad && r.tokens <= FEW;
+  const int tokens = (int)r.tokens;
+  int slices = 1;  // (of more than 2048 tokens always 1, see part_shape)
+  if (!grad && tokens > 0) slices = run_parts<T>(r, w.part, nullptr, nullptr, nullptr, s);
+  if (!grad && (tokens <= 2048 || slices > 1)) {
+    policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, tokens, w.part, slices, a.cu,
+                                               a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
+                                               a.logps, w.seq, nullptr, nullptr);
     return;
   }
-  // the loss alone
-  const int slices = r.tokens > 0 ? run_parts<T>(r, w.part, nullptr, nullptr, nullptr, s) : 1;
-  policy_finish_kernel<T><<<1, 1024, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, (int)r.tokens, w.part, slices, a.cu,
-                                             a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, a.loss, a.stats,
-                                             a.logps, w.seq, nullptr, nullptr);
+  const RowCoef rc{nullptr, a.cu, a.seqs, a.old, a.ref, a.adv, a.lo, a.hi, a.kl_coef, few ? nullptr : w.seq,
+                   tokens, a.logps, w.stat, w.coef, w.lps};
+  if (!few) policy_weights_kernel<<<1, 1024, 0, s>>>(r.targets, tokens, r.V, a.cu, a.seqs, w.seq);
+  if (grad) run_rows<T>(r, rc, s);
+  else
+    policy_terms_kernel<T><<<(tokens + 255) / 256, 256, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, w.part, rc);
+  policy_sum_kernel<<<1, 1024, 0, s>>>(tokens, w.stat, w.coef, w.lps, a.kl_coef, a.ref != nullptr, a.loss, a.stats);
 }
 
 }  // namespace

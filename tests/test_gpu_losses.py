@@ -212,6 +212,12 @@ def test_policy_loss(case, per):
         check(got[1], stats, dstats + tol, "stats")
         check(got[2], r.lp, r.E * U + U * r.lp.abs(), "logps")
         check(got[3], r.grad(c), r.grad_bound(c, dc + 4 * U * c.abs(), HALF[dtype]), "dlogits")
+        only = ops.policy_loss(z, tg, cu, old, adv, rf, clip_low=0.2, clip_high=0.3, kl_coef=kl, per_sequence=per,
+                               want_grad=False)
+        assert only[3] is None
+        check(only[0], loss.view(1), (dloss + tol).view(1), "loss alone")
+        check(only[1], stats, dstats + tol, "stats alone")
+        check(only[2], r.lp, r.E * U + U * r.lp.abs(), "logps alone")
 
 
 # more sequences than a workgroup keeps the boundaries of (1024); as many tokens as a
