@@ -48,23 +48,14 @@ AXON_DEV float one_exp(float v) { return v == -INFINITY ? 0.f : v - v + 1.f; }  
 AXON_DEV int odd_head(const float*) { return 0; }
 AXON_DEV int odd_head(const bf16* row) { return (int)((uintptr_t)row >> 1 & 1); }
 
-// exp(v - m) for many v <= m as 2^(v log2 e - m log2 e): one fused multiply-add and the
-// hardware exponential.  m log2 e is rounded, which scales every result by the same
-// 2^d; ``fix`` = 2^-d undoes it once, on the sum.  Where m log2 e might overflow (rows
-// or slices of nothing but the type's lowest values), neighbouring values lie so far
-// apart that only v = m gives more than 0: then any power of two serves as the factor,
-// and the product is exact.
+// exp(v - m) for many v <= m as 2^((v - m) log2 e).  The difference comes first: of equal
+// values it is 0 and the power 1, and its rounding grows with |v - m| alone.  (One
+// operation less, 2^(v log2 e - m log2 e) with a rounded m log2 e, is off by that
+// rounding, which grows with |m| and overflows the power.)
 struct ExpFrom {
-  static constexpr float L = 1.4426950408889634f;
-  float m, scale, base, fix;
-  AXON_DEV explicit ExpFrom(float top) {
-    m = top == -INFINITY ? 0.f : top;  // -inf - (-inf) is not a number
-    const bool low = m < -2e38f;
-    scale = low ? 0.0625f : L;
-    base = m * scale;
-    fix = low ? 1.f : 1.f - fmaf(m, L, -base) * 0.6931471805599453f;
-  }
-  AXON_DEV float operator()(float v) const { return __builtin_amdgcn_exp2f(fmaf(v, scale, -base)); }
+  float m;
+  AXON_DEV explicit ExpFrom(float top) : m(top == -INFINITY ? 0.f : top) {}  // -inf - (-inf) is not a number
+  AXON_DEV float operator()(float v) const { return __builtin_amdgcn_exp2f((v - m) * 1.4426950408889634f); }
 };
 
 // N groups of 8 logits into a thread's (m, s)
@@ -81,7 +72,7 @@ AXON_DEV void take_runs(float& m, float& s, const float (&v)[N][8]) {
   for (int k = 0; k < N; ++k)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum += e(v[k][j]);
-  s = s * __expf(m - (top == -INFINITY ? 0.f : top)) + sum * e.fix;
+  s = s * __expf(m - e.m) + sum;
   m = top;
 }
 
@@ -507,7 +498,7 @@ AXON_DEV void grad_slice(const T* row, int V, int tg, int first, float w, float2
   constexpr int STRIDE = 256 * 8;
   const int c0 = first + threadIdx.x * 8;
   const ExpFrom e(st.x);
-  const float f = -w / st.y * e.fix;
+  const float f = -w / st.y;
   const int h = odd_head(row), n = V - h;
   tg -= h;
   row += h;
@@ -785,7 +776,7 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
     return;
   }
   const ExpFrom e(m);
-  const float f = -w / s * e.fix;
+  const float f = -w / s;
   auto grad = [&](const Run8<T>& q, TO* to) {
     float v[8];
 #pragma unroll
