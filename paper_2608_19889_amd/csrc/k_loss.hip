@@ -301,6 +301,19 @@ __global__ void __launch_bounds__(1024) preference_finish_kernel(
   }
 }
 
+// exp(x) - x - 1, from e = exp(x) - 1.  The difference of the two cancels as x does (a
+// policy that has hardly moved from its reference), so up to 1/2 it is the series
+// x^2 (1/2! + x/3! + .. + x^8/10!), whose rest is below 2^-31 of it.
+AXON_DEV float kl_term(float x, float e) {
+  if (!(fabsf(x) < 0.5f)) return x == INFINITY ? x : e - x;
+  float s = 2.75573192e-7f;
+  const float over[8] = {2.75573192e-6f, 2.48015873e-5f, 1.98412698e-4f, 1.38888889e-3f,
+                         8.33333333e-3f, 4.16666667e-2f, 1.66666667e-1f, 0.5f};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s = fmaf(s, x, over[i]);
+  return x * x * s;
+}
+
 struct PolicyTerms {
   float lp, c;  // log-probability; dloss / dlp of weight 1
   float surrogate, kl;
@@ -335,7 +348,7 @@ AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A,
   if (has_ref) {
     float er = -low;
     const float g = sum(ref, -lp, er), x = fabsf(g) < INFINITY ? g + er : g, dkl = -expm1f(x);
-    p.kl = -dkl - x;
+    p.kl = kl_term(x, -dkl);
     p.c += kl_coef * dkl;
   }
   return p;

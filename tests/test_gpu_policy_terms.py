@@ -1,0 +1,50 @@
+"""The policy loss's and the preference loss's terms on the GPU where they cancel,
+vanish or are infinite, against float64.
+
+u = 2^-24.  With a vocabulary of one, or one logit over -infinity, a row's sum of
+exponentials is 1 and its log-probability exactly z - m, so nothing but the terms'
+own arithmetic is off:
+  * the KL term k(x) = exp(x) - x - 1: below |x| = 1/2 a series of positive weight,
+    5 u of itself; from there a difference whose exp(x) - 1 is within an ulp, 2 u |exp(x)
+    - 1| / k(x) <= 8.7 u (at 1/2) and its own rounding;
+  * the weighted sum is float64, each result rounded once: 12 u of the mean KL term.
+"""
+import math
+
+import pytest
+import torch
+
+import paper_2608_19889_amd as ops
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+F = torch.float32
+INF = float("inf")
+# tokens: coefficients by each row's workgroup, by a launch before the rows, and a loss
+# alone of more than 2048 tokens
+COUNTS = [1, 40, 300, 3000]
+
+
+def one_logit(n, vocab=1):
+    """(logits, targets) of n rows whose targets have log-probability 0."""
+    z = torch.full((n, vocab), -INF, device="cuda")
+    z[:, 0] = torch.randn(n, device="cuda")
+    return z, torch.zeros(n, dtype=torch.int32, device="cuda")
+
+
+@pytest.mark.parametrize("size", [1e-7, 1e-5, 1e-3, 0.05, 0.45, 0.55, 3.0, 40.0])
+@pytest.mark.parametrize("sign", [-1, 1])
+@pytest.mark.parametrize("n", COUNTS)
+def test_kl_term_of_any_size(n, sign, size):
+    z, tg = one_logit(n)
+    ref = sign * size * (0.9 + 0.2 * torch.rand(n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)))
+    zero = torch.zeros(n, device="cuda")
+    x = ref.double()
+    # float64: the series where expm1(x) - x would cancel
+    want = torch.where(x.abs() < 0.1, sum(x ** k / math.factorial(k) for k in range(2, 14)), torch.expm1(x) - x).mean()
+    for grad in (True, False):
+        for per in (False, True):
+            loss, stats, _, _ = ops.policy_loss(z, tg, [0, n], zero, zero, ref, kl_coef=1.0, per_sequence=per,
+                                                want_grad=grad)
+            assert abs(float(stats[1]) - float(want)) <= 12 * U * float(want), (float(stats[1]), float(want))
+            assert float(loss) == float(stats[1])
