@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
         if (slices > 1) st[u] = join_slices(part, t, slices);
         w = 1.0 / (cu ? n * weights[seq.of(held, t)] : n);
         p = policy_token(zt[u], st[u].x, st[u].y, o[u], a[u], ref != nullptr, rf[u], lo, hi, kl_coef);
-        sum[0] += w * (double)(p.surrogate + (ref ? kl_coef * p.kl : 0.f));
+        sum[0] += w * ((double)p.surrogate + (ref ? (double)kl_coef * p.kl : 0.0));
         sum[1] += w * (double)p.surrogate;
         sum[2] += w * (double)p.kl;
         sum[3] += p.clipped ? w : 0.0;
@@ -455,7 +455,7 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
       logps[t] = p.lp;
       if (coef) {
         stat[t] = st[u];
-        coef[t] = (float)w * p.c;
+        coef[t] = (float)(w * p.c);
       }
     }
   }
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(1024) policy_sum_kernel(int tokens, const floa
   for (int t = threadIdx.x; t < tokens; t += 1024) {
     const float2 p = terms[t];
     const double v = w[t];
-    sum[0] += v * (double)(p.x + (has_ref ? kl_coef * p.y : 0.f));
+    sum[0] += v * ((double)p.x + (has_ref ? (double)kl_coef * p.y : 0.0));
     sum[1] += v * (double)p.x;
     sum[2] += v * (double)p.y;
     sum[3] += v * (double)clipped[t];
@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
   if (policy) {
     if (i == 0) {
       const PolicyTerms p = policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef);
-      coef = (float)weight * p.c;
+      coef = (float)(weight * p.c);
       put_terms(rc, t, p, weight);
     }
     __syncthreads();

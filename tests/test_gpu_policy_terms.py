@@ -48,3 +48,20 @@ def test_kl_term_of_any_size(n, sign, size):
                                                 want_grad=grad)
             assert abs(float(stats[1]) - float(want)) <= 12 * U * float(want), (float(stats[1]), float(want))
             assert float(loss) == float(stats[1])
+
+
+@pytest.mark.parametrize("n", [2, 40, 300, 3000])
+def test_loss_of_advantages_that_cancel(n):
+    """Normalized advantages of a policy that has not moved: the first terms are 1 and -1
+    and sum to nothing, and the loss is what the KL term leaves, kl_coef times its mean.
+    kl_coef is exact; 12 u as above, of values that differ by a factor of 1.2 at most."""
+    z, tg = one_logit(n)
+    zero = torch.zeros(n, device="cuda")
+    adv = torch.ones(n, device="cuda")
+    adv[1::2] = -1
+    ref = -1e-3 * (1 + 0.1 * torch.rand(n, device="cuda", generator=torch.Generator("cuda").manual_seed(n)))
+    for grad in (True, False):
+        loss, stats, _, _ = ops.policy_loss(z, tg, [0, n], zero, adv, ref, kl_coef=0.125, want_grad=grad)
+        assert float(stats[0]) == 0 and float(stats[1]) > 4e-7
+        # the first terms' sum: n terms of 1 / n, exact but for float64
+        assert abs(float(loss) - 0.125 * float(stats[1])) <= 2 * U * float(loss) + n * 2.0 ** -53
