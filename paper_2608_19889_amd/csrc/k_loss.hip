@@ -349,7 +349,7 @@ AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A,
     float er = -low;
     const float g = sum(ref, -lp, er), x = fabsf(g) < INFINITY ? g + er : g, dkl = -expm1f(x);
     p.kl = kl_term(x, -dkl);
-    p.c += kl_coef * dkl;
+    if (kl_coef > 0.f) p.c += kl_coef * dkl;  // kl_coef = 0: no term, also where it is infinite
   }
   return p;
 }
@@ -447,7 +447,7 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
         if (slices > 1) st[u] = join_slices(part, t, slices);
         w = 1.0 / (cu ? n * weights[seq.of(held, t)] : n);
         p = policy_token(zt[u], st[u].x, st[u].y, o[u], a[u], ref != nullptr, rf[u], lo, hi, kl_coef);
-        sum[0] += w * ((double)p.surrogate + (ref ? (double)kl_coef * p.kl : 0.0));
+        sum[0] += w * ((double)p.surrogate + (kl_coef > 0.f ? (double)kl_coef * p.kl : 0.0));
         sum[1] += w * (double)p.surrogate;
         sum[2] += w * (double)p.kl;
         sum[3] += p.clipped ? w : 0.0;
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(1024) policy_finish_kernel(
 // the same sums from the terms that the rows' own pass left (see RowCoef)
 __global__ void __launch_bounds__(1024) policy_sum_kernel(int tokens, const float2* __restrict__ terms,
                                                           const float* __restrict__ clipped,
-                                                          const double* __restrict__ w, float kl_coef, bool has_ref,
+                                                          const double* __restrict__ w, float kl_coef,
                                                           float* __restrict__ loss, float* __restrict__ stats) {
   __shared__ double red[4][16];
   double sum[4] = {};
@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(1024) policy_sum_kernel(int tokens, const floa
   for (int t = threadIdx.x; t < tokens; t += 1024) {
     const float2 p = terms[t];
     const double v = w[t];
-    sum[0] += v * ((double)p.x + (has_ref ? (double)kl_coef * p.y : 0.0));
+    sum[0] += v * ((double)p.x + (kl_coef > 0.f ? (double)kl_coef * p.y : 0.0));
     sum[1] += v * (double)p.x;
     sum[2] += v * (double)p.y;
     sum[3] += v * (double)clipped[t];
@@ -1020,7 +1020,7 @@ void policy(const LogitRows& r, const PolicyArgs& a, void* wsp, hipStream_t s) {
   if (grad) run_rows<T>(r, rc, s);
   else
     policy_terms_kernel<T><<<(tokens + 255) / 256, 256, 0, s>>>((const T*)r.z, r.ld, r.V, r.targets, w.part, rc);
-  policy_sum_kernel<<<1, 1024, 0, s>>>(tokens, w.stat, w.coef, w.lps, a.kl_coef, a.ref != nullptr, a.loss, a.stats);
+  policy_sum_kernel<<<1, 1024, 0, s>>>(tokens, w.stat, w.coef, w.lps, a.kl_coef, a.loss, a.stats);
 }
 
 }  // namespace

@@ -65,3 +65,23 @@ def test_loss_of_advantages_that_cancel(n):
         assert float(stats[0]) == 0 and float(stats[1]) > 4e-7
         # the first terms' sum: n terms of 1 / n, exact but for float64
         assert abs(float(loss) - 0.125 * float(stats[1])) <= 2 * U * float(loss) + n * 2.0 ** -53
+
+
+@pytest.mark.parametrize("n", [4, 300, 3000])
+def test_no_kl_coefficient_no_kl_term(n):
+    """kl_coef = 0 with a reference: its mean is reported, the loss and the gradient have
+    no second term, also where it is infinite (a token that the policy has ruled out)."""
+    g = torch.Generator("cuda").manual_seed(n)
+    z = torch.randn((n, 50), generator=g, device="cuda")
+    tg = torch.randint(0, 50, (n,), generator=g, device="cuda", dtype=torch.int32)
+    z[1, int(tg[1])] = -INF
+    lp = ops.token_logprobs(z, tg)
+    adv = torch.randn(n, generator=g, device="cuda")
+    old = torch.where(torch.isfinite(lp), lp, -5.0)
+    ref = torch.full((n,), -3.0, device="cuda")
+    for grad in (True, False):
+        want = ops.policy_loss(z, tg, [0, n], old, adv, want_grad=grad)
+        got = ops.policy_loss(z, tg, [0, n], old, adv, ref, kl_coef=0.0, want_grad=grad)
+        assert bool(torch.isfinite(got[0]).all()) and torch.equal(got[0], want[0])
+        assert float(got[1][1]) == INF and torch.equal(got[1][::2], want[1][::2])
+        assert not grad or (bool(torch.isfinite(got[3]).all()) and torch.equal(got[3], want[3]))
