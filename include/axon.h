@@ -373,9 +373,9 @@ int axon_token_logprobs_backward(int64_t tokens, int32_t vocab, const void* logi
  * model (d_ref_logps, float [2 pairs], or NULL: zeros),
  *   margin_i = beta ((s_2i - ref_2i) - (s_2i+1 - ref_2i+1)),
  *   loss = mean over i of -(1 - e) log sigmoid(margin_i) - e log sigmoid(-margin_i),
- * beta > 0, e = label_smoothing in [0, 0.5).  Writes d_loss [1], d_seq_logps
- * [2 pairs], d_margins [pairs] (float) and the loss's gradient (dlogits; NULL: not
- * computed). */
+ * beta > 0, e = label_smoothing in [0, 0.5) (with e == 0 no second term).  Writes
+ * d_loss [1], d_seq_logps [2 pairs], d_margins [pairs] (float) and the loss's gradient
+ * (dlogits; NULL: not computed). */
 int axon_preference_loss(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
                          const int32_t* d_targets, int32_t pairs, const int32_t* d_cu_seqlens,
                          const int32_t* h_cu_seqlens, const float* d_ref_logps, float beta, float label_smoothing,

@@ -260,7 +260,7 @@ AXON_DEV void pair_coefs(const double* lps, int tokens, const int32_t* cu, int s
     }
     const double u = (double)beta * (r0 - r1), e = (double)smoothing;
     if (write) out.margins[i] = (float)u;
-    total[0] += (1.0 - e) * softplus_f64(-u) + e * softplus_f64(u);
+    total[0] += (1.0 - e) * softplus_f64(-u) + (e > 0.0 ? e * softplus_f64(u) : 0.0);  // (u may be infinite)
     const double yes = 1.0 / (1.0 + exp(-u)), no = 1.0 / (1.0 + exp(u));
     const double d = (double)beta / pairs * (e * yes - (1.0 - e) * no);
     sums[2 * i] = d;

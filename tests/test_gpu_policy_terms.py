@@ -85,3 +85,25 @@ def test_no_kl_coefficient_no_kl_term(n):
         assert bool(torch.isfinite(got[0]).all()) and torch.equal(got[0], want[0])
         assert float(got[1][1]) == INF and torch.equal(got[1][::2], want[1][::2])
         assert not grad or (bool(torch.isfinite(got[3]).all()) and torch.equal(got[3], want[3]))
+
+
+@pytest.mark.parametrize("n", [10, 1200])
+def test_no_smoothing_no_swapped_term(n):
+    """A rejected answer that the policy has ruled out (log-probability -infinity): the
+    margin is infinite, its pair's loss and gradient 0 without label smoothing, the loss
+    infinite with it."""
+    g = torch.Generator("cuda").manual_seed(n)
+    z = torch.randn((n, 50), generator=g, device="cuda")
+    tg = torch.randint(0, 50, (n,), generator=g, device="cuda", dtype=torch.int32)
+    cu = [0, n // 5, n // 2, n - 3, n]
+    first = ops.preference_loss(z[n // 2:], tg[n // 2:], [0, n - 3 - n // 2, n - n // 2])
+    z[n // 2 - 1, int(tg[n // 2 - 1])] = -INF
+    for grad in (True, False):
+        loss, s, u, dz = ops.preference_loss(z, tg, cu, want_grad=grad)
+        assert float(s[1]) == -INF and float(u[0]) == INF
+        assert abs(float(loss) - float(first[0]) / 2) <= 4 * U * float(first[0])
+        if grad:
+            assert not dz[:n // 2].any()
+            # the other pair's: half of what it has alone, both rounded
+            assert float((dz[n // 2:] - first[3] / 2).abs().max()) <= 8 * U * float(first[3].abs().max())
+    assert float(ops.preference_loss(z, tg, cu, label_smoothing=0.1)[0]) == INF
