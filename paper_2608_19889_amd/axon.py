@@ -227,7 +227,7 @@ def _row_operator(f):
     be ready on this one; they are kept from reuse until its work is done."""
     @functools.wraps(f)
     def call(*args, stream=None, **kw):
-        first = None
+        first, maps = None, []
         for t in (*args, *kw.values()):
             if isinstance(t, torch.Tensor):
                 if first is None:
@@ -237,11 +237,12 @@ def _row_operator(f):
                 elif t.get_device() != at:
                     raise ValueError(f"{f.__name__}: tensors on {first.device} and {t.device} in one call")
             elif isinstance(t, dict):
-                for g in t.values():
-                    if first is None or g.get_device() != at:
-                        raise ValueError(f"{f.__name__}: a gradient buffer on {g.device}")
+                maps.append(t)
         if first is None:
             raise ValueError(f"{f.__name__} takes tensors on the GPU")
+        for g in _tensors(maps):
+            if g.get_device() != at:
+                raise ValueError(f"{f.__name__}: a gradient buffer on {g.device}")
         if stream is None and at == torch.cuda.current_device():
             return f(*args, **kw)
         device = first.device
