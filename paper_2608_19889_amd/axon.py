@@ -257,7 +257,10 @@ def _row_operator(f):
                 t.record_stream(stream)
             with torch.cuda.stream(stream):
                 return f(*args, **kw)
-    call.__doc__ = (f.__doc__ or "") + "\n\n``stream``: the torch stream (or its raw handle) to run on; None: the current one."
+    call.__doc__ = (f.__doc__ or "") + """
+
+    ``stream``: the torch stream (or its raw handle) to run on; None: the current one.
+    Not recorded by autograd: the results have no history, whatever the inputs require."""
     return call
 
 
@@ -310,6 +313,7 @@ def _like(out, x: torch.Tensor, dtype, name: str) -> torch.Tensor:
         return torch.empty_like(x, dtype=dtype, memory_format=torch.contiguous_format)
     if out.shape != x.shape or (dtype is not None and out.dtype != dtype):
         raise ValueError(f"{name} must be {tuple(x.shape)} {dtype or ''}, got {tuple(out.shape)} {out.dtype}")
+    torch.autograd.graph.increment_version(out)  # (written through a pointer, which autograd does not see)
     return out
 
 
