@@ -480,6 +480,7 @@ class Model:
                                      ctypes.byref(handle)))
         del keep
         self._h = handle
+        self.device = torch.device("cuda", torch.cuda.current_device())
 
     # ---- calls
     def prefill(self, tokens: torch.Tensor, cu_seqlens: list, block_table: torch.Tensor | None = None,
@@ -527,6 +528,10 @@ class Model:
         self._keep = (cu_d, tokens, targets, keep)
         return loss
 
+    def _check_device(self, tokens):
+        if tokens.device != self.device:
+            raise ValueError(f"tensors on {tokens.device}, the model on {self.device}")
+
     def _train_args(self, tokens, cu_seqlens, targets, grads):
         """The C arguments up to the targets, those of the gradients, and what has to
         live until the step has run."""
@@ -552,6 +557,7 @@ class Model:
         B = len(cu_seqlens) - 1
         if B < 2 or B % 2:
             raise ValueError("sequences come in pairs, chosen then rejected")
+        self._check_device(tokens)
         args, gargs, keep = self._train_args(tokens, cu_seqlens, targets, grads)
         ref_logps = _vector(ref_logps, B, torch.float32, "ref_logps")
         out = torch.empty((1 + B + B // 2,), dtype=torch.float32, device=tokens.device)
@@ -569,6 +575,7 @@ class Model:
         """A training step with the clipped policy loss (axon_policy_loss_and_grads):
         tokens, targets and grads as in :meth:`loss_and_grads`, the loss as
         :func:`policy_loss`.  Returns (loss [1], stats [3], logps [tokens])."""
+        self._check_device(tokens)
         args, gargs, keep = self._train_args(tokens, cu_seqlens, targets, grads)
         T = int(cu_seqlens[-1])
         old_logps, advantages, ref_logps = (_vector(t, T, torch.float32, n) for t, n in (
