@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(1024) colsum_final_kernel(const float* __restr
   for (int i = 0; i < 16; ++i) s += sums[i][lane];
   if (c < c1) d0[c] = s;
   else if (c < c2) d1[c - c1] = s;
-  else if (d2) d2[c - c2] = s;
+  else d2[c - c2] = s;
 }
 
 // ---------------------------------------------------------------- attention
@@ -778,7 +778,7 @@ void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t
 // at most ROW_PARTS partials
 static int row_chunk(int T) { return (T + ROW_PARTS - 1) / ROW_PARTS; }
 
-void launch_colsum_final(const float* part, int n, int C, float* d0, int c1, float* d1, int c2, float* d2,
+static void colsum_final(const float* part, int n, int C, float* d0, int c1, float* d1, int c2, float* d2,
                          hipStream_t s) {
   colsum_final_kernel<<<(C + 63) / 64, 1024, 0, s>>>(part, n, C, d0, c1, d1, c2, d2);
 }
@@ -799,7 +799,7 @@ void launch_norm_bwd(const float* x, const bf16* g, const float* dy, int np, int
     else if (D <= 4096) go(norm_bwd_kernel<4>);
     else go(norm_bwd_kernel<8>);
   }
-  launch_colsum_final(part, n, D, dg, D, nullptr, D, nullptr, s);
+  colsum_final(part, n, D, dg, D, nullptr, D, nullptr, s);
 }
 
 void launch_attn_bwd(const bf16* q, KVView kv, const bf16* o, const float* dof, int np, int64_t stride, bf16* dob,
@@ -828,7 +828,7 @@ void launch_rope_bwd(const float* dq, const float* dkh, const float* dvh, const 
   const int nq = (H + 2 * KVh) * hd, rows = row_chunk(T), n = (T + rows - 1) / rows;
   rope_bwd_kernel<<<dim3((nq / 8 + 127) / 128, n), 128, 0, s>>>(dq, dkh, dvh, cos_t, sin_t, cu, nseq, T, H, KVh, hd,
                                                                dqkv, dbq ? bpart : nullptr, rows, plain);
-  if (dbq) launch_colsum_final(bpart, n, nq, dbq, H * hd, dbk, (H + KVh) * hd, dbv, s);
+  if (dbq) colsum_final(bpart, n, nq, dbq, H * hd, dbk, (H + KVh) * hd, dbv, s);
 }
 
 void launch_embed_bwd(const int32_t* tok, const float* dx, int T, int D, int V, float* dE, bool clear, hipStream_t s) {
@@ -847,7 +847,7 @@ void launch_gelu_bwd(const float* z, const float* da, int np, int64_t stride, in
   if (T <= 0) return;
   const int rows = row_chunk(T), n = (T + rows - 1) / rows;
   gelu_bwd_kernel<<<dim3((I / 8 + 127) / 128, n), 128, 0, s>>>(z, da, np, stride, T, I, dz, part, rows);
-  launch_colsum_final(part, n, I, dbias, I, nullptr, I, nullptr, s);
+  colsum_final(part, n, I, dbias, I, nullptr, I, nullptr, s);
 }
 
 void launch_position_bwd(const float* dx, const int32_t* cu, int nseq, int D, int P, float* dP, hipStream_t s) {

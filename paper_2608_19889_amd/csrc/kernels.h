@@ -211,10 +211,6 @@ void launch_untile_transpose(const bf16* W, int64_t N, int K, bf16* dst, int64_t
 constexpr int ROW_PARTS = 512, NORM_BWD_COLS = 8192;
 void launch_norm_bwd(const float* x, const bf16* g, const float* dy, int np, int64_t stride, int T, int D, float eps,
                      float* dx, int accumulate, bf16* dxb, float* dg, float* part, float* dgrow, hipStream_t s);
-// d0 / d1 / d2 = the column sums of part [n][C], n >= 1, in a fixed order: columns
-// below c1 go to d0, below c2 to d1, the rest to d2 (a null one is not written)
-void launch_colsum_final(const float* part, int n, int C, float* d0, int c1, float* d1, int c2, float* d2,
-                         hipStream_t s);
 // attention backward over nseq fresh sequences in slots 0.. (contiguous cache):
 // dq [T][H][hd] and each query head's share of dk / dv, dkh / dvh [T][H][hd]
 // (float), from q [T][H][hd] and o (row-pair layout) bf16, the gradient of o as
