@@ -775,13 +775,14 @@ __global__ void __launch_bounds__(THREADS) logit_row_kernel(const T* z, int64_t 
   s = over_waves<NW>(p.y * __expf(p.x - (m == -INFINITY ? 0.f : m)), [](float a, float b) { return a + b; });
   float w = given;
   if (policy) {
+    PolicyTerms p{};
     if (i == 0) {
-      const PolicyTerms p = policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef);
+      p = policy_token(zt, m, s, given, adv, rc.ref != nullptr, ref, rc.lo, rc.hi, rc.kl_coef);
       coef = (float)(weight * p.c);
-      put_terms(rc, t, p, weight);
     }
     __syncthreads();
     w = coef;
+    if (i == 0) put_terms(rc, t, p, weight);
   }
   // a coefficient of 0 (clipped): zeros, whatever the row holds
   if (w == 0.f) {
