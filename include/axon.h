@@ -328,8 +328,8 @@ int axon_policy_loss_and_grads(axon_model* m, int32_t batch, const int32_t* d_to
 /* Layer norm of ``rows`` >= 0 rows of 1 <= cols <= 16384 columns, the normalization
  * of the GPT-2 definition (Technical Supplement, "A Complete Model Definition"):
  *   y = (x - mean) / sqrt(variance + eps) * gain + bias,
- * mean and biased variance of the row; gain and bias [cols] of param_dtype, bias may
- * be NULL (none).  y may be x (same dtype and stride). */
+ * mean and biased variance of the row, eps > 0; gain and bias [cols] of param_dtype,
+ * bias may be NULL (none).  y may be x (same dtype and stride). */
 int axon_layernorm(int64_t rows, int32_t cols, const void* x, int32_t x_dtype, int64_t ldx, const void* gain,
                    const void* bias, int32_t param_dtype, float eps, void* y, int32_t y_dtype, int64_t ldy,
                    void* stream);

@@ -126,7 +126,8 @@ void launch_layernorm(const float* x, const bf16* g, const bf16* beta, bf16* h, 
 //
 // A row's sums cost one exchange between its wavefronts: each takes the mean of its
 // own columns first and its sums around that, and the joined ones follow from the
-// wavefronts' (n_w columns, mean m_w, sum of squares Q_w around m_w):
+// wavefronts' (n_w columns, mean m_w, sum of squares Q_w around m_w; Chan, Golub and
+// LeVeque's updating formula):
 //   mean = sum n_w m_w / n,  Q = sum Q_w + n_w (m_w - mean)^2,
 // so nothing is lost to a common offset of the row, as a sum of x^2 would lose it.
 

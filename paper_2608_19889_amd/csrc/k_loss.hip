@@ -6,16 +6,22 @@
 // S = sum_v exp(z_v - m); a target outside [0, V) makes the row not count: lp = 0,
 // nothing of the row is read and its gradient is zero.  A loss is a function of the
 // lp, so its gradient is dz_v = c ([v = y] - p_v) with c = dloss / dlp and p_v =
-// exp(z_v - m) / S.  Everything but the passes over the logits is a few operations
-// per token, done by one workgroup, the sums in float64 (a sequence's cancels against
-// the reference's).
+// exp(z_v - m) / S.  S is a float32 sum of float32 exponentials.  What follows is a few
+// operations per token: log-probabilities are joined and sums over tokens added in
+// float64 (a sequence's cancels against the reference's); a policy token's own terms are
+// float32 (see policy_token).
 //
-//   logit_part_kernel   reads the rows: (m, S) of every slice of a row
-//   *_finish_kernel     joins a row's slices; loss, statistics, c of every token
-//                       (preference_few_kernel: with the gradient, for few tokens)
-//   logit_grad_kernel   reads the rows again and writes the gradient
-//   logit_row_kernel    all of it in one pass, where c depends on the row alone; then
-//   policy_sum_kernel   adds up the loss's terms
+//   logit_part_kernel       reads the rows: (m, S) of every slice of a row
+//   *_finish_kernel         one workgroup joins the rows' slices; loss, statistics, c of
+//                           every token (the policy's: the loss alone, and in a step)
+//   preference_few_kernel   the same and the gradient, for few tokens, by every workgroup
+//   logit_grad_kernel       reads the rows again and writes the gradient
+// where c depends on the row alone (the policy loss, a caller's own):
+//   policy_weights_kernel   the tokens' weights (of few tokens: by each row's workgroup)
+//   logit_row_kernel        a row's (m, S), terms, c and gradient in one pass
+//   policy_terms_kernel     the terms from logit_part_kernel's (m, S): many tokens' loss
+//                           alone
+//   policy_sum_kernel       adds up the loss's terms
 //
 // All are HBM bound (V 4 or 2 bytes a row against a few exponentials).  No atomics:
 // every sum has one order.
@@ -321,9 +327,9 @@ struct PolicyTerms {
 };
 // one token (see policy_finish_kernel), from its logit and its row's (m, S), in float32:
 // where one workgroup does a batch's tokens, float64 exponentials took longer than
-// everything else there.  The log-probability's three terms and the other policy's are added with
-// their rounding errors kept, so the ratio is off by the last digits of S and of two
-// logarithms.
+// everything else there.  The log-probability's three terms and the other policy's are
+// added with their rounding errors kept (Knuth's two-sum), so the ratio is off by the
+// last digits of S and of two logarithms, and by its own exponential's.
 AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A, bool has_ref, float ref, float lo,
                                   float hi, float kl_coef) {
   auto sum = [](float a, float b, float& low) {  // a + b, its rounding error added to low
