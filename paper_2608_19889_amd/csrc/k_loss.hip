@@ -329,7 +329,7 @@ struct PolicyTerms {
 // where one workgroup does a batch's tokens, float64 exponentials took longer than
 // everything else there.  The log-probability's three terms and the other policy's are
 // added with their rounding errors kept (Knuth's two-sum), so the ratio is off by the
-// last digits of S and of two logarithms, and by its own exponential's.
+// last digits of S and of a logarithm below 1/2, and by its own exponential's.
 AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A, bool has_ref, float ref, float lo,
                                   float hi, float kl_coef) {
   auto sum = [](float a, float b, float& low) {  // a + b, its rounding error added to low
@@ -338,8 +338,13 @@ AXON_DEV PolicyTerms policy_token(float z, float m, float s, float old, float A,
     return r;
   };
   PolicyTerms p;
-  float low = 0.f;
-  const float lp = sum(sum(z, -m, low), -logf(s), low);
+  // log s = k log 2 + log f, s = 2^k f, f within a factor of root 2 of 1 (Cody and Waite's
+  // split: k times the first 16 bits of log 2 is exact, k times the rest goes to low): log
+  // f is small, and so is its rounding, where log s as one float is off by up to 5e-7
+  const float k = (float)__builtin_amdgcn_frexp_expf(s * 0.70710678f);
+  float low = k * -1.42860682e-6f;
+  const float f = __builtin_amdgcn_ldexpf(s, (int)-k);
+  const float lp = sum(sum(sum(z, -m, low), k * -0.693145752f, low), -logf(f), low);
   p.lp = fabsf(lp) < INFINITY ? lp + low : lp;  // (an infinite sum's error is not a number)
   float el = low;
   const float d = sum(lp, -old, el), e = expf(d);

@@ -107,3 +107,26 @@ def test_no_smoothing_no_swapped_term(n):
             # the other pair's: half of what it has alone, both rounded
             assert float((dz[n // 2:] - first[3] / 2).abs().max()) <= 8 * U * float(first[3].abs().max())
     assert float(ops.preference_loss(z, tg, cu, label_smoothing=0.1)[0]) == INF
+
+
+# vocabularies whose logarithm lies nearly half a step between two float32 values
+BETWEEN = [v for v in range(3001, 60000, 2) if abs(float(torch.tensor(math.log(v), dtype=F)) - math.log(v)) > 0.46 * 2.0 ** -20]
+
+
+@pytest.mark.parametrize("n", [1, 300, 3000])
+@pytest.mark.parametrize("vocab", [BETWEEN[0], BETWEEN[7]])
+def test_ratio_of_a_long_row(vocab, n):
+    """Rows of equal logits: the sum is exactly the vocabulary, log p = -log(vocab), and
+    the loss -A q with A = 1 and q = exp(-log(vocab) - old).  log(vocab) is k log 2, held in
+    two floats, and a logarithm below 0.35 within an ulp, 0.5 u; the exponential is off
+    by an ulp, 2 u, its correction by the kept errors and the result by u each: 4.5 u.
+    (As one float32, log(vocab) is off by 7.4 u here.)"""
+    assert math.log(vocab) > 8
+    z = torch.full((n, vocab), 3.25, device="cuda")
+    tg = torch.arange(n, device="cuda", dtype=torch.int32) % vocab
+    old = torch.full((n,), -math.log(vocab), device="cuda")
+    want = -math.exp(-math.log(vocab) - float(old[0]))
+    one = torch.ones(n, device="cuda")
+    for grad in (True, False):
+        loss = ops.policy_loss(z, tg, [0, n], old, one, want_grad=grad)[0]
+        assert abs(float(loss) - want) <= 4.5 * U, ((float(loss) - want) / U, grad)
