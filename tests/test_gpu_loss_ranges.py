@@ -95,3 +95,25 @@ def test_a_single_large_logit(n, dtype):
     check_every_operator(z, tg, cu, losses=False)
     tg = torch.where(tg >= 0, 4000, tg).int()
     check_every_operator(z, tg, cu)
+
+
+@pytest.mark.parametrize("tokens", [128, 1000])
+def test_errors_of_many_rows_do_not_add_up(tokens):
+    """A sequence's log-probability adds up its tokens' errors, so they must not share a
+    sign: their mean over 4000 rows and more is at most half a step, u / 2.  (Single rows
+    are off by about 1 u, their mean by 1 / sqrt(4000) of that by chance.)  Each row is a
+    pair's chosen sequence, its reference the exact value rounded to float32: the margin
+    is the error and what that rounding left, in full."""
+    g = torch.Generator(device="cuda").manual_seed(64)
+    cu = [0] + [t + 1 for t in range(tokens) for _ in range(2)]
+    errors = []
+    for _ in range(-(-4096 // tokens)):
+        z = 2 * torch.randn(tokens, 32000, generator=g, device="cuda")
+        tg = z.argmax(-1).int()
+        lp = torch.log_softmax(z.double(), -1).gather(1, tg.long()[:, None])[:, 0]
+        ref = torch.zeros(2 * tokens, device="cuda")
+        ref[::2] = lp.float()
+        margins = ops.preference_loss(z, tg, cu, ref, beta=1.0, want_grad=False)[2]
+        errors.append(margins.double() - (lp - ref[::2].double()))
+    errors = torch.cat(errors)
+    assert float(errors.abs().max()) <= 12 * U and abs(float(errors.mean())) <= U / 2, float(errors.mean()) / U
