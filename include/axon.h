@@ -392,10 +392,10 @@ int axon_preference_loss(int64_t tokens, int32_t vocab, const void* logits, int3
  * sequences with counted positions of each one's mean: 1 / (sequences n_seq).  The
  * first term's gradient is zero where the clipped value is the smaller; a position
  * with A == 0 has no first term, with kl_coef == 0 none has a second.  clip_low in
- * [0, 1], clip_high >= 0, kl_coef >= 0 (0 without d_ref_logps).  cu_seqlens [batch + 1] as above.  Writes d_loss [1],
- * d_stats [3] (the w-weighted means of the first term, of exp(r - l) - (r - l) - 1
- * (0 without d_ref_logps) and of the clipped positions), d_logps [tokens] and the
- * gradient (dlogits; NULL: not computed).  No counted position: loss, stats and
+ * [0, 1], clip_high >= 0, kl_coef >= 0 (0 without d_ref_logps).  cu_seqlens [batch + 1]
+ * as above.  Writes d_loss [1], d_stats [3] (the w-weighted means of the first term, of
+ * exp(r - l) - (r - l) - 1 (0 without d_ref_logps) and of the clipped positions), d_logps
+ * [tokens] and the gradient (dlogits; NULL: not computed).  No counted position: loss, stats and
  * gradient 0. */
 int axon_policy_loss(int64_t tokens, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
                      const int32_t* d_targets, int32_t batch, const int32_t* d_cu_seqlens, const int32_t* h_cu_seqlens,
