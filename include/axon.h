@@ -404,6 +404,106 @@ int axon_policy_loss(int64_t tokens, int32_t vocab, const void* logits, int32_t 
                      float* d_logps, void* dlogits, int32_t grad_dtype, int64_t ldg, void* workspace,
                      int64_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------- sampling answers to a prompt
+ *
+ * Operators of a decode step on the caller's tensors, for many answers to one prompt:
+ * the prompt's keys and values stand in a paged cache once, every answer's own behind
+ * them in pages of its own.  Conventions as for the row operators: rows ``ld`` elements
+ * apart, work on ``stream``, nothing allocated or synchronized, kernels only (a caller
+ * may capture them; lengths, tables and settings are read on the device at every
+ * replay), the same bits from the same inputs.
+ *
+ * The cache: K and V [num_pages][kv_heads][page_size][head_dim], AXON_BF16 or AXON_F32,
+ * 16-byte aligned; head_dim 64 or 128, page_size a multiple of 16. */
+typedef struct {
+  void* k;
+  void* v;
+  int32_t dtype;
+  int32_t kv_heads;
+  int32_t head_dim;
+  int32_t page_size;
+  int32_t num_pages;
+} axon_kv_pages;
+
+/* The sequences of a call, 1..4096.  Sequence b's new tokens are rows cu_seqlens[b] ..
+ * cu_seqlens[b + 1] - 1 of the call's tensors (prefix sums from 0, [seqs + 1]; the host
+ * copy is what is checked), or row b when both are NULL.  Rows behind the last
+ * sequence's (a batch padded to a fixed size) are neither read nor written.  d_lens[b]
+ * keys of the sequence were in the cache before the call; the new ones follow as its
+ * keys d_lens[b], d_lens[b] + 1, ...  d_lens[b] < 0: the sequence takes no part
+ * (nothing of it is stored, its attention is 0).  Key j is in page d_block_table[b]
+ * [j / page_size]; an entry outside [0, num_pages), and what is past the row's
+ * table_stride pages, is no page: what would go there is not stored, and keys there are
+ * masked out. */
+typedef struct {
+  int32_t seqs;
+  int32_t table_stride;
+  const int32_t* d_cu_seqlens;
+  const int32_t* h_cu_seqlens;
+  const int32_t* d_lens;
+  const int32_t* d_block_table;
+} axon_kv_batch;
+
+/* Shared prefixes, 0..4096: the sequences cu_groups[g] .. cu_groups[g + 1] - 1 (prefix
+ * sums from 0, [groups + 1], up to seqs) all have the first d_prefix_lens[g] keys of the
+ * pages d_prefix_table[g] before their own.  Sequences past the last group have none. */
+typedef struct {
+  int32_t groups;
+  int32_t table_stride;
+  const int32_t* d_cu_groups;
+  const int32_t* h_cu_groups;
+  const int32_t* d_prefix_lens;
+  const int32_t* d_prefix_table;
+} axon_kv_prefix;
+
+/* Rotates the new tokens' queries and keys by their positions and stores keys and values
+ * in the cache.  q [tokens][heads][head_dim] (rows ldq apart; heads 0: none), k and v
+ * [tokens][kv_heads][head_dim], of the cache's type; q_out as q (it may be q).  Key j of
+ * sequence b is at position p = d_offsets[b] + j (NULL: j; with a shared prefix, its
+ * length).  The pair (x, y) of dimension i becomes
+ *   scale (x cos a - y sin a, y cos a + x sin a),  a = p d_inv_freq[i] (float64, product
+ * and reduction as well), i < rot / 2; a pair is the dimensions (i, rot / 2 + i), or
+ * (2 i, 2 i + 1) with interleaved == 1; those from ``rot`` (even, 0..head_dim) on stay
+ * as they are.  Any long-context scaling is a choice of d_inv_freq and scale.  No two
+ * tokens may go to one place in the cache. */
+int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch* batch, int64_t tokens, int32_t heads,
+                     const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* q_out,
+                     int64_t ldqo, const double* d_inv_freq, int32_t rot, int32_t interleaved, float scale,
+                     const int32_t* d_offsets, void* stream);
+
+/* Attention of the new tokens (their keys and values are in the cache): out [tokens]
+ * [heads][head_dim] (of the cache's type; it may be q) is the softmax of scale q k over
+ * the group's prefix and the sequence's own keys up to the token itself, times v; query
+ * head h reads kv head h / (heads / kv_heads).  Each prefix is read once for all of its
+ * sequences.  A token with no key has out 0.  d_lse: float [tokens][heads], the logarithm
+ * of the sum of exp(scale q k) (-inf: no key), or NULL.  What the cache holds at masked
+ * places (behind the last key, later tokens) is not used, whatever it is.  prefix may be
+ * NULL. */
+int64_t axon_prefix_attention_workspace(const axon_kv_pages* pages, const axon_kv_batch* batch,
+                                        const axon_kv_prefix* prefix, int64_t tokens, int32_t heads);
+int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_batch* batch, const axon_kv_prefix* prefix,
+                          int64_t tokens, int32_t heads, const void* q, int64_t ldq, float scale, void* out,
+                          int64_t ldo, float* d_lse, void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Draws a token from each row of logits [rows][vocab] (vocab up to 2^22) by the row's
+ * number d_uniform in [0, 1) (others are taken as the nearest; NaN as 0).  Each setting
+ * is an array over the rows, or (NULL) the number behind it:
+ *   temperature T > 0: weights exp((z - max z) / T); not > 0 (a number: 0): the largest;
+ *   top_k > 0: only the k largest stay;
+ *   top_p < 1: of these, the fewest of the largest whose weights reach top_p of theirs
+ *           (at least one; a number: in (0, 1]);
+ *   min_p > 0: of these, those of at least min_p of the largest weight (1 at most).
+ * Of equal logits the lower index is the larger.  The token is the first, in ascending
+ * order, at which the running sum of the weights that stay passes d_uniform of their
+ * sum; its d_logps is the logarithm of its share of that sum (0 for the largest).  -inf
+ * and NaN are never drawn; +inf takes all the weight; a row without any other value gives
+ * token -1, which does not count as a target, and 0. */
+int64_t axon_sample_tokens_workspace(int64_t rows, int32_t vocab);
+int axon_sample_tokens(int64_t rows, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
+                       const float* d_uniform, const float* d_temperature, float temperature, const int32_t* d_top_k,
+                       int32_t top_k, const float* d_top_p, float top_p, const float* d_min_p, float min_p,
+                       int32_t* d_tokens, float* d_logps, void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Current length of every slot (host copy kept by the library, no device
  * access).  Writes min(n, max_batch) entries to ``lens``; returns the number of
  * active slots (the batch of the last prefill), or a negative status. */

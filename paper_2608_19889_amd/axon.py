@@ -36,7 +36,8 @@ EXPORTED = ["axon_init_model", "axon_prefill", "axon_decode_step", "axon_decode_
             "axon_layernorm", "axon_layernorm_backward", "axon_layernorm_backward_workspace",
             "axon_token_loss_workspace", "axon_token_logprobs", "axon_token_logprobs_backward",
             "axon_preference_loss", "axon_policy_loss", "axon_preference_loss_and_grads",
-            "axon_policy_loss_and_grads"]
+            "axon_policy_loss_and_grads", "axon_rope_append", "axon_prefix_attention",
+            "axon_prefix_attention_workspace", "axon_sample_tokens", "axon_sample_tokens_workspace"]
 
 # kernel classes of the timing records
 T_GEMV, T_GEMM, T_ATTN_DECODE, T_ATTN_PREFILL, T_GEMV_GROUPED, T_ATTN_BWD = 0, 1, 2, 3, 4, 5
@@ -61,6 +62,24 @@ class AxonWeight(ctypes.Structure):
     _fields_ = [("name", ctypes.c_char_p), ("dtype", ctypes.c_int32), ("ndim", ctypes.c_int32),
                 ("shape", ctypes.c_int64 * 2), ("data", ctypes.c_void_p),
                 ("on_device", ctypes.c_int32)]
+
+
+class AxonKvPages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("dtype", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32)]
+
+
+class AxonKvBatch(ctypes.Structure):
+    _fields_ = [("seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("d_cu_seqlens", ctypes.c_void_p),
+                ("h_cu_seqlens", ctypes.POINTER(ctypes.c_int32)), ("d_lens", ctypes.c_void_p),
+                ("d_block_table", ctypes.c_void_p)]
+
+
+class AxonKvPrefix(ctypes.Structure):
+    _fields_ = [("groups", ctypes.c_int32), ("table_stride", ctypes.c_int32), ("d_cu_groups", ctypes.c_void_p),
+                ("h_cu_groups", ctypes.POINTER(ctypes.c_int32)), ("d_prefix_lens", ctypes.c_void_p),
+                ("d_prefix_table", ctypes.c_void_p)]
 
 
 class AxonError(RuntimeError):
@@ -121,6 +140,8 @@ def lib():
         grad, work = [p, i32, i64], [p, i64, p]              # dlogits, dtype, ld; workspace, its bytes, stream
         step = [p, i32, p, p, i32p, p]                       # model, batch, tokens, cu_seqlens (both), targets
         grads = [ctypes.POINTER(AxonWeight), i32, p]
+        paged = [ctypes.POINTER(AxonKvPages), ctypes.POINTER(AxonKvBatch)]
+        shared = ctypes.POINTER(AxonKvPrefix)
         for name, args, res in [
                 ("axon_preference_loss_and_grads", [*step, p, f32, f32, p, p, p, *grads], ctypes.c_int),
                 ("axon_policy_loss_and_grads", [*step, p, p, p, f32, f32, f32, i32, p, p, p, *grads], ctypes.c_int),
@@ -132,6 +153,13 @@ def lib():
                 ("axon_token_logprobs", [*logits, p, *work], ctypes.c_int),
                 ("axon_token_logprobs_backward", [*logits, p, *grad, p], ctypes.c_int),
                 ("axon_preference_loss", [*logits, i32, p, i32p, p, f32, f32, p, p, p, *grad, *work], ctypes.c_int),
+                ("axon_rope_append", [*paged, i64, i32, p, i64, p, i64, p, i64, p, i64, p, i32, i32, f32, p, p],
+                 ctypes.c_int),
+                ("axon_prefix_attention_workspace", [*paged, shared, i64, i32], i64),
+                ("axon_prefix_attention", [*paged, shared, i64, i32, p, i64, f32, p, i64, p, *work], ctypes.c_int),
+                ("axon_sample_tokens_workspace", [i64, i32], i64),
+                ("axon_sample_tokens", [i64, i32, p, i32, i64, p, p, f32, p, i32, p, f32, p, f32, p, p, *work],
+                 ctypes.c_int),
                 ("axon_policy_loss", [*logits, i32, p, i32p, p, p, p, f32, f32, f32, i32, p, p, p, *grad, *work],
                  ctypes.c_int)]:
             getattr(L, name).argtypes = args
@@ -463,6 +491,177 @@ def policy_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: list, o
                                   at + 16, *gargs, ws.data_ptr(), need, _current(z)))
     loss, stats, logps = out.split_with_sizes((1, 3, tokens))
     return loss, stats, logps, g
+
+
+# ---------------------------------------------------------------- sampling answers
+
+def _head_rows(t: torch.Tensor, heads, hd: int, dtype, name: str, out: bool = False):
+    """(the tensor, its row stride) of [tokens, heads, hd] with contiguous heads.  An
+    input of another layout is copied; an output is refused."""
+    if t.dim() != 3 or t.shape[2] != hd or (heads is not None and t.shape[1] != heads) or t.dtype != dtype:
+        raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {hd}] {dtype}, got {tuple(t.shape)} {t.dtype}")
+    tokens, heads, _ = t.shape
+    row = heads * hd
+    ld = row if tokens < 2 else t.stride(0)
+    if t.stride(2) == 1 and (heads < 2 or t.stride(1) == hd) and ld >= row:
+        return t, ld
+    if out:
+        raise ValueError(f"{name} must have contiguous heads and rows that do not overlap")
+    return t.contiguous(), row
+
+
+def _pages_arg(k_cache: torch.Tensor, v_cache: torch.Tensor) -> AxonKvPages:
+    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
+        raise ValueError("k_cache and v_cache must be [pages, kv heads, page size, head dim] of one type, got "
+                         f"{tuple(k_cache.shape)} {k_cache.dtype} and {tuple(v_cache.shape)} {v_cache.dtype}")
+    if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
+        raise ValueError("k_cache and v_cache must be contiguous")
+    pages, kv, ps, hd = k_cache.shape
+    return AxonKvPages(k_cache.data_ptr(), v_cache.data_ptr(), _code(k_cache, "the cache"), kv, hd, ps, pages)
+
+
+def _table(t: torch.Tensor, lens: torch.Tensor, name: str, lens_name: str):
+    if t.dim() != 2 or t.dtype != torch.int32:
+        raise ValueError(f"{name} must be int32 [sequences, pages], got {tuple(t.shape)} {t.dtype}")
+    return t.contiguous(), _vector(lens, t.shape[0], torch.int32, lens_name)
+
+
+def _sums(values, device_copy, n: int, name: str, like):
+    """(host array, device tensor) of n + 1 prefix sums; (None, None) for None."""
+    if values is None:
+        return None, None
+    if len(values) != n + 1:
+        raise ValueError(f"{name} must have {n + 1} entries, got {len(values)}")
+    return _cu_args(values, device_copy, like)
+
+
+def _batch_arg(block_table, lens, cu_seqlens, cu_device, like):
+    """The C structure and the tensors that it points at."""
+    table, lens = _table(block_table, lens, "block_table", "lens")
+    host, cu = _sums(cu_seqlens, cu_device, table.shape[0], "cu_seqlens", like)
+    return AxonKvBatch(table.shape[0], table.shape[1], _ptr(cu), host, lens.data_ptr(), table.data_ptr()), (table, lens, cu)
+
+
+@_row_operator
+def rope_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
+                v_cache: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor,
+                inv_freq: torch.Tensor | None = None, cu_seqlens: list | None = None,
+                cu_device: torch.Tensor | None = None, offsets: torch.Tensor | None = None,
+                interleaved: bool = False, scale: float = 1.0, out: torch.Tensor | None = None):
+    """Rotates the new tokens' q [tokens, heads, head dim] and k [tokens, kv heads, head
+    dim] by their positions and stores k and v in the paged cache [pages, kv heads, page
+    size, head dim] (axon_rope_append); returns the rotated q (``out`` may be q; None for
+    q None).  block_table int32 [sequences, pages]; lens int32 [sequences], the keys that
+    each had before (negative: it takes no part); cu_seqlens a host list of prefix sums of
+    the tokens (None: one each; cu_device as in :func:`preference_loss`); inv_freq float64
+    [rotated dimensions / 2] (None: no rotation); offsets int32 [sequences], the position
+    of each one's first key."""
+    pages = _pages_arg(k_cache, v_cache)
+    hd, dtype = pages.head_dim, k_cache.dtype
+    kv_, ldk = _head_rows(k, pages.kv_heads, hd, dtype, "k")
+    vv, ldv = _head_rows(v, pages.kv_heads, hd, dtype, "v")
+    tokens = k.shape[0]
+    batch, keep = _batch_arg(block_table, lens, cu_seqlens, cu_device, k)
+    if v.shape[0] != tokens or (q is not None and q.shape[0] != tokens):
+        raise ValueError("q, k and v must have the same tokens")
+    if inv_freq is not None:
+        inv_freq = _vector(inv_freq, inv_freq.numel(), torch.float64, "inv_freq")
+    offsets = _vector(offsets, block_table.shape[0], torch.int32, "offsets")
+    heads, qv, ldq, ov, ldo = 0, None, 0, None, 0
+    if q is not None:
+        qv, ldq = _head_rows(q, None, hd, dtype, "q")
+        heads = q.shape[1]
+        out = _like(out, q, dtype, "out")
+        ov, ldo = _head_rows(out, heads, hd, dtype, "out", out=True)
+    elif out is not None:
+        raise ValueError("out without q")
+    _check(lib().axon_rope_append(pages, batch, tokens, heads, _ptr(qv), ldq, kv_.data_ptr(), ldk, vv.data_ptr(), ldv,
+                                  _ptr(ov), ldo, _ptr(inv_freq), 0 if inv_freq is None else 2 * inv_freq.numel(),
+                                  int(interleaved), scale, _ptr(offsets), _current(k)))
+    torch.autograd.graph.increment_version((k_cache, v_cache))
+    return out
+
+
+@_row_operator
+def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, block_table: torch.Tensor,
+                     lens: torch.Tensor, prefix_table: torch.Tensor | None = None,
+                     prefix_lens: torch.Tensor | None = None, cu_groups: list | None = None,
+                     groups_device: torch.Tensor | None = None, cu_seqlens: list | None = None,
+                     cu_device: torch.Tensor | None = None, scale: float | None = None,
+                     out: torch.Tensor | None = None, want_lse: bool = False):
+    """Attention of new tokens q [tokens, heads, head dim], already in the cache, over a
+    prefix that sequences share and each one's own keys up to the token itself
+    (axon_prefix_attention).  Cache, block_table, lens and cu_seqlens as the
+    :func:`rope_append` before it took them.  prefix_table int32 [groups, pages] and
+    prefix_lens int32 [groups]; cu_groups a host list of prefix sums of the groups'
+    sequences (None: one group of all; groups_device its device copy).  scale: 1 /
+    sqrt(head dim) by default; ``out`` may be q.  Returns out, with want_lse (out,
+    logarithms of the sums, float32 [tokens, heads])."""
+    pages = _pages_arg(k_cache, v_cache)
+    hd, dtype = pages.head_dim, k_cache.dtype
+    qv, ldq = _head_rows(q, None, hd, dtype, "q")
+    tokens, heads = q.shape[:2]
+    batch, keep = _batch_arg(block_table, lens, cu_seqlens, cu_device, q)
+    prefix = None
+    if prefix_table is not None:
+        if prefix_lens is None:
+            raise ValueError("prefix_table without prefix_lens")
+        table, plens = _table(prefix_table, prefix_lens, "prefix_table", "prefix_lens")
+        if cu_groups is None:
+            if table.shape[0] != 1:
+                raise ValueError("several groups need cu_groups")
+            cu_groups = [0, batch.seqs]
+        host, cu = _sums(cu_groups, groups_device, table.shape[0], "cu_groups", q)
+        prefix = AxonKvPrefix(table.shape[0], table.shape[1], cu.data_ptr(), host, plens.data_ptr(), table.data_ptr())
+        keep = (keep, table, plens, cu)
+    elif prefix_lens is not None or cu_groups is not None:
+        raise ValueError("prefix_lens and cu_groups need prefix_table")
+    out = _like(out, q, dtype, "out")
+    ov, ldo = _head_rows(out, heads, hd, dtype, "out", out=True)
+    lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
+    need = lib().axon_prefix_attention_workspace(pages, batch, prefix, tokens, heads)
+    ws = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib().axon_prefix_attention(pages, batch, prefix, tokens, heads, qv.data_ptr(), ldq,
+                                       hd ** -0.5 if scale is None else scale, ov.data_ptr(), ldo, _ptr(lse),
+                                       ws.data_ptr(), need, _current(q)))
+    return (out, lse) if want_lse else out
+
+
+def _setting(value, rows: int, dtype, name: str):
+    """(an array over the rows or None, the number for all of them)"""
+    if isinstance(value, torch.Tensor):
+        return _vector(value, rows, dtype, name), 0
+    return None, value
+
+
+@_row_operator
+def sample_tokens(logits: torch.Tensor, uniform: torch.Tensor, temperature: float | torch.Tensor = 1.0,
+                  top_k: int | torch.Tensor = 0, top_p: float | torch.Tensor = 1.0,
+                  min_p: float | torch.Tensor = 0.0, out: torch.Tensor | None = None):
+    """Draws a token from each row of logits [rows, vocab] (float32 or bfloat16) by its
+    number uniform (float32 [rows], in [0, 1)), after temperature, top-k, top-p and min-p,
+    each a number or a tensor over the rows (int32 for top_k, else float32); temperature 0
+    takes the largest, top_k 0, top_p 1 and min_p 0 keep all (axon_sample_tokens).  Returns
+    (tokens int32 [rows] (``out`` if given), logprobs float32 [rows]: under the distribution
+    drawn from; :func:`token_logprobs` gives the model's)."""
+    z, rows, vocab, ld = _rows(logits, "logits")
+    uniform = _vector(uniform, rows, torch.float32, "uniform")
+    settings = [_setting(v, rows, t, n) for v, t, n in (
+        (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
+        (min_p, torch.float32, "min_p"))]
+    if out is None:
+        out = torch.empty(rows, dtype=torch.int32, device=z.device)
+    else:
+        if out.shape != (rows,) or out.dtype != torch.int32 or not out.is_contiguous():
+            raise ValueError(f"out must be int32 [{rows}] and contiguous")
+        torch.autograd.graph.increment_version(out)
+    logps = torch.empty(rows, dtype=torch.float32, device=z.device)
+    need = lib().axon_sample_tokens_workspace(rows, vocab)
+    ws = torch.empty(need, dtype=torch.uint8, device=z.device)
+    _check(lib().axon_sample_tokens(rows, vocab, z.data_ptr(), _code(logits, "logits"), ld, uniform.data_ptr(),
+                                    *(x for t, n in settings for x in (_ptr(t), n)), out.data_ptr(), logps.data_ptr(),
+                                    ws.data_ptr(), need, _current(z)))
+    return out, logps
 
 
 class Model:

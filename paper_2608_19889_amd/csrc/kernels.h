@@ -485,4 +485,82 @@ inline int moe_combine_blocks(int D) { return (D / 4 + 255) / 256; }
 void launch_moe_combine(float* x, const float* y, const int32_t* inv, const float* w, int T, int D, int k,
                         hipStream_t s, const bf16* g = nullptr, bf16* xg = nullptr, float* ss_out = nullptr);
 
+// ---- paged cache of a caller (k_append.hip, k_prefix.hip)
+// K and V pages [num_pages][kv_heads][ps][hd], ps a multiple of 16.  Sequence b's own
+// keys are listed by row b of ``table`` (ps keys a page); lens[b] of them were there
+// before this call's tokens cu[b] .. cu[b + 1] - 1 (token b when cu is null), which
+// follow them.  lens[b] < 0: the sequence takes no part.
+constexpr int KV_MAX_SEQS = 4096;  // sequences, and groups, of a call
+struct PagedKV {
+  void* k;
+  void* v;
+  int kv_heads, hd, ps, num_pages;
+};
+struct PagedSeqs {
+  int seqs;
+  const int32_t* cu;  // [seqs + 1], or null: one token each
+  const int32_t* lens;
+  const int32_t* table;
+  int stride;
+};
+// Sequences cu[g] .. cu[g + 1] - 1 share the lens[g] keys of row g of ``table``,
+// which come before their own.
+struct SharedPrefix {
+  int groups;
+  const int32_t* cu;
+  const int32_t* lens;
+  const int32_t* table;
+  int stride;
+};
+template <typename T>
+struct AppendArgs {
+  PagedKV kv;
+  PagedSeqs seqs;
+  int tokens, heads;
+  const T *q, *k, *v;
+  T* q_out;  // may be q
+  int64_t ldq, ldk, ldv, ldqo;
+  const double* inv_freq;  // [rot / 2]
+  int rot;
+  bool interleaved;
+  float scale;
+  const int32_t* offsets;  // or null
+};
+template <typename T>
+void launch_rope_append(const AppendArgs<T>& a, hipStream_t s);
+
+template <typename T>
+struct PrefixAttnArgs {
+  PagedKV kv;
+  PagedSeqs seqs;
+  SharedPrefix shared;  // groups 0: none
+  int tokens, heads;
+  const T* q;
+  T* out;
+  int64_t ldq, ldo;
+  float scale;
+  float* lse;  // [tokens][heads] or null
+};
+template <typename T>
+void launch_prefix_attn(const PrefixAttnArgs<T>& a, hipStream_t s);
+
+// ---- sampling (k_sample.hip)
+struct SampleArgs {
+  const void* logits;
+  bool bf16_logits;
+  int64_t ld;
+  int rows, vocab;
+  const float* uniform;
+  const float* temperature;  // [rows] each, or null: the number beside it
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  float temperature_all, top_p_all, min_p_all;
+  int32_t top_k_all;
+  int32_t* tokens;
+  float* logps;
+};
+constexpr int SAMPLE_MAX_VOCAB = 1 << 22;
+void launch_sample(const SampleArgs& a, hipStream_t s);
+
 }  // namespace axon

@@ -1,0 +1,365 @@
+"""Rotating and appending to a paged cache, and attention over it with shared
+prefixes, on the GPU against float64."""
+import math
+
+import pytest
+import torch
+
+import paper_2608_19889_amd as ops
+from paged_util import B, F, HALF, U, Paged, check
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------ rope_append
+
+def rotated(x, pos, inv_freq, rot, interleaved, scale):
+    """(float64 result, |x| + |y| of each pair)"""
+    x = x.cpu().double()
+    size = x.abs()
+    out = x.clone()
+    if rot:
+        a = pos.double()[:, None, None] * inv_freq.cpu()
+        c, s = torch.cos(a) * scale, torch.sin(a) * scale
+        i = torch.arange(0, rot, 2) if interleaved else torch.arange(rot // 2)
+        j = i + 1 if interleaved else i + rot // 2
+        out[..., i] = x[..., i] * c - x[..., j] * s
+        out[..., j] = x[..., j] * c + x[..., i] * s
+        size[..., i] = size[..., j] = x[..., i].abs() + x[..., j].abs()
+    return out, size
+
+
+def check_append(p, rot, interleaved=False, scale=1.0, offsets=None, theta=10000.0, inplace=False, fused=False,
+                 pad_rows=0, no_q=False):
+    """A cosine or sine is off by 7 u: its argument's rounding (pi u / 2 of a half turn),
+    the function's 4 ulp and the product with scale; the two products and their sum add
+    2 u of (|x| + |y|) scale each at most: 10 u in all, and the stored value's rounding."""
+    inv = theta ** (-torch.arange(0, rot, 2, dtype=torch.float64, device="cuda") / max(rot, 1)) if rot else None
+    q, k, v = p.q, p.k, p.v
+    if fused:
+        rows = torch.cat([q, k, v], 1)
+        q, k, v = rows[:, :p.heads], rows[:, p.heads:p.heads + p.kv], rows[:, p.heads + p.kv:]
+    if pad_rows:
+        more = lambda t: torch.cat([t, torch.full_like(t[:1], float("nan")).expand(pad_rows, -1, -1)])  # noqa: E731
+        q, k, v = more(q), more(k), more(v)
+    off = None if offsets is None else torch.tensor(offsets, dtype=torch.int32, device="cuda")
+    kc, vc = p.k_cache.cpu().double(), p.v_cache.cpu().double()
+    kc_bound, vc_bound = torch.zeros_like(kc), torch.zeros_like(vc)
+    seq = torch.repeat_interleave(torch.arange(len(p.new)), torch.tensor(p.new))
+    slot = torch.tensor([int(p.lens[b]) + i for b, n in enumerate(p.new) for i in range(n)], dtype=torch.int64)
+    pos = slot + (0 if offsets is None else torch.tensor(offsets)[seq])
+    qr, qs = rotated(p.q, pos, inv, rot, interleaved, scale)
+    kr, ks = rotated(p.k, pos, inv, rot, interleaved, scale)
+    half = HALF[p.dtype]
+    # dimensions behind the rotated ones are copied
+    err = lambda r, s: torch.where(torch.arange(p.hd) < rot, 10 * U * s * abs(scale) * (1 + half) + half * r.abs(), 0.0)  # noqa: E731
+    table = p.table.cpu()
+    active = [int(p.lens[b]) >= 0 for b in seq.tolist()]
+    for t in range(p.T):
+        if not active[t]:
+            continue
+        col = int(slot[t]) // p.page
+        page = int(table[seq[t], col]) if col < table.shape[1] else -1
+        if 0 <= page < p.num_pages:
+            at = (page, slice(None), int(slot[t]) % p.page)
+            kc[at], kc_bound[at], vc[at] = kr[t], err(kr[t], ks[t]), p.v[t].cpu().double()
+    before = torch.full((p.T + pad_rows, p.heads, p.hd), 7.0, dtype=p.dtype, device="cuda")
+    out = q if inplace else before
+    cu = p.cu_seqlens if not pad_rows else p.cu
+    got = ops.rope_append(None if no_q else q, k, v, p.k_cache, p.v_cache, p.table, p.lens, inv, cu_seqlens=cu,
+                          offsets=off, interleaved=interleaved, scale=scale, out=None if no_q else out)
+    torch.cuda.synchronize()
+    if no_q:
+        assert got is None
+    else:
+        assert got is out
+        keep = torch.tensor(active)
+        check(got[:p.T][keep.cuda()], qr[keep], err(qr, qs)[keep], "q")
+        if not inplace:
+            assert (got[:p.T][~keep.cuda()] == 7).all() and (got[p.T:] == 7).all()
+    nan = torch.isnan(kc)
+    assert torch.equal(torch.isnan(p.k_cache.cpu()), nan)
+    check(torch.nan_to_num(p.k_cache.cpu().double()), torch.nan_to_num(kc), kc_bound, "k cache")
+    check(p.v_cache, vc, vc_bound, "v cache")
+
+
+ONE = [(0, [(p, 1) for p in (0, 15, 16, 31, 40, 7)])]
+RAGGED = [(0, [(0, 5), (15, 1), (16, 33), (3, 16), (0, 1), (47, 70)])]
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("heads,kv,hd,rot", [(9, 3, 64, 64), (4, 4, 128, 128), (28, 4, 128, 64), (2, 1, 64, 2),
+                                             (3, 1, 64, 20), (5, 5, 128, 36), (25, 25, 64, 0)])
+@pytest.mark.parametrize("groups", [ONE, RAGGED], ids=["one", "ragged"])
+def test_append(groups, heads, kv, hd, rot, interleaved, dtype):
+    check_append(Paged(groups, heads, kv, hd, dtype, seed=rot), rot, interleaved)
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("page", [16, 48, 256])
+def test_append_far_positions_pages_and_scale(page, dtype):
+    p = Paged(RAGGED, 8, 2, 64, dtype, page=page)
+    check_append(p, 64, scale=1.3, offsets=[0, 1 << 20, 2000000000, 999999, 2147483647, 5], theta=500000.0, fused=True)
+
+
+def test_append_strides_in_place_and_without_queries():
+    for kw in (dict(fused=True), dict(inplace=True), dict(fused=True, inplace=True), dict(no_q=True)):
+        check_append(Paged(RAGGED, 6, 2, 64, B, seed=3), 64, **kw)
+    # rows at odd elements: nothing is aligned to more than an element
+    for dtype in (F, B):
+        p = Paged(RAGGED, 6, 2, 64, dtype, seed=3)
+        odd = torch.zeros((p.T, 6 * 64 + 3), dtype=dtype, device="cuda")
+        view = odd.as_strided((p.T, 6, 64), (6 * 64 + 3, 64, 1), 1)
+        view.copy_(p.q)
+        p.q = view
+        check_append(p, 64, inplace=True)
+        assert (odd[:, 0] == 0).all() and (odd[:, -2:] == 0).all()
+
+
+def test_append_leaves_what_is_behind_the_last_sequence_and_inactive_ones():
+    p = Paged(RAGGED, 4, 2, 64, B)
+    check_append(p, 64, pad_rows=3)
+    p = Paged(ONE, 4, 2, 64, F)
+    p.lens[1] = -1
+    p.lens[4] = -2147483648
+    check_append(p, 64)
+    p = Paged(RAGGED, 4, 2, 64, F)
+    p.lens[2] = -1
+    check_append(p, 32)
+
+
+def test_append_without_a_page_stores_nothing():
+    p = Paged(RAGGED, 4, 2, 64, B, spare=4)
+    p.table[2, 2], p.table[5, 3], p.table[5, 6], p.table[0, 0] = -1, p.num_pages, 2147483647, -2147483648
+    check_append(p, 64)
+    p = Paged(ONE, 4, 2, 64, F)
+    p.lens[0], p.lens[3] = 1 << 30, p.table.shape[1] * p.page  # past the row
+    check_append(p, 64, offsets=[0] * 6)
+
+
+def test_append_offsets_past_32_bits():
+    """An element of the cache past 2^31 elements (4 GiB of bf16)."""
+    pages, page, kv, hd = (1 << 31) // (16 * 2 * 128) + 8, 16, 2, 128
+    k_cache, v_cache = (torch.zeros((pages, kv, page, hd), dtype=B, device="cuda") for _ in range(2))
+    table = torch.tensor([[pages - 1], [3]], dtype=torch.int32, device="cuda")
+    lens = torch.tensor([9, 2], dtype=torch.int32, device="cuda")
+    k, v, q = (torch.randn(2, n, hd, device="cuda").to(B) for n in (kv, kv, 4))
+    ops.rope_append(None, k, v, k_cache, v_cache, table, lens)
+    assert torch.equal(k_cache[pages - 1, :, 9], k[0]) and torch.equal(v_cache[pages - 1, :, 9], v[0])
+    assert torch.equal(k_cache[3, :, 2], k[1])
+    k_cache[pages - 1, :, 9] = 0
+    assert int(k_cache[pages - 1].count_nonzero()) == 0
+    lens[0] = 0
+    k_cache[pages - 1, :, 0], v_cache[pages - 1, :, 0] = k[0], v[0]
+    out = ops.prefix_attention(q, k_cache, v_cache, table, lens)
+    assert torch.equal(out[0], v[0].repeat_interleave(2, 0))
+
+
+# ------------------------------------------------------------------ prefix_attention
+
+def check_attention(p, scale=None):
+    ref = p.attention(scale=scale)
+    got, lse = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, scale=scale, want_lse=True,
+                                    **p.attention_args())
+    torch.cuda.synchronize()
+    check(got, ref[0], ref[1], "out")
+    check(lse, ref[2], ref[3], "lse")
+
+
+HEADS = [(9, 3, 64), (28, 4, 128), (32, 8, 64), (4, 4, 128), (7, 1, 64), (25, 25, 64), (40, 1, 128)]
+DECODE = {
+    "one": [(1, [(0, 1)])],
+    "tail": [(63, [(0, 1), (1, 1), (14, 1), (15, 1), (16, 1)]), (64, [(62, 1), (63, 1), (64, 1)]), (65, [(127, 1)])],
+    "no prefix": [(0, [(0, 1), (100, 1)]), (0, [(17, 1)])],
+    "groups": [(200, [(5, 1)] * 3), (1, [(300, 1)]), (129, [(0, 1), (33, 1), (7, 1), (64, 1), (9, 1)])],
+    "many": [(150, [(i % 23, 1) for i in range(40)])],
+}
+CHUNKS = {
+    "chunk": [(70, [(0, 5), (15, 1), (40, 33)])],
+    "long chunk": [(0, [(0, 130)]), (33, [(3, 70), (64, 64), (0, 1)])],
+    "empty chunks": [(20, [(0, 0), (5, 3), (8, 0)]), (9, [(0, 2)])],
+}
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("heads,kv,hd", HEADS)
+@pytest.mark.parametrize("groups", DECODE.values(), ids=DECODE.keys())
+def test_attention_of_single_tokens(groups, heads, kv, hd, dtype):
+    check_attention(Paged(groups, heads, kv, hd, dtype))
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("heads,kv,hd", HEADS[:5])
+@pytest.mark.parametrize("groups", CHUNKS.values(), ids=CHUNKS.keys())
+def test_attention_of_chunks(groups, heads, kv, hd, dtype):
+    check_attention(Paged(groups, heads, kv, hd, dtype, seed=1))
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("page", [32, 48, 256])
+def test_attention_pages_that_end_inside_a_tile(page, dtype):
+    check_attention(Paged(DECODE["tail"] + CHUNKS["chunk"], 8, 2, 128, dtype, page=page))
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+def test_attention_long_prefix_in_many_parts(dtype):
+    check_attention(Paged([(5000, [(700, 1), (3, 1)]), (1, [(2500, 1)])], 4, 1, 64, dtype))
+    check_attention(Paged([(3001, [(0, 40), (90, 1)])], 8, 1, 128, dtype))
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+def test_attention_masked_rows_and_places(dtype):
+    # inactive sequences, prefixes of no keys, missing pages, lengths past the table
+    p = Paged(DECODE["groups"], 8, 2, 64, dtype)
+    p.lens[1] = -1
+    p.lens[8] = -5
+    p.prefix_lens[2] = -3
+    check_attention(p)
+    p = Paged(CHUNKS["chunk"], 8, 2, 64, dtype)
+    p.table[2, 1] = -1
+    p.prefix_table[0, 0], p.prefix_table[0, 3] = p.num_pages, -2147483648
+    check_attention(p)
+    p = Paged(DECODE["one"], 8, 2, 64, dtype)
+    p.table[0, 0] = -7
+    p.prefix_table[0, 0] = 1 << 30
+    check_attention(p)  # a row without a key
+    assert float(ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens).abs().max()) == 0
+    p = Paged(DECODE["tail"], 8, 2, 64, dtype, junk=False)
+    p.prefix_lens[0], p.lens[2] = p.prefix_table.shape[1] * 16, p.table.shape[1] * 16 - 1
+    want = p.attention()
+    p.prefix_lens[0], p.lens[2] = 1 << 30, 2147483647
+    got = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **p.attention_args())
+    check(got, want[0], want[1], "lengths past the table")
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+def test_attention_later_tokens_do_not_show(dtype):
+    """NaN and infinities in a chunk's later tokens leave the earlier ones as they are."""
+    p = Paged([(40, [(20, 12), (0, 70)])], 4, 2, 64, dtype)
+    want = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **p.attention_args()).clone()
+    for b, j, val in ((0, 25, math.nan), (0, 27, math.inf), (0, 28, -math.inf), (1, 33, math.inf), (1, 64, math.nan)):
+        page, at = int(p.table[b, j // 16]), j % 16
+        p.k_cache[page, :, at, ::3] = val
+        p.v_cache[page, :, at, ::2] = val
+    got = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **p.attention_args())
+    assert torch.equal(got[:5], want[:5]) and torch.equal(got[12:12 + 33], want[12:12 + 33])
+    # an infinite value that is attended to shows, at its dimensions only
+    p = Paged([(40, [(20, 12)])], 4, 2, 64, dtype)
+    p.v_cache[int(p.table[0, 1]), :, 25 - 16, 3] = math.inf
+    p.v_cache[int(p.table[0, 1]), :, 27 - 16, 3] = -math.inf
+    got = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **p.attention_args())
+    assert torch.isfinite(got[:5]).all() and (got[5:7, :, 3] == math.inf).all() and torch.isnan(got[7:, :, 3]).all()
+    assert torch.isfinite(got[..., :3]).all() and torch.isfinite(got[..., 4:]).all()
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+def test_attention_scores_far_apart(dtype):
+    """One key takes all the weight, wherever it stands; scores that grow along the keys
+    rescale what was summed before."""
+    p = Paged([(300, [(150, 1), (0, 1)])], 4, 2, 64, dtype)
+    p.q *= 12
+    check_attention(p)
+    check_attention(p, scale=0.0)
+    check_attention(p, scale=-0.7)
+
+
+def test_attention_strides_and_in_place():
+    for dtype in (F, B):
+        p = Paged(CHUNKS["chunk"], 6, 2, 64, dtype)
+        wide = torch.zeros((p.T, 6 * 64 + 5), dtype=dtype, device="cuda")
+        view = wide.as_strided((p.T, 6, 64), (6 * 64 + 5, 64, 1), 3)
+        view.copy_(p.q)
+        p.q = view
+        check_attention(p)
+        ref = p.attention()
+        got = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, out=p.q, **p.attention_args())
+        assert got.data_ptr() == view.data_ptr()
+        check(got, ref[0], ref[1], "in place")
+        assert (wide.as_strided((p.T, 3), (6 * 64 + 5, 1), 0) == 0).all() and (wide[:, -2:] == 0).all()
+
+
+def test_attention_rows_behind_the_last_sequence_are_left():
+    p = Paged(CHUNKS["chunk"], 6, 2, 64, B)
+    ref = p.attention()
+    q = torch.cat([p.q, torch.full((3, 6, 64), float("nan"), dtype=B, device="cuda")])
+    out = torch.full_like(q, 7)
+    got = ops.prefix_attention(q, p.k_cache, p.v_cache, p.table, p.lens, out=out, **p.attention_args())
+    check(got[:p.T], ref[0], ref[1], "out")
+    assert (got[p.T:] == 7).all()
+
+
+def test_attention_more_sequences_than_groups_cover():
+    p = Paged(DECODE["groups"], 8, 2, 64, B)
+    p.cu_groups = [0, 2, 3, 5]  # the last four have no prefix
+    check_attention(p)
+
+
+def test_same_bits_again():
+    for dtype in (F, B):
+        p = Paged([(2000, [(300, 1), (3, 1)]), (70, [(9, 20)])], 8, 2, 128, dtype)
+        a, b = (ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **p.attention_args()) for _ in range(2))
+        assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------ streams and graphs
+
+def test_other_stream():
+    p = Paged(CHUNKS["chunk"], 8, 2, 64, B)
+    want = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **p.attention_args())
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    got = ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, stream=s, **p.attention_args())
+    s.synchronize()
+    assert torch.equal(got, want)
+
+
+def test_captured_decode_step_follows_its_lengths():
+    """One graph of append and attention, replayed while lengths, tables and tokens
+    change on the device, against eager calls."""
+    p = Paged([(100, [(13, 1), (0, 1), (31, 1)]), (20, [(63, 1)])], 8, 2, 64, B)
+    table = torch.full((4, 8), -1, dtype=torch.int32, device="cuda")
+    table[:, :p.table.shape[1]] = p.table
+    free = iter(sorted(set(range(p.num_pages + 20)) - set(p.table.flatten().tolist()) -
+                       set(p.prefix_table.flatten().tolist())))
+    grow = lambda c: torch.cat([c, torch.zeros((20, *c.shape[1:]), dtype=c.dtype, device="cuda")])  # noqa: E731
+    kc, vc = grow(p.k_cache), grow(p.v_cache)
+    kc2, vc2 = kc.clone(), vc.clone()
+    groups = torch.tensor(p.cu_groups, dtype=torch.int32, device="cuda")
+    offsets = torch.tensor([100, 100, 100, 20], dtype=torch.int32, device="cuda")
+    inv = 1e4 ** (-torch.arange(0, 64, 2, dtype=torch.float64, device="cuda") / 64)
+    lens = p.lens.clone()
+    q, k, v = p.q.clone(), p.k.clone(), p.v.clone()
+
+    def step(kc, vc):
+        r = ops.rope_append(q, k, v, kc, vc, table, lens, inv, offsets=offsets)
+        return ops.prefix_attention(r, kc, vc, table, lens, prefix_table=p.prefix_table, prefix_lens=p.prefix_lens,
+                                    cu_groups=p.cu_groups, groups_device=groups, want_lse=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(kc2, vc2)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = step(kc, vc)
+    for i in range(5):
+        for b in range(4):
+            col = int(lens[b]) // 16
+            if int(table[b, col]) < 0:
+                table[b, col] = next(free)
+        for t in (q, k, v):
+            t.copy_(torch.randn_like(t, dtype=F))
+        graph.replay()
+        want, want_lse = step(kc2, vc2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, want_lse), i
+        assert torch.equal(torch.nan_to_num(kc), torch.nan_to_num(kc2))
+        lens += 1
+
+
+def test_a_buffer_counts_as_modified():
+    p = Paged(ONE, 4, 2, 64, F)
+    versions = [t._version for t in (p.k_cache, p.v_cache, p.q)]
+    ops.rope_append(p.q, p.k, p.v, p.k_cache, p.v_cache, p.table, p.lens, out=p.q)
+    assert all(t._version > n for t, n in zip((p.k_cache, p.v_cache, p.q), versions))
