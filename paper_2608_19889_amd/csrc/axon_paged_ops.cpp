@@ -3,6 +3,7 @@
 // Argument checks only; the kernels are in k_append.hip, k_prefix.hip and k_sample.hip.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "kernels.h"
@@ -122,8 +123,12 @@ extern "C" int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch*
 
 extern "C" int64_t axon_prefix_attention_workspace(const axon_kv_pages* pages, const axon_kv_batch* batch,
                                                    const axon_kv_prefix* prefix, int64_t tokens, int32_t heads) {
-  (void)pages, (void)batch, (void)prefix, (void)tokens, (void)heads;
-  return 0;
+  if (!pages || !batch || tokens < 0 || tokens > MAX_TOKENS || pages->kv_heads < 1 || heads < 1 ||
+      heads % pages->kv_heads || (pages->head_dim != 64 && pages->head_dim != 128) || batch->seqs < 1 ||
+      batch->seqs > KV_MAX_SEQS || (prefix && (prefix->groups < 0 || prefix->groups > KV_MAX_SEQS)))
+    return 0;
+  return prefix_attn_workspace(tokens, batch->seqs, prefix ? prefix->groups : 0, heads, pages_of(*pages),
+                               pages->dtype == AXON_F32);
 }
 
 extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_batch* batch,
@@ -142,6 +147,12 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
     if (!std::isfinite(scale)) return fail(AXON_E_INVALID, "scale must be finite");
     if (d_lse)
       if (int r = check_array("d_lse", d_lse, 4)) return r;
+    const int groups = prefix ? prefix->groups : 0;
+    const int64_t longest = std::max(batch->table_stride, groups ? prefix->table_stride : 0);
+    if (prefix_attn_units(tokens, batch->seqs, groups, heads, pages_of(*pages), longest) >= (int64_t)1 << 31 ||
+        axon_prefix_attention_workspace(pages, batch, prefix, tokens, heads) >= (int64_t)1 << 40)
+      return fail(AXON_E_CAPACITY, num(tokens) + " tokens of " + num(heads) + " heads over tables of " + num(longest) +
+                                       " pages are too many for one call");
     if (int r = check_workspace(workspace, workspace_bytes,
                                 axon_prefix_attention_workspace(pages, batch, prefix, tokens, heads)))
       return r;
@@ -152,7 +163,7 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
       using T = std::remove_pointer_t<decltype(t)>;
       launch_prefix_attn(PrefixAttnArgs<T>{pages_of(*pages), seqs_of(*batch), shared, (int)tokens, heads, (const T*)q,
                                            (T*)out, ldq, ldo, scale, d_lse},
-                         (hipStream_t)stream);
+                         workspace, (hipStream_t)stream);
     };
     if (pages->dtype == AXON_BF16) launch((bf16*)nullptr);
     else launch((float*)nullptr);

@@ -541,8 +541,11 @@ struct PrefixAttnArgs {
   float scale;
   float* lse;  // [tokens][heads] or null
 };
+// upper bound of the units of work that lengths within ``pages`` pages a row can make
+int64_t prefix_attn_units(int64_t tokens, int seqs, int groups, int heads, const PagedKV& kv, int64_t pages);
+int64_t prefix_attn_workspace(int64_t tokens, int seqs, int groups, int heads, const PagedKV& kv, bool f32);
 template <typename T>
-void launch_prefix_attn(const PrefixAttnArgs<T>& a, hipStream_t s);
+void launch_prefix_attn(const PrefixAttnArgs<T>& a, void* workspace, hipStream_t s);
 
 // ---- sampling (k_sample.hip)
 struct SampleArgs {
