@@ -485,7 +485,7 @@ int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_batch* batch
                           int64_t tokens, int32_t heads, const void* q, int64_t ldq, float scale, void* out,
                           int64_t ldo, float* d_lse, void* workspace, int64_t workspace_bytes, void* stream);
 
-/* Draws a token from each row of logits [rows][vocab] (vocab up to 2^22) by the row's
+/* Draws a token from each row of logits [rows][vocab] (up to 65535 and 2^22) by the row's
  * number d_uniform in [0, 1) (others are taken as the nearest; NaN as 0).  Each setting
  * is an array over the rows, or (NULL) the number behind it:
  *   temperature T > 0: weights exp((z - max z) / T); not > 0 (a number: 0): the largest;

@@ -172,8 +172,8 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
 }
 
 extern "C" int64_t axon_sample_tokens_workspace(int64_t rows, int32_t vocab) {
-  (void)rows, (void)vocab;
-  return 0;
+  if (rows < 0 || rows > SAMPLE_MAX_ROWS || vocab < 1 || vocab > SAMPLE_MAX_VOCAB) return 0;
+  return sample_workspace(rows, vocab);
 }
 
 extern "C" int axon_sample_tokens(int64_t rows, int32_t vocab, const void* logits, int32_t dtype, int64_t ld,
@@ -182,7 +182,8 @@ extern "C" int axon_sample_tokens(int64_t rows, int32_t vocab, const void* logit
                                   const float* d_min_p, float min_p, int32_t* d_tokens, float* d_logps, void* workspace,
                                   int64_t workspace_bytes, void* stream) {
   return entry([&]() -> int {
-    if (rows < 0 || rows > 1 << 20) return fail(AXON_E_INVALID, "rows must be in [0, 2^20], got " + num(rows));
+    if (rows < 0 || rows > SAMPLE_MAX_ROWS)
+      return fail(AXON_E_INVALID, "rows must be in [0, " + num(SAMPLE_MAX_ROWS) + "], got " + num(rows));
     if (vocab < 1 || vocab > SAMPLE_MAX_VOCAB)
       return fail(AXON_E_INVALID, "vocab must be in [1, " + num(SAMPLE_MAX_VOCAB) + "], got " + num(vocab));
     if (int r = check_rows("logits", logits, dtype, ld, rows, vocab)) return r;
@@ -213,7 +214,7 @@ extern "C" int axon_sample_tokens(int64_t rows, int32_t vocab, const void* logit
     if (int r = check_workspace(workspace, workspace_bytes, axon_sample_tokens_workspace(rows, vocab))) return r;
     launch_sample(SampleArgs{logits, dtype == AXON_BF16, ld, (int)rows, vocab, d_uniform, d_temperature, d_top_k,
                              d_top_p, d_min_p, temperature, top_p, min_p, top_k, d_tokens, d_logps},
-                  (hipStream_t)stream);
+                  workspace, (hipStream_t)stream);
     return check_launch("sampling");
   });
 }

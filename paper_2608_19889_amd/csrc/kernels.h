@@ -563,7 +563,8 @@ struct SampleArgs {
   int32_t* tokens;
   float* logps;
 };
-constexpr int SAMPLE_MAX_VOCAB = 1 << 22;
-void launch_sample(const SampleArgs& a, hipStream_t s);
+constexpr int SAMPLE_MAX_VOCAB = 1 << 22, SAMPLE_MAX_ROWS = 65535;
+int64_t sample_workspace(int64_t rows, int vocab);
+void launch_sample(const SampleArgs& a, void* workspace, hipStream_t s);
 
 }  // namespace axon

@@ -100,7 +100,7 @@ ATTEND_BAD = [
 ]
 SAMPLE_BAD = [
     (dict(rows=-1), ax.AXON_E_INVALID, "rows"),
-    (dict(rows=(1 << 20) + 1), ax.AXON_E_INVALID, "rows"),
+    (dict(rows=65536), ax.AXON_E_INVALID, "rows"),
     (dict(vocab=0), ax.AXON_E_INVALID, "vocab"),
     (dict(vocab=(1 << 22) + 1, ld=1 << 23), ax.AXON_E_INVALID, "vocab"),
     (dict(z=None), ax.AXON_E_INVALID, "logits is NULL"),
