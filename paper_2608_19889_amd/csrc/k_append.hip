@@ -24,54 +24,138 @@ AXON_DEV int find_sequence(const int32_t* cu, int n, int t) {
   return b;
 }
 
+// 16 bytes of a head, of any element alignment in the caller's rows
 template <typename T>
+constexpr int RUN = 16 / sizeof(T);
+template <typename T>
+struct Run {
+  typedef typename std::conditional<sizeof(T) == 2, bf16x8_any, f32x4_any>::type V;
+  V v;
+  AXON_DEV void load(const T* p) { v = *(const V*)p; }
+  AXON_DEV void store(T* p) const { *(V*)p = v; }
+};
+
+// Where a token's head lies in its row and where it goes
+template <typename T>
+struct Place {
+  const T* src;
+  T* dst;
+};
+
+// A workgroup per token.  RUNS: a thread takes the pairs of 16 bytes of first dimensions
+// with the 16 bytes of second ones (halves) or of 16 bytes (interleaved), or copies 16
+// bytes; it has them in flight while the angles are worked out.  Otherwise (a rotated
+// part that is no whole number of 16-byte runs) a pair or a value at a time.
+template <typename T, bool RUNS>
 __global__ void __launch_bounds__(APPEND_THREADS) rope_append_kernel(AppendArgs<T> a) {
   __shared__ float cs[MAX_HALF], sn[MAX_HALF];
-  const int t = blockIdx.x;
+  constexpr int E = RUN<T>;
+  const int t = blockIdx.x, tid = threadIdx.x;
   const int b = a.seqs.cu ? find_sequence(a.seqs.cu, a.seqs.seqs, t) : t;
   if (b >= a.seqs.seqs) return;  // behind the last sequence
   const int len = a.seqs.lens[b];
   if (len < 0) return;
   const int64_t slot = (int64_t)len + (a.seqs.cu ? t - a.seqs.cu[b] : 0);
-  const int half = a.rot >> 1, hd = a.kv.hd;
-  if ((int)threadIdx.x < half) {
-    const double turns = (double)(slot + (a.offsets ? a.offsets[b] : 0)) * a.inv_freq[threadIdx.x] * 0.15915494309189535;
-    float s, c;
-    sincospif((float)(2. * (turns - rint(turns))), &s, &c);
-    cs[threadIdx.x] = c * a.scale;
-    sn[threadIdx.x] = s * a.scale;
-  }
-  __syncthreads();
   const int64_t pg = slot / a.kv.ps;
   const int page = pg < a.seqs.stride ? a.seqs.table[(int64_t)b * a.seqs.stride + pg] : -1;
   const bool stored = page >= 0 && page < a.kv.num_pages;
-  // element (head h, dimension 0) of this token's place in a cache
-  const int64_t at = ((int64_t)page * a.kv.kv_heads * a.kv.ps + slot % a.kv.ps) * hd;
-  const int64_t head_stride = (int64_t)a.kv.ps * hd;
-  for (int i = threadIdx.x; i < (a.heads + a.kv.kv_heads) * hd; i += APPEND_THREADS) {
-    const int h = i / hd, d = i % hd;
-    const bool is_q = h < a.heads;
-    if (!is_q && !stored) continue;
-    const T* src = is_q ? a.q + t * a.ldq + h * hd : a.k + t * a.ldk + (h - a.heads) * hd;
-    T* dst = is_q ? a.q_out + t * a.ldqo + h * hd : (T*)a.kv.k + at + (h - a.heads) * head_stride;
-    if (d >= a.rot) {
-      dst[d] = src[d];
-      continue;
+  const int half = a.rot >> 1, hd = a.kv.hd, kv = a.kv.kv_heads;
+  // element (head 0, dimension 0) of this token's place in a cache, and a head's distance
+  const int64_t at = ((int64_t)page * kv * a.kv.ps + slot % a.kv.ps) * hd, head_stride = (int64_t)a.kv.ps * hd;
+  auto place = [&](int h) {  // query heads, key heads, value heads
+    if (h < a.heads) return Place<T>{a.q + t * a.ldq + h * hd, a.q_out + t * a.ldqo + h * hd};
+    h -= a.heads;
+    if (h < kv) return Place<T>{a.k + t * a.ldk + h * hd, (T*)a.kv.k + at + h * head_stride};
+    h -= kv;
+    return Place<T>{a.v + t * a.ldv + h * hd, (T*)a.kv.v + at + h * head_stride};
+  };
+  // a head's items: the rotated ones, then the copied ones; value heads are copied
+  const int step = RUNS ? E : 1;
+  const int turned = a.interleaved && RUNS ? a.rot / E : half / step, per_head = turned + (hd - a.rot) / step;
+  const int rotated = (a.heads + (stored ? kv : 0)) * per_head, all = rotated + (stored ? kv * (hd / step) : 0);
+  struct Item {
+    Place<T> p;
+    int d, d2;  // the dimensions read; d2 < 0: copied
+  };
+  auto item = [&](int i) {
+    Item x;
+    if (i < rotated) {
+      const int h = i / per_head, c = i - h * per_head;
+      x.p = place(h);
+      if (c < turned) {
+        x.d = a.interleaved ? c * (RUNS ? E : 2) : c * step;
+        x.d2 = a.interleaved ? x.d + (RUNS ? 0 : 1) : x.d + half;
+      } else {
+        x.d = a.rot + (c - turned) * step;
+        x.d2 = -1;
+      }
+    } else {
+      i -= rotated;
+      const int h = i / (hd / step);
+      x.p = place(a.heads + kv + h);
+      x.d = (i - h * (hd / step)) * step;
+      x.d2 = -1;
     }
-    if (a.interleaved ? d & 1 : d >= half) continue;  // its pair's first dimension does both
-    const int j = a.interleaved ? d >> 1 : d, d2 = a.interleaved ? d + 1 : d + half;
-    const float x = to_f32(src[d]), y = to_f32(src[d2]);
-    dst[d] = from_f32<T>(x * cs[j] - y * sn[j]);
-    dst[d2] = from_f32<T>(y * cs[j] + x * sn[j]);
+    return x;
+  };
+  Item x;
+  Run<T> u, w;
+  auto load = [&](int i) {
+    x = item(i);
+    u.load(x.p.src + x.d);
+    if (x.d2 > x.d) w.load(x.p.src + x.d2);
+  };
+  if constexpr (RUNS)
+    if (tid < all) load(tid);
+  if (tid < half) {
+    const double turns = (double)(slot + (a.offsets ? a.offsets[b] : 0)) * a.inv_freq[tid] * 0.15915494309189535;
+    float s, c;
+    sincospif((float)(2. * (turns - rint(turns))), &s, &c);
+    cs[tid] = c * a.scale;
+    sn[tid] = s * a.scale;
   }
-  if (!stored) return;
-  for (int i = threadIdx.x; i < a.kv.kv_heads * hd; i += APPEND_THREADS)
-    ((T*)a.kv.v)[at + i / hd * head_stride + i % hd] = a.v[t * a.ldv + i];
+  __syncthreads();
+  for (int i = tid; i < all; i += APPEND_THREADS) {
+    if constexpr (!RUNS) {
+      x = item(i);
+      if (x.d2 < 0) {
+        x.p.dst[x.d] = x.p.src[x.d];
+        continue;
+      }
+      const int j = a.interleaved ? x.d >> 1 : x.d;
+      const float p = to_f32(x.p.src[x.d]), q = to_f32(x.p.src[x.d2]);
+      x.p.dst[x.d] = from_f32<T>(p * cs[j] - q * sn[j]);
+      x.p.dst[x.d2] = from_f32<T>(q * cs[j] + p * sn[j]);
+    } else {
+      if (i != tid) load(i);
+      if (x.d2 > x.d) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const float p = to_f32((T)u.v[e]), q = to_f32((T)w.v[e]), c = cs[x.d + e], s = sn[x.d + e];
+          u.v[e] = from_f32<T>(p * c - q * s);
+          w.v[e] = from_f32<T>(q * c + p * s);
+        }
+        w.store(x.p.dst + x.d2);
+      } else if (x.d2 == x.d) {
+#pragma unroll
+        for (int e = 0; e < E; e += 2) {
+          const float p = to_f32((T)u.v[e]), q = to_f32((T)u.v[e + 1]), c = cs[(x.d + e) >> 1], s = sn[(x.d + e) >> 1];
+          u.v[e] = from_f32<T>(p * c - q * s);
+          u.v[e + 1] = from_f32<T>(q * c + p * s);
+        }
+      }
+      u.store(x.p.dst + x.d);
+    }
+  }
 }
 
 template <typename T>
 void launch_rope_append(const AppendArgs<T>& a, hipStream_t s) {
-  if (a.tokens > 0) rope_append_kernel<T><<<a.tokens, APPEND_THREADS, 0, s>>>(a);
+  if (a.tokens <= 0) return;
+  if (a.rot % (a.interleaved ? RUN<T> : 2 * RUN<T>) == 0)
+    rope_append_kernel<T, true><<<a.tokens, APPEND_THREADS, 0, s>>>(a);
+  else
+    rope_append_kernel<T, false><<<a.tokens, APPEND_THREADS, 0, s>>>(a);
 }
 template void launch_rope_append<float>(const AppendArgs<float>&, hipStream_t);
 template void launch_rope_append<bf16>(const AppendArgs<bf16>&, hipStream_t);
