@@ -82,6 +82,21 @@ PagedSeqs seqs_of(const axon_kv_batch& b) {
   return PagedSeqs{b.seqs, b.d_cu_seqlens, b.d_lens, b.d_block_table, b.table_stride};
 }
 
+int check_attention(const axon_kv_pages* pages, const axon_kv_batch* batch, const axon_kv_prefix* prefix,
+                    int64_t tokens, int32_t heads) {
+  if (int r = check_pages(pages)) return r;
+  if (int r = check_batch(batch, tokens, pages->page_size)) return r;
+  if (int r = check_prefix(prefix, batch->seqs, pages->page_size)) return r;
+  return check_heads(heads, pages->kv_heads);
+}
+
+PrefixAttnShape shape_of(const axon_kv_pages& pages, const axon_kv_batch& batch, const axon_kv_prefix* prefix,
+                         int64_t tokens, int32_t heads) {
+  const int groups = prefix ? prefix->groups : 0;
+  return PrefixAttnShape{tokens, batch.seqs, groups, heads, pages.kv_heads, pages.head_dim, batch.h_cu_seqlens,
+                         groups ? prefix->h_cu_groups : nullptr};
+}
+
 }  // namespace
 
 extern "C" int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch* batch, int64_t tokens, int32_t heads,
@@ -123,12 +138,13 @@ extern "C" int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch*
 
 extern "C" int64_t axon_prefix_attention_workspace(const axon_kv_pages* pages, const axon_kv_batch* batch,
                                                    const axon_kv_prefix* prefix, int64_t tokens, int32_t heads) {
-  if (!pages || !batch || tokens < 0 || tokens > MAX_TOKENS || pages->kv_heads < 1 || heads < 1 ||
-      heads % pages->kv_heads || (pages->head_dim != 64 && pages->head_dim != 128) || batch->seqs < 1 ||
-      batch->seqs > KV_MAX_SEQS || (prefix && (prefix->groups < 0 || prefix->groups > KV_MAX_SEQS)))
-    return 0;
-  return prefix_attn_workspace(tokens, batch->seqs, prefix ? prefix->groups : 0, heads, pages_of(*pages),
-                               pages->dtype == AXON_F32);
+  int64_t bytes = 0;
+  entry([&]() -> int {
+    if (!check_attention(pages, batch, prefix, tokens, heads))
+      bytes = prefix_attn_workspace(shape_of(*pages, *batch, prefix, tokens, heads));
+    return AXON_OK;
+  });
+  return bytes;
 }
 
 extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_batch* batch,
@@ -136,10 +152,7 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
                                      int64_t ldq, float scale, void* out, int64_t ldo, float* d_lse, void* workspace,
                                      int64_t workspace_bytes, void* stream) {
   return entry([&]() -> int {
-    if (int r = check_pages(pages)) return r;
-    if (int r = check_batch(batch, tokens, pages->page_size)) return r;
-    if (int r = check_prefix(prefix, batch->seqs, pages->page_size)) return r;
-    if (int r = check_heads(heads, pages->kv_heads)) return r;
+    if (int r = check_attention(pages, batch, prefix, tokens, heads)) return r;
     const int64_t cols = (int64_t)heads * pages->head_dim;
     if (int r = check_rows("q", q, pages->dtype, ldq, tokens, cols)) return r;
     if (int r = check_rows("out", out, pages->dtype, ldo, tokens, cols)) return r;
@@ -147,15 +160,13 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
     if (!std::isfinite(scale)) return fail(AXON_E_INVALID, "scale must be finite");
     if (d_lse)
       if (int r = check_array("d_lse", d_lse, 4)) return r;
-    const int groups = prefix ? prefix->groups : 0;
-    const int64_t longest = std::max(batch->table_stride, groups ? prefix->table_stride : 0);
-    if (prefix_attn_units(tokens, batch->seqs, groups, heads, pages_of(*pages), longest) >= (int64_t)1 << 31 ||
-        axon_prefix_attention_workspace(pages, batch, prefix, tokens, heads) >= (int64_t)1 << 40)
+    const PrefixAttnShape shape = shape_of(*pages, *batch, prefix, tokens, heads);
+    const int64_t longest = std::max(batch->table_stride, shape.groups ? prefix->table_stride : 0);
+    const int64_t need = prefix_attn_workspace(shape);
+    if (prefix_attn_units(shape, longest * pages->page_size) >= (int64_t)1 << 31 || need >= (int64_t)1 << 40)
       return fail(AXON_E_CAPACITY, num(tokens) + " tokens of " + num(heads) + " heads over tables of " + num(longest) +
                                        " pages are too many for one call");
-    if (int r = check_workspace(workspace, workspace_bytes,
-                                axon_prefix_attention_workspace(pages, batch, prefix, tokens, heads)))
-      return r;
+    if (int r = check_workspace(workspace, workspace_bytes, need)) return r;
     const SharedPrefix shared = prefix ? SharedPrefix{prefix->groups, prefix->d_cu_groups, prefix->d_prefix_lens,
                                                       prefix->d_prefix_table, prefix->table_stride}
                                        : SharedPrefix{};
@@ -163,7 +174,7 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
       using T = std::remove_pointer_t<decltype(t)>;
       launch_prefix_attn(PrefixAttnArgs<T>{pages_of(*pages), seqs_of(*batch), shared, (int)tokens, heads, (const T*)q,
                                            (T*)out, ldq, ldo, scale, d_lse},
-                         workspace, (hipStream_t)stream);
+                         shape, workspace, (hipStream_t)stream);
     };
     if (pages->dtype == AXON_BF16) launch((bf16*)nullptr);
     else launch((float*)nullptr);

@@ -5,16 +5,23 @@
 // A *segment* is a list of keys and the tokens that read it: a group's prefix with the
 // tokens of all of its sequences, or a sequence's own keys with its own tokens.  The
 // rows of a segment and kv head are its tokens' query heads of that kv head, so a
-// prefix is multiplied with everything that shares it.  Rows go in tiles: a *wide* one
-// of 128 (32 to a wavefront, every wavefront over all keys), or, when a segment has at
-// most 16 rows, a *narrow* one (all rows in every wavefront, the keys shared out).
+// prefix is multiplied with everything that shares it.  Rows go in tiles: a segment of
+// at most 16 rows is one *narrow* tile (a single token's own keys), any other is cut
+// into *wide* ones of 256 rows.  Each kind has its kernel:
+//   prefix_wide_kernel    a workgroup of 8 wavefronts, 32 rows each, over keys that all
+//                         of them read from LDS (with few rows the keys are halved
+//                         between wavefronts): matrix instructions' work
+//   prefix_narrow_kernel  every wavefront by itself over 16 keys at a time, many of them
+//                         on a CU: memory's work
+//   prefix_join_kernel    joins the parts that they leave
 //
-// Work is cut into units of 64 keys of a tile, in the order (segment, kv head, tile,
-// keys), and every workgroup takes an equal run of consecutive units, whatever the
-// lengths are, which only the device knows.  Where a run covers part of a tile's keys it
-// leaves (max, sum, product) of them; a second kernel joins a row's parts of both
-// segments.  Both are deterministic: what is added to what depends on the lengths alone.
+// Work is cut into units of keys of a tile, in the order (segment, kv head, tile, keys),
+// and every worker takes an equal run of consecutive units, whatever the lengths are,
+// which only the device knows.  Of the keys of a tile in its run it leaves (max, sum,
+// product).  What is added to what depends on the lengths alone: the same bits every
+// time.
 #include <algorithm>
+#include <type_traits>
 
 #include "common.h"
 #include "kernels.h"
@@ -22,17 +29,16 @@
 namespace axon {
 
 constexpr float LOG2E_F = 1.4426950408889634f;
-constexpr int PA_THREADS = 256;
-constexpr int PA_KEYS = 64;   // keys of a unit, 16 staged by each wavefront
-constexpr int PA_WIDE = 128;  // rows of a wide tile
-constexpr int PA_NARROW = 16;
-constexpr int PA_BLOCKS = PA_WIDE / 16;  // 16-row blocks of a wide tile's part
-constexpr int PA_BATCH = PA_THREADS / 4;  // units whose pages are looked up at a time
+constexpr int WIDE_THREADS = 512, WIDE_WAVES = 8, WIDE_KEYS = 64, WIDE_ROWS = 256;
+constexpr int WIDE_LDS = 128 << 10;                   // of staged keys and values
+constexpr int NARROW_THREADS = 256, NARROW_WAVES = 4, NARROW_KEYS = 16, NARROW_ROWS = 16;
+constexpr int WIDE_LEAST = 8, NARROW_LEAST = 8;        // steps of a worker
+constexpr int SLOT_BLOCKS = WIDE_ROWS / 16;           // 16-row blocks of a wide part
 
 // ---------------------------------------------------------------- plan
 
 struct Segment {
-  int tok0, tokens;  // rows: query heads of the group of tokens tok0 ..
+  int tok0, tokens;  // rows: query heads of tokens tok0 ..
   int64_t len;       // keys of every token (prefix), or before token 0 (own)
   int room;          // keys that the table row can list
   const int32_t* table;
@@ -43,10 +49,12 @@ template <typename T>
 AXON_DEV Segment segment_of(const PrefixAttnArgs<T>& a, int s) {
   Segment g;
   const int groups = a.shared.groups;
+  int end;
+  auto among = [](int v, int n) { return min(max(v, 0), n); };
   if (s < groups) {
-    const int lo = a.shared.cu[s], hi = a.shared.cu[s + 1];
+    const int lo = among(a.shared.cu[s], a.seqs.seqs), hi = among(a.shared.cu[s + 1], a.seqs.seqs);
     g.tok0 = a.seqs.cu ? a.seqs.cu[lo] : lo;
-    g.tokens = (a.seqs.cu ? a.seqs.cu[hi] : hi) - g.tok0;
+    end = a.seqs.cu ? a.seqs.cu[hi] : hi;
     g.len = a.shared.lens[s];
     g.table = a.shared.table + (int64_t)s * a.shared.stride;
     g.room = a.shared.stride * a.kv.ps;
@@ -54,43 +62,202 @@ AXON_DEV Segment segment_of(const PrefixAttnArgs<T>& a, int s) {
   } else {
     const int b = s - groups;
     g.tok0 = a.seqs.cu ? a.seqs.cu[b] : b;
-    g.tokens = a.seqs.cu ? a.seqs.cu[b + 1] - g.tok0 : 1;
+    end = a.seqs.cu ? a.seqs.cu[b + 1] : b + 1;
     g.len = a.seqs.lens[b];
     g.table = a.seqs.table + (int64_t)b * a.seqs.stride;
     g.room = a.seqs.stride * a.kv.ps;
     g.own = true;
   }
+  g.tok0 = among(g.tok0, a.tokens);
+  g.tokens = among(end, a.tokens) - g.tok0;
   return g;
 }
-AXON_DEV int tile_rows(int rows) { return rows <= PA_NARROW ? PA_NARROW : PA_WIDE; }
-AXON_DEV int tiles_of(int rows) { return (rows + tile_rows(rows) - 1) / tile_rows(rows); }
-// keys that some row of tile rt reads (G query heads a token)
-AXON_DEV int tile_keys(const Segment& g, int G, int rt) {
+// keys that some of rows ``row0`` .. row0 + n - 1 reads (G query heads a token)
+AXON_DEV int tile_keys(const Segment& g, int G, int row0, int n) {
   if (g.len < 0 || g.tokens <= 0) return 0;
-  int64_t n = g.len;
-  if (g.own) n += min(g.tokens - 1, (rt * PA_WIDE + PA_WIDE - 1) / G) + 1;
-  return (int)min(n, (int64_t)g.room);
+  const int64_t k = g.own ? g.len + min(g.tokens - 1, (row0 + n - 1) / G) + 1 : g.len;
+  return (int)min(k, (int64_t)g.room);
 }
-AXON_DEV int units_of(int keys) { return (keys + PA_KEYS - 1) / PA_KEYS; }
+// keys that row r reads
+AXON_DEV int row_keys(const Segment& g, int G, int r) {
+  return (int)min(g.own ? g.len + r / G + 1 : g.len, (int64_t)g.room);
+}
 
-// the place of a part: blocks of 16 rows, [16][hd] products, 16 maxima, 16 sums
+// The tiles of one kind, their units, and their steps: as many as units, and START more
+// at its beginning that stand for what a tile costs by itself (looking up pages, loading
+// queries, filling the pipeline).  Workers share the steps.
+template <bool WIDE>
+struct Tiles {
+  static constexpr int ROWS = WIDE ? WIDE_ROWS : NARROW_ROWS, KEYS = WIDE ? WIDE_KEYS : NARROW_KEYS;
+  static constexpr int START = 4;
+  static AXON_DEV int of(const Segment& g, int G) {  // of a kv head
+    const int rows = g.tokens * G;
+    return rows > NARROW_ROWS ? (WIDE ? (rows + ROWS - 1) / ROWS : 0) : (WIDE || rows <= 0 ? 0 : 1);
+  }
+  static AXON_DEV int units(const Segment& g, int G, int rt) {
+    return (tile_keys(g, G, rt * ROWS, ROWS) + KEYS - 1) / KEYS;
+  }
+  static AXON_DEV int steps(const Segment& g, int G, int rt) {
+    const int u = units(g, G, rt);
+    return u ? u + START : 0;
+  }
+  // (steps, tiles) of a kv head
+  static AXON_DEV int2 sizes(const Segment& g, int G) {
+    const int n = of(g, G);
+    int u = 0;
+    if (g.own)
+      for (int rt = 0; rt < n; ++rt) u += steps(g, G, rt);
+    else if (n)
+      u = n * steps(g, G, 0);
+    return int2{u, n};
+  }
+};
+
+// where the parts of a tile are: slots first .. first + count - 1
+struct TileParts {
+  int32_t first, count;
+};
+// [prefix, own][kv head][first row of the tile among all tokens' rows]
+AXON_DEV int64_t info_at(bool own, int kvh, int KV, int64_t rows, int tok0, int G, int row0) {
+  return ((own ? KV : 0) + kvh) * rows + (int64_t)tok0 * G + row0;
+}
+// a block of 16 rows of a part: [16][hd] products, 16 maxima, 16 sums
 constexpr int part_floats(int hd) { return 16 * hd + 32; }
 
-// where the parts of the tile that starts at row ``row`` of (kind, kv head) are
-struct TileParts {
-  int32_t first;  // block of the first one, the others PA_BLOCKS apart
-  int32_t count;
+// A place in the order of steps
+struct Place {
+  int s, kvh, rt, step, tile;  // tile: number among all tiles of the kind
+};
+template <int WAVES>
+struct PlanShared {
+  int64_t sum[2][WAVES];
+  int place[WAVES][4];
+  int next[2];
+};
+
+// Steps of all segments (total), and what the threads before this one (segments s0 ..
+// s1 - 1 are its own) have; every thread of the workgroup calls it.
+template <typename T, bool WIDE, int THREADS>
+struct Plan {
+  const PrefixAttnArgs<T>& a;
+  PlanShared<THREADS / 64>& sh;
+  int G, KV, segs, s0, s1;
+  int64_t total, before[2], mine[2];  // steps, tiles
+  AXON_DEV Plan(const PrefixAttnArgs<T>& args, PlanShared<THREADS / 64>& shared) : a(args), sh(shared) {
+    KV = a.kv.kv_heads;
+    G = a.heads / KV;
+    segs = a.shared.groups + a.seqs.seqs;
+    const int each = (segs + THREADS - 1) / THREADS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    s0 = min(segs, (int)threadIdx.x * each);
+    s1 = min(segs, s0 + each);
+    mine[0] = mine[1] = 0;
+    for (int s = s0; s < s1; ++s) {
+      const int2 n = Tiles<WIDE>::sizes(segment_of(a, s), G);
+      mine[0] += (int64_t)n.x * KV;
+      mine[1] += (int64_t)n.y * KV;
+    }
+    int64_t upto[2] = {mine[0], mine[1]};
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int64_t v = __shfl_up(upto[j], d);
+        if (lane >= d) upto[j] += v;
+      }
+    if (lane == 63) {
+      sh.sum[0][wave] = upto[0];
+      sh.sum[1][wave] = upto[1];
+    }
+    __syncthreads();
+    total = 0;
+    before[0] = upto[0] - mine[0];
+    before[1] = upto[1] - mine[1];
+#pragma unroll
+    for (int w = 0; w < THREADS / 64; ++w) {
+      if (w < wave) {
+        before[0] += sh.sum[0][w];
+        before[1] += sh.sum[1][w];
+      }
+      total += sh.sum[0][w];
+    }
+  }
+  // step ``at`` (< total) of worker ``w`` of the workgroup, for get(w) after a barrier
+  AXON_DEV void find(int w, int64_t at) {
+    if (at < before[0] || at >= before[0] + mine[0]) return;  // one thread goes on
+    int64_t u0 = before[0], t0 = before[1];
+    for (int s = s0; s < s1; ++s) {
+      const int2 n = Tiles<WIDE>::sizes(segment_of(a, s), G);
+      if (at < u0 + (int64_t)n.x * KV) {
+        sh.place[w][0] = s;
+        sh.place[w][1] = (int)(at - u0);
+        sh.place[w][2] = (int)t0;
+        sh.place[w][3] = n.x;
+        return;
+      }
+      u0 += (int64_t)n.x * KV;
+      t0 += (int64_t)n.y * KV;
+    }
+  }
+  AXON_DEV Place get(int w, Segment& g) const {
+    Place p;
+    p.s = __builtin_amdgcn_readfirstlane(sh.place[w][0]);
+    const int off = __builtin_amdgcn_readfirstlane(sh.place[w][1]), per = __builtin_amdgcn_readfirstlane(sh.place[w][3]);
+    p.tile = __builtin_amdgcn_readfirstlane(sh.place[w][2]);
+    g = segment_of(a, p.s);
+    p.kvh = off / per;
+    p.step = off % per;
+    p.rt = 0;
+    p.tile += p.kvh * Tiles<WIDE>::of(g, G);
+    for (;;) {
+      const int n = Tiles<WIDE>::steps(g, G, p.rt);
+      if (p.step < n) return p;
+      p.step -= n;
+      ++p.rt;
+      ++p.tile;
+    }
+  }
+  // the next tile that has units (there is one); lane-parallel over segments without any
+  AXON_DEV void advance(Place& p, Segment& g) const {
+    const int lane = threadIdx.x & 63;
+    p.step = 0;
+    for (;;) {
+      ++p.tile;
+      if (++p.rt < Tiles<WIDE>::of(g, G)) {
+        if (Tiles<WIDE>::units(g, G, p.rt)) return;
+        continue;
+      }
+      p.rt = 0;
+      if (++p.kvh < KV) return;  // (the first tile of a segment has units if any has)
+      p.kvh = 0;
+      ++p.s;
+      for (;;) {
+        int2 n = {0, 0};
+        if (p.s + lane < segs) n = Tiles<WIDE>::sizes(segment_of(a, p.s + lane), G);
+        const uint64_t has = __ballot(n.x > 0);
+        const int skip = has ? __ffsll((long long)has) - 1 : 64;
+        int tiles = lane < skip ? n.y : 0;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d);
+        p.tile += __builtin_amdgcn_readfirstlane(tiles) * KV;
+        p.s += skip;
+        if (has || p.s >= segs) break;
+      }
+      p.s = __builtin_amdgcn_readfirstlane(p.s);
+      g = segment_of(a, min(p.s, segs - 1));
+      return;
+    }
+  }
 };
 
 // ---------------------------------------------------------------- tiles in LDS
 
-// A unit's keys and values: [64][HD] each, 16-byte chunks of a row at chunk ^ swizzle,
+// Keys and values of a unit: rows of HD, the 16-byte chunks of a row at chunk ^ swizzle,
 // so that the lanes that read together meet different banks.
 template <typename T, int HD>
 struct Lds {
   static constexpr int CH = HD * sizeof(T) / 16;  // chunks of a row
   static constexpr int EL = 16 / sizeof(T);       // elements of a chunk
-  static constexpr int TILE = PA_KEYS * HD;       // elements of K or V
+  static constexpr int RPI = 64 / CH;             // rows of a wavefront's 16-byte copy
   static AXON_DEV int swz_k(int key) { return (CH >= 16 ? key & 15 : (key >> 1) & 7); }
   static AXON_DEV int swz_v(int key) {
     if (sizeof(T) == 4) return ((key >> 2) & 1) << 3 | ((key >> 3) & 1) << 2;
@@ -98,23 +265,18 @@ struct Lds {
   }
   static AXON_DEV int k_at(int key, int d) { return key * HD + ((d / EL) ^ swz_k(key)) * EL + d % EL; }
   static AXON_DEV int v_at(int key, int d) { return key * HD + ((d / EL) ^ swz_v(key)) * EL + d % EL; }
-};
-
-// copies the 16 keys of this wavefront (rows 16 wave .. of the unit) that start at
-// element ``src`` of both caches into a stage
-template <typename T, int HD>
-AXON_DEV void stage_keys(const T* kc, const T* vc, int64_t src, T* stage, int wave, int lane) {
-  using L = Lds<T, HD>;
-  constexpr int RPI = 64 / L::CH;  // rows of an instruction
+  // rows key0 .. key0 + n - 1 of a unit, which lie one after another at ``src``, to
+  // row 0 .. of ``dst`` (a wavefront's copy)
+  template <bool K>
+  static AXON_DEV void stage(const T* src, T* dst, int key0, int n, int lane) {
 #pragma unroll
-  for (int i = 0; i < 16 / RPI; ++i) {
-    const int r = i * RPI + lane / L::CH, c = lane % L::CH;
-    const int64_t at = src + r * HD;
-    T* dst = stage + (16 * wave + i * RPI) * HD;
-    load_lds16((const bf16*)(kc + at + (c ^ L::swz_k(r)) * L::EL), (bf16x8*)dst);
-    load_lds16((const bf16*)(vc + at + (c ^ L::swz_v(r)) * L::EL), (bf16x8*)(dst + L::TILE));
+    for (int i = 0; i < n / RPI; ++i) {
+      const int r = i * RPI + lane / CH, c = lane % CH;
+      const int sw = K ? swz_k(key0 + r) : swz_v(key0 + r);
+      load_lds16((const bf16*)(src + r * HD + (c ^ sw) * EL), (bf16x8*)(dst + i * RPI * HD));
+    }
   }
-}
+};
 
 // ---------------------------------------------------------------- arithmetic
 
@@ -168,111 +330,119 @@ AXON_DEV f32x4 mul_narrow4(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
+// The transposing LDS reads of read_tr8 for N column blocks at once, rows ``STEP`` bytes
+// apart: r[d][i] from at[d] + i STEP.  As assembly, with their wait: before the builtin
+// the compiler waits for every copy to LDS in flight, the later stages' too (a third of
+// the kernel's time).
+AXON_DEV uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+template <int STEP>
+AXON_DEV void read_tr(const uint32_t (&at)[4], bf16x4 (&r)[4][4]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %2, %16 offset:%21\n\tds_read_b64_tr_b16 %3, %16 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %4, %17\n\tds_read_b64_tr_b16 %5, %17 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %6, %17 offset:%21\n\tds_read_b64_tr_b16 %7, %17 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %8, %18\n\tds_read_b64_tr_b16 %9, %18 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %10, %18 offset:%21\n\tds_read_b64_tr_b16 %11, %18 offset:%22\n\t"
+      "ds_read_b64_tr_b16 %12, %19\n\tds_read_b64_tr_b16 %13, %19 offset:%20\n\t"
+      "ds_read_b64_tr_b16 %14, %19 offset:%21\n\tds_read_b64_tr_b16 %15, %19 offset:%22\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]),
+        "=&v"(r[1][2]), "=&v"(r[1][3]), "=&v"(r[2][0]), "=&v"(r[2][1]), "=&v"(r[2][2]), "=&v"(r[2][3]),
+        "=&v"(r[3][0]), "=&v"(r[3][1]), "=&v"(r[3][2]), "=&v"(r[3][3])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP)
+      : "memory");
+}
+template <int STEP>
+AXON_DEV void read_tr(const uint32_t (&at)[2], bf16x4 (&r)[2][4]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %2, %8 offset:%11\n\tds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %9\n\tds_read_b64_tr_b16 %5, %9 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %6, %9 offset:%11\n\tds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]),
+        "=&v"(r[1][2]), "=&v"(r[1][3])
+      : "v"(at[0]), "v"(at[1]), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP)
+      : "memory");
+}
+// the same, one read of each of 4 or 8 addresses
+AXON_DEV void read_tr(const uint32_t (&at)[4], bf16x4 (&r)[4]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %2, %6\n\t"
+      "ds_read_b64_tr_b16 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3])
+      : "memory");
+}
+AXON_DEV void read_tr(const uint32_t (&at)[8], bf16x4 (&r)[8]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %9\n\tds_read_b64_tr_b16 %2, %10\n\t"
+      "ds_read_b64_tr_b16 %3, %11\n\tds_read_b64_tr_b16 %4, %12\n\tds_read_b64_tr_b16 %5, %13\n\t"
+      "ds_read_b64_tr_b16 %6, %14\n\tds_read_b64_tr_b16 %7, %15\n\ts_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "v"(at[4]), "v"(at[5]), "v"(at[6]), "v"(at[7])
+      : "memory");
+}
+
 AXON_DEV bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
 AXON_DEV bool finite(bf16 v) { return finite((float)v); }
 
-// ---------------------------------------------------------------- the kernel
-
-template <typename T, int HD>
-struct Ctx {
-  const PrefixAttnArgs<T>& a;
-  T* tiles;       // two stages of K and V
-  int32_t* pids;  // pages of a batch of units, 4 to a unit, -1: none
-  int32_t* odd;   // [2][4]: keys of each stage's wavefront whose values were not all finite
-  float* parts;
-  int G, lane, wave;
-  float sc;  // |scale| log2 e
-};
-
 // A masked key has p = 0, but 0 times what stands there is NaN when that is infinite or
-// NaN.  So the values of a unit with masked keys are made finite where they are staged;
-// returns which of the wavefront's 16 keys had others (those that are not masked get
-// them added by add_odd).
+// NaN.  So the values of a unit with masked keys are made finite where they are staged
+// (n rows of a wavefront); returns which rows had others.  Where a row of the tile sees
+// those keys, they are added by add_odd.
 template <typename T, int HD>
-AXON_DEV int make_finite(T* v, int lane) {
-  constexpr int EL = Lds<T, HD>::EL, CH = Lds<T, HD>::CH;
+AXON_DEV int make_finite(T* v, int n, int lane) {
+  using L = Lds<T, HD>;
   typedef typename std::conditional<sizeof(T) == 2, bf16x8, f32x4>::type Chunk;
   int keys = 0;
 #pragma unroll
-  for (int i = 0; i < 16 * CH / 64; ++i) {
+  for (int i = 0; i < n / L::RPI; ++i) {
     Chunk* p = (Chunk*)v + i * 64 + lane;
     Chunk c = *p;
     bool ok = true;
 #pragma unroll
-    for (int j = 0; j < EL; ++j) ok = ok && finite(c[j]);
+    for (int j = 0; j < L::EL; ++j) ok = ok && finite(c[j]);
     const uint64_t odd = __ballot(!ok);
     if (!odd) continue;
     if (!ok) {
 #pragma unroll
-      for (int j = 0; j < EL; ++j) c[j] = finite(c[j]) ? c[j] : (T)0.f;
+      for (int j = 0; j < L::EL; ++j) c[j] = finite(c[j]) ? c[j] : (T)0.f;
       *p = c;
     }
 #pragma unroll
-    for (int r = 0; r < 64 / CH; ++r)
-      if (odd >> (r * CH) & ((1ull << (CH - 1) << 1) - 1)) keys |= 1 << (i * (64 / CH) + r);
+    for (int r = 0; r < L::RPI; ++r)
+      if (odd >> (r * L::CH) & ((1ull << (L::CH - 1) << 1) - 1)) keys |= 1 << (i * L::RPI + r);
   }
   return keys;
 }
 
-// Runs f(u, stage, pages, odd) over units first .. last - 1 of a segment (64 keys each,
-// from key 64 u): the stage that holds them, which of its 16-key blocks have a page, and
-// which of its keys make_finite changed.  Keys from ``least`` on are masked for some row.
-// barrier: f reads all of a unit's keys, not only the 16 that the wavefront staged.
-template <typename T, int HD, typename F>
-AXON_DEV void for_units(const Ctx<T, HD>& x, const Segment& g, int kvh, int first, int last, int least, bool barrier,
-                        F&& f) {
-  constexpr int TILE = Lds<T, HD>::TILE;
-  const auto& kv = x.a.kv;
-  for (int u0 = first; u0 < last; u0 += PA_BATCH) {
-    const int n = min(last - u0, PA_BATCH);
-    __syncthreads();  // the stages and pages of what came before are read
-    {
-      const int key = (u0 * 4 + (int)threadIdx.x) * 16;
-      int page = -1;
-      if ((int)threadIdx.x < 4 * n && key < g.room) page = g.table[key / kv.ps];
-      x.pids[threadIdx.x] = page >= 0 && page < kv.num_pages ? page : -1;
-    }
-    __syncthreads();
-    auto stage = [&](int i) {
-      const int key = (u0 + i) * PA_KEYS + 16 * x.wave;
-      const int page = max(__builtin_amdgcn_readfirstlane(x.pids[4 * i + x.wave]), 0);  // (none: masked, but read)
-      const int64_t src = (((int64_t)page * kv.kv_heads + kvh) * kv.ps + key % kv.ps) * HD;
-      stage_keys<T, HD>((const T*)kv.k, (const T*)kv.v, src, x.tiles + (i & 1) * 2 * TILE, x.wave, x.lane);
-    };
-    stage(0);
-    for (int i = 0; i < n; ++i) {
-      T* st = x.tiles + (i & 1) * 2 * TILE;
-      int pages = 0;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) pages |= (x.pids[4 * i + j] >= 0) << j;
-      pages = __builtin_amdgcn_readfirstlane(pages);
-      const bool masked = (u0 + i) * PA_KEYS + PA_KEYS > least || pages != 15;
-      // (the unit is here; what was read of the stage that is filled next as well)
-      asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-      if (masked) {
-        const int odd = make_finite<T, HD>(st + TILE + 16 * x.wave * HD, x.lane);
-        if (x.lane == 0) x.odd[4 * (i & 1) + x.wave] = odd;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      }
-      if (barrier) phase_barrier();
-      if (i + 1 < n) stage(i + 1);
-      f(u0 + i, st, pages, masked ? x.odd + 4 * (i & 1) : nullptr);
-    }
+template <typename T, int HD>
+struct Cache {
+  const PrefixAttnArgs<T>& a;
+  const Segment& g;
+  int kvh;
+  // page of a key, -1: none
+  AXON_DEV int page(int key) const {
+    const int p = key < g.room ? g.table[key / a.kv.ps] : -1;
+    return p >= 0 && p < a.kv.num_pages ? p : -1;
   }
-}
+  AXON_DEV int64_t at(int page, int key) const {
+    return (((int64_t)page * a.kv.kv_heads + kvh) * a.kv.ps + key % a.kv.ps) * HD;
+  }
+};
 
-// Adds the infinite and NaN values that make_finite took out of block ``blk`` of unit u
-// where the lane's row sees their keys: o[i], i < N, is dimension dim(i).
+// Adds the infinite and NaN values of keys key0 + (bits of odd) where the lane's row sees
+// them: o[i], i < N, is dimension dim(i).
 template <typename T, int HD, int N, typename D>
-AXON_DEV void add_odd(const Ctx<T, HD>& x, const Segment& g, int kvh, int u, int blk, int odd, int limit, float (&o)[N],
-                      D&& dim) {
-  const auto& kv = x.a.kv;
+AXON_DEV void add_odd(const Cache<T, HD>& c, int key0, int odd, int limit, float (&o)[N], D&& dim) {
   for (; odd; odd &= odd - 1) {
-    const int key = u * PA_KEYS + 16 * blk + __ffs(odd) - 1;
+    const int key = key0 + __ffs(odd) - 1;
     if (key >= limit) continue;
-    const int page = g.table[key / kv.ps];
-    if (page < 0 || page >= kv.num_pages) continue;
-    const T* v = (const T*)kv.v + (((int64_t)page * kv.kv_heads + kvh) * kv.ps + key % kv.ps) * HD;
+    const int page = c.page(key);
+    if (page < 0) continue;
+    const T* v = (const T*)c.a.kv.v + c.at(page, key);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float e = to_f32(v[dim(i)]);
@@ -281,115 +451,184 @@ AXON_DEV void add_odd(const Ctx<T, HD>& x, const Segment& g, int kvh, int u, int
   }
 }
 
-// Row r of a tile's segment as an element of q: its token and head
+// Row r of a segment as it lies in q
 template <typename T, int HD>
-AXON_DEV const T* q_row(const Ctx<T, HD>& x, const Segment& g, int kvh, int r) {
-  return x.a.q + (int64_t)(g.tok0 + r / x.G) * x.a.ldq + (int64_t)(kvh * x.G + r % x.G) * HD;
-}
-// keys that row r sees
-template <typename T, int HD>
-AXON_DEV int row_limit(const Ctx<T, HD>& x, const Segment& g, int r) {
-  return (int)min(g.own ? g.len + r / x.G + 1 : g.len, (int64_t)g.room);
+AXON_DEV const T* q_row(const PrefixAttnArgs<T>& a, const Segment& g, int G, int kvh, int r) {
+  return a.q + (int64_t)(g.tok0 + r / G) * a.ldq + (int64_t)(kvh * G + r % G) * HD;
 }
 
+// The reference m of a row's weights 2^(score - m): the running maximum (in base 2, times
+// the scale), or up to 8 less, so that the sum and the products are hardly rescaled after
+// the first keys (a weight is 256 at most).
+template <int N, typename V>
+AXON_DEV void raise(float& m, float top, float& l, V (&o)[N]) {
+  if (!__any(top > m + 8.f)) return;
+  const float m_new = fmaxf(m, top);
+  const float fall = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
+  m = m_new;
+  l *= fall;
+#pragma unroll
+  for (int d = 0; d < N; ++d) o[d] *= fall;
+}
+
+// ---------------------------------------------------------------- wide tiles
+
 template <typename T, int HD>
-AXON_DEV void wide_tile(const Ctx<T, HD>& x, const Segment& g, int kvh, int rt, int first, int last, int block) {
+struct Wide {
+  using L = Lds<T, HD>;
+  static constexpr int TILE = WIDE_KEYS * HD, STAGES = WIDE_LDS / (2 * TILE * (int)sizeof(T));
+  static constexpr int MY_KEYS = WIDE_KEYS / WIDE_WAVES;     // staged by a wavefront
+  static constexpr int LOADS = 2 * (MY_KEYS / L::RPI);       // its copies
+  static constexpr int BATCH = WIDE_THREADS / 4;             // units whose pages are looked up at a time
+  struct Shared {
+    alignas(16) T tiles[STAGES][2][TILE];
+    int32_t pids[WIDE_THREADS];        // pages of a batch, 4 a unit, -1: none
+    int32_t odd[STAGES][WIDE_WAVES];   // make_finite's rows
+    PlanShared<WIDE_WAVES> plan;
+  };
+};
+
+// Units first .. last - 1 of a tile of ``rows`` rows from row0 on; the part of key group
+// k goes to blocks part + k groups' rows / 16.
+template <typename T, int HD>
+AXON_DEV void wide_tile(const PrefixAttnArgs<T>& a, float sc, typename Wide<T, HD>::Shared& sh, const Segment& g, int G,
+                        int kvh, int row0, int first, int last, float* part) {
+  using W = Wide<T, HD>;
   using L = Lds<T, HD>;
   using V8 = typename Vec8<T>::t;
   constexpr int DT = HD / 32, QS = HD / 16;
-  const int hl = x.lane >> 5, c = x.lane & 31;
-  const int rows = g.tokens * x.G, r0 = rt * PA_WIDE + 32 * x.wave, r = min(r0 + c, rows - 1);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int hl = lane >> 5, c = lane & 31;
+  const int rows = g.tokens * G, here = min(rows - row0, WIDE_ROWS);
+  // up to 128 rows: two groups of 4 wavefronts, each half of a unit's keys
+  const bool halves = here <= WIDE_ROWS / 2;
+  const int kgroup = halves ? wave >> 2 : 0, r0 = row0 + 32 * (halves ? wave & 3 : wave), r = min(r0 + c, rows - 1);
+  const bool works = r0 < rows;
+  const Cache<T, HD> cache{a, g, kvh};
   V8 q[QS];
   {
-    const T* p = q_row(x, g, kvh, r) + 8 * hl;
+    const T* p = q_row<T, HD>(a, g, G, kvh, r) + 8 * hl;
 #pragma unroll
-    for (int k = 0; k < QS; ++k) q[k] = load_q8<T>(p + 16 * k, x.a.scale < 0.f);
+    for (int k = 0; k < QS; ++k) q[k] = load_q8<T>(p + 16 * k, a.scale < 0.f);
   }
-  const int limit = row_limit(x, g, r);
-  const int least = row_limit(x, g, min(r0, rows - 1)), most = row_limit(x, g, min(r0 + 31, rows - 1));
+  const int limit = row_keys(g, G, r), least = row_keys(g, G, min(r0, rows - 1));
+  const int most = row_keys(g, G, min(r0 + 31, rows - 1)), tile_least = row_keys(g, G, row0);
   f32x16 o[DT] = {};
-  float m = -INFINITY, l = 0.f;  // m: the largest score times sc
-  for_units(x, g, kvh, first, last, row_limit(x, g, rt * PA_WIDE), true, [&](int u, const T* st, int pages, const int* odd) {
-    const int key0 = u * PA_KEYS;
-    if (r0 >= rows || key0 >= most) return;
-    f32x16 s[2] = {};
+  float m = -INFINITY, l = 0.f;
+  for (int u0 = first; u0 < last; u0 += W::BATCH) {
+    const int n = min(last - u0, W::BATCH);
+    __syncthreads();  // the stages and pages of what came before are read
+    if ((int)threadIdx.x < 4 * n) sh.pids[threadIdx.x] = cache.page((4 * u0 + (int)threadIdx.x) * 16);
+    __syncthreads();
+    auto stage = [&](int i) {
+      const int in_unit = W::MY_KEYS * wave, key = (u0 + i) * WIDE_KEYS + in_unit;
+      const int page = max(__builtin_amdgcn_readfirstlane(sh.pids[4 * i + in_unit / 16]), 0);  // (none: masked, but read)
+      const int64_t src = cache.at(page, key);
+      T* dst = sh.tiles[i % W::STAGES][0] + in_unit * HD;
+      L::template stage<true>((const T*)a.kv.k + src, dst, in_unit, W::MY_KEYS, lane);
+      L::template stage<false>((const T*)a.kv.v + src, dst + W::TILE, in_unit, W::MY_KEYS, lane);
+    };
+    for (int i = 0; i < W::STAGES - 1 && i < n; ++i) stage(i);
+    for (int i = 0; i < n; ++i) {
+      const int key0 = (u0 + i) * WIDE_KEYS, at = i % W::STAGES;
+      int pages = 0;  // which of the 16-key blocks exist
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int k = 0; k < QS; ++k) {
-        const int d = 16 * k + 8 * hl;
-        s[kb] = mul_wide(read8(st + L::k_at(32 * kb + c, d), st + L::k_at(32 * kb + c, d + 4)), q[k], s[kb]);
+      for (int j = 0; j < 4; ++j) pages |= (sh.pids[4 * i + j] >= 0) << j;
+      pages = __builtin_amdgcn_readfirstlane(pages);
+      const bool tile_masked = key0 + WIDE_KEYS > tile_least || pages != 15;
+      // the unit is here (later ones may not be), and what was read of the stage that is
+      // filled next as well
+      wait_loads<W::LOADS, W::STAGES - 2>(min(n - 1 - i, W::STAGES - 2));
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (tile_masked) {
+        const int odd = make_finite<T, HD>(sh.tiles[at][1] + W::MY_KEYS * wave * HD, W::MY_KEYS, lane);
+        if (lane == 0) sh.odd[at][wave] = odd;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       }
-    // s[kb][i]: key key0 + 32 kb + 8 (i / 4) + 4 hl + i % 4, row c
-    const bool masked = key0 + PA_KEYS > least || pages != 15;
-    if (masked) {
+      phase_barrier();
+      if (i + W::STAGES - 1 < n) stage(i + W::STAGES - 1);
+      if (!works || key0 >= most) continue;
+      const T *ks = sh.tiles[at][0], *vs = sh.tiles[at][1];
+      const bool masked = key0 + WIDE_KEYS > least || pages != 15;
+#pragma unroll 1
+      for (int kb = halves ? kgroup : 0; kb < (halves ? kgroup + 1 : 2); ++kb) {
+        // the LDS reads of a product stand together before it: one at a time, each matrix
+        // instruction waited for its operand
+        V8 kf[QS];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * kb + 8 * (i >> 2) + 4 * hl + (i & 3);
-          if (key0 + key >= limit || !(pages >> (key >> 4) & 1)) s[kb][i] = -INFINITY;
+        for (int k = 0; k < QS; ++k) {
+          const int d = 16 * k + 8 * hl;
+          kf[k] = read8(ks + L::k_at(32 * kb + c, d), ks + L::k_at(32 * kb + c, d + 4));
         }
-    }
-    float top = -INFINITY;
+        if (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
+        f32x16 s = {};
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-    top = fmaxf(top, lane_xor32(top)) * x.sc;
-    const float m_new = fmaxf(m, top);
-    const float base = m_new == -INFINITY ? 0.f : m_new;
-    const float fall = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    l *= fall;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] *= fall;
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
-      f32x16 p;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], x.sc, -base));
-        l += p[i];
-      }
-      if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {  // keys 16 e .. of the block
-          bf16x8 pb;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) pb[j] = (bf16)p[8 * e + j];
-#pragma unroll
-          for (int d = 0; d < DT; ++d) {
-            const int key = 32 * kb + 16 * e + 4 * hl + ((x.lane & 15) >> 2);
-            const int dim = 32 * d + 16 * ((x.lane >> 4) & 1) + 4 * (x.lane & 3);
-            o[d] = mul_wide(read_tr8(st + L::TILE + L::v_at(key, dim), st + L::TILE + L::v_at(key + 8, dim)), pb, o[d]);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * kb + 8 * (i >> 2) + 4 * hl + (i & 3);
+        for (int k = 0; k < QS; ++k) s = mul_wide(kf[k], q[k], s);
+        bf16x4 vf[DT][4];  // keys 8 i + 4 hl .. of the block; read under the product
+        if constexpr (sizeof(T) == 2) {
+          uint32_t at[DT];
 #pragma unroll
           for (int d = 0; d < DT; ++d)
-            o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(st[L::TILE + L::v_at(key, 32 * d + c)], p[i], o[d], 0, 0, 0);
+            at[d] = lds_address(vs + L::v_at(32 * kb + 4 * hl + ((lane & 15) >> 2), 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)));
+          __builtin_amdgcn_sched_barrier(0);
+          read_tr<8 * HD * 2>(at, vf);
         }
+        // s[i]: key key0 + 32 kb + 8 (i / 4) + 4 hl + i % 4, row c
+        if (masked) {
+          const int seen = limit - key0 - 32 * kb - 4 * hl;
+          const int seen0 = pages >> (2 * kb) & 1 ? seen : 0, seen1 = pages >> (2 * kb + 1) & 1 ? seen : 0;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < (i < 8 ? seen0 : seen1) ? s[i] : -INFINITY;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        raise(m, fmaxf(top, lane_xor32(top)) * sc, l, o);
+        const float base = m == -INFINITY ? 0.f : m;
+        f32x16 p;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -base));
+          sum += p[i];
+        }
+        l += sum;
+        if constexpr (sizeof(T) == 2) {
+          bf16x8 pb[2];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pb[i / 8][i % 8] = (bf16)p[i];
+#pragma unroll
+          for (int e = 0; e < 2; ++e)  // keys 16 e .. of the block
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+              o[d] = mul_wide(__builtin_shufflevector(vf[d][2 * e], vf[d][2 * e + 1], 0, 1, 2, 3, 4, 5, 6, 7), pb[e], o[d]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int key = 32 * kb + 8 * (i >> 2) + 4 * hl + (i & 3);
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vs[L::v_at(key, 32 * d + c)], p[i], o[d], 0, 0, 0);
+          }
+        }
+        if (tile_masked)
+          for (int w = 32 / W::MY_KEYS * kb; w < 32 / W::MY_KEYS * (kb + 1); ++w)
+            if (const int odd = __builtin_amdgcn_readfirstlane(sh.odd[at][w])) {
+              float e[16 * DT];
+#pragma unroll
+              for (int i = 0; i < 16 * DT; ++i) e[i] = o[i / 16][i % 16];
+              add_odd(cache, key0 + W::MY_KEYS * w, odd, limit, e,
+                      [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hl + i % 4; });
+#pragma unroll
+              for (int i = 0; i < 16 * DT; ++i) o[i / 16][i % 16] = e[i];
+            }
       }
     }
-    if (odd)
-      for (int blk = 0; blk < 4; ++blk)
-        if (const int keys = __builtin_amdgcn_readfirstlane(odd[blk])) {
-          float e[16 * DT];
-#pragma unroll
-          for (int i = 0; i < 16 * DT; ++i) e[i] = o[i / 16][i % 16];
-          add_odd(x, g, kvh, u, blk, keys, limit, e, [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hl + i % 4; });
-#pragma unroll
-          for (int i = 0; i < 16 * DT; ++i) o[i / 16][i % 16] = e[i];
-        }
-  });
+  }
   if (r0 + c >= rows) return;
   l += lane_xor32(l);
-  float* part = x.parts + (int64_t)(block + 2 * x.wave + (c >> 4)) * part_floats(HD);
-  const int row = c & 15;
+  const int block = (halves ? 8 * kgroup + 2 * (wave & 3) : 2 * wave) + (c >> 4), row = c & 15;
+  part += (int64_t)block * part_floats(HD);
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -401,32 +640,139 @@ AXON_DEV void wide_tile(const Ctx<T, HD>& x, const Segment& g, int kvh, int rt, 
   }
 }
 
+// Worker w of n takes steps total w / n .. total (w + 1) / n - 1: as many as there are,
+// unless that leaves one too little to be worth the part it writes.
+AXON_DEV int workers(int most, int64_t total, int least) {
+  return (int)max(min((int64_t)most, total / least), min(total, (int64_t)1));
+}
+AXON_DEV int worker_of(int64_t step, int64_t total, int n) { return (int)(((step + 1) * n - 1) / total); }
+
+// What worker ``me`` does of the tile at p (its steps at .. at + take - 1): units first ..
+// last - 1; the one with the tile's first unit notes where the parts are.
+struct Work {
+  int take, first, last;
+};
+template <bool WIDE, int HD, typename T>
+AXON_DEV Work work_of(const PrefixAttnArgs<T>& a, const Segment& g, const Place& p, int G, int KV, int64_t at, int64_t end,
+                      int64_t total, int me, int n, TileParts* info, bool leader) {
+  constexpr int START = Tiles<WIDE>::START;
+  const int steps = Tiles<WIDE>::steps(g, G, p.rt);
+  Work w;
+  w.take = (int)min((int64_t)(steps - p.step), end - at);
+  w.first = max(p.step - START, 0);
+  w.last = max(p.step + w.take - START, 0);
+  if (leader && p.step <= START && w.last > 0)
+    info[info_at(g.own, p.kvh, KV, (int64_t)a.tokens * G, g.tok0, G, p.rt * Tiles<WIDE>::ROWS)] =
+        TileParts{p.tile + me, worker_of(at - p.step + steps - 1, total, n) - me + 1};
+  return w;
+}
+
 template <typename T, int HD>
-AXON_DEV void narrow_tile(const Ctx<T, HD>& x, const Segment& g, int kvh, int first, int last, int block) {
+__global__ void __launch_bounds__(WIDE_THREADS, 2) prefix_wide_kernel(PrefixAttnArgs<T> a, float sc, TileParts* info,
+                                                                      float* parts, int slots) {
+  __shared__ typename Wide<T, HD>::Shared sh;
+  Plan<T, true, WIDE_THREADS> plan(a, sh.plan);
+  const int G = plan.G, KV = plan.KV;
+  // Consecutive runs on one XCD, whose L2 holds what they share; fewer workers than
+  // workgroups: over all XCDs.
+  const int n = workers(gridDim.x, plan.total, WIDE_LEAST);
+  const int me = n < (int)gridDim.x || n % 8 ? blockIdx.x : blockIdx.x % 8 * (n / 8) + blockIdx.x / 8;
+  if (me >= n) return;
+  int64_t at = plan.total * me / n;
+  const int64_t end = plan.total * (me + 1) / n;
+  plan.find(0, at);
+  __syncthreads();
+  Segment g;
+  Place p = plan.get(0, g);
+  for (;;) {
+    const int slot = p.tile + me;
+    if (slot >= slots) return;  // (cu_seqlens are not those of the host)
+    const Work w = work_of<true, HD>(a, g, p, G, KV, at, end, plan.total, me, n, info, threadIdx.x == 0);
+    if (w.last > w.first)
+      wide_tile<T, HD>(a, sc, sh, g, G, p.kvh, p.rt * WIDE_ROWS, w.first, w.last,
+                       parts + (int64_t)slot * SLOT_BLOCKS * part_floats(HD));
+    at += w.take;
+    if (at >= end) return;
+    plan.advance(p, g);
+  }
+}
+
+// ---------------------------------------------------------------- narrow tiles
+
+template <typename T, int HD>
+struct Narrow {
+  using L = Lds<T, HD>;
+  static constexpr int TILE = NARROW_KEYS * HD, QS = HD / 32;
+  static constexpr int LOADS = NARROW_KEYS / L::RPI + QS * (int)sizeof(T) / 2;  // of a unit
+  struct Shared {
+    alignas(16) T v[NARROW_WAVES][2][TILE];
+    PlanShared<NARROW_WAVES> plan;
+  };
+};
+
+// Units first .. last - 1 of a tile, by one wavefront: keys to registers, where a lane
+// has those of one key that multiply its dimensions, values through LDS, a unit ahead.
+template <typename T, int HD>
+AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[2][Narrow<T, HD>::TILE], const Segment& g, int G,
+                          int kvh, int first, int last, float* part) {
+  using N = Narrow<T, HD>;
   using L = Lds<T, HD>;
   using V8 = typename Vec8<T>::t;
-  constexpr int DT = HD / 16, QS = HD / 32;
-  const int gq = x.lane >> 4, c = x.lane & 15;
-  const int rows = g.tokens * x.G, r = min(c, rows - 1);
-  V8 q[QS];
-  {
-    const T* p = q_row(x, g, kvh, r) + 8 * gq;
+  constexpr int DT = HD / 16, QS = N::QS;
+  const int lane = threadIdx.x & 63, gq = lane >> 4, c = lane & 15;
+  const int rows = g.tokens * G, r = min(c, rows - 1);
+  const Cache<T, HD> cache{a, g, kvh};
+  int pages = 0;  // of units u & ~63 .., one a lane
+  V8 q[QS], k[2][QS];
+  auto look_up = [&](int u0) { pages = u0 + lane < last ? cache.page((u0 + lane) * NARROW_KEYS) : -1; };
+  auto page_of = [&](int u) { return __builtin_amdgcn_readlane(pages, (u - first) & 63); };
+  auto fetch = [&](int u, int b) {
+    const int64_t src = cache.at(max(page_of(u), 0), u * NARROW_KEYS);  // (none: masked, but read)
+    L::template stage<false>((const T*)a.kv.v + src, lds[b], 0, NARROW_KEYS, lane);
+    const T* kp = (const T*)a.kv.k + src + c * HD + 8 * gq;
 #pragma unroll
-    for (int k = 0; k < QS; ++k) q[k] = load_q8<T>(p + 32 * k, x.a.scale < 0.f);
+    for (int j = 0; j < QS; ++j) k[b][j] = read8(kp + 32 * j, kp + 32 * j + 4);
+  };
+  look_up(first);
+  {
+    const T* p = q_row<T, HD>(a, g, G, kvh, r) + 8 * gq;
+#pragma unroll
+    for (int j = 0; j < QS; ++j) q[j] = load_q8<T>(p + 32 * j, a.scale < 0.f);
   }
-  const int limit = row_limit(x, g, r), least = row_limit(x, g, 0);
+  const int limit = row_keys(g, G, r), least = row_keys(g, G, 0);
   f32x4 o[DT] = {};
   float m = -INFINITY, l = 0.f;
-  for_units(x, g, kvh, first, last, least, false, [&](int u, const T* st, int pages, const int* odd) {
-    const int mine = 16 * x.wave, key0 = u * PA_KEYS + mine;
+  fetch(first, 0);
+  auto unit = [&](int u, const int b) {
+    const int key0 = u * NARROW_KEYS;
+    const bool there = page_of(u) >= 0, masked = key0 + NARROW_KEYS > least || !there;
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stage that is filled next is read)
+    if (u + 1 < last) {
+      if (((u + 1 - first) & 63) == 0) look_up(u + 1);
+      fetch(u + 1, b ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N::LOADS) : "memory");
+    } else {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+    T* vs = lds[b];
+    const int odd = masked ? make_finite<T, HD>(vs, NARROW_KEYS, lane) : 0;
     f32x4 s = {};
 #pragma unroll
-    for (int k = 0; k < QS; ++k) {
-      const int d = 32 * k + 8 * gq;
-      s = mul_narrow(read8(st + L::k_at(mine + c, d), st + L::k_at(mine + c, d + 4)), q[k], s);
+    for (int j = 0; j < QS; ++j) s = mul_narrow(k[b][j], q[j], s);
+    typename std::conditional<sizeof(T) == 2, bf16x4, f32x4>::type p, v[DT];
+    if constexpr (sizeof(T) == 2) {
+      uint32_t at[DT];
+#pragma unroll
+      for (int d = 0; d < DT; ++d) at[d] = lds_address(vs + L::v_at(4 * gq + (c >> 2), 16 * d + 4 * (c & 3)));
+      __builtin_amdgcn_sched_barrier(0);
+      read_tr(at, v);
+    } else {
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[d][i] = vs[L::v_at(4 * gq + i, 16 * d + c)];
     }
     // s[i]: key key0 + 4 gq + i, row c
-    const bool there = pages >> x.wave & 1, masked = key0 + 16 > least || !there;
     if (masked) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -434,236 +780,88 @@ AXON_DEV void narrow_tile(const Ctx<T, HD>& x, const Segment& g, int kvh, int fi
     }
     float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     top = fmaxf(top, lane_xor16(top));
-    top = fmaxf(top, lane_xor32(top)) * x.sc;
-    const float m_new = fmaxf(m, top);
-    const float base = m_new == -INFINITY ? 0.f : m_new;
-    const float fall = __builtin_amdgcn_exp2f(m - base);
-    m = m_new;
-    l *= fall;
-#pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] *= fall;
-    typename std::conditional<sizeof(T) == 2, bf16x4, f32x4>::type p;
+    raise(m, fmaxf(top, lane_xor32(top)) * sc, l, o);
+    const float base = m == -INFINITY ? 0.f : m;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float e = __builtin_amdgcn_exp2f(fmaf(s[i], x.sc, -base));
+      const float e = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -base));
       l += e;
       p[i] = from_f32<T>(e);
     }
 #pragma unroll
-    for (int d = 0; d < DT; ++d) {
-      decltype(p) v;
-      if constexpr (sizeof(T) == 2) {
-        typedef __attribute__((address_space(3))) bf16x4 lds4;
-        v = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(
-            (lds4*)(st + L::TILE + L::v_at(mine + 4 * gq + (c >> 2), 16 * d + 4 * (c & 3))));
-      } else {
+    for (int d = 0; d < DT; ++d) o[d] = mul_narrow4(v[d], p, o[d]);
+    if (odd) {
+      float e[4 * DT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = st[L::TILE + L::v_at(mine + 4 * gq + i, 16 * d + c)];
-      }
-      o[d] = mul_narrow4(v, p, o[d]);
+      for (int i = 0; i < 4 * DT; ++i) e[i] = o[i / 4][i % 4];
+      add_odd(cache, key0, there ? odd : 0, limit, e, [&](int i) { return 16 * (i / 4) + 4 * gq + i % 4; });
+#pragma unroll
+      for (int i = 0; i < 4 * DT; ++i) o[i / 4][i % 4] = e[i];
     }
-    if (odd)
-      if (const int keys = __builtin_amdgcn_readfirstlane(odd[x.wave])) {
-        float e[4 * DT];
-#pragma unroll
-        for (int i = 0; i < 4 * DT; ++i) e[i] = o[i / 4][i % 4];
-        add_odd(x, g, kvh, u, x.wave, keys, limit, e, [&](int i) { return 16 * (i / 4) + 4 * gq + i % 4; });
-#pragma unroll
-        for (int i = 0; i < 4 * DT; ++i) o[i / 4][i % 4] = e[i];
-      }
-  });
+  };
+  for (int u = first; u < last; u += 2) {
+    unit(u, 0);
+    if (u + 1 < last) unit(u + 1, 1);
+  }
   l += lane_xor16(l);
   l += lane_xor32(l);
-  // the four wavefronts' keys
-  float* so = (float*)x.tiles;  // [4][16][HD]
-  float* sm = so + 4 * 16 * HD;  // [4][16] maxima, then sums
-  __syncthreads();
+  if (c >= rows) return;
 #pragma unroll
-  for (int d = 0; d < DT; ++d) *(f32x4*)(so + (x.wave * 16 + c) * HD + 16 * d + 4 * gq) = o[d];
+  for (int d = 0; d < DT; ++d) *(f32x4*)(part + c * HD + 16 * d + 4 * gq) = o[d];
   if (gq == 0) {
-    sm[x.wave * 16 + c] = m;
-    sm[64 + x.wave * 16 + c] = l;
-  }
-  __syncthreads();
-  float* part = x.parts + (int64_t)block * part_floats(HD);
-  for (int i = threadIdx.x; i < rows * HD / 4; i += PA_THREADS) {
-    const int row = i / (HD / 4), d = i % (HD / 4) * 4;
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w * 16 + row]);
-    f32x4 sum = {};
-    float ls = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w * 16 + row] - top);
-      ls += f * sm[64 + w * 16 + row];
-      if (f > 0.f) sum += f * *(const f32x4*)(so + (w * 16 + row) * HD + d);
-    }
-    *(f32x4*)(part + row * HD + d) = sum;
-    if (d == 0) {
-      part[16 * HD + row] = top;
-      part[16 * HD + 16 + row] = ls;
-    }
+    part[16 * HD + c] = m;
+    part[16 * HD + 16 + c] = l;
   }
 }
 
 template <typename T, int HD>
-constexpr int stage_bytes() {
-  // two stages; a narrow tile's join needs [4][16][HD] + 128 floats
-  const int tiles = 2 * 2 * PA_KEYS * HD * (int)sizeof(T), join = (64 * HD + 128) * 4;
-  return tiles > join ? tiles : join;
+__global__ void __launch_bounds__(NARROW_THREADS, 3) prefix_narrow_kernel(PrefixAttnArgs<T> a, float sc, TileParts* info,
+                                                                          float* parts, int slots) {
+  __shared__ typename Narrow<T, HD>::Shared sh;
+  Plan<T, false, NARROW_THREADS> plan(a, sh.plan);
+  const int G = plan.G, KV = plan.KV, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // a wavefront is a worker; as the wide kernel's otherwise
+  const int grid = gridDim.x * NARROW_WAVES, n = workers(grid, plan.total, NARROW_LEAST);
+  const int wg = n < grid || gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+  // (fewer workers than wavefronts: spread over the workgroups)
+  auto worker = [&](int w) { return n < grid ? w * (int)gridDim.x + wg : wg * NARROW_WAVES + w; };
+  for (int w = 0; w < NARROW_WAVES; ++w)
+    if (worker(w) < n) plan.find(w, plan.total * worker(w) / n);
+  __syncthreads();
+  const int me = worker(wave);
+  if (me >= n) return;
+  int64_t at = plan.total * me / n;
+  const int64_t end = plan.total * (me + 1) / n;
+  Segment g;
+  Place p = plan.get(wave, g);
+  for (;;) {
+    const int slot = p.tile + me;
+    if (slot >= slots) return;
+    const Work w = work_of<false, HD>(a, g, p, G, KV, at, end, plan.total, me, n, info, (threadIdx.x & 63) == 0);
+    if (w.last > w.first)
+      narrow_tile<T, HD>(a, sc, sh.v[wave], g, G, p.kvh, w.first, w.last, parts + (int64_t)slot * part_floats(HD));
+    at += w.take;
+    if (at >= end) return;
+    plan.advance(p, g);
+  }
 }
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(PA_THREADS, 2) prefix_attn_kernel(PrefixAttnArgs<T> a, float sc, TileParts* info,
-                                                                 float* parts) {
-  __shared__ __align__(16) char lds[stage_bytes<T, HD>()];
-  __shared__ int32_t pids[PA_THREADS], odd[8];
-  __shared__ int64_t scan[2][PA_THREADS / 64];
-  __shared__ int start[4];
-  const int KV = a.kv.kv_heads, G = a.heads / KV, segs = a.shared.groups + a.seqs.seqs;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // units and part blocks of each thread's segments, and before them
-  const int each = (segs + PA_THREADS - 1) / PA_THREADS, s0 = min(segs, (int)threadIdx.x * each), s1 = min(segs, s0 + each);
-  auto sizes = [&](const Segment& g, int& units, int& blocks) {  // of one kv head
-    const int rows = g.tokens * G, tiles = tiles_of(rows);
-    units = 0;
-    if (g.own && tiles > 1)
-      for (int rt = 0; rt < tiles; ++rt) units += units_of(tile_keys(g, G, rt));
-    else
-      units = tiles * units_of(tile_keys(g, G, tiles - 1));
-    blocks = tiles * (tile_rows(rows) / 16);
-  };
-  int64_t mine[2] = {};
-  for (int s = s0; s < s1; ++s) {
-    int u, b;
-    sizes(segment_of(a, s), u, b);
-    mine[0] += (int64_t)u * KV;
-    mine[1] += (int64_t)b * KV;
-  }
-  int64_t upto[2] = {mine[0], mine[1]};
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int64_t v = __shfl_up(upto[j], d);
-      if (lane >= d) upto[j] += v;
-    }
-  if (lane == 63) {
-    scan[0][wave] = upto[0];
-    scan[1][wave] = upto[1];
-  }
-  __syncthreads();
-  int64_t total = 0, before[2] = {upto[0] - mine[0], upto[1] - mine[1]};
-#pragma unroll
-  for (int w = 0; w < PA_THREADS / 64; ++w) {
-    if (w < wave) {
-      before[0] += scan[0][w];
-      before[1] += scan[1][w];
-    }
-    total += scan[0][w];
-  }
-  // Consecutive runs on one XCD, whose L2 holds what they share; fewer units than
-  // workgroups: one each, over all XCDs.
-  const int n = (int)min((int64_t)gridDim.x, total);
-  const int wg = n < (int)gridDim.x || n % 8 ? blockIdx.x : blockIdx.x % 8 * (n / 8) + blockIdx.x / 8;
-  if (wg >= n) return;
-  int64_t at = total * wg / n;
-  const int64_t end = total * (wg + 1) / n;
-  if (before[0] <= at && at < before[0] + mine[0]) {  // one thread
-    int64_t u0 = before[0], b0 = before[1];
-    for (int s = s0; s < s1; ++s) {
-      int u, b;
-      sizes(segment_of(a, s), u, b);
-      if (at < u0 + (int64_t)u * KV) {
-        start[0] = s;
-        start[1] = (int)(at - u0);
-        start[2] = (int)b0;
-        start[3] = u;
-        break;
-      }
-      u0 += (int64_t)u * KV;
-      b0 += (int64_t)b * KV;
-    }
-  }
-  __syncthreads();
-  // the first segment from s on that has units, where sequences take no part: the
-  // workgroup looks at as many at a time as it has threads
-  auto next_segment = [&](int s, int& block) {
-    for (;; s += PA_THREADS) {
-      int u = 0, b = 0;
-      if (s + (int)threadIdx.x < segs) sizes(segment_of(a, s + threadIdx.x), u, b);
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        start[0] = PA_THREADS;
-        start[1] = 0;
-      }
-      __syncthreads();
-      if (u) atomicMin(&start[0], (int)threadIdx.x);
-      __syncthreads();
-      const int first = start[0];
-      if ((int)threadIdx.x < first) atomicAdd(&start[1], b * KV);
-      __syncthreads();
-      block += __builtin_amdgcn_readfirstlane(start[1]);
-      if (first < PA_THREADS || s + PA_THREADS >= segs) return s + __builtin_amdgcn_readfirstlane(first);
-    }
-  };
-  int s = __builtin_amdgcn_readfirstlane(start[0]), block = __builtin_amdgcn_readfirstlane(start[2]);
-  const int off = __builtin_amdgcn_readfirstlane(start[1]), per_head = __builtin_amdgcn_readfirstlane(start[3]);
-  const Ctx<T, HD> x{a, (T*)lds, pids, odd, parts, G, lane, wave, sc};
-  Segment g = segment_of(a, s);
-  int kvh = off / per_head, u = off % per_head, rt = 0;
-  {
-    const int rows = g.tokens * G;
-    block += kvh * tiles_of(rows) * (tile_rows(rows) / 16);
-    for (;;) {  // the tile
-      const int nu = units_of(tile_keys(g, G, rt));
-      if (u < nu) break;
-      u -= nu;
-      ++rt;
-      block += tile_rows(rows) / 16;
-    }
-  }
-  while (at < end) {
-    const int rows = g.tokens * G, nu = units_of(tile_keys(g, G, rt));
-    if (nu > 0) {
-      const int take = (int)min((int64_t)(nu - u), end - at);
-      const int64_t tile0 = at - u;  // the tile's first unit
-      if (u == 0 && threadIdx.x == 0) {
-        const int w1 = (int)(((tile0 + nu) * n - 1) / total);  // who has its last unit
-        const int64_t row0 = (int64_t)g.tok0 * G + rt * PA_WIDE;
-        info[((g.own ? KV : 0) + kvh) * (int64_t)a.tokens * G + row0] = TileParts{block + PA_BLOCKS * wg, w1 - wg + 1};
-      }
-      if (rows <= PA_NARROW) narrow_tile(x, g, kvh, u, u + take, block + PA_BLOCKS * wg);
-      else wide_tile(x, g, kvh, rt, u, u + take, block + PA_BLOCKS * wg);
-      at += take;
-    }
-    u = 0;
-    block += tile_rows(rows) / 16;
-    if (++rt >= tiles_of(rows)) {
-      rt = 0;
-      if (++kvh == KV) {
-        kvh = 0;
-        if (at >= end) break;
-        g = segment_of(a, ++s);  // (units are left, so a segment that has some follows)
-        if (!units_of(tile_keys(g, G, tiles_of(g.tokens * G) - 1))) {
-          s = next_segment(s, block);
-          g = segment_of(a, s);
-        }
-      }
-    }
-  }
-}
+// ---------------------------------------------------------------- the join
 
 // A row's parts of both segments: out = sum f o / sum f l, f = 2^(m - max).  A workgroup
-// per (token, kv head), HD / 4 lanes a row.
+// per (token, kv head): HD / 4 lanes for a part of a row, the parts shared out over as
+// many groups of them as it has for the R rows at a time, whose sums are joined in LDS.
+constexpr int JOIN_MAX = 1024;
 template <typename T, int HD>
-__global__ void __launch_bounds__(PA_THREADS) prefix_join_kernel(PrefixAttnArgs<T> a, const TileParts* info,
-                                                                 const float* parts) {
-  constexpr int LANES = HD / 4;
-  constexpr int64_t NEXT = PA_BLOCKS * part_floats(HD);  // from a tile's part to its next
+__global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T> a, const TileParts* info, const float* wide,
+                                                               const float* narrow, int wide_slots, int narrow_slots,
+                                                               int R) {
+  constexpr int LANES = HD / 4, AHEAD = 4;
+  __shared__ f32x4 sum_o[JOIN_MAX];
+  __shared__ float sum_m[JOIN_MAX / LANES], sum_l[JOIN_MAX / LANES];
   const int t = blockIdx.x, kvh = blockIdx.y, KV = a.kv.kv_heads, G = a.heads / KV;
-  const int lane = threadIdx.x & 63;
+  const int lane = threadIdx.x & 63, d = threadIdx.x % LANES, team = threadIdx.x / LANES;
+  const int groups = (int)blockDim.x / (LANES * R), group = team / R;  // of parts
   auto among = [&](const int32_t* cu, int n, int v) {  // how many of cu[1 .. n] are <= v
     int c = 0;
     for (int i = lane; i - lane < n; i += 64) c += __popcll(__ballot(i < n && cu[i + 1] <= v));
@@ -674,34 +872,74 @@ __global__ void __launch_bounds__(PA_THREADS) prefix_join_kernel(PrefixAttnArgs<
   const bool active = a.seqs.lens[b] >= 0;
   const int grp = a.shared.groups ? among(a.shared.cu, a.shared.groups, b) : 0;
   const bool has[2] = {grp < a.shared.groups, true};
-  for (int j = threadIdx.x / LANES; j < G; j += PA_THREADS / LANES) {
-    const int d = threadIdx.x % LANES * 4;
-    const float *at[2], *ml[2];  // the first part's row; its maximum (and, 16 on, sum)
-    int count[2] = {0, 0};
-    float top = -INFINITY;
-    for (int k = 0; k < 2; ++k) {
-      if (!has[k] || !active) continue;
-      const Segment g = segment_of(a, k ? a.shared.groups + b : grp);
-      const int r = (t - g.tok0) * G + j, rt = r / tile_rows(g.tokens * G), row = r - rt * PA_WIDE;
-      if (tile_keys(g, G, rt) <= 0) continue;
-      const TileParts p = info[(k * KV + kvh) * (int64_t)a.tokens * G + (int64_t)g.tok0 * G + rt * PA_WIDE];
-      const float* first = parts + (int64_t)(p.first + row / 16) * part_floats(HD);
-      at[k] = first + row % 16 * HD + d;
-      ml[k] = first + 16 * HD + row % 16;
-      count[k] = p.count;
-      for (int i = 0; i < count[k]; ++i) top = fmaxf(top, ml[k][i * NEXT]);
-    }
+  for (int j0 = 0; j0 < G; j0 += R) {
+    const int j = j0 + team % R;
     f32x4 o = {};
-    float l = 0.f;
-    if (top > -INFINITY)
-      for (int k = 0; k < 2; ++k)
-        for (int i = 0; i < count[k]; ++i) {
-          const float f = __builtin_amdgcn_exp2f(ml[k][i * NEXT] - top);
-          l += f * ml[k][i * NEXT + 16];
-          if (f > 0.f) o += f * *(const f32x4*)(at[k] + i * NEXT);
+    float top = -INFINITY, l = 0.f;
+    for (int k = 0; k < 2; ++k) {
+      if (!has[k] || !active || j >= G) continue;
+      const Segment g = segment_of(a, k ? a.shared.groups + b : grp);
+      const int r = (t - g.tok0) * G + j, rows = g.tokens * G;
+      const bool is_wide = rows > NARROW_ROWS;
+      const int row0 = is_wide ? r / WIDE_ROWS * WIDE_ROWS : 0, row = r - row0;
+      if (tile_keys(g, G, row0, is_wide ? WIDE_ROWS : NARROW_ROWS) <= 0) continue;
+      const TileParts p = info[info_at(k, kvh, KV, (int64_t)a.tokens * G, g.tok0, G, row0)];
+      if (p.first < 0 || p.count < 0 || p.count > (is_wide ? wide_slots : narrow_slots) - p.first) continue;
+      // a tile of up to 128 rows has two parts in a slot
+      const bool halves = is_wide && rows - row0 <= WIDE_ROWS / 2;
+      const int64_t step = (int64_t)(is_wide ? (halves ? SLOT_BLOCKS / 2 : SLOT_BLOCKS) : 1) * part_floats(HD);
+      const int count = halves ? 2 * p.count : p.count;
+      const float* part = (is_wide ? wide : narrow) + ((int64_t)p.first * (is_wide ? SLOT_BLOCKS : 1) + row / 16) * part_floats(HD);
+      const float *po = part + row % 16 * HD + 4 * d, *pm = part + 16 * HD + row % 16;
+      for (int i0 = group; i0 < count; i0 += AHEAD * groups) {
+        f32x4 v[AHEAD];
+        float m[AHEAD], s[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {  // (loads without a condition stay in flight together)
+          const int64_t at = min(i0 + i * groups, count - 1) * step;
+          m[i] = pm[at];
+          s[i] = pm[at + 16];
+          v[i] = *(const f32x4*)(po + at);
         }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    T* out = a.out + (int64_t)t * a.ldo + (int64_t)(kvh * G + j) * HD + d;
+        float next = top;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) next = fmaxf(next, m[i]);
+        const float fall = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next);
+        top = next;
+        l = fall > 0.f ? l * fall : l != l ? l : 0.f;
+        o = fall > 0.f ? o * fall : f32x4{};
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+          if (i0 + i * groups >= count) continue;
+          const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
+          l += f > 0.f || s[i] != s[i] ? f * s[i] : 0.f;  // (scores that are all NaN: no maximum)
+          o += f > 0.f ? f * v[i] : f32x4{};
+        }
+      }
+    }
+    if (groups > 1) {
+      sum_o[threadIdx.x] = o;
+      if (d == 0) {
+        sum_m[team] = top;
+        sum_l[team] = l;
+      }
+      __syncthreads();
+      if (group == 0) {
+        for (int i = 1; i < groups; ++i) top = fmaxf(top, sum_m[team + i * R]);
+        o = f32x4{};
+        l = 0.f;
+        for (int i = 0; i < groups; ++i) {
+          const float m = sum_m[team + i * R], s = sum_l[team + i * R];
+          const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top);
+          l += f > 0.f || s != s ? f * s : 0.f;
+          o += f > 0.f ? f * sum_o[threadIdx.x + i * R * LANES] : f32x4{};
+        }
+      }
+      __syncthreads();
+    }
+    if (group > 0 || j >= G) continue;
+    T* out = a.out + (int64_t)t * a.ldo + (int64_t)(kvh * G + j) * HD + 4 * d;
+    const float inv = 1.f / l;
 #pragma unroll
     for (int i = 0; i < 4; ++i) out[i] = from_f32<T>(l == 0.f ? 0.f : o[i] * inv);
     if (a.lse && d == 0)
@@ -713,46 +951,65 @@ __global__ void __launch_bounds__(PA_THREADS) prefix_join_kernel(PrefixAttnArgs<
 
 namespace {
 
-int wgs_of(bool f32, int hd) { return f32 && hd == 128 ? 256 : 512; }
-// (upper bounds of) the part blocks and rows of a call
-int64_t blocks_of(int64_t tokens, int seqs, int groups, int heads, int kv_heads, int wgs) {
-  const int64_t G = heads / kv_heads, rows = tokens * G;
-  // a segment of r rows: one block, or 8 ceil(r / 128) <= r / 16 + 8 and less than r
-  // (r > 16), so at most min(r, r / 16 + 8) of them
-  auto bound = [&](int64_t segs) { return std::min(rows / 16 + PA_BLOCKS * segs, rows + segs); };
-  return (bound(seqs) + (groups ? bound(groups) : 0)) * kv_heads + (int64_t)PA_BLOCKS * wgs;
+constexpr int WIDE_WGS = 256, NARROW_WGS = 768;
+
+struct Sizes {
+  int64_t wide, narrow;       // slots of each kind (0: no such tile)
+  int64_t wide_at, narrow_at, bytes;
+};
+Sizes sizes_of(const PrefixAttnShape& x) {
+  const int64_t G = x.heads / x.kv_heads;
+  auto token = [&](int b) -> int64_t { return x.h_cu ? x.h_cu[b] : b; };
+  int64_t wide = 0, narrow = 0;
+  auto add = [&](int64_t tokens) {
+    const int64_t rows = tokens * G;
+    if (rows > NARROW_ROWS) wide += (rows + WIDE_ROWS - 1) / WIDE_ROWS;
+    else if (rows > 0) ++narrow;
+  };
+  for (int g = 0; g < x.groups; ++g) add(token(x.h_groups[g + 1]) - token(x.h_groups[g]));
+  for (int b = 0; b < x.seqs; ++b) add(x.h_cu ? x.h_cu[b + 1] - x.h_cu[b] : 1);
+  Sizes s;
+  s.wide = wide ? wide * x.kv_heads + WIDE_WGS : 0;
+  s.narrow = narrow ? narrow * x.kv_heads + NARROW_WGS * NARROW_WAVES : 0;
+  s.wide_at = (2 * x.tokens * x.heads * (int64_t)sizeof(TileParts) + 15) / 16 * 16;
+  s.narrow_at = s.wide_at + s.wide * SLOT_BLOCKS * part_floats(x.hd) * 4;
+  s.bytes = s.narrow_at + s.narrow * part_floats(x.hd) * 4;
+  return s;
 }
 
 }  // namespace
 
-int64_t prefix_attn_workspace(int64_t tokens, int seqs, int groups, int heads, const PagedKV& kv, bool f32) {
-  const int64_t rows = 2 * tokens * heads;
-  return (rows * (int64_t)sizeof(TileParts) + 15) / 16 * 16 +
-         blocks_of(tokens, seqs, groups, heads, kv.kv_heads, wgs_of(f32, kv.hd)) * part_floats(kv.hd) * 4;
-}
+int64_t prefix_attn_workspace(const PrefixAttnShape& x) { return sizes_of(x).bytes; }
 
-int64_t prefix_attn_units(int64_t tokens, int seqs, int groups, int heads, const PagedKV& kv, int64_t pages) {
-  const int64_t rows = tokens * (heads / kv.kv_heads), tiles = seqs + groups + 2 * (rows / PA_WIDE);
-  return tiles * kv.kv_heads * ((pages * kv.ps + PA_KEYS - 1) / PA_KEYS);
+int64_t prefix_attn_units(const PrefixAttnShape& x, int64_t keys) {
+  const Sizes s = sizes_of(x);
+  return std::max(s.wide * ((keys + WIDE_KEYS - 1) / WIDE_KEYS), s.narrow * ((keys + NARROW_KEYS - 1) / NARROW_KEYS));
 }
 
 template <typename T, int HD>
-static void launch(const PrefixAttnArgs<T>& a, void* workspace, hipStream_t s) {
+static void launch(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* workspace, hipStream_t s) {
+  const Sizes n = sizes_of(x);
   TileParts* info = (TileParts*)workspace;
-  float* parts = (float*)((char*)workspace + (2 * (int64_t)a.tokens * a.heads * sizeof(TileParts) + 15) / 16 * 16);
+  float *wide = (float*)((char*)workspace + n.wide_at), *narrow = (float*)((char*)workspace + n.narrow_at);
   // a scale of 0 leaves every score, masked ones apart, the same
   const float sc = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * LOG2E_F;
-  prefix_attn_kernel<T, HD><<<wgs_of(sizeof(T) == 4, HD), PA_THREADS, 0, s>>>(a, sc, info, parts);
-  prefix_join_kernel<T, HD><<<dim3(a.tokens, a.kv.kv_heads), PA_THREADS, 0, s>>>(a, info, parts);
+  if (n.wide) prefix_wide_kernel<T, HD><<<WIDE_WGS, WIDE_THREADS, 0, s>>>(a, sc, info, wide, (int)n.wide);
+  if (n.narrow) prefix_narrow_kernel<T, HD><<<NARROW_WGS, NARROW_THREADS, 0, s>>>(a, sc, info, narrow, (int)n.narrow);
+  // few tokens: many threads each, whose parts are many
+  const int G = a.heads / a.kv.kv_heads, threads = (int64_t)a.tokens * a.kv.kv_heads <= 1024 ? JOIN_MAX : 256;
+  int R = 1;
+  while (R < G && R < threads / (HD / 4)) R *= 2;
+  prefix_join_kernel<T, HD><<<dim3(a.tokens, a.kv.kv_heads), threads, 0, s>>>(a, info, wide, narrow, (int)n.wide,
+                                                                             (int)n.narrow, R);
 }
 
 template <typename T>
-void launch_prefix_attn(const PrefixAttnArgs<T>& a, void* workspace, hipStream_t s) {
+void launch_prefix_attn(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* workspace, hipStream_t s) {
   if (!a.tokens) return;
-  if (a.kv.hd == 64) launch<T, 64>(a, workspace, s);
-  else launch<T, 128>(a, workspace, s);
+  if (a.kv.hd == 64) launch<T, 64>(a, x, workspace, s);
+  else launch<T, 128>(a, x, workspace, s);
 }
-template void launch_prefix_attn<float>(const PrefixAttnArgs<float>&, void*, hipStream_t);
-template void launch_prefix_attn<bf16>(const PrefixAttnArgs<bf16>&, void*, hipStream_t);
+template void launch_prefix_attn<float>(const PrefixAttnArgs<float>&, const PrefixAttnShape&, void*, hipStream_t);
+template void launch_prefix_attn<bf16>(const PrefixAttnArgs<bf16>&, const PrefixAttnShape&, void*, hipStream_t);
 
 }  // namespace axon

@@ -541,11 +541,17 @@ struct PrefixAttnArgs {
   float scale;
   float* lse;  // [tokens][heads] or null
 };
-// upper bound of the units of work that lengths within ``pages`` pages a row can make
-int64_t prefix_attn_units(int64_t tokens, int seqs, int groups, int heads, const PagedKV& kv, int64_t pages);
-int64_t prefix_attn_workspace(int64_t tokens, int seqs, int groups, int heads, const PagedKV& kv, bool f32);
+// what the host knows of a call
+struct PrefixAttnShape {
+  int64_t tokens;
+  int seqs, groups, heads, kv_heads, hd;
+  const int32_t *h_cu, *h_groups;
+};
+// upper bound of the units of work that rows of ``keys`` keys can make
+int64_t prefix_attn_units(const PrefixAttnShape& x, int64_t keys);
+int64_t prefix_attn_workspace(const PrefixAttnShape& x);
 template <typename T>
-void launch_prefix_attn(const PrefixAttnArgs<T>& a, void* workspace, hipStream_t s);
+void launch_prefix_attn(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* workspace, hipStream_t s);
 
 // ---- sampling (k_sample.hip)
 struct SampleArgs {
