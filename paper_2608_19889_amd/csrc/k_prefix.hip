@@ -30,7 +30,6 @@ namespace axon {
 
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr int WIDE_THREADS = 512, WIDE_WAVES = 8, WIDE_KEYS = 64, WIDE_ROWS = 256;
-constexpr int WIDE_LDS = 128 << 10;                   // of staged keys and values
 constexpr int NARROW_THREADS = 256, NARROW_WAVES = 4, NARROW_KEYS = 16, NARROW_ROWS = 16;
 constexpr int WIDE_LEAST = 8, NARROW_LEAST = 8;        // steps of a worker
 constexpr int SLOT_BLOCKS = WIDE_ROWS / 16;           // 16-row blocks of a wide part
@@ -251,6 +250,18 @@ struct Plan {
 
 // ---------------------------------------------------------------- tiles in LDS
 
+AXON_DEV uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
+// 16 bytes of each lane from global memory to LDS (lane L's to lds + 16 L), in flight
+// until a wait for vmcnt.  As assembly where the waits are all written out: of the builtin
+// the compiler knows that it writes LDS, and before a transposing read it then waits for
+// every copy in flight, those of the later stages too (a third of the kernel's time).
+AXON_DEV void copy_lds16(const void* src, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off"
+               :
+               : "v"(src), "s"(__builtin_amdgcn_readfirstlane(lds))
+               : "memory", "m0");
+}
+
 // Keys and values of a unit: rows of HD, the 16-byte chunks of a row at chunk ^ swizzle,
 // so that the lanes that read together meet different banks.
 template <typename T, int HD>
@@ -265,15 +276,17 @@ struct Lds {
   }
   static AXON_DEV int k_at(int key, int d) { return key * HD + ((d / EL) ^ swz_k(key)) * EL + d % EL; }
   static AXON_DEV int v_at(int key, int d) { return key * HD + ((d / EL) ^ swz_v(key)) * EL + d % EL; }
-  // rows key0 .. key0 + n - 1 of a unit, which lie one after another at ``src``, to
-  // row 0 .. of ``dst`` (a wavefront's copy)
-  template <bool K>
+  // Rows key0 .. key0 + n - 1 of a unit, which lie one after another at ``src``, to
+  // row 0 .. of ``dst`` (a wavefront's copy).
+  template <bool K, bool ASM>
   static AXON_DEV void stage(const T* src, T* dst, int key0, int n, int lane) {
 #pragma unroll
     for (int i = 0; i < n / RPI; ++i) {
       const int r = i * RPI + lane / CH, c = lane % CH;
       const int sw = K ? swz_k(key0 + r) : swz_v(key0 + r);
-      load_lds16((const bf16*)(src + r * HD + (c ^ sw) * EL), (bf16x8*)(dst + i * RPI * HD));
+      const T* from = src + r * HD + (c ^ sw) * EL;
+      if constexpr (ASM) copy_lds16(from, lds_address(dst + i * RPI * HD));
+      else load_lds16((const bf16*)from, (bf16x8*)(dst + i * RPI * HD));
     }
   }
 };
@@ -330,43 +343,8 @@ AXON_DEV f32x4 mul_narrow4(f32x4 a, f32x4 b, f32x4 c) {
   return c;
 }
 
-// The transposing LDS reads of read_tr8 for N column blocks at once, rows ``STEP`` bytes
-// apart: r[d][i] from at[d] + i STEP.  As assembly, with their wait: before the builtin
-// the compiler waits for every copy to LDS in flight, the later stages' too (a third of
-// the kernel's time).
-AXON_DEV uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p; }
-template <int STEP>
-AXON_DEV void read_tr(const uint32_t (&at)[4], bf16x4 (&r)[4][4]) {
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %16\n\tds_read_b64_tr_b16 %1, %16 offset:%20\n\t"
-      "ds_read_b64_tr_b16 %2, %16 offset:%21\n\tds_read_b64_tr_b16 %3, %16 offset:%22\n\t"
-      "ds_read_b64_tr_b16 %4, %17\n\tds_read_b64_tr_b16 %5, %17 offset:%20\n\t"
-      "ds_read_b64_tr_b16 %6, %17 offset:%21\n\tds_read_b64_tr_b16 %7, %17 offset:%22\n\t"
-      "ds_read_b64_tr_b16 %8, %18\n\tds_read_b64_tr_b16 %9, %18 offset:%20\n\t"
-      "ds_read_b64_tr_b16 %10, %18 offset:%21\n\tds_read_b64_tr_b16 %11, %18 offset:%22\n\t"
-      "ds_read_b64_tr_b16 %12, %19\n\tds_read_b64_tr_b16 %13, %19 offset:%20\n\t"
-      "ds_read_b64_tr_b16 %14, %19 offset:%21\n\tds_read_b64_tr_b16 %15, %19 offset:%22\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]),
-        "=&v"(r[1][2]), "=&v"(r[1][3]), "=&v"(r[2][0]), "=&v"(r[2][1]), "=&v"(r[2][2]), "=&v"(r[2][3]),
-        "=&v"(r[3][0]), "=&v"(r[3][1]), "=&v"(r[3][2]), "=&v"(r[3][3])
-      : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP)
-      : "memory");
-}
-template <int STEP>
-AXON_DEV void read_tr(const uint32_t (&at)[2], bf16x4 (&r)[2][4]) {
-  asm volatile(
-      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
-      "ds_read_b64_tr_b16 %2, %8 offset:%11\n\tds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
-      "ds_read_b64_tr_b16 %4, %9\n\tds_read_b64_tr_b16 %5, %9 offset:%10\n\t"
-      "ds_read_b64_tr_b16 %6, %9 offset:%11\n\tds_read_b64_tr_b16 %7, %9 offset:%12\n\t"
-      "s_waitcnt lgkmcnt(0)"
-      : "=&v"(r[0][0]), "=&v"(r[0][1]), "=&v"(r[0][2]), "=&v"(r[0][3]), "=&v"(r[1][0]), "=&v"(r[1][1]),
-        "=&v"(r[1][2]), "=&v"(r[1][3])
-      : "v"(at[0]), "v"(at[1]), "n"(STEP), "n"(2 * STEP), "n"(3 * STEP)
-      : "memory");
-}
-// the same, one read of each of 4 or 8 addresses
+// Transposing LDS reads of 4 or 8 places, as assembly with their wait: before the builtin
+// the compiler waits for every copy to LDS in flight, the next unit's too.
 AXON_DEV void read_tr(const uint32_t (&at)[4], bf16x4 (&r)[4]) {
   asm volatile(
       "ds_read_b64_tr_b16 %0, %4\n\tds_read_b64_tr_b16 %1, %5\n\tds_read_b64_tr_b16 %2, %6\n\t"
@@ -428,6 +406,11 @@ struct Cache {
     const int p = key < g.room ? g.table[key / a.kv.ps] : -1;
     return p >= 0 && p < a.kv.num_pages ? p : -1;
   }
+  // the 16-key block of a key, as a number of such blocks from the cache's start
+  AXON_DEV int block(int key) const {
+    const int p = page(key);
+    return p < 0 ? -1 : (p * a.kv.kv_heads + kvh) * (a.kv.ps / 16) + key % a.kv.ps / 16;
+  }
   AXON_DEV int64_t at(int page, int key) const {
     return (((int64_t)page * a.kv.kv_heads + kvh) * a.kv.ps + key % a.kv.ps) * HD;
   }
@@ -476,168 +459,352 @@ AXON_DEV void raise(float& m, float top, float& l, V (&o)[N]) {
 template <typename T, int HD>
 struct Wide {
   using L = Lds<T, HD>;
-  static constexpr int TILE = WIDE_KEYS * HD, STAGES = WIDE_LDS / (2 * TILE * (int)sizeof(T));
-  static constexpr int MY_KEYS = WIDE_KEYS / WIDE_WAVES;     // staged by a wavefront
-  static constexpr int LOADS = 2 * (MY_KEYS / L::RPI);       // its copies
-  static constexpr int BATCH = WIDE_THREADS / 4;             // units whose pages are looked up at a time
+  // bf16: 4 stages of 64 keys; float32 (keys and values twice as wide): 2 or 4
+  static constexpr int TILE = WIDE_KEYS * HD, STAGES = sizeof(T) == 4 && HD == 128 ? 2 : 4;
+  static constexpr int MY_KEYS = WIDE_KEYS / WIDE_WAVES;  // staged by a wavefront
+  static constexpr int LOADS = 2 * (MY_KEYS / L::RPI);    // its copies
+  static constexpr int BATCH = WIDE_THREADS / 4;          // units whose pages are looked up at a time
   struct Shared {
     alignas(16) T tiles[STAGES][2][TILE];
-    int32_t pids[WIDE_THREADS];        // pages of a batch, 4 a unit, -1: none
-    int32_t odd[STAGES][WIDE_WAVES];   // make_finite's rows
+    int32_t blocks[WIDE_THREADS];     // where a batch's 16-key blocks are in the cache, 4 a unit, -1: none
+    int32_t odd[STAGES][WIDE_WAVES];  // make_finite's rows
     PlanShared<WIDE_WAVES> plan;
   };
 };
 
-// Units first .. last - 1 of a tile of ``rows`` rows from row0 on; the part of key group
-// k goes to blocks part + k groups' rows / 16.
+// A wavefront's 32 rows of a wide tile over blocks of 32 keys in LDS
 template <typename T, int HD>
-AXON_DEV void wide_tile(const PrefixAttnArgs<T>& a, float sc, typename Wide<T, HD>::Shared& sh, const Segment& g, int G,
-                        int kvh, int row0, int first, int last, float* part) {
+struct WideRows {
   using W = Wide<T, HD>;
   using L = Lds<T, HD>;
   using V8 = typename Vec8<T>::t;
-  constexpr int DT = HD / 32, QS = HD / 16;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int hl = lane >> 5, c = lane & 31;
-  const int rows = g.tokens * G, here = min(rows - row0, WIDE_ROWS);
-  // up to 128 rows: two groups of 4 wavefronts, each half of a unit's keys
-  const bool halves = here <= WIDE_ROWS / 2;
-  const int kgroup = halves ? wave >> 2 : 0, r0 = row0 + 32 * (halves ? wave & 3 : wave), r = min(r0 + c, rows - 1);
-  const bool works = r0 < rows;
-  const Cache<T, HD> cache{a, g, kvh};
+  static constexpr int DT = HD / 32, QS = HD / 16;
+  const PrefixAttnArgs<T>& a;
+  const Segment& g;
+  const Cache<T, HD> cache;
+  float sc;
+  int G, row0, lane, wave, hl, c, rows, kgroup, r0, limit, least, most, tile_least;
+  bool halves, works;
   V8 q[QS];
-  {
+  f32x16 o[DT] = {};
+  float m = -INFINITY, l = 0.f;
+
+  AXON_DEV WideRows(const PrefixAttnArgs<T>& args, float scale, const Segment& seg, int group, int kvh, int first_row)
+      : a(args), g(seg), cache{args, seg, kvh}, sc(scale), G(group), row0(first_row) {
+    lane = threadIdx.x & 63;
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    hl = lane >> 5;
+    c = lane & 31;
+    rows = g.tokens * G;
+    // up to 128 rows: two groups of 4 wavefronts, each half of a unit's keys
+    halves = min(rows - row0, WIDE_ROWS) <= WIDE_ROWS / 2;
+    kgroup = halves ? wave >> 2 : 0;
+    r0 = row0 + 32 * (halves ? wave & 3 : wave);
+    works = r0 < rows;
+    const int r = min(r0 + c, rows - 1);
     const T* p = q_row<T, HD>(a, g, G, kvh, r) + 8 * hl;
 #pragma unroll
     for (int k = 0; k < QS; ++k) q[k] = load_q8<T>(p + 16 * k, a.scale < 0.f);
+    limit = row_keys(g, G, r);
+    least = row_keys(g, G, min(r0, rows - 1));
+    most = row_keys(g, G, min(r0 + 31, rows - 1));
+    tile_least = row_keys(g, G, row0);
   }
-  const int limit = row_keys(g, G, r), least = row_keys(g, G, min(r0, rows - 1));
-  const int most = row_keys(g, G, min(r0 + 31, rows - 1)), tile_least = row_keys(g, G, row0);
-  f32x16 o[DT] = {};
-  float m = -INFINITY, l = 0.f;
-  for (int u0 = first; u0 < last; u0 += W::BATCH) {
-    const int n = min(last - u0, W::BATCH);
+
+  // s = the scores of block kb: s[i] of key 32 kb + 8 (i / 4) + 4 hl + i % 4 and row c
+  AXON_DEV void read_k(const T* ks, int kb, V8 (&kf)[QS]) const {
+#pragma unroll
+    for (int k = 0; k < QS; ++k) {
+      const int d = 16 * k + 8 * hl;
+      kf[k] = read8(ks + L::k_at(32 * kb + c, d), ks + L::k_at(32 * kb + c, d + 4));
+    }
+  }
+  AXON_DEV void scores(const V8 (&kf)[QS], f32x16& s) const {
+    s = f32x16{};
+#pragma unroll
+    for (int k = 0; k < QS; ++k) s = mul_wide(kf[k], q[k], s);
+  }
+  // s = the weights of block kb of the unit at key0
+  AXON_DEV void weights(f32x16& s, int key0, int kb, int pages, const int32_t* odd) {
+    if (key0 + WIDE_KEYS > least || pages != 15) {
+      const int seen = limit - key0 - 32 * kb - 4 * hl;
+      const int seen0 = pages >> (2 * kb) & 1 ? seen : 0, seen1 = pages >> (2 * kb + 1) & 1 ? seen : 0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < (i < 8 ? seen0 : seen1) ? s[i] : -INFINITY;
+    }
+    float top = s[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    raise(m, fmaxf(top, lane_xor32(top)) * sc, l, o);
+    const float base = m == -INFINITY ? 0.f : m;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -base));
+      sum += s[i];
+    }
+    l += sum;
+    if (odd)
+      for (int w = 32 / W::MY_KEYS * kb; w < 32 / W::MY_KEYS * (kb + 1); ++w)
+        if (const int keys = __builtin_amdgcn_readfirstlane(odd[w])) {
+          float e[16 * DT];
+#pragma unroll
+          for (int i = 0; i < 16 * DT; ++i) e[i] = o[i / 16][i % 16];
+          add_odd(cache, key0 + W::MY_KEYS * w, keys, limit, e,
+                  [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hl + i % 4; });
+#pragma unroll
+          for (int i = 0; i < 16 * DT; ++i) o[i / 16][i % 16] = e[i];
+        }
+  }
+  AXON_DEV void store(float* part) {
+    if (r0 + c >= rows) return;
+    l += lane_xor32(l);
+    const int block = (halves ? 8 * kgroup + 2 * (wave & 3) : 2 * wave) + (c >> 4), row = c & 15;
+    part += (int64_t)block * part_floats(HD);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        *(f32x4*)(part + row * HD + 32 * d + 8 * j + 4 * hl) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
+    if (hl == 0) {
+      part[16 * HD + row] = m;
+      part[16 * HD + 16 + row] = l;
+    }
+  }
+};
+
+// Staging of a batch of units: pages looked up, each wavefront copies 8 keys of a unit.
+template <typename T, int HD>
+struct WideStages {
+  using W = Wide<T, HD>;
+  using L = Lds<T, HD>;
+  typename W::Shared& sh;
+  const WideRows<T, HD>& x;
+  int u0 = 0, n = 0, next = 0;  // the batch
+  bool all_there = true;
+
+  AXON_DEV void look_up(int first, int count) {
+    u0 = first;
+    n = count;
     __syncthreads();  // the stages and pages of what came before are read
-    if ((int)threadIdx.x < 4 * n) sh.pids[threadIdx.x] = cache.page((4 * u0 + (int)threadIdx.x) * 16);
-    __syncthreads();
-    auto stage = [&](int i) {
-      const int in_unit = W::MY_KEYS * wave, key = (u0 + i) * WIDE_KEYS + in_unit;
-      const int page = max(__builtin_amdgcn_readfirstlane(sh.pids[4 * i + in_unit / 16]), 0);  // (none: masked, but read)
-      const int64_t src = cache.at(page, key);
-      T* dst = sh.tiles[i % W::STAGES][0] + in_unit * HD;
-      L::template stage<true>((const T*)a.kv.k + src, dst, in_unit, W::MY_KEYS, lane);
-      L::template stage<false>((const T*)a.kv.v + src, dst + W::TILE, in_unit, W::MY_KEYS, lane);
+    const int key = (4 * u0 + (int)threadIdx.x) * 16;
+    const bool mine = (int)threadIdx.x < 4 * n;
+    const int b = mine ? x.cache.block(key) : 0;
+    if (mine) sh.blocks[threadIdx.x] = b;
+    all_there = __syncthreads_and(b >= 0);
+    fetch(0);
+  }
+  // (the block of the next copy is read a unit ahead)
+  AXON_DEV void fetch(int i) { next = sh.blocks[4 * min(i, n - 1) + W::MY_KEYS * x.wave / 16]; }
+  AXON_DEV void copy(int i) {
+    const int in_unit = W::MY_KEYS * x.wave;
+    const int b = max(__builtin_amdgcn_readfirstlane(next), 0);  // (none: masked, but read)
+    fetch(i + 1);
+    const int64_t src = ((int64_t)b * 16 + in_unit % 16) * HD;
+    T* dst = sh.tiles[i % W::STAGES][0] + in_unit * HD;
+    L::template stage<true, true>((const T*)x.a.kv.k + src, dst, in_unit, W::MY_KEYS, x.lane);
+    L::template stage<false, true>((const T*)x.a.kv.v + src, dst + W::TILE, in_unit, W::MY_KEYS, x.lane);
+  }
+  // which of a unit's 16-key blocks have a page
+  AXON_DEV int pages(int i) const {
+    if (all_there) return 15;
+    int p = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p |= (sh.blocks[4 * i + j] >= 0) << j;
+    return __builtin_amdgcn_readfirstlane(p);
+  }
+  // whether some key of the unit is masked for some row of the tile
+  AXON_DEV bool masked(int i) const { return (u0 + i + 1) * WIDE_KEYS > x.tile_least || pages(i) != 15; }
+  // this wavefront's keys of unit i are in LDS when at most ``later`` units' copies are in
+  // flight; they are made finite where some key is masked
+  template <int MOST>
+  AXON_DEV void arrive(int i, int later) {
+    wait_loads<W::LOADS, MOST>(later);
+    if (masked(i)) {
+      const int at = i % W::STAGES;
+      const int odd = make_finite<T, HD>(sh.tiles[at][1] + W::MY_KEYS * x.wave * HD, W::MY_KEYS, x.lane);
+      if (x.lane == 0) sh.odd[at][x.wave] = odd;
+    }
+  }
+  // ends a phase: what was read of LDS is here, what was written there is to be seen
+  AXON_DEV void barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    phase_barrier();
+  }
+};
+
+// Units first .. last - 1 of the tile of row0.  A wavefront alternates between phases of
+// matrix instructions (a unit's scores, the product with the values of the unit before)
+// and of everything else (the weights); wavefronts 4 .. 7 are a phase behind 0 .. 3, with
+// which they share the SIMDs, so that one's matrix instructions run beside the other's
+// exponentials.  HALVES: a wavefront takes 32 of a unit's keys, else all 64.
+template <bool HALVES, int HD>
+AXON_DEV void wide_phases(WideRows<bf16, HD>& x, WideStages<bf16, HD>& st, int first, int last) {
+  using W = Wide<bf16, HD>;
+  using L = Lds<bf16, HD>;
+  using X = WideRows<bf16, HD>;
+  constexpr int DT = X::DT, S = W::STAGES, NB = HALVES ? 1 : 2;
+  static_assert(S == 4, "what the phases of copies and waits count on");
+  const int late = x.wave >> 2, kb0 = HALVES ? x.kgroup : 0;
+  for (int u0 = first; u0 < last; u0 += W::BATCH) {
+    st.look_up(u0, min(last - u0, W::BATCH));
+    const int n = st.n;
+    // Phase p of all wavefronts: unit u is multiplied from phase 2 u (scores) to 2 u + 3
+    // (the late ones' product), so unit u + 4 is copied over it in phase 2 u + 4, and
+    // waited for before phase 2 u + 8.
+    int p = 0;
+    auto begin = [&] {
+      if (!(p & 1) && (p >> 1) + 2 < n) st.copy((p >> 1) + 2);
     };
-    for (int i = 0; i < W::STAGES - 1 && i < n; ++i) stage(i);
-    for (int i = 0; i < n; ++i) {
-      const int key0 = (u0 + i) * WIDE_KEYS, at = i % W::STAGES;
-      int pages = 0;  // which of the 16-key blocks exist
+    auto end = [&] {
+      ++p;
+      const int u = p >> 1;
+      if (!(p & 1) && u < n) st.template arrive<1>(u, min(n - 1 - u, 1));
+      st.barrier();
+    };
+    st.copy(0);
+    if (n > 1) st.copy(1);
+    st.template arrive<1>(0, min(n - 1, 1));
+    st.barrier();
+    if (late) {
+      begin();
+      end();
+    }
+    bf16x8 w[NB][2];  // the weights of the unit before, and its values' place
+    const bf16* wv = nullptr;
+    // The operands of DT matrix instructions are read from LDS before the DT before them
+    // are issued (one at a time, each instruction would wait for its own): f[0], f[1] in
+    // turn.  First K, 16 dimensions an operand; then V, keys 16 e .., two times 4 a lane.
+    bf16x8 f[2][DT];
+    f32x16 s[NB];
+    auto read_k = [&](const bf16* tile, int b, int half) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) pages |= (sh.pids[4 * i + j] >= 0) << j;
-      pages = __builtin_amdgcn_readfirstlane(pages);
-      const bool tile_masked = key0 + WIDE_KEYS > tile_least || pages != 15;
-      // the unit is here (later ones may not be), and what was read of the stage that is
-      // filled next as well
-      wait_loads<W::LOADS, W::STAGES - 2>(min(n - 1 - i, W::STAGES - 2));
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (tile_masked) {
-        const int odd = make_finite<T, HD>(sh.tiles[at][1] + W::MY_KEYS * wave * HD, W::MY_KEYS, lane);
-        if (lane == 0) sh.odd[at][wave] = odd;
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      for (int k = 0; k < DT; ++k)
+        f[half][k] = *(const bf16x8*)(tile + L::k_at(32 * (kb0 + b) + x.c, 16 * (half * DT + k) + 8 * x.hl));
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto scores = [&](int b, int half) {
+      if (half == 0) s[b] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < DT; ++k) s[b] = mul_wide(f[half][k], x.q[half * DT + k], s[b]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto read_v = [&](int b, int e) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const int key = 32 * b + 16 * e + 4 * x.hl + ((x.lane & 15) >> 2);
+        const int dim = 32 * d + 16 * ((x.lane >> 4) & 1) + 4 * (x.lane & 3);
+        f[e][d] = read_tr8(wv + L::v_at(key, dim), wv + L::v_at(key + 8, dim));
       }
-      phase_barrier();
-      if (i + W::STAGES - 1 < n) stage(i + W::STAGES - 1);
-      if (!works || key0 >= most) continue;
-      const T *ks = sh.tiles[at][0], *vs = sh.tiles[at][1];
-      const bool masked = key0 + WIDE_KEYS > least || pages != 15;
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    auto product = [&](int b, int e) {
+#pragma unroll
+      for (int d = 0; d < DT; ++d) x.o[d] = mul_wide(f[e][d], w[b][e], x.o[d]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // (f[1] is free when the first values are read into f[0])
+    auto products = [&] {
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        read_v(b, 1);
+        product(b, 0);
+        if (b + 1 < NB) read_v(b + 1, 0);
+        product(b, 1);
+      }
+    };
+    static_assert(X::QS == 2 * DT, "as many operands of K as of V");
+    for (int i = 0; i < n; ++i) {
+      const bf16* tile = st.sh.tiles[i % S][0];
+      begin();
+      if (x.works) {
+        read_k(tile, 0, 0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          read_k(tile, b, 1);
+          scores(b, 0);
+          if (b + 1 < NB) read_k(tile, b + 1, 0);
+          else if (wv) read_v(0, 0);
+          scores(b, 1);
+        }
+        if (wv) products();
+      }
+      end();
+      begin();
+      if (x.works) {
+        const int pages = st.pages(i);
+        const int32_t* odd = st.masked(i) ? st.sh.odd[i % S] : nullptr;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          x.weights(s[b], (u0 + i) * WIDE_KEYS, kb0 + b, pages, odd);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) w[b][j / 8][j % 8] = (bf16)s[b][j];
+        }
+        wv = tile + W::TILE + 32 * kb0 * HD;
+      }
+      end();
+    }
+    begin();
+    if (x.works) {
+      read_v(0, 0);
+      products();
+    }
+    end();
+    if (!late) {
+      begin();
+      end();
+    }
+  }
+}
+
+template <int HD>
+AXON_DEV void wide_tile(const PrefixAttnArgs<bf16>& a, float sc, typename Wide<bf16, HD>::Shared& sh, const Segment& g,
+                        int G, int kvh, int row0, int first, int last, float* part) {
+  WideRows<bf16, HD> x(a, sc, g, G, kvh, row0);
+  WideStages<bf16, HD> st{sh, x};
+  if (x.halves) wide_phases<true>(x, st, first, last);
+  else wide_phases<false>(x, st, first, last);
+  x.store(part);
+}
+
+// In float32 the matrix instructions take 16 times as long: all wavefronts in step.
+template <int HD>
+AXON_DEV void wide_tile(const PrefixAttnArgs<float>& a, float sc, typename Wide<float, HD>::Shared& sh, const Segment& g,
+                        int G, int kvh, int row0, int first, int last, float* part) {
+  using W = Wide<float, HD>;
+  using L = Lds<float, HD>;
+  using X = WideRows<float, HD>;
+  constexpr int S = W::STAGES;
+  X x(a, sc, g, G, kvh, row0);
+  WideStages<float, HD> st{sh, x};
+  for (int u0 = first; u0 < last; u0 += W::BATCH) {
+    st.look_up(u0, min(last - u0, W::BATCH));
+    const int n = st.n;
+    for (int i = 0; i < S - 1 && i < n; ++i) st.copy(i);
+    for (int i = 0; i < n; ++i) {
+      st.template arrive<S - 2>(i, min(n - 1 - i, S - 2));
+      st.barrier();
+      if (i + S - 1 < n) st.copy(i + S - 1);
+      const int key0 = (u0 + i) * WIDE_KEYS;
+      if (!x.works || key0 >= x.most) continue;
+      const float* tile = sh.tiles[i % S][0];
 #pragma unroll 1
-      for (int kb = halves ? kgroup : 0; kb < (halves ? kgroup + 1 : 2); ++kb) {
-        // the LDS reads of a product stand together before it: one at a time, each matrix
-        // instruction waited for its operand
-        V8 kf[QS];
+      for (int kb = x.kgroup; kb < (x.halves ? x.kgroup + 1 : 2); ++kb) {
+        f32x8 kf[X::QS];
+        x.read_k(tile, kb, kf);
+        f32x16 s;
+        x.scores(kf, s);
+        x.weights(s, key0, kb, st.pages(i), st.masked(i) ? sh.odd[i % S] : nullptr);
 #pragma unroll
-        for (int k = 0; k < QS; ++k) {
-          const int d = 16 * k + 8 * hl;
-          kf[k] = read8(ks + L::k_at(32 * kb + c, d), ks + L::k_at(32 * kb + c, d + 4));
-        }
-        if (sizeof(T) == 2) __builtin_amdgcn_sched_barrier(0);
-        f32x16 s = {};
+        for (int j = 0; j < 16; ++j)
 #pragma unroll
-        for (int k = 0; k < QS; ++k) s = mul_wide(kf[k], q[k], s);
-        bf16x4 vf[DT][4];  // keys 8 i + 4 hl .. of the block; read under the product
-        if constexpr (sizeof(T) == 2) {
-          uint32_t at[DT];
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-            at[d] = lds_address(vs + L::v_at(32 * kb + 4 * hl + ((lane & 15) >> 2), 32 * d + 16 * ((lane >> 4) & 1) + 4 * (lane & 3)));
-          __builtin_amdgcn_sched_barrier(0);
-          read_tr<8 * HD * 2>(at, vf);
-        }
-        // s[i]: key key0 + 32 kb + 8 (i / 4) + 4 hl + i % 4, row c
-        if (masked) {
-          const int seen = limit - key0 - 32 * kb - 4 * hl;
-          const int seen0 = pages >> (2 * kb) & 1 ? seen : 0, seen1 = pages >> (2 * kb + 1) & 1 ? seen : 0;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < (i < 8 ? seen0 : seen1) ? s[i] : -INFINITY;
-        }
-        float top = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-        raise(m, fmaxf(top, lane_xor32(top)) * sc, l, o);
-        const float base = m == -INFINITY ? 0.f : m;
-        f32x16 p;
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          p[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -base));
-          sum += p[i];
-        }
-        l += sum;
-        if constexpr (sizeof(T) == 2) {
-          bf16x8 pb[2];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) pb[i / 8][i % 8] = (bf16)p[i];
-#pragma unroll
-          for (int e = 0; e < 2; ++e)  // keys 16 e .. of the block
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-              o[d] = mul_wide(__builtin_shufflevector(vf[d][2 * e], vf[d][2 * e + 1], 0, 1, 2, 3, 4, 5, 6, 7), pb[e], o[d]);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = 32 * kb + 8 * (i >> 2) + 4 * hl + (i & 3);
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-              o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(vs[L::v_at(key, 32 * d + c)], p[i], o[d], 0, 0, 0);
-          }
-        }
-        if (tile_masked)
-          for (int w = 32 / W::MY_KEYS * kb; w < 32 / W::MY_KEYS * (kb + 1); ++w)
-            if (const int odd = __builtin_amdgcn_readfirstlane(sh.odd[at][w])) {
-              float e[16 * DT];
-#pragma unroll
-              for (int i = 0; i < 16 * DT; ++i) e[i] = o[i / 16][i % 16];
-              add_odd(cache, key0 + W::MY_KEYS * w, odd, limit, e,
-                      [&](int i) { return 32 * (i / 16) + 8 * (i % 16 / 4) + 4 * hl + i % 4; });
-#pragma unroll
-              for (int i = 0; i < 16 * DT; ++i) o[i / 16][i % 16] = e[i];
-            }
+          for (int d = 0; d < X::DT; ++d)
+            x.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                tile[W::TILE + L::v_at(32 * kb + 8 * (j >> 2) + 4 * x.hl + (j & 3), 32 * d + x.c)], s[j], x.o[d], 0, 0, 0);
       }
     }
   }
-  if (r0 + c >= rows) return;
-  l += lane_xor32(l);
-  const int block = (halves ? 8 * kgroup + 2 * (wave & 3) : 2 * wave) + (c >> 4), row = c & 15;
-  part += (int64_t)block * part_floats(HD);
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *(f32x4*)(part + row * HD + 32 * d + 8 * j + 4 * hl) = f32x4{o[d][4 * j], o[d][4 * j + 1], o[d][4 * j + 2], o[d][4 * j + 3]};
-  if (hl == 0) {
-    part[16 * HD + row] = m;
-    part[16 * HD + 16 + row] = l;
-  }
+  x.store(part);
 }
 
 // Worker w of n takes steps total w / n .. total (w + 1) / n - 1: as many as there are,
@@ -689,7 +856,7 @@ __global__ void __launch_bounds__(WIDE_THREADS, 2) prefix_wide_kernel(PrefixAttn
     if (slot >= slots) return;  // (cu_seqlens are not those of the host)
     const Work w = work_of<true, HD>(a, g, p, G, KV, at, end, plan.total, me, n, info, threadIdx.x == 0);
     if (w.last > w.first)
-      wide_tile<T, HD>(a, sc, sh, g, G, p.kvh, p.rt * WIDE_ROWS, w.first, w.last,
+      wide_tile<HD>(a, sc, sh, g, G, p.kvh, p.rt * WIDE_ROWS, w.first, w.last,
                        parts + (int64_t)slot * SLOT_BLOCKS * part_floats(HD));
     at += w.take;
     if (at >= end) return;
@@ -728,7 +895,7 @@ AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[2][Narr
   auto page_of = [&](int u) { return __builtin_amdgcn_readlane(pages, (u - first) & 63); };
   auto fetch = [&](int u, int b) {
     const int64_t src = cache.at(max(page_of(u), 0), u * NARROW_KEYS);  // (none: masked, but read)
-    L::template stage<false>((const T*)a.kv.v + src, lds[b], 0, NARROW_KEYS, lane);
+    L::template stage<false, false>((const T*)a.kv.v + src, lds[b], 0, NARROW_KEYS, lane);
     const T* kp = (const T*)a.kv.k + src + c * HD + 8 * gq;
 #pragma unroll
     for (int j = 0; j < QS; ++j) k[b][j] = read8(kp + 32 * j, kp + 32 * j + 4);
