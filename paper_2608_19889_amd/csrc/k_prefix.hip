@@ -31,7 +31,7 @@ namespace axon {
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr int WIDE_THREADS = 512, WIDE_WAVES = 8, WIDE_KEYS = 64, WIDE_ROWS = 256;
 constexpr int NARROW_THREADS = 256, NARROW_WAVES = 4, NARROW_KEYS = 16, NARROW_ROWS = 16;
-constexpr int WIDE_LEAST = 8, NARROW_LEAST = 8;        // steps of a worker
+constexpr int WIDE_LEAST = 4, NARROW_LEAST = 2;        // steps of a worker
 constexpr int SLOT_BLOCKS = WIDE_ROWS / 16;           // 16-row blocks of a wide part
 
 // ---------------------------------------------------------------- plan
