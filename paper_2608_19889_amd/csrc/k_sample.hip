@@ -29,11 +29,18 @@ typedef unsigned long long u64;
 constexpr int S_THREADS = 1024;
 constexpr int BINS = 2 * S_THREADS;
 
-// 2^x for x <= 0 (0 below -1100): 2^f on [-1/2, 1/2] as the polynomial of degree 10
-// through 2^f at Chebyshev's nodes, 4e-16 of itself off and exactly 1 at 0
-AXON_DEV double exp2_neg(double x) {
-  x = fmax(x, -1100.);  // (NaN, from infinities: no weight either)
-  const double n = rint(x), f = x - n;
+// 2^x for x <= 0 as v 2^n, v in [0.7, 1.42]: 2^f on [-1/2, 1/2] as the polynomial of
+// degree 10 through 2^f at Chebyshev's nodes, 4e-16 of itself off and exactly 1 at 0.
+// Rounding to whole numbers by an addition, whose low bits are n, and no other conversion:
+// those take four times as long as sums and products.
+struct Exp2 {
+  double v;
+  int n;
+};
+AXON_DEV Exp2 exp2_neg(double x) {
+  x = fmax(x, -1000.);  // (NaN, from infinities: no weight either)
+  constexpr double WHOLE = 6755399441055744.;  // 1.5 2^52
+  const double t = x + WHOLE, f = x - (t - WHOLE);
   double v = 7.072585949269224e-09;
   v = fma(v, f, 1.0208690299958306e-07);
   v = fma(v, f, 1.321544258792169e-06);
@@ -44,97 +51,99 @@ AXON_DEV double exp2_neg(double x) {
   v = fma(v, f, 0.05550410866444772);
   v = fma(v, f, 0.24022650695910097);
   v = fma(v, f, 0.69314718055995);
-  v = fma(v, f, 1.0);
-  return ldexp(v, (int)n);
+  return Exp2{fma(v, f, 1.), __double2loint(t)};
+}
+AXON_DEV double as_double(Exp2 e) {
+  return __hiloint2double(__double2hiint(e.v) + (e.n << 20), __double2loint(e.v));
+}
+// round(v 2^(n + scale)) for scale <= 62: v + 2 has v's first 51 bits behind the point
+AXON_DEV u64 as_fixed(Exp2 e, int scale) {
+  const u64 m = ((u64)__double_as_longlong(e.v + 2.) & ((1ull << 52) - 1)) << 11;
+  const int r = 62 - scale - e.n;
+  return r > 63 ? 0 : (m + (r ? 1ull << (r - 1) : 0)) >> r;
 }
 
 // a logit as it is compared: NaN cannot be chosen, zeros have one sign
 AXON_DEV float sane(float z) { return z == 0.f ? 0.f : z == z ? z : -INFINITY; }
-// its bits in ascending order
+// its bits in ascending order, as many as the type has
+template <typename T>
 AXON_DEV uint32_t order_key(float z) {
-  const uint32_t u = __float_as_uint(z);
-  return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+  const uint32_t u = __float_as_uint(z), k = u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
+  return sizeof(T) == 2 ? k >> 16 : k;
 }
-AXON_DEV float key_value(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
+template <typename T>
+AXON_DEV float key_value(uint32_t k) {
+  if (sizeof(T) == 2) k = k << 16 | (k >> 15 ? 0 : 0xffff);
+  return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu));
+}
+
+// A value that a filter can keep
+struct Candidate {
+  float z;
+  int i;
+  u64 w;
+};
+constexpr int FEW = 256;  // candidates that are compared each with each
 
 struct Shared {
-  u64 mass[BINS];
-  uint32_t cnt[BINS];
-  u64 wave_mass[16];
-  uint32_t wave_cnt[16];
-  u64 mass_before, mass_in;
-  uint32_t cnt_before, cnt_in;
-  int found;
-  float red[16];
-};
-
-// number and weight in front of a place, and the place
-struct Found {
-  int at;
-  u64 mass_before, mass_in;
-  uint32_t cnt_before, cnt_in;
+  u64 bins[BINS];
+  Candidate few[FEW];
+  u64 wave_sum[S_THREADS / 64];
+  u64 before, in;
+  int found, count;
+  u64 sum[2];
+  float red[S_THREADS / 64];
 };
 
 AXON_DEV void clear_bins(Shared& sh) {
   __syncthreads();
-  for (int i = threadIdx.x; i < BINS; i += S_THREADS) {
-    sh.mass[i] = 0;
-    sh.cnt[i] = 0;
-  }
+  for (int i = threadIdx.x; i < BINS; i += S_THREADS) sh.bins[i] = 0;
   if (threadIdx.x == 0) sh.found = -1;
   __syncthreads();
 }
 
+AXON_DEV u64 wave_total(u64 v) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+  return v;
+}
+
 // Over each thread's two entries, in the threads' order: the entry at which the running
-// sum (of numbers or of weights) reaches target(total) >= 1.
-template <bool COUNT, typename F>
-AXON_DEV Found find_entry(Shared& sh, const u64 (&m)[2], const uint32_t (&c)[2], u64 m0, uint32_t c0, F&& target,
-                          u64* total = nullptr) {
+// sum (from ``from`` on) reaches target(total) >= 1; what is before it and in it.
+struct Found {
+  int at;
+  u64 before, in;
+};
+template <typename F>
+AXON_DEV Found find_entry(Shared& sh, const u64 (&v)[2], u64 from, F&& target, u64* total = nullptr) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u64 ms = m[0] + m[1];
-  uint32_t csum = c[0] + c[1];
-  const u64 own_m = ms;
-  const uint32_t own_c = csum;
+  u64 upto = v[0] + v[1];
+#pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const u64 mu = __shfl_up(ms, d);
-    const uint32_t cu = __shfl_up(csum, d);
-    if (lane >= d) {
-      ms += mu;
-      csum += cu;
-    }
+    const u64 u = __shfl_up(upto, d);
+    if (lane >= d) upto += u;
   }
-  if (lane == 63) {
-    sh.wave_mass[wave] = ms;
-    sh.wave_cnt[wave] = csum;
-  }
+  if (lane == 63) sh.wave_sum[wave] = upto;
   __syncthreads();
-  u64 mb = m0 + ms - own_m, mt = m0;
-  uint32_t cb = c0 + csum - own_c, ct = c0;
-  for (int w = 0; w < 16; ++w) {
-    if (w < wave) {
-      mb += sh.wave_mass[w];
-      cb += sh.wave_cnt[w];
-    }
-    mt += sh.wave_mass[w];
-    ct += sh.wave_cnt[w];
+  u64 before = from + upto - v[0] - v[1], sum = from;
+#pragma unroll
+  for (int w = 0; w < S_THREADS / 64; ++w) {
+    before += w < wave ? sh.wave_sum[w] : 0;
+    sum += sh.wave_sum[w];
   }
-  const u64 want = target(COUNT ? (u64)ct : mt);
-  if (total) *total = COUNT ? (u64)ct : mt;
+  const u64 want = target(sum);
+  if (total) *total = sum;
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const u64 before = COUNT ? (u64)cb : mb, after = before + (COUNT ? (u64)c[j] : m[j]);
-    if (before < want && want <= after) {
+    if (before < want && want <= before + v[j]) {
       sh.found = 2 * threadIdx.x + j;
-      sh.mass_before = mb;
-      sh.mass_in = m[j];
-      sh.cnt_before = cb;
-      sh.cnt_in = c[j];
+      sh.before = before;
+      sh.in = v[j];
     }
-    mb += m[j];
-    cb += c[j];
+    before += v[j];
   }
   __syncthreads();
-  return Found{sh.found, sh.mass_before, sh.mass_in, sh.cnt_before, sh.cnt_in};
+  return Found{sh.found, sh.before, sh.in};
 }
 
 // ---------------------------------------------------------------- one reading of the logits
@@ -162,9 +171,6 @@ AXON_DEV Settings settings_of(const SampleArgs& a, int r) {
 // whether the row's sum of weights is needed: for the share p of it, or to draw from all
 AXON_DEV bool needs_sum(const Settings& s) { return !s.greedy && !s.by_rank && (s.p < 1.f || !(s.low > 0.f)); }
 AXON_DEV double per_unit(const Settings& s) { return s.greedy ? 0. : 1.4426950408889634 / (double)s.t; }
-// a weight relative to ``top``
-AXON_DEV double weight_to(float z, float top, double c) { return z == top ? 1. : exp2_neg(((double)z - top) * c); }
-
 template <typename T>
 constexpr int RUN = 16 / sizeof(T);  // values of a 16-byte load
 template <typename T>
@@ -234,10 +240,17 @@ __global__ void __launch_bounds__(SCAN_THREADS) sample_scan_kernel(SampleArgs a,
   if (!needs_sum(s)) return;
   const double c = per_unit(s);
   double sum = 0.;
+  if (fabsf(all) < INFINITY) {
 #pragma unroll
-  for (int j = 0; j < ROUNDS; ++j)
+    for (int j = 0; j < ROUNDS; ++j)
 #pragma unroll
-    for (int i = 0; i < N; ++i) sum += all == -INFINITY ? 0. : weight_to(v[j][i], all, c);
+      for (int i = 0; i < N; ++i) sum += as_double(exp2_neg(((double)v[j][i] - all) * c));
+  } else if (all > 0.f) {  // infinities share all
+#pragma unroll
+    for (int j = 0; j < ROUNDS; ++j)
+#pragma unroll
+      for (int i = 0; i < N; ++i) sum += v[j][i] == all ? 1. : 0.;
+  }
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
   if (lane == 0) out.chunk_sum[chunk] = sum;
@@ -245,12 +258,11 @@ __global__ void __launch_bounds__(SCAN_THREADS) sample_scan_kernel(SampleArgs a,
 
 // ---------------------------------------------------------------- the rest of a row
 
-constexpr int LIST = 4096;        // blocks that are listed; more: all of the row
+constexpr int LIST = 2048;        // blocks that are listed; more: all of the row
 constexpr int MAX_BLOCKS = 8192;  // maxima that fit into LDS (262144 logits)
 
 // The values of a row that can matter: those of the listed blocks, or (n < 0) of all.
-// What is below ``cut`` is passed over.  A thread's first 16 bytes stay in registers
-// from pass to pass, the others are read again.
+// What is below ``cut`` is passed over.
 template <typename T>
 struct Row {
   static constexpr int N = RUN<T>, LANES = BLOCK / N;
@@ -259,18 +271,13 @@ struct Row {
   float cut;
   int n;
   const int32_t* list;
-  float v0[N];
   AXON_DEV int items() const { return n < 0 ? (V + N - 1) / N : n * LANES; }
   AXON_DEV int first(int e) const { return n < 0 ? e * N : list[e / LANES] * BLOCK + e % LANES * N; }
-  AXON_DEV void fill() {
-    if ((int)threadIdx.x < items()) load_run(z, first(threadIdx.x), V, v0);
-  }
   template <typename F>
   AXON_DEV void each(F&& f) const {
     float v[N], next[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = v0[i];
     const int end = items();
+    if ((int)threadIdx.x < end) load_run(z, first(threadIdx.x), V, v);
 #pragma unroll 1
     for (int e = threadIdx.x; e < end; e += S_THREADS) {
       const int at = first(e);
@@ -284,88 +291,171 @@ struct Row {
   }
 };
 
-// the value on the border in descending order, and what is above it
+// up to FEW values of the row that ``take`` takes, in sh.few in any order; their number
+// (more than FEW: not all of them are there)
+template <typename R, typename P, typename W>
+AXON_DEV int gather(Shared& sh, const R& row, P&& take, W&& weight) {
+  __syncthreads();
+  if (threadIdx.x == 0) sh.count = 0;
+  __syncthreads();
+  row.each([&](float z, int i) {
+    if (!take(z)) return;
+    const int n = atomicAdd(&sh.count, 1);
+    if (n < FEW) sh.few[n] = Candidate{z, i, weight(z)};
+  });
+  __syncthreads();
+  return sh.count;
+}
+// Four threads to a candidate (thread / 4): f(candidate) over a quarter each
+template <typename F>
+AXON_DEV void others(const Shared& sh, int n, F&& f) {
+  for (int j = threadIdx.x & 3; j < n; j += 4) f(sh.few[j]);
+}
+AXON_DEV u64 quad_sum(u64 v) {
+  v += __shfl_xor(v, 1);
+  return v + __shfl_xor(v, 2);
+}
+// whether a comes before b in descending order
+AXON_DEV bool ahead(const Candidate& a, const Candidate& b) { return a.z > b.z || (a.z == b.z && a.i < b.i); }
+
+// The border in descending order: values above key are kept, of those on it the indices
+// up to last.  COUNT: target() values are kept, else as many as it takes for their weights
+// to reach target(); all there are if that is not reached.  mass: the kept weights (not
+// COUNT).
 struct Border {
   uint32_t key;
-  u64 mass_above;
-  uint32_t cnt_above, cnt_on;
-  u64 want;  // the target
+  int last;
 };
-// over the values from key ``lo`` to key ``hi``, which hold all that count
-template <bool COUNT, typename R, typename W, typename F>
-AXON_DEV Border find_border(Shared& sh, const R& row, uint32_t lo, uint32_t hi, W&& weight, F&& target) {
-  Border b{};
+template <bool COUNT, typename T, typename W>
+AXON_DEV Border find_border(Shared& sh, const Row<T>& row, uint32_t lo, uint32_t hi, W&& weight, u64 want) {
+  u64 above = 0;  // (number or weight) of what is above hi
   for (;;) {
     int shift = 0;
     while ((hi - lo) >> shift >= BINS) ++shift;
     clear_bins(sh);
     row.each([&](float z, int) {
-      const uint32_t k = order_key(z);
+      const uint32_t k = order_key<T>(z);
       if (k < lo || k > hi) return;
-      const uint32_t bin = (k - lo) >> shift;
-      atomicAdd(&sh.cnt[bin], 1u);
-      const u64 w = weight(z);
-      if (w) atomicAdd(&sh.mass[bin], w);
+      const u64 w = COUNT ? 1 : weight(z);
+      if (w) atomicAdd(&sh.bins[(k - lo) >> shift], w);
     });
     __syncthreads();
     const int e = BINS - 1 - 2 * threadIdx.x;
-    const u64 m[2] = {sh.mass[e], sh.mass[e - 1]};
-    const uint32_t c[2] = {sh.cnt[e], sh.cnt[e - 1]};
-    const Found f = find_entry<COUNT>(sh, m, c, b.mass_above, b.cnt_above, [&](u64 total) {
-      if (!b.want) b.want = min(target(total), total);
-      return b.want;
-    });
+    const u64 v[2] = {sh.bins[e], sh.bins[e - 1]};
+    const Found f = find_entry(sh, v, above, [&](u64 total) { return want = min(want, total); });
     const uint32_t bin = BINS - 1 - f.at;
     lo += bin << shift;
     hi = min(hi, lo + ((1u << shift) - 1));
-    b = Border{lo, f.mass_before, f.cnt_before, f.cnt_in, b.want};
-    if (lo == hi) return b;
-    if (f.cnt_in == 1) {  // one value is left: which
+    above = f.before;
+    if (lo == hi) {
+      // all have one value: as many of them as are wanted, the lowest indices
+      const u64 each = COUNT ? 1 : weight(key_value<T>(lo)), most = f.in / each, take = (want - above + each - 1) / each;
+      int last = row.V;
+      if (take < most) {
+        const int width = (row.V + BINS - 1) / BINS;  // <= BINS
+        clear_bins(sh);
+        row.each([&](float z, int i) {
+          if (order_key<T>(z) == lo) atomicAdd(&sh.bins[i / width], (u64)1);
+        });
+        __syncthreads();
+        const u64 b[2] = {sh.bins[2 * threadIdx.x], sh.bins[2 * threadIdx.x + 1]};
+        const Found g = find_entry(sh, b, 0, [&](u64) { return take; });
+        u64 w[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int in = 2 * threadIdx.x + j, i = g.at * width + in;
+          w[j] = in < width && i < row.V && order_key<T>(sane(to_f32(row.z[i]))) == lo;
+        }
+        __syncthreads();
+        last = g.at * width + find_entry(sh, w, g.before, [&](u64) { return take; }).at;
+      }
+      return Border{lo, last};
+    }
+    const int n = gather(sh, row, [&](float z) { const uint32_t k = order_key<T>(z); return lo <= k && k <= hi; },
+                         [&](float z) { return COUNT ? (u64)1 : weight(z); });
+    if (n <= FEW) {  // few enough to compare
+      const int i = threadIdx.x >> 2;
+      if (i < n) {
+        const Candidate me = sh.few[i];
+        u64 before = 0;
+        others(sh, n, [&](const Candidate& c) { before += ahead(c, me) ? c.w : 0; });
+        before = above + quad_sum(before);
+        if ((threadIdx.x & 3) == 0 && before < want && want <= before + me.w) sh.found = i;
+      }
       __syncthreads();
-      row.each([&](float z, int) {
-        const uint32_t k = order_key(z);
-        if (lo <= k && k <= hi) sh.found = (int)k;
-      });
-      __syncthreads();
-      b.key = (uint32_t)sh.found;
-      return b;
+      const Candidate me = sh.few[min(sh.found, n - 1)];
+      return Border{order_key<T>(me.z), me.i};
     }
   }
 }
 
-// the index at which the running sum of weight(z, i) reaches target(total); weight is 0
-// below the row's cut
-template <typename R, typename W, typename F>
-AXON_DEV int find_index(Shared& sh, const R& row, W&& weight, F&& target, u64* total) {
-  const int width = (row.V + BINS - 1) / BINS;  // <= BINS
+// the workgroup's sum of f over the row's values
+template <typename R, typename F>
+AXON_DEV u64 row_sum(Shared& sh, const R& row, F&& f) {
+  u64 sum = 0;
+  row.each([&](float z, int i) { sum += f(z, i); });
+  sum = wave_total(sum);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh.wave_sum[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  sum = 0;
+#pragma unroll
+  for (int w = 0; w < S_THREADS / 64; ++w) sum += sh.wave_sum[w];
+  return sum;
+}
+
+// The index at which the running sum of weight(z, i) reaches target(total), which is set.
+// weight is 0 below the row's cut.
+template <typename T, typename W, typename F>
+AXON_DEV int find_index(Shared& sh, const Row<T>& row, W&& weight, F&& target, u64* total) {
+  int width = (row.V + BINS - 1) / BINS;  // of a bin, <= BINS
   clear_bins(sh);
-  row.each([&](float z, int i) {
-    const u64 w = weight(z, i);
-    if (w) atomicAdd(&sh.mass[i / width], w);
-  });
+  if (row.n >= 0) {
+    row.each([&](float z, int i) {
+      const u64 w = weight(z, i);
+      if (w) atomicAdd(&sh.bins[i / width], w);
+    });
+  } else {
+    // all of the row: a wavefront adds up a chunk
+    width = CHUNK;
+    for (int c = threadIdx.x >> 6; c < chunks_of(row.V); c += S_THREADS / 64) {
+      u64 sum = 0;
+#pragma unroll 2
+      for (int j = 0; j < CHUNK / (64 * RUN<T>); ++j) {
+        float v[RUN<T>];
+        const int first = c * CHUNK + (j * 64 + (threadIdx.x & 63)) * RUN<T>;
+        load_run(row.z, first, row.V, v);
+#pragma unroll
+        for (int i = 0; i < RUN<T>; ++i)
+          if (v[i] >= row.cut) sum += weight(v[i], first + i);
+      }
+      sum = wave_total(sum);
+      if ((threadIdx.x & 63) == 0) sh.bins[c] = sum;
+    }
+  }
   __syncthreads();
   u64 want = 0;
   const int e = 2 * threadIdx.x;
-  const u64 m[2] = {sh.mass[e], sh.mass[e + 1]};
-  const uint32_t c[2] = {};
-  const Found f = find_entry<false>(sh, m, c, 0, 0, [&](u64 t) { return want = target(t); }, total);
-  const int first = f.at * width;
+  const u64 v[2] = {sh.bins[e], sh.bins[e + 1]};
+  const Found f = find_entry(sh, v, 0, [&](u64 t) { return want = target(t); }, total);
   u64 w[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const int i = first + e + j;
-    w[j] = e + j < width && i < row.V ? weight(sane(to_f32(row.z[i])), i) : 0;
+    const int i = f.at * width + e + j;
+    const float z = i < row.V ? sane(to_f32(row.z[i])) : -INFINITY;
+    w[j] = e + j < width && z >= row.cut ? weight(z, i) : 0;
   }
   __syncthreads();
-  return first + find_entry<false>(sh, w, c, f.mass_before, 0, [&](u64) { return want; }).at;
+  return f.at * width + find_entry(sh, w, f.before, [&](u64) { return want; }).at;
 }
 
-// the workgroup's maximum (of negated values: minimum)
+// the workgroup's maximum
 AXON_DEV float block_top(Shared& sh, float v) {
   v = wave_max(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = v;
   __syncthreads();
+#pragma unroll
   for (int w = 0; w < S_THREADS / 64; ++w) v = fmaxf(v, sh.red[w]);
   return v;
 }
@@ -375,14 +465,15 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
   __shared__ Shared sh;
   __shared__ float maxima[MAX_BLOCKS];
   __shared__ int32_t list[LIST];
+  constexpr float LOWEST = -3.402823466e38f;
   const int r = blockIdx.x, V = a.vocab, chunks = chunks_of(V), blocks = chunks * CHUNK_BLOCKS, tid = threadIdx.x;
   const T* z = (const T*)a.logits + r * a.ld;
   const RowSums in = row_sums(ws, r, V);
   const Settings s = settings_of(a, r);
-  float top = -INFINITY;
-  for (int i = tid; i < chunks; i += S_THREADS) top = fmaxf(top, in.chunk_max[i]);
+  const float uniform = a.uniform[r];
   const bool filtered = !s.greedy && (s.by_rank || s.p < 1.f || s.low > 0.f), fits = blocks <= MAX_BLOCKS;
-  float lowest = INFINITY;  // of the maxima that are numbers
+  float top = -INFINITY, lowest = INFINITY;  // of the maxima that are numbers
+  for (int i = tid; i < chunks; i += S_THREADS) top = fmaxf(top, in.chunk_max[i]);
   if (filtered && fits)
     for (int i = tid; i < blocks; i += S_THREADS) {
       const float m = in.block_max[i];
@@ -416,73 +507,74 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
     return;
   }
   const int scale = 62 - (V > 1 ? 32 - __clz(V - 1) : 0);
-  const double c = per_unit(s);
-  auto weight_of = [&](float v) { return weight_to(v, top, c); };
-  auto fixed = [&](double w) { return (u64)rint(ldexp(w, scale)); };
-  auto weight = [&](float v) { return fixed(weight_of(v)); };
+  const double c = per_unit(s), unit = ldexp(1., scale);
+  auto parts = [&](float v) { return exp2_neg(v == top ? 0. : ((double)v - top) * c); };
+  auto weight = [&](float v) { return as_fixed(parts(v), scale); };
   // the place in the kept weights' running sum, 1 .. sum
   auto drawn = [&](u64 sum) {
-    return min((u64)((double)fminf(fmaxf(a.uniform[r], 0.f), 1.f) * (double)sum), sum - 1) + 1;
+    return min((u64)((double)fminf(fmaxf(uniform, 0.f), 1.f) * (double)sum), sum - 1) + 1;
   };
-  u64 total;
+  u64 total = 0;
   int token;
   if (!filtered) {
     u64 w[2], want = 0;
-    const uint32_t none[2] = {};
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const int i = 2 * tid + j;
-      const double f = i < chunks ? weight_of(in.chunk_max[i]) : 0.;
-      w[j] = fixed(f) ? fixed(f * in.chunk_sum[i]) : 0;  // (a chunk whose weights are all 0 is not one to look in)
+      const float m = i < chunks ? in.chunk_max[i] : -INFINITY;
+      // (a chunk whose weights are all 0 is not one to look in)
+      w[j] = m > -INFINITY && weight(m) ? (u64)rint(as_double(parts(m)) * in.chunk_sum[i] * unit) : 0;
     }
-    const Found f = find_entry<false>(sh, w, none, 0, 0, [&](u64 sum) { return want = drawn(sum); }, &total);
+    const Found f = find_entry(sh, w, 0, [&](u64 sum) { return want = drawn(sum); }, &total);
     const int first = f.at * CHUNK + 2 * tid;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) w[j] = first + j < V ? weight(sane(to_f32(z[first + j]))) : 0;
+    for (int j = 0; j < 2; ++j) {
+      const float v = first + j < V ? sane(to_f32(z[first + j])) : -INFINITY;
+      w[j] = v > -INFINITY ? weight(v) : 0;
+    }
     __syncthreads();
-    token = f.at * CHUNK +
-            find_entry<false>(sh, w, none, 0, 0, [&](u64 sum) { return min(want - f.mass_before, sum); }).at;
+    token = f.at * CHUNK + find_entry(sh, w, 0, [&](u64 sum) { return min(want - f.before, sum); }).at;
   } else {
+    const double share = (double)fmaxf(s.p, 0.f), least = s.low > 0.f ? (double)fminf(s.low, 1.f) : -1.;
     double sum = 0.;  // of all weights
     if (needs_sum(s)) {
-      for (int i = tid; i < chunks; i += S_THREADS) sum += weight_of(in.chunk_max[i]) * in.chunk_sum[i];
+      for (int i = tid; i < chunks; i += S_THREADS) {
+        const float m = in.chunk_max[i];
+        if (m > -INFINITY) sum += as_double(parts(m)) * in.chunk_sum[i];
+      }
 #pragma unroll
       for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-      __syncthreads();
-      if ((tid & 63) == 0) sh.wave_mass[tid >> 6] = __double_as_longlong(sum);
+      if ((tid & 63) == 0) sh.wave_sum[tid >> 6] = __double_as_longlong(sum);
       __syncthreads();
       sum = 0.;
-      for (int w = 0; w < S_THREADS / 64; ++w) sum += __longlong_as_double(sh.wave_mass[w]);
+      for (int w = 0; w < S_THREADS / 64; ++w) sum += __longlong_as_double(sh.wave_sum[w]);
     }
-    const double share = (double)fmaxf(s.p, 0.f);
-    // nothing below ``cut`` is kept
-    float cut = -3.402823466e38f;
+    // Nothing below ``cut`` is kept (a top-k's weight, of which top-p takes its share,
+    // has to be there in full).
+    float cut = LOWEST;
+    if (s.low > 0.f && !(s.by_rank && s.p < 1.f)) cut = (float)(top + log2(least) / c);
     if (s.by_rank || s.p < 1.f) {
       lowest = -block_top(sh, -lowest);
       const float per_bin = (BINS - 1) / (top - lowest);
       if (fits && per_bin > 0.f && per_bin < INFINITY) {
         clear_bins(sh);
-        for (int i = tid; i < blocks; i += S_THREADS)
-          if (maxima[i] > -INFINITY) {
-            const int bin = min((int)((top - maxima[i]) * per_bin), BINS - 1);
-            if (s.by_rank) atomicAdd(&sh.cnt[bin], 1u);
-            else atomicAdd(&sh.mass[bin], weight(maxima[i]));
-          }
+        // (the share, a little more: these weights are rounded differently)
+        const u64 want = s.by_rank ? (u64)s.k : (u64)(share * sum * (1ll << 32) * 1.0001) + 1;
+        const float c32 = (float)c;
+        for (int i = tid; i < blocks; i += S_THREADS) {
+          const float m = maxima[i];
+          if (m > -INFINITY)
+            atomicAdd(&sh.bins[min((int)((top - m) * per_bin), BINS - 1)],
+                      s.by_rank ? (u64)1 : (u64)(__builtin_amdgcn_exp2f((m - top) * c32) * 4294967296.f));
+        }
         __syncthreads();
-        const int e = 2 * tid;
-        const u64 m[2] = {sh.mass[e], sh.mass[e + 1]};
-        const uint32_t n[2] = {sh.cnt[e], sh.cnt[e + 1]};
-        // (a little more than the share, whose sum was rounded otherwise)
-        const u64 want = s.by_rank ? (u64)s.k : (u64)(ldexp(share * sum, scale) * (1. + 1e-9)) + 1;
-        const Found f = s.by_rank ? find_entry<true>(sh, m, n, 0, 0, [&](u64) { return want; })
-                                  : find_entry<false>(sh, m, n, 0, 0, [&](u64) { return want; });
+        const u64 v[2] = {sh.bins[2 * tid], sh.bins[2 * tid + 1]};
+        const Found f = find_entry(sh, v, 0, [&](u64) { return want; });
         // every value of bins 0 .. f.at, with the roundings of a bin's number
-        if (f.at >= 0) cut = top - (f.at + 1) / per_bin * 1.000001f;
+        if (f.at >= 0) cut = fmaxf(cut, top - (f.at + 1) / per_bin * 1.000001f);
       }
-    } else {
-      cut = (float)(top + log2((double)fminf(s.low, 1.f)) / c);
     }
-    cut = fmaxf(cut - fabsf(cut) * 1e-6f, -3.402823466e38f);
+    cut = fmaxf(cut - fabsf(cut) * 1e-6f, LOWEST);
     Row<T> row{z, V, cut, -1, list};
     if (fits) {
       __syncthreads();
@@ -496,47 +588,70 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
       __syncthreads();
       if (sh.found <= LIST) row.n = sh.found;
     }
-    row.fill();
-    const uint32_t lo = order_key(cut), hi = order_key(top);
-    // the lowest value that is kept, how many have it and how many of them are kept
-    uint32_t border = 0, on = 0, kept_on = 0;
-    u64 mass = 0;  // of what top-k keeps
-    if (s.by_rank) {
-      const Border b = find_border<true>(sh, row, lo, hi, weight, [&](u64) { return (u64)s.k; });
-      border = b.key;
-      on = b.cnt_on;
-      kept_on = (uint32_t)(b.want - b.cnt_above);
-      mass = b.mass_above + kept_on * weight(key_value(border));
+    const int n = row.n < 0 ? FEW + 1 : gather(sh, row, [](float) { return true; }, weight);
+    if (n <= FEW) {
+      // few: each compared with each, by rank and weight, then by index
+      if (tid == 0) sh.sum[0] = sh.sum[1] = 0;
+      if (tid == 0) sh.found = 0;
+      __syncthreads();
+      const int me = tid >> 2;
+      const bool leads = me < n && (tid & 3) == 0;
+      const Candidate x = sh.few[min(me, n - 1)];
+      u64 rank = 0, before = 0;
+      others(sh, n, [&](const Candidate& o) {
+        const bool is = ahead(o, x);
+        rank += is;
+        before += is ? o.w : 0;
+      });
+      rank = quad_sum(rank);
+      before = quad_sum(before);
+      const bool first = !s.by_rank || rank < (u64)s.k;
+      if (s.by_rank && s.p < 1.f) {
+        if (leads && first) atomicAdd(&sh.sum[0], x.w);
+        __syncthreads();
+      }
+      const double of = s.by_rank ? (double)sh.sum[0] : sum * unit;
+      bool kept = first && x.w > 0 && (double)x.w >= least * unit;
+      if (s.p < 1.f) kept = kept && before < max((u64)ceil(share * of), (u64)1);
+      if (leads && kept) atomicAdd(&sh.sum[1], x.w);
+      __syncthreads();
+      if (leads && !kept) sh.few[me].w = 0;
+      __syncthreads();
+      total = sh.sum[1];
+      const u64 want = drawn(total);
+      before = 0;
+      others(sh, n, [&](const Candidate& o) { before += o.i < x.i ? o.w : 0; });
+      before = quad_sum(before);
+      if (leads && kept && before < want && want <= before + x.w) sh.found = x.i;
+      __syncthreads();
+      token = sh.found;
+    } else {
+      const uint32_t lo = order_key<T>(cut), hi = order_key<T>(top);
+      Border b{0, V};
+      if (s.by_rank) b = find_border<true>(sh, row, lo, hi, weight, (u64)s.k);
+      if (s.p < 1.f) {
+        const double of = s.by_rank ? (double)row_sum(sh, row, [&](float v, int i) {
+          const uint32_t k = order_key<T>(v);
+          return k > b.key || (k == b.key && i <= b.last) ? weight(v) : 0;
+        }) : sum * unit;
+        b = find_border<false>(sh, row, max(lo, b.key), hi, weight, max((u64)ceil(share * of), (u64)1));
+      }
+      token = find_index(
+          sh, row,
+          [&](float v, int i) {
+            const uint32_t k = order_key<T>(v);
+            if (v == -INFINITY || k < b.key || (k == b.key && i > b.last)) return (u64)0;
+            const u64 w = weight(v);
+            return (double)w >= least * unit ? w : (u64)0;
+          },
+          drawn, &total);
     }
-    if (s.p < 1.f) {
-      const double of = s.by_rank ? (double)mass : ldexp(sum, scale);
-      const Border b = find_border<false>(sh, row, max(lo, border), hi, weight,
-                                          [&](u64) { return max((u64)ceil(share * of), (u64)1); });
-      const u64 w = weight(key_value(b.key));
-      border = b.key;
-      on = b.cnt_on;
-      kept_on = (uint32_t)((b.want - b.mass_above + w - 1) / w);
-    }
-    int last_on = V;  // the last index on the border that is kept
-    if (kept_on < on)
-      last_on = find_index(sh, row, [&](float v, int) { return (u64)(order_key(v) == border); },
-                           [&](u64) { return (u64)kept_on; }, &total);
-    const double least = s.low > 0.f ? (double)fminf(s.low, 1.f) : -1.;
-    token = find_index(
-        sh, row,
-        [&](float v, int i) {
-          const uint32_t key = order_key(v);
-          if (v == -INFINITY || key < border || (key == border && i > last_on)) return (u64)0;
-          const double w = weight_of(v);
-          return w >= least ? fixed(w) : (u64)0;
-        },
-        drawn, &total);
   }
   if (tid == 0) {
     a.tokens[r] = token;
     const float v = sane(to_f32(z[token]));
     const double x = v == top ? 0. : ((double)v - top) / s.t;
-    a.logps[r] = (float)(x - log(ldexp((double)total, -scale)));
+    a.logps[r] = (float)(x - log((double)total / unit));
   }
 }
 
