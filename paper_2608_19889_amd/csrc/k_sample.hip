@@ -198,15 +198,15 @@ AXON_DEV void load_run(const T* z, int i, int V, float (&v)[RUN<T>]) {
 
 struct RowSums {  // of a row, in the workspace
   float* block_max;   // [chunks 64]
-  float* chunk_max;   // [chunks]
   double* chunk_sum;  // [chunks], relative to chunk_max
+  float* chunk_max;   // [chunks]
 };
 inline __host__ __device__ int chunks_of(int V) { return (V + CHUNK - 1) / CHUNK; }
-inline __host__ __device__ int64_t row_bytes(int V) { return (int64_t)chunks_of(V) * (CHUNK_BLOCKS * 4 + 4 + 8) + 4 * (chunks_of(V) & 1); }
+inline __host__ __device__ int64_t row_bytes(int V) { return ((int64_t)chunks_of(V) * (CHUNK_BLOCKS * 4 + 8 + 4) + 15) / 16 * 16; }
 AXON_DEV RowSums row_sums(void* ws, int r, int V) {
   const int n = chunks_of(V);
-  char* p = (char*)ws + r * row_bytes(V);
-  return RowSums{(float*)(p + 8 * n), (float*)(p + 8 * n) + n * CHUNK_BLOCKS, (double*)p};
+  float* p = (float*)((char*)ws + r * row_bytes(V));
+  return RowSums{p, (double*)(p + n * CHUNK_BLOCKS), p + n * (CHUNK_BLOCKS + 2)};
 }
 
 // a wavefront per chunk; a lane's load is RUN values, 32 / RUN lanes a block
@@ -463,7 +463,7 @@ AXON_DEV float block_top(Shared& sh, float v) {
 template <typename T>
 __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, void* ws) {
   __shared__ Shared sh;
-  __shared__ float maxima[MAX_BLOCKS];
+  __shared__ alignas(16) float maxima[MAX_BLOCKS];
   __shared__ int32_t list[LIST];
   constexpr float LOWEST = -3.402823466e38f;
   const int r = blockIdx.x, V = a.vocab, chunks = chunks_of(V), blocks = chunks * CHUNK_BLOCKS, tid = threadIdx.x;
@@ -472,14 +472,28 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
   const Settings s = settings_of(a, r);
   const float uniform = a.uniform[r];
   const bool filtered = !s.greedy && (s.by_rank || s.p < 1.f || s.low > 0.f), fits = blocks <= MAX_BLOCKS;
-  float top = -INFINITY, lowest = INFINITY;  // of the maxima that are numbers
-  for (int i = tid; i < chunks; i += S_THREADS) top = fmaxf(top, in.chunk_max[i]);
-  if (filtered && fits)
-    for (int i = tid; i < blocks; i += S_THREADS) {
-      const float m = in.block_max[i];
-      maxima[i] = m;
-      if (m > -INFINITY) lowest = fminf(lowest, m);
+  // (loads of everything that is needed, in flight together)
+  const float chunk_max = tid < chunks ? in.chunk_max[tid] : -INFINITY;
+  const bool summed = needs_sum(s);
+  const double chunk_sum = summed && tid < chunks ? in.chunk_sum[tid] : 0.;
+  float top = chunk_max, lowest = INFINITY;  // of the maxima that are numbers
+  for (int i = tid + S_THREADS; i < chunks; i += S_THREADS) top = fmaxf(top, in.chunk_max[i]);
+  if (filtered && fits) {
+    f32x4 m[MAX_BLOCKS / (4 * S_THREADS)];
+#pragma unroll
+    for (int j = 0; j < MAX_BLOCKS / (4 * S_THREADS); ++j) {
+      const int i = 4 * (j * S_THREADS + tid);
+      m[j] = i < blocks ? *(const f32x4*)(in.block_max + i) : f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
     }
+#pragma unroll
+    for (int j = 0; j < MAX_BLOCKS / (4 * S_THREADS); ++j) {
+      const int i = 4 * (j * S_THREADS + tid);
+      if (i < blocks) *(f32x4*)(maxima + i) = m[j];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (m[j][k] > -INFINITY) lowest = fminf(lowest, m[j][k]);
+    }
+  }
   top = block_top(sh, top);
   if (top == -INFINITY) {
     if (tid == 0) {
@@ -537,8 +551,9 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
   } else {
     const double share = (double)fmaxf(s.p, 0.f), least = s.low > 0.f ? (double)fminf(s.low, 1.f) : -1.;
     double sum = 0.;  // of all weights
-    if (needs_sum(s)) {
-      for (int i = tid; i < chunks; i += S_THREADS) {
+    if (summed) {
+      if (chunk_max > -INFINITY) sum = as_double(parts(chunk_max)) * chunk_sum;
+      for (int i = tid + S_THREADS; i < chunks; i += S_THREADS) {
         const float m = in.chunk_max[i];
         if (m > -INFINITY) sum += as_double(parts(m)) * in.chunk_sum[i];
       }
