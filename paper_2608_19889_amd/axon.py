@@ -498,32 +498,35 @@ def policy_loss(logits: torch.Tensor, targets: torch.Tensor, cu_seqlens: list, o
 def _head_rows(t: torch.Tensor, heads, hd: int, dtype, name: str, out: bool = False):
     """(the tensor, its row stride) of [tokens, heads, hd] with contiguous heads.  An
     input of another layout is copied; an output is refused."""
-    if t.dim() != 3 or t.shape[2] != hd or (heads is not None and t.shape[1] != heads) or t.dtype != dtype:
-        raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {hd}] {dtype}, got {tuple(t.shape)} {t.dtype}")
-    tokens, heads, _ = t.shape
-    row = heads * hd
-    ld = row if tokens < 2 else t.stride(0)
-    if t.stride(2) == 1 and (heads < 2 or t.stride(1) == hd) and ld >= row:
-        return t, ld
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != hd or (heads is not None and shape[1] != heads) or t.dtype != dtype:
+        raise ValueError(f"{name} must be [tokens, {heads or 'heads'}, {hd}] {dtype}, got {tuple(shape)} {t.dtype}")
+    row = shape[1] * hd
+    ld, step, one = t.stride()
+    if one == 1 and (step == hd or shape[1] < 2) and (ld >= row or shape[0] < 2):
+        return t, max(ld, row)
     if out:
         raise ValueError(f"{name} must have contiguous heads and rows that do not overlap")
     return t.contiguous(), row
 
 
 def _pages_arg(k_cache: torch.Tensor, v_cache: torch.Tensor) -> AxonKvPages:
-    if k_cache.dim() != 4 or k_cache.shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
+    shape = k_cache.shape
+    if len(shape) != 4 or shape != v_cache.shape or k_cache.dtype != v_cache.dtype:
         raise ValueError("k_cache and v_cache must be [pages, kv heads, page size, head dim] of one type, got "
-                         f"{tuple(k_cache.shape)} {k_cache.dtype} and {tuple(v_cache.shape)} {v_cache.dtype}")
+                         f"{tuple(shape)} {k_cache.dtype} and {tuple(v_cache.shape)} {v_cache.dtype}")
     if not (k_cache.is_contiguous() and v_cache.is_contiguous()):
         raise ValueError("k_cache and v_cache must be contiguous")
-    pages, kv, ps, hd = k_cache.shape
+    pages, kv, ps, hd = shape
     return AxonKvPages(k_cache.data_ptr(), v_cache.data_ptr(), _code(k_cache, "the cache"), kv, hd, ps, pages)
 
 
 def _table(t: torch.Tensor, lens: torch.Tensor, name: str, lens_name: str):
-    if t.dim() != 2 or t.dtype != torch.int32:
-        raise ValueError(f"{name} must be int32 [sequences, pages], got {tuple(t.shape)} {t.dtype}")
-    return t.contiguous(), _vector(lens, t.shape[0], torch.int32, lens_name)
+    """(the tables, their lengths, rows, columns)"""
+    shape = t.shape
+    if len(shape) != 2 or t.dtype != torch.int32:
+        raise ValueError(f"{name} must be int32 [sequences, pages], got {tuple(shape)} {t.dtype}")
+    return t.contiguous(), _vector(lens, shape[0], torch.int32, lens_name), shape[0], shape[1]
 
 
 def _sums(values, device_copy, n: int, name: str, like):
@@ -537,9 +540,9 @@ def _sums(values, device_copy, n: int, name: str, like):
 
 def _batch_arg(block_table, lens, cu_seqlens, cu_device, like):
     """The C structure and the tensors that it points at."""
-    table, lens = _table(block_table, lens, "block_table", "lens")
-    host, cu = _sums(cu_seqlens, cu_device, table.shape[0], "cu_seqlens", like)
-    return AxonKvBatch(table.shape[0], table.shape[1], _ptr(cu), host, lens.data_ptr(), table.data_ptr()), (table, lens, cu)
+    table, lens, seqs, columns = _table(block_table, lens, "block_table", "lens")
+    host, cu = _sums(cu_seqlens, cu_device, seqs, "cu_seqlens", like)
+    return AxonKvBatch(seqs, columns, _ptr(cu), host, lens.data_ptr(), table.data_ptr()), (table, lens, cu)
 
 
 @_row_operator
@@ -558,14 +561,16 @@ def rope_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cach
     of each one's first key."""
     pages = _pages_arg(k_cache, v_cache)
     hd, dtype = pages.head_dim, k_cache.dtype
-    kv_, ldk = _head_rows(k, pages.kv_heads, hd, dtype, "k")
+    kv, ldk = _head_rows(k, pages.kv_heads, hd, dtype, "k")
     vv, ldv = _head_rows(v, pages.kv_heads, hd, dtype, "v")
     tokens = k.shape[0]
     batch, keep = _batch_arg(block_table, lens, cu_seqlens, cu_device, k)
     if v.shape[0] != tokens or (q is not None and q.shape[0] != tokens):
         raise ValueError("q, k and v must have the same tokens")
+    rot = 0
     if inv_freq is not None:
-        inv_freq = _vector(inv_freq, inv_freq.numel(), torch.float64, "inv_freq")
+        rot = 2 * inv_freq.numel()
+        inv_freq = _vector(inv_freq, rot // 2, torch.float64, "inv_freq")
     offsets = _vector(offsets, block_table.shape[0], torch.int32, "offsets")
     heads, qv, ldq, ov, ldo = 0, None, 0, None, 0
     if q is not None:
@@ -575,9 +580,8 @@ def rope_append(q: torch.Tensor | None, k: torch.Tensor, v: torch.Tensor, k_cach
         ov, ldo = _head_rows(out, heads, hd, dtype, "out", out=True)
     elif out is not None:
         raise ValueError("out without q")
-    _check(lib().axon_rope_append(pages, batch, tokens, heads, _ptr(qv), ldq, kv_.data_ptr(), ldk, vv.data_ptr(), ldv,
-                                  _ptr(ov), ldo, _ptr(inv_freq), 0 if inv_freq is None else 2 * inv_freq.numel(),
-                                  int(interleaved), scale, _ptr(offsets), _current(k)))
+    _check(lib().axon_rope_append(pages, batch, tokens, heads, _ptr(qv), ldq, kv.data_ptr(), ldk, vv.data_ptr(), ldv,
+                                  _ptr(ov), ldo, _ptr(inv_freq), rot, int(interleaved), scale, _ptr(offsets), _current(k)))
     torch.autograd.graph.increment_version((k_cache, v_cache))
     return out
 
@@ -606,13 +610,13 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     if prefix_table is not None:
         if prefix_lens is None:
             raise ValueError("prefix_table without prefix_lens")
-        table, plens = _table(prefix_table, prefix_lens, "prefix_table", "prefix_lens")
+        table, plens, groups, columns = _table(prefix_table, prefix_lens, "prefix_table", "prefix_lens")
         if cu_groups is None:
-            if table.shape[0] != 1:
+            if groups != 1:
                 raise ValueError("several groups need cu_groups")
             cu_groups = [0, batch.seqs]
-        host, cu = _sums(cu_groups, groups_device, table.shape[0], "cu_groups", q)
-        prefix = AxonKvPrefix(table.shape[0], table.shape[1], cu.data_ptr(), host, plens.data_ptr(), table.data_ptr())
+        host, cu = _sums(cu_groups, groups_device, groups, "cu_groups", q)
+        prefix = AxonKvPrefix(groups, columns, cu.data_ptr(), host, plens.data_ptr(), table.data_ptr())
         keep = (keep, table, plens, cu)
     elif prefix_lens is not None or cu_groups is not None:
         raise ValueError("prefix_lens and cu_groups need prefix_table")
