@@ -163,7 +163,7 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
     const PrefixAttnShape shape = shape_of(*pages, *batch, prefix, tokens, heads);
     const int64_t longest = std::max(batch->table_stride, shape.groups ? prefix->table_stride : 0);
     const int64_t need = prefix_attn_workspace(shape);
-    if (prefix_attn_units(shape, longest * pages->page_size) >= (int64_t)1 << 31 || need >= (int64_t)1 << 40)
+    if (prefix_attn_steps(shape, longest * pages->page_size) >= (int64_t)1 << 31 || need >= (int64_t)1 << 40)
       return fail(AXON_E_CAPACITY, num(tokens) + " tokens of " + num(heads) + " heads over tables of " + num(longest) +
                                        " pages are too many for one call");
     if (int r = check_workspace(workspace, workspace_bytes, need)) return r;

@@ -7,19 +7,18 @@
 // rows of a segment and kv head are its tokens' query heads of that kv head, so a
 // prefix is multiplied with everything that shares it.  Rows go in tiles: a segment of
 // at most 16 rows is one *narrow* tile (a single token's own keys), any other is cut
-// into *wide* ones of 256 rows.  Each kind has its kernel:
-//   prefix_wide_kernel    a workgroup of 8 wavefronts, 32 rows each, over keys that all
-//                         of them read from LDS (with few rows the keys are halved
-//                         between wavefronts): matrix instructions' work
-//   prefix_narrow_kernel  every wavefront by itself over 16 keys at a time, many of them
-//                         on a CU: memory's work
-//   prefix_join_kernel    joins the parts that they leave
+// into *wide* ones of 256 rows.  A workgroup works on tiles of one kind:
+//   wide    its 8 wavefronts take 32 rows each, over keys that all of them read from LDS
+//           (with few rows the keys are halved between wavefronts): matrix instructions'
+//           work
+//   narrow  every wavefront by itself, over 16 keys at a time: memory's work
+// and a second kernel joins a row's parts.
 //
 // Work is cut into units of keys of a tile, in the order (segment, kv head, tile, keys),
-// and every worker takes an equal run of consecutive units, whatever the lengths are,
-// which only the device knows.  Of the keys of a tile in its run it leaves (max, sum,
-// product).  What is added to what depends on the lengths alone: the same bits every
-// time.
+// and every worker (a workgroup, or a narrow one's wavefront) takes an equal run of
+// consecutive units, whatever the lengths are, which only the device knows.  Of the keys
+// of a tile in its run it leaves (max, sum, product).  What is added to what depends on
+// the lengths alone: the same bits every time.
 #include <algorithm>
 #include <type_traits>
 
@@ -29,10 +28,9 @@
 namespace axon {
 
 constexpr float LOG2E_F = 1.4426950408889634f;
-constexpr int WIDE_THREADS = 512, WIDE_WAVES = 8, WIDE_KEYS = 64, WIDE_ROWS = 256;
-constexpr int NARROW_THREADS = 256, NARROW_WAVES = 4, NARROW_KEYS = 16, NARROW_ROWS = 16;
-constexpr int WIDE_LEAST = 4, NARROW_LEAST = 2;        // steps of a worker
-constexpr int SLOT_BLOCKS = WIDE_ROWS / 16;           // 16-row blocks of a wide part
+constexpr int PA_WGS = 256, PA_THREADS = 512, PA_WAVES = 8;
+constexpr int WIDE_KEYS = 64, WIDE_ROWS = 256, NARROW_KEYS = 16, NARROW_ROWS = 16;
+constexpr int SLOT_BLOCKS = WIDE_ROWS / 16;  // 16-row blocks of a wide part
 
 // ---------------------------------------------------------------- plan
 
@@ -44,32 +42,35 @@ struct Segment {
   bool own;
 };
 
+// segment s, whose tokens and length are known
+template <typename T>
+AXON_DEV Segment segment_with(const PrefixAttnArgs<T>& a, int s, int tok0, int tokens, int64_t len) {
+  const int groups = a.shared.groups;
+  Segment g{tok0, tokens, len, 0, nullptr, s >= groups};
+  const int stride = g.own ? a.seqs.stride : a.shared.stride;
+  g.table = g.own ? a.seqs.table + (int64_t)(s - groups) * stride : a.shared.table + (int64_t)s * stride;
+  g.room = stride * a.kv.ps;
+  return g;
+}
 template <typename T>
 AXON_DEV Segment segment_of(const PrefixAttnArgs<T>& a, int s) {
-  Segment g;
   const int groups = a.shared.groups;
-  int end;
   auto among = [](int v, int n) { return min(max(v, 0), n); };
+  int tok0, end;
+  int64_t len;
   if (s < groups) {
     const int lo = among(a.shared.cu[s], a.seqs.seqs), hi = among(a.shared.cu[s + 1], a.seqs.seqs);
-    g.tok0 = a.seqs.cu ? a.seqs.cu[lo] : lo;
+    len = a.shared.lens[s];
+    tok0 = a.seqs.cu ? a.seqs.cu[lo] : lo;
     end = a.seqs.cu ? a.seqs.cu[hi] : hi;
-    g.len = a.shared.lens[s];
-    g.table = a.shared.table + (int64_t)s * a.shared.stride;
-    g.room = a.shared.stride * a.kv.ps;
-    g.own = false;
   } else {
     const int b = s - groups;
-    g.tok0 = a.seqs.cu ? a.seqs.cu[b] : b;
+    len = a.seqs.lens[b];
+    tok0 = a.seqs.cu ? a.seqs.cu[b] : b;
     end = a.seqs.cu ? a.seqs.cu[b + 1] : b + 1;
-    g.len = a.seqs.lens[b];
-    g.table = a.seqs.table + (int64_t)b * a.seqs.stride;
-    g.room = a.seqs.stride * a.kv.ps;
-    g.own = true;
   }
-  g.tok0 = among(g.tok0, a.tokens);
-  g.tokens = among(end, a.tokens) - g.tok0;
-  return g;
+  tok0 = among(tok0, a.tokens);
+  return segment_with(a, s, tok0, among(end, a.tokens) - tok0, len);
 }
 // keys that some of rows ``row0`` .. row0 + n - 1 reads (G query heads a token)
 AXON_DEV int tile_keys(const Segment& g, int G, int row0, int n) {
@@ -82,13 +83,18 @@ AXON_DEV int row_keys(const Segment& g, int G, int r) {
   return (int)min(g.own ? g.len + r / G + 1 : g.len, (int64_t)g.room);
 }
 
-// The tiles of one kind, their units, and their steps: as many as units, and START more
+// The tiles of one kind, their units, and their steps: STEP for each unit, and START more
 // at its beginning that stand for what a tile costs by itself (looking up pages, loading
-// queries, filling the pipeline).  Workers share the steps.
-template <bool WIDE>
+// queries, filling the pipeline).  Workers share the steps.  A narrow unit is one step; a
+// wide one takes a workgroup as long as 9 (128 dimensions) or 14 (64) narrow ones take its
+// 8 wavefronts.  Measured, with START six units (us, attention of 64 answers to 4096 tokens,
+// 256 to 16 prompts of 64 dimensions, 48 to 50011): STEP 4 and START 12 44, 115, 135;
+// 8 and 48 36, 77, 114; 12 and 72 35, 68, 123.
+template <bool WIDE, int HD>
 struct Tiles {
   static constexpr int ROWS = WIDE ? WIDE_ROWS : NARROW_ROWS, KEYS = WIDE ? WIDE_KEYS : NARROW_KEYS;
-  static constexpr int START = 4;
+  static constexpr int STEP = !WIDE ? 1 : HD == 128 ? 9 : 14, START = WIDE ? 6 * STEP : 4;
+  static constexpr int LEAST = WIDE ? 4 * STEP : 2;  // steps that are worth a worker
   static AXON_DEV int of(const Segment& g, int G) {  // of a kv head
     const int rows = g.tokens * G;
     return rows > NARROW_ROWS ? (WIDE ? (rows + ROWS - 1) / ROWS : 0) : (WIDE || rows <= 0 ? 0 : 1);
@@ -98,7 +104,7 @@ struct Tiles {
   }
   static AXON_DEV int steps(const Segment& g, int G, int rt) {
     const int u = units(g, G, rt);
-    return u ? u + START : 0;
+    return u ? STEP * u + START : 0;
   }
   // (steps, tiles) of a kv head
   static AXON_DEV int2 sizes(const Segment& g, int G) {
@@ -112,103 +118,130 @@ struct Tiles {
   }
 };
 
-// where the parts of a tile are: slots first .. first + count - 1
-struct TileParts {
-  int32_t first, count;
+// Where a row's parts are: in 16-row blocks ``block``, block + step, ... of the parts
+struct RowParts {
+  int32_t block;
+  int32_t count;  // 512 times the number, 16 times the step (1 .. 16), the row in its block
 };
-// [prefix, own][kv head][first row of the tile among all tokens' rows]
-AXON_DEV int64_t info_at(bool own, int kvh, int KV, int64_t rows, int tok0, int G, int row0) {
-  return ((own ? KV : 0) + kvh) * rows + (int64_t)tok0 * G + row0;
+AXON_DEV RowParts row_parts(int block, int count, int step, int row) {
+  return RowParts{block, count << 9 | step << 4 | row};
+}
+// [prefix, own][kv head][row among all tokens' rows]
+AXON_DEV int64_t info_at(bool own, int kvh, int KV, int64_t rows, int64_t row) {
+  return ((own ? KV : 0) + kvh) * rows + row;
 }
 // a block of 16 rows of a part: [16][hd] products, 16 maxima, 16 sums
 constexpr int part_floats(int hd) { return 16 * hd + 32; }
 
-// A place in the order of steps
+// a worker's steps: equal shares, the first ones a step more
+struct Shares {
+  int n, each, more;  // workers
+  AXON_DEV Shares(int workers, int total) : n(workers), each(total / max(workers, 1)), more(total - workers * each) {}
+  AXON_DEV int start(int w) const { return each * w + min(w, more); }
+  AXON_DEV int of(int step) const {
+    const int longer = (each + 1) * more;
+    return step < longer ? step / (each + 1) : more + (step - longer) / max(each, 1);
+  }
+};
+
+// A place in the order of a kind's steps
 struct Place {
   int s, kvh, rt, step, tile;  // tile: number among all tiles of the kind
 };
-template <int WAVES>
 struct PlanShared {
-  int64_t sum[2][WAVES];
-  int place[WAVES][4];
-  int next[2];
+  int sum[4][PA_WAVES];
+  int place[PA_WAVES][8];
 };
 
-// Steps of all segments (total), and what the threads before this one (segments s0 ..
-// s1 - 1 are its own) have; every thread of the workgroup calls it.
-template <typename T, bool WIDE, int THREADS>
+// inclusive sum over the lanes before, by row and half moves of registers
+template <int CTRL, int ROWS>
+AXON_DEV int add_moved(int v) {
+  return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, true);
+}
+AXON_DEV int wave_scan(int v) {
+  v = add_moved<0x111, 0xf>(v);  // from 1, 2, 4, 8 lanes before in a row of 16
+  v = add_moved<0x112, 0xf>(v);
+  v = add_moved<0x114, 0xf>(v);
+  v = add_moved<0x118, 0xf>(v);
+  v = add_moved<0x142, 0xa>(v);  // a row's last lane to the next row
+  return add_moved<0x143, 0xc>(v);  // and the first half's to the second
+}
+
+// Steps and tiles of all segments, of each kind, and of those before a thread's own
+// (s0 .. s1 - 1); every thread of the workgroup calls it.
+template <typename T, int HD>
 struct Plan {
   const PrefixAttnArgs<T>& a;
-  PlanShared<THREADS / 64>& sh;
+  PlanShared& sh;
   int G, KV, segs, s0, s1;
-  int64_t total, before[2], mine[2];  // steps, tiles
-  AXON_DEV Plan(const PrefixAttnArgs<T>& args, PlanShared<THREADS / 64>& shared) : a(args), sh(shared) {
+  int total[2], before[4], mine[4];  // narrow and wide: steps (0, 1), tiles (2, 3)
+  AXON_DEV Plan(const PrefixAttnArgs<T>& args, PlanShared& shared) : a(args), sh(shared) {
     KV = a.kv.kv_heads;
     G = a.heads / KV;
     segs = a.shared.groups + a.seqs.seqs;
-    const int each = (segs + THREADS - 1) / THREADS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int each = (segs + PA_THREADS - 1) / PA_THREADS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     s0 = min(segs, (int)threadIdx.x * each);
     s1 = min(segs, s0 + each);
-    mine[0] = mine[1] = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) mine[j] = 0;
     for (int s = s0; s < s1; ++s) {
-      const int2 n = Tiles<WIDE>::sizes(segment_of(a, s), G);
-      mine[0] += (int64_t)n.x * KV;
-      mine[1] += (int64_t)n.y * KV;
+      const Segment g = segment_of(a, s);
+      const int2 n = Tiles<false, HD>::sizes(g, G), w = Tiles<true, HD>::sizes(g, G);
+      mine[0] += n.x * KV;
+      mine[1] += w.x * KV;
+      mine[2] += n.y * KV;
+      mine[3] += w.y * KV;
     }
-    int64_t upto[2] = {mine[0], mine[1]};
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int64_t v = __shfl_up(upto[j], d);
-        if (lane >= d) upto[j] += v;
-      }
-    if (lane == 63) {
-      sh.sum[0][wave] = upto[0];
-      sh.sum[1][wave] = upto[1];
+    for (int j = 0; j < 4; ++j) {
+      const int upto = wave_scan(mine[j]);
+      before[j] = upto - mine[j];
+      if (lane == 63) sh.sum[j][wave] = upto;
     }
     __syncthreads();
-    total = 0;
-    before[0] = upto[0] - mine[0];
-    before[1] = upto[1] - mine[1];
+    total[0] = total[1] = 0;
 #pragma unroll
-    for (int w = 0; w < THREADS / 64; ++w) {
-      if (w < wave) {
-        before[0] += sh.sum[0][w];
-        before[1] += sh.sum[1][w];
+    for (int w = 0; w < PA_WAVES; ++w)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int v = sh.sum[j][w];
+        before[j] += w < wave ? v : 0;
+        if (j < 2) total[j] += v;
       }
-      total += sh.sum[0][w];
-    }
   }
-  // step ``at`` (< total) of worker ``w`` of the workgroup, for get(w) after a barrier
-  AXON_DEV void find(int w, int64_t at) {
-    if (at < before[0] || at >= before[0] + mine[0]) return;  // one thread goes on
-    int64_t u0 = before[0], t0 = before[1];
+  // notes step ``at`` of worker ``w`` of the workgroup, for get(w) after a barrier
+  template <bool WIDE>
+  AXON_DEV void find(int w, int at) {
+    if (at < before[WIDE] || at >= before[WIDE] + mine[WIDE]) return;  // one thread goes on
+    int u0 = before[WIDE], t0 = before[2 + WIDE];
     for (int s = s0; s < s1; ++s) {
-      const int2 n = Tiles<WIDE>::sizes(segment_of(a, s), G);
-      if (at < u0 + (int64_t)n.x * KV) {
-        sh.place[w][0] = s;
-        sh.place[w][1] = (int)(at - u0);
-        sh.place[w][2] = (int)t0;
-        sh.place[w][3] = n.x;
+      const Segment g = segment_of(a, s);
+      const int2 n = Tiles<WIDE, HD>::sizes(g, G);
+      if (at < u0 + n.x * KV) {
+        const int kvh = (at - u0) / n.x;
+        int* p = sh.place[w];
+        p[0] = s;
+        p[1] = kvh;
+        p[2] = at - u0 - kvh * n.x;
+        p[3] = t0 + kvh * n.y;
+        p[4] = g.tok0;
+        p[5] = g.tokens;
+        p[6] = (int)g.len;  // (a length is 32 bits)
         return;
       }
-      u0 += (int64_t)n.x * KV;
-      t0 += (int64_t)n.y * KV;
+      u0 += n.x * KV;
+      t0 += n.y * KV;
     }
   }
+  template <bool WIDE>
   AXON_DEV Place get(int w, Segment& g) const {
-    Place p;
-    p.s = __builtin_amdgcn_readfirstlane(sh.place[w][0]);
-    const int off = __builtin_amdgcn_readfirstlane(sh.place[w][1]), per = __builtin_amdgcn_readfirstlane(sh.place[w][3]);
-    p.tile = __builtin_amdgcn_readfirstlane(sh.place[w][2]);
-    g = segment_of(a, p.s);
-    p.kvh = off / per;
-    p.step = off % per;
-    p.rt = 0;
-    p.tile += p.kvh * Tiles<WIDE>::of(g, G);
+    int v[7];
+#pragma unroll
+    for (int j = 0; j < 7; ++j) v[j] = __builtin_amdgcn_readfirstlane(sh.place[w][j]);
+    g = segment_with(a, v[0], v[4], v[5], (int64_t)v[6]);
+    Place p{v[0], v[1], 0, v[2], v[3]};
     for (;;) {
-      const int n = Tiles<WIDE>::steps(g, G, p.rt);
+      const int n = Tiles<WIDE, HD>::steps(g, G, p.rt);
       if (p.step < n) return p;
       p.step -= n;
       ++p.rt;
@@ -216,37 +249,50 @@ struct Plan {
     }
   }
   // the next tile that has units (there is one); lane-parallel over segments without any
+  template <bool WIDE>
   AXON_DEV void advance(Place& p, Segment& g) const {
     const int lane = threadIdx.x & 63;
     p.step = 0;
+    ++p.tile;
+    if (++p.rt < Tiles<WIDE, HD>::of(g, G)) return;  // (a tile of a segment has units if any has)
+    p.rt = 0;
+    if (++p.kvh < KV) return;
+    p.kvh = 0;
+    ++p.s;
     for (;;) {
-      ++p.tile;
-      if (++p.rt < Tiles<WIDE>::of(g, G)) {
-        if (Tiles<WIDE>::units(g, G, p.rt)) return;
-        continue;
-      }
-      p.rt = 0;
-      if (++p.kvh < KV) return;  // (the first tile of a segment has units if any has)
-      p.kvh = 0;
-      ++p.s;
-      for (;;) {
-        int2 n = {0, 0};
-        if (p.s + lane < segs) n = Tiles<WIDE>::sizes(segment_of(a, p.s + lane), G);
-        const uint64_t has = __ballot(n.x > 0);
-        const int skip = has ? __ffsll((long long)has) - 1 : 64;
-        int tiles = lane < skip ? n.y : 0;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) tiles += __shfl_xor(tiles, d);
-        p.tile += __builtin_amdgcn_readfirstlane(tiles) * KV;
-        p.s += skip;
-        if (has || p.s >= segs) break;
-      }
-      p.s = __builtin_amdgcn_readfirstlane(p.s);
-      g = segment_of(a, min(p.s, segs - 1));
-      return;
+      int2 n = {0, 0};
+      if (p.s + lane < segs) n = Tiles<WIDE, HD>::sizes(segment_of(a, p.s + lane), G);
+      const uint64_t has = __ballot(n.x > 0);
+      const int skip = has ? __ffsll((long long)has) - 1 : 64;
+      if (skip > 0) p.tile += __builtin_amdgcn_readlane(wave_scan(lane < skip ? n.y : 0), 63) * KV;
+      p.s = __builtin_amdgcn_readfirstlane(p.s + skip);
+      if (has || p.s >= segs) break;
     }
+    g = segment_of(a, min(p.s, segs - 1));
   }
 };
+
+// What worker ``me`` does of the tile at p (its steps at .. at + take - 1): units first ..
+// last - 1.
+struct Work {
+  int take, first, last;
+  bool leads;  // has the tile's first unit
+  int parts;   // that the tile will have, if so
+};
+template <bool WIDE, int HD>
+AXON_DEV Work work_of(const Segment& g, const Place& p, int G, int at, int end, const Shares& shares, int me) {
+  using X = Tiles<WIDE, HD>;
+  const int steps = X::steps(g, G, p.rt);
+  // a unit belongs to who has its first step
+  auto unit_at = [](int step) { return max(step - X::START + X::STEP - 1, 0) / X::STEP; };
+  Work w;
+  w.take = min(steps - p.step, end - at);
+  w.first = unit_at(p.step);
+  w.last = unit_at(p.step + w.take);
+  w.leads = w.first == 0 && w.last > 0;
+  w.parts = w.leads ? shares.of(at - p.step + steps - X::STEP) - me + 1 : 0;
+  return w;
+}
 
 // ---------------------------------------------------------------- tiles in LDS
 
@@ -306,15 +352,23 @@ struct Vec8<float> {
   typedef f32x8 t;
 };
 
-// 8 elements of a query row, negated for a negative scale (any element alignment)
+// 8 elements of a query row (any element alignment)
+AXON_DEV bf16x8 load_q8_as(const bf16* p, bf16x8) { return *(const bf16x8_any*)p; }
+AXON_DEV f32x8 load_q8_as(const float* p, f32x8) {
+  const f32x4 a = *(const f32x4_any*)p, b = *(const f32x4_any*)(p + 4);
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
 template <typename T>
-AXON_DEV typename Vec8<T>::t load_q8(const T* p, bool negate) {
-  typename Vec8<T>::t v;
-  Run8<T> r;
-  r.load(p);
+AXON_DEV typename Vec8<T>::t load_q8(const T* p) {
+  return load_q8_as(p, typename Vec8<T>::t{});
+}
+// for a negative scale
+template <typename V, int N>
+AXON_DEV void negate(V (&q)[N]) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = from_f32<T>(negate ? -r[j] : r[j]);
-  return v;
+  for (int k = 0; k < N; ++k)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[k][j] = -q[k][j];
 }
 AXON_DEV bf16x8 read8(const bf16* p, const bf16*) { return *(const bf16x8*)p; }
 AXON_DEV f32x8 read8(const float* p, const float* p2) {
@@ -461,14 +515,13 @@ struct Wide {
   using L = Lds<T, HD>;
   // bf16: 4 stages of 64 keys; float32 (keys and values twice as wide): 2 or 4
   static constexpr int TILE = WIDE_KEYS * HD, STAGES = sizeof(T) == 4 && HD == 128 ? 2 : 4;
-  static constexpr int MY_KEYS = WIDE_KEYS / WIDE_WAVES;  // staged by a wavefront
+  static constexpr int MY_KEYS = WIDE_KEYS / PA_WAVES;  // staged by a wavefront
   static constexpr int LOADS = 2 * (MY_KEYS / L::RPI);    // its copies
-  static constexpr int BATCH = WIDE_THREADS / 4;          // units whose pages are looked up at a time
+  static constexpr int BATCH = PA_THREADS / 4;          // units whose pages are looked up at a time
   struct Shared {
     alignas(16) T tiles[STAGES][2][TILE];
-    int32_t blocks[WIDE_THREADS];     // where a batch's 16-key blocks are in the cache, 4 a unit, -1: none
-    int32_t odd[STAGES][WIDE_WAVES];  // make_finite's rows
-    PlanShared<WIDE_WAVES> plan;
+    int32_t blocks[PA_THREADS];     // where a batch's 16-key blocks are in the cache, 4 a unit, -1: none
+    int32_t odd[STAGES][PA_WAVES];  // make_finite's rows
   };
 };
 
@@ -504,7 +557,7 @@ struct WideRows {
     const int r = min(r0 + c, rows - 1);
     const T* p = q_row<T, HD>(a, g, G, kvh, r) + 8 * hl;
 #pragma unroll
-    for (int k = 0; k < QS; ++k) q[k] = load_q8<T>(p + 16 * k, a.scale < 0.f);
+    for (int k = 0; k < QS; ++k) q[k] = load_q8<T>(p + 16 * k);
     limit = row_keys(g, G, r);
     least = row_keys(g, G, min(r0, rows - 1));
     most = row_keys(g, G, min(r0 + 31, rows - 1));
@@ -524,28 +577,38 @@ struct WideRows {
 #pragma unroll
     for (int k = 0; k < QS; ++k) s = mul_wide(kf[k], q[k], s);
   }
-  // s = the weights of block kb of the unit at key0
-  AXON_DEV void weights(f32x16& s, int key0, int kb, int pages, const int32_t* odd) {
+  // s[b] = the weights of blocks kb0 + b of the unit at key0, all to one reference: raising
+  // it rescales the products that are there, and no weights wait for theirs then
+  template <int NB>
+  AXON_DEV void weights(f32x16 (&s)[NB], int key0, int kb0, int pages, const int32_t* odd) {
     if (key0 + WIDE_KEYS > least || pages != 15) {
-      const int seen = limit - key0 - 32 * kb - 4 * hl;
-      const int seen0 = pages >> (2 * kb) & 1 ? seen : 0, seen1 = pages >> (2 * kb + 1) & 1 ? seen : 0;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = 8 * (i >> 2) + (i & 3) < (i < 8 ? seen0 : seen1) ? s[i] : -INFINITY;
+      for (int b = 0; b < NB; ++b) {
+        const int kb = kb0 + b, seen = limit - key0 - 32 * kb - 4 * hl;
+        const int seen0 = pages >> (2 * kb) & 1 ? seen : 0, seen1 = pages >> (2 * kb + 1) & 1 ? seen : 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 8 * (i >> 2) + (i & 3) < (i < 8 ? seen0 : seen1) ? s[b][i] : -INFINITY;
+      }
     }
-    float top = s[0];
+    float top = s[0][0];
 #pragma unroll
-    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
     raise(m, fmaxf(top, lane_xor32(top)) * sc, l, o);
     const float base = m == -INFINITY ? 0.f : m;
-    float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], sc, -base));
-      sum += s[i];
+    for (int b = 0; b < NB; ++b) {
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], sc, -base));
+        sum += s[b][i];
+      }
+      l += sum;
     }
-    l += sum;
     if (odd)
-      for (int w = 32 / W::MY_KEYS * kb; w < 32 / W::MY_KEYS * (kb + 1); ++w)
+      for (int w = 32 / W::MY_KEYS * kb0; w < 32 / W::MY_KEYS * (kb0 + NB); ++w)
         if (const int keys = __builtin_amdgcn_readfirstlane(odd[w])) {
           float e[16 * DT];
 #pragma unroll
@@ -734,12 +797,11 @@ AXON_DEV void wide_phases(WideRows<bf16, HD>& x, WideStages<bf16, HD>& st, int f
       if (x.works) {
         const int pages = st.pages(i);
         const int32_t* odd = st.masked(i) ? st.sh.odd[i % S] : nullptr;
+        x.weights(s, (u0 + i) * WIDE_KEYS, kb0, pages, odd);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          x.weights(s[b], (u0 + i) * WIDE_KEYS, kb0 + b, pages, odd);
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int j = 0; j < 16; ++j) w[b][j / 8][j % 8] = (bf16)s[b][j];
-        }
         wv = tile + W::TILE + 32 * kb0 * HD;
       }
       end();
@@ -762,6 +824,7 @@ AXON_DEV void wide_tile(const PrefixAttnArgs<bf16>& a, float sc, typename Wide<b
                         int G, int kvh, int row0, int first, int last, float* part) {
   WideRows<bf16, HD> x(a, sc, g, G, kvh, row0);
   WideStages<bf16, HD> st{sh, x};
+  if (a.scale < 0.f) negate(x.q);
   if (x.halves) wide_phases<true>(x, st, first, last);
   else wide_phases<false>(x, st, first, last);
   x.store(part);
@@ -776,6 +839,7 @@ AXON_DEV void wide_tile(const PrefixAttnArgs<float>& a, float sc, typename Wide<
   using X = WideRows<float, HD>;
   constexpr int S = W::STAGES;
   X x(a, sc, g, G, kvh, row0);
+  if (a.scale < 0.f) negate(x.q);
   WideStages<float, HD> st{sh, x};
   for (int u0 = first; u0 < last; u0 += W::BATCH) {
     st.look_up(u0, min(last - u0, W::BATCH));
@@ -792,76 +856,19 @@ AXON_DEV void wide_tile(const PrefixAttnArgs<float>& a, float sc, typename Wide<
       for (int kb = x.kgroup; kb < (x.halves ? x.kgroup + 1 : 2); ++kb) {
         f32x8 kf[X::QS];
         x.read_k(tile, kb, kf);
-        f32x16 s;
-        x.scores(kf, s);
+        f32x16 s[1];
+        x.scores(kf, s[0]);
         x.weights(s, key0, kb, st.pages(i), st.masked(i) ? sh.odd[i % S] : nullptr);
 #pragma unroll
         for (int j = 0; j < 16; ++j)
 #pragma unroll
           for (int d = 0; d < X::DT; ++d)
             x.o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-                tile[W::TILE + L::v_at(32 * kb + 8 * (j >> 2) + 4 * x.hl + (j & 3), 32 * d + x.c)], s[j], x.o[d], 0, 0, 0);
+                tile[W::TILE + L::v_at(32 * kb + 8 * (j >> 2) + 4 * x.hl + (j & 3), 32 * d + x.c)], s[0][j], x.o[d], 0, 0, 0);
       }
     }
   }
   x.store(part);
-}
-
-// Worker w of n takes steps total w / n .. total (w + 1) / n - 1: as many as there are,
-// unless that leaves one too little to be worth the part it writes.
-AXON_DEV int workers(int most, int64_t total, int least) {
-  return (int)max(min((int64_t)most, total / least), min(total, (int64_t)1));
-}
-AXON_DEV int worker_of(int64_t step, int64_t total, int n) { return (int)(((step + 1) * n - 1) / total); }
-
-// What worker ``me`` does of the tile at p (its steps at .. at + take - 1): units first ..
-// last - 1; the one with the tile's first unit notes where the parts are.
-struct Work {
-  int take, first, last;
-};
-template <bool WIDE, int HD, typename T>
-AXON_DEV Work work_of(const PrefixAttnArgs<T>& a, const Segment& g, const Place& p, int G, int KV, int64_t at, int64_t end,
-                      int64_t total, int me, int n, TileParts* info, bool leader) {
-  constexpr int START = Tiles<WIDE>::START;
-  const int steps = Tiles<WIDE>::steps(g, G, p.rt);
-  Work w;
-  w.take = (int)min((int64_t)(steps - p.step), end - at);
-  w.first = max(p.step - START, 0);
-  w.last = max(p.step + w.take - START, 0);
-  if (leader && p.step <= START && w.last > 0)
-    info[info_at(g.own, p.kvh, KV, (int64_t)a.tokens * G, g.tok0, G, p.rt * Tiles<WIDE>::ROWS)] =
-        TileParts{p.tile + me, worker_of(at - p.step + steps - 1, total, n) - me + 1};
-  return w;
-}
-
-template <typename T, int HD>
-__global__ void __launch_bounds__(WIDE_THREADS, 2) prefix_wide_kernel(PrefixAttnArgs<T> a, float sc, TileParts* info,
-                                                                      float* parts, int slots) {
-  __shared__ typename Wide<T, HD>::Shared sh;
-  Plan<T, true, WIDE_THREADS> plan(a, sh.plan);
-  const int G = plan.G, KV = plan.KV;
-  // Consecutive runs on one XCD, whose L2 holds what they share; fewer workers than
-  // workgroups: over all XCDs.
-  const int n = workers(gridDim.x, plan.total, WIDE_LEAST);
-  const int me = n < (int)gridDim.x || n % 8 ? blockIdx.x : blockIdx.x % 8 * (n / 8) + blockIdx.x / 8;
-  if (me >= n) return;
-  int64_t at = plan.total * me / n;
-  const int64_t end = plan.total * (me + 1) / n;
-  plan.find(0, at);
-  __syncthreads();
-  Segment g;
-  Place p = plan.get(0, g);
-  for (;;) {
-    const int slot = p.tile + me;
-    if (slot >= slots) return;  // (cu_seqlens are not those of the host)
-    const Work w = work_of<true, HD>(a, g, p, G, KV, at, end, plan.total, me, n, info, threadIdx.x == 0);
-    if (w.last > w.first)
-      wide_tile<HD>(a, sc, sh, g, G, p.kvh, p.rt * WIDE_ROWS, w.first, w.last,
-                       parts + (int64_t)slot * SLOT_BLOCKS * part_floats(HD));
-    at += w.take;
-    if (at >= end) return;
-    plan.advance(p, g);
-  }
 }
 
 // ---------------------------------------------------------------- narrow tiles
@@ -871,56 +878,56 @@ struct Narrow {
   using L = Lds<T, HD>;
   static constexpr int TILE = NARROW_KEYS * HD, QS = HD / 32;
   static constexpr int LOADS = NARROW_KEYS / L::RPI + QS * (int)sizeof(T) / 2;  // of a unit
+  static constexpr int DEPTH = sizeof(T) == 4 && HD == 128 ? 2 : 3;             // units in flight or in use
   struct Shared {
-    alignas(16) T v[NARROW_WAVES][2][TILE];
-    PlanShared<NARROW_WAVES> plan;
+    alignas(16) T v[PA_WAVES][DEPTH][TILE];
   };
 };
 
 // Units first .. last - 1 of a tile, by one wavefront: keys to registers, where a lane
-// has those of one key that multiply its dimensions, values through LDS, a unit ahead.
+// has those of one key that multiply its dimensions, values through LDS.
 template <typename T, int HD>
-AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[2][Narrow<T, HD>::TILE], const Segment& g, int G,
-                          int kvh, int first, int last, float* part) {
+AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[Narrow<T, HD>::DEPTH][Narrow<T, HD>::TILE],
+                          const Segment& g, int G, int kvh, int first, int last, float* part) {
   using N = Narrow<T, HD>;
   using L = Lds<T, HD>;
   using V8 = typename Vec8<T>::t;
-  constexpr int DT = HD / 16, QS = N::QS;
+  constexpr int DT = HD / 16, QS = N::QS, D = N::DEPTH;
   const int lane = threadIdx.x & 63, gq = lane >> 4, c = lane & 15;
   const int rows = g.tokens * G, r = min(c, rows - 1);
   const Cache<T, HD> cache{a, g, kvh};
-  int pages = 0;  // of units u & ~63 .., one a lane
-  V8 q[QS], k[2][QS];
-  auto look_up = [&](int u0) { pages = u0 + lane < last ? cache.page((u0 + lane) * NARROW_KEYS) : -1; };
-  auto page_of = [&](int u) { return __builtin_amdgcn_readlane(pages, (u - first) & 63); };
-  auto fetch = [&](int u, int b) {
-    const int64_t src = cache.at(max(page_of(u), 0), u * NARROW_KEYS);  // (none: masked, but read)
+  int blocks = 0;  // of 64 units, one a lane; -1: no page
+  bool there[D];
+  V8 q[QS], k[D][QS];
+  {
+    const T* p = q_row<T, HD>(a, g, G, kvh, r) + 8 * gq;
+#pragma unroll
+    for (int j = 0; j < QS; ++j) q[j] = load_q8<T>(p + 32 * j);
+  }
+  auto fetch = [&](int u, const int b) {
+    if (((u - first) & 63) == 0) blocks = u + lane < last ? cache.block((u + lane) * NARROW_KEYS) : -1;
+    const int at = __builtin_amdgcn_readlane(blocks, (u - first) & 63);
+    there[b] = at >= 0;
+    const int64_t src = (int64_t)max(at, 0) * NARROW_KEYS * HD;  // (none: masked, but read)
     L::template stage<false, false>((const T*)a.kv.v + src, lds[b], 0, NARROW_KEYS, lane);
     const T* kp = (const T*)a.kv.k + src + c * HD + 8 * gq;
 #pragma unroll
     for (int j = 0; j < QS; ++j) k[b][j] = read8(kp + 32 * j, kp + 32 * j + 4);
   };
-  look_up(first);
-  {
-    const T* p = q_row<T, HD>(a, g, G, kvh, r) + 8 * gq;
-#pragma unroll
-    for (int j = 0; j < QS; ++j) q[j] = load_q8<T>(p + 32 * j, a.scale < 0.f);
-  }
   const int limit = row_keys(g, G, r), least = row_keys(g, G, 0);
   f32x4 o[DT] = {};
   float m = -INFINITY, l = 0.f;
-  fetch(first, 0);
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the tile before is read)
+#pragma unroll
+  for (int b = 0; b < D - 1; ++b)
+    if (first + b < last) fetch(first + b, b);
+  if (a.scale < 0.f) negate(q);
   auto unit = [&](int u, const int b) {
     const int key0 = u * NARROW_KEYS;
-    const bool there = page_of(u) >= 0, masked = key0 + NARROW_KEYS > least || !there;
+    const bool masked = key0 + NARROW_KEYS > least || !there[b];
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the stage that is filled next is read)
-    if (u + 1 < last) {
-      if (((u + 1 - first) & 63) == 0) look_up(u + 1);
-      fetch(u + 1, b ^ 1);
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N::LOADS) : "memory");
-    } else {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    }
+    if (u + D - 1 < last) fetch(u + D - 1, (b + D - 1) % D);
+    wait_loads<N::LOADS, D - 1>(min(last - 1 - u, D - 1));
     T* vs = lds[b];
     const int odd = masked ? make_finite<T, HD>(vs, NARROW_KEYS, lane) : 0;
     f32x4 s = {};
@@ -943,7 +950,7 @@ AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[2][Narr
     if (masked) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (key0 + 4 * gq + i >= limit || !there) s[i] = -INFINITY;
+        if (key0 + 4 * gq + i >= limit || !there[b]) s[i] = -INFINITY;
     }
     float top = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     top = fmaxf(top, lane_xor16(top));
@@ -961,15 +968,15 @@ AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[2][Narr
       float e[4 * DT];
 #pragma unroll
       for (int i = 0; i < 4 * DT; ++i) e[i] = o[i / 4][i % 4];
-      add_odd(cache, key0, there ? odd : 0, limit, e, [&](int i) { return 16 * (i / 4) + 4 * gq + i % 4; });
+      add_odd(cache, key0, there[b] ? odd : 0, limit, e, [&](int i) { return 16 * (i / 4) + 4 * gq + i % 4; });
 #pragma unroll
       for (int i = 0; i < 4 * DT; ++i) o[i / 4][i % 4] = e[i];
     }
   };
-  for (int u = first; u < last; u += 2) {
-    unit(u, 0);
-    if (u + 1 < last) unit(u + 1, 1);
-  }
+  for (int u = first; u < last; u += D)
+#pragma unroll
+    for (int b = 0; b < D; ++b)
+      if (u + b < last) unit(u + b, b);
   l += lane_xor16(l);
   l += lane_xor32(l);
   if (c >= rows) return;
@@ -981,35 +988,92 @@ AXON_DEV void narrow_tile(const PrefixAttnArgs<T>& a, float sc, T (&lds)[2][Narr
   }
 }
 
+// ---------------------------------------------------------------- the kernel
+
+// Where the parts of the kinds lie, in blocks
+struct PartsAt {
+  int wide_slots, narrow_slots;  // a wide one has SLOT_BLOCKS blocks, the narrow ones follow
+  AXON_DEV int narrow() const { return wide_slots * SLOT_BLOCKS; }
+};
+
 template <typename T, int HD>
-__global__ void __launch_bounds__(NARROW_THREADS, 3) prefix_narrow_kernel(PrefixAttnArgs<T> a, float sc, TileParts* info,
-                                                                          float* parts, int slots) {
-  __shared__ typename Narrow<T, HD>::Shared sh;
-  Plan<T, false, NARROW_THREADS> plan(a, sh.plan);
+__global__ void __launch_bounds__(PA_THREADS, 2) prefix_attn_kernel(PrefixAttnArgs<T> a, float sc, RowParts* info,
+                                                                    float* parts, PartsAt at_) {
+  union Stages {
+    typename Wide<T, HD>::Shared wide;
+    typename Narrow<T, HD>::Shared narrow;
+  };
+  __shared__ Stages sh;
+  __shared__ PlanShared plan_sh;
+  Plan<T, HD> plan(a, plan_sh);
   const int G = plan.G, KV = plan.KV, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  // a wavefront is a worker; as the wide kernel's otherwise
-  const int grid = gridDim.x * NARROW_WAVES, n = workers(grid, plan.total, NARROW_LEAST);
-  const int wg = n < grid || gridDim.x % 8 ? blockIdx.x : blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
-  // (fewer workers than wavefronts: spread over the workgroups)
-  auto worker = [&](int w) { return n < grid ? w * (int)gridDim.x + wg : wg * NARROW_WAVES + w; };
-  for (int w = 0; w < NARROW_WAVES; ++w)
-    if (worker(w) < n) plan.find(w, plan.total * worker(w) / n);
-  __syncthreads();
-  const int me = worker(wave);
-  if (me >= n) return;
-  int64_t at = plan.total * me / n;
-  const int64_t end = plan.total * (me + 1) / n;
-  Segment g;
-  Place p = plan.get(wave, g);
-  for (;;) {
-    const int slot = p.tile + me;
-    if (slot >= slots) return;
-    const Work w = work_of<false, HD>(a, g, p, G, KV, at, end, plan.total, me, n, info, (threadIdx.x & 63) == 0);
-    if (w.last > w.first)
-      narrow_tile<T, HD>(a, sc, sh.v[wave], g, G, p.kvh, w.first, w.last, parts + (int64_t)slot * part_floats(HD));
-    at += w.take;
-    if (at >= end) return;
-    plan.advance(p, g);
+  const int64_t all_rows = (int64_t)a.tokens * G;
+  // The workgroups of an XCD (blockIdx % 8) are shared out over the kinds as the steps
+  // are; consecutive runs go to one XCD, whose L2 holds what they share.
+  constexpr int PER = PA_WGS / 8;
+  const int total_n = __builtin_amdgcn_readfirstlane(plan.total[0]), total_w = __builtin_amdgcn_readfirstlane(plan.total[1]);
+  const int wide_wgs = !total_w ? 0 : !total_n ? PER : min(max((int)((float)PER * total_w / ((float)total_w + total_n) + 0.5f), 1), PER - 1);
+  const int xcd = blockIdx.x % 8, nth = blockIdx.x / 8;
+  if (nth < wide_wgs) {
+    const Shares shares(min(8 * wide_wgs, max(total_w / Tiles<true, HD>::LEAST, 1)), total_w);
+    // (fewer workers than workgroups: over all XCDs)
+    const int me = shares.n < 8 * wide_wgs ? (int)blockIdx.x : xcd * wide_wgs + nth;
+    if (me >= shares.n) return;
+    int at = shares.start(me);
+    const int end = shares.start(me + 1);
+    plan.template find<true>(0, at);
+    __syncthreads();
+    Segment g;
+    Place p = plan.template get<true>(0, g);
+    for (;;) {
+      const int slot = p.tile + me;
+      if (slot >= at_.wide_slots) return;  // (cu_seqlens are not those of the host)
+      const Work w = work_of<true, HD>(g, p, G, at, end, shares, me);
+      const int row0 = p.rt * WIDE_ROWS, here = min(g.tokens * G - row0, WIDE_ROWS);
+      if (w.leads && (int)threadIdx.x < here) {
+        // a tile of up to 128 rows has two parts in a slot
+        const bool halves = here <= WIDE_ROWS / 2;
+        info[info_at(g.own, p.kvh, KV, all_rows, (int64_t)g.tok0 * G + row0 + threadIdx.x)] =
+            row_parts(slot * SLOT_BLOCKS + ((int)threadIdx.x >> 4), halves ? 2 * w.parts : w.parts,
+                      halves ? SLOT_BLOCKS / 2 : SLOT_BLOCKS, threadIdx.x & 15);
+      }
+      if (w.last > w.first)
+        wide_tile<HD>(a, sc, sh.wide, g, G, p.kvh, row0, w.first, w.last, parts + (int64_t)slot * SLOT_BLOCKS * part_floats(HD));
+      at += w.take;
+      if (at >= end) return;
+      plan.template advance<true>(p, g);
+    }
+  } else {
+    // a wavefront is a worker
+    const int wgs = PER - wide_wgs, waves = 8 * wgs * PA_WAVES;
+    const Shares shares(min(waves, max(total_n / Tiles<false, HD>::LEAST, min(total_n, 1))), total_n);
+    // (fewer workers than wavefronts: over all workgroups)
+    auto worker = [&](int w) {
+      const int wg = nth - wide_wgs;
+      return shares.n < waves ? w * 8 * wgs + wg * 8 + xcd : (xcd * wgs + wg) * PA_WAVES + w;
+    };
+    for (int w = 0; w < PA_WAVES; ++w)
+      if (worker(w) < shares.n) plan.template find<false>(w, shares.start(worker(w)));
+    __syncthreads();
+    const int me = worker(wave);
+    if (me >= shares.n) return;
+    int at = shares.start(me);
+    const int end = shares.start(me + 1);
+    Segment g;
+    Place p = plan.template get<false>(wave, g);
+    for (;;) {
+      const int slot = p.tile + me, lane = threadIdx.x & 63;
+      if (slot >= at_.narrow_slots) return;
+      const Work w = work_of<false, HD>(g, p, G, at, end, shares, me);
+      if (w.leads && lane < g.tokens * G)
+        info[info_at(g.own, p.kvh, KV, all_rows, (int64_t)g.tok0 * G + lane)] = row_parts(at_.narrow() + slot, w.parts, 1, lane);
+      if (w.last > w.first)
+        narrow_tile<T, HD>(a, sc, sh.narrow.v[wave], g, G, p.kvh, w.first, w.last,
+                           parts + (int64_t)(at_.narrow() + slot) * part_floats(HD));
+      at += w.take;
+      if (at >= end) return;
+      plan.template advance<false>(p, g);
+    }
   }
 }
 
@@ -1020,15 +1084,18 @@ __global__ void __launch_bounds__(NARROW_THREADS, 3) prefix_narrow_kernel(Prefix
 // many groups of them as it has for the R rows at a time, whose sums are joined in LDS.
 constexpr int JOIN_MAX = 1024;
 template <typename T, int HD>
-__global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T> a, const TileParts* info, const float* wide,
-                                                               const float* narrow, int wide_slots, int narrow_slots,
-                                                               int R) {
+__global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T> a, const RowParts* info, const float* parts,
+                                                               int blocks, int R) {
   constexpr int LANES = HD / 4, AHEAD = 4;
   __shared__ f32x4 sum_o[JOIN_MAX];
   __shared__ float sum_m[JOIN_MAX / LANES], sum_l[JOIN_MAX / LANES];
   const int t = blockIdx.x, kvh = blockIdx.y, KV = a.kv.kv_heads, G = a.heads / KV;
-  const int lane = threadIdx.x & 63, d = threadIdx.x % LANES, team = threadIdx.x / LANES;
+  const int lane = threadIdx.x & 63, d = threadIdx.x % LANES, team = threadIdx.x / LANES, row = team % R;
   const int groups = (int)blockDim.x / (LANES * R), group = team / R;  // of parts
+  // (read before it is known whether they are there, beside what says it)
+  RowParts where[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) where[k] = info[info_at(k, kvh, KV, (int64_t)a.tokens * G, (int64_t)t * G + min(row, G - 1))];
   auto among = [&](const int32_t* cu, int n, int v) {  // how many of cu[1 .. n] are <= v
     int c = 0;
     for (int i = lane; i - lane < n; i += 64) c += __popcll(__ballot(i < n && cu[i + 1] <= v));
@@ -1038,26 +1105,19 @@ __global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T>
   if (b >= a.seqs.seqs) return;  // behind the last sequence
   const bool active = a.seqs.lens[b] >= 0;
   const int grp = a.shared.groups ? among(a.shared.cu, a.shared.groups, b) : 0;
-  const bool has[2] = {grp < a.shared.groups, true};
+  const bool has[2] = {active && grp < a.shared.groups && a.shared.lens[min(grp, a.shared.groups - 1)] > 0, active};
   for (int j0 = 0; j0 < G; j0 += R) {
-    const int j = j0 + team % R;
+    const int j = j0 + row;
     f32x4 o = {};
     float top = -INFINITY, l = 0.f;
     for (int k = 0; k < 2; ++k) {
-      if (!has[k] || !active || j >= G) continue;
-      const Segment g = segment_of(a, k ? a.shared.groups + b : grp);
-      const int r = (t - g.tok0) * G + j, rows = g.tokens * G;
-      const bool is_wide = rows > NARROW_ROWS;
-      const int row0 = is_wide ? r / WIDE_ROWS * WIDE_ROWS : 0, row = r - row0;
-      if (tile_keys(g, G, row0, is_wide ? WIDE_ROWS : NARROW_ROWS) <= 0) continue;
-      const TileParts p = info[info_at(k, kvh, KV, (int64_t)a.tokens * G, g.tok0, G, row0)];
-      if (p.first < 0 || p.count < 0 || p.count > (is_wide ? wide_slots : narrow_slots) - p.first) continue;
-      // a tile of up to 128 rows has two parts in a slot
-      const bool halves = is_wide && rows - row0 <= WIDE_ROWS / 2;
-      const int64_t step = (int64_t)(is_wide ? (halves ? SLOT_BLOCKS / 2 : SLOT_BLOCKS) : 1) * part_floats(HD);
-      const int count = halves ? 2 * p.count : p.count;
-      const float* part = (is_wide ? wide : narrow) + ((int64_t)p.first * (is_wide ? SLOT_BLOCKS : 1) + row / 16) * part_floats(HD);
-      const float *po = part + row % 16 * HD + 4 * d, *pm = part + 16 * HD + row % 16;
+      if (!has[k] || j >= G) continue;
+      const RowParts p = j0 ? info[info_at(k, kvh, KV, (int64_t)a.tokens * G, (int64_t)t * G + j)] : where[k];
+      const int count = p.count >> 9, apart = p.count >> 4 & 31, in = p.count & 15;
+      if (p.block < 0 || count < 1 || (int64_t)p.block + (int64_t)(count - 1) * apart >= blocks) continue;
+      const int64_t step = (int64_t)apart * part_floats(HD);
+      const float* part = parts + (int64_t)p.block * part_floats(HD);
+      const float *po = part + in * HD + 4 * d, *pm = part + 16 * HD + in;
       for (int i0 = group; i0 < count; i0 += AHEAD * groups) {
         f32x4 v[AHEAD];
         float m[AHEAD], s[AHEAD];
@@ -1118,11 +1178,10 @@ __global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T>
 
 namespace {
 
-constexpr int WIDE_WGS = 256, NARROW_WGS = 768;
-
 struct Sizes {
-  int64_t wide, narrow;       // slots of each kind (0: no such tile)
-  int64_t wide_at, narrow_at, bytes;
+  int64_t wide, narrow;  // slots of each kind (0: no such tile)
+  int64_t parts_at, bytes;
+  int64_t blocks() const { return wide * SLOT_BLOCKS + narrow; }
 };
 Sizes sizes_of(const PrefixAttnShape& x) {
   const int64_t G = x.heads / x.kv_heads;
@@ -1136,11 +1195,10 @@ Sizes sizes_of(const PrefixAttnShape& x) {
   for (int g = 0; g < x.groups; ++g) add(token(x.h_groups[g + 1]) - token(x.h_groups[g]));
   for (int b = 0; b < x.seqs; ++b) add(x.h_cu ? x.h_cu[b + 1] - x.h_cu[b] : 1);
   Sizes s;
-  s.wide = wide ? wide * x.kv_heads + WIDE_WGS : 0;
-  s.narrow = narrow ? narrow * x.kv_heads + NARROW_WGS * NARROW_WAVES : 0;
-  s.wide_at = (2 * x.tokens * x.heads * (int64_t)sizeof(TileParts) + 15) / 16 * 16;
-  s.narrow_at = s.wide_at + s.wide * SLOT_BLOCKS * part_floats(x.hd) * 4;
-  s.bytes = s.narrow_at + s.narrow * part_floats(x.hd) * 4;
+  s.wide = wide ? wide * x.kv_heads + PA_WGS : 0;
+  s.narrow = narrow ? narrow * x.kv_heads + PA_WGS * PA_WAVES : 0;
+  s.parts_at = (2 * x.tokens * x.heads * (int64_t)sizeof(RowParts) + 15) / 16 * 16;
+  s.bytes = s.parts_at + s.blocks() * part_floats(x.hd) * 4;
   return s;
 }
 
@@ -1148,26 +1206,25 @@ Sizes sizes_of(const PrefixAttnShape& x) {
 
 int64_t prefix_attn_workspace(const PrefixAttnShape& x) { return sizes_of(x).bytes; }
 
-int64_t prefix_attn_units(const PrefixAttnShape& x, int64_t keys) {
+int64_t prefix_attn_steps(const PrefixAttnShape& x, int64_t keys) {
   const Sizes s = sizes_of(x);
-  return std::max(s.wide * ((keys + WIDE_KEYS - 1) / WIDE_KEYS), s.narrow * ((keys + NARROW_KEYS - 1) / NARROW_KEYS));
+  return std::max({s.wide * 14 * ((keys + WIDE_KEYS - 1) / WIDE_KEYS + 6), s.narrow * ((keys + NARROW_KEYS - 1) / NARROW_KEYS + 4),
+                   s.blocks()});  // (14: the largest step)
 }
 
 template <typename T, int HD>
 static void launch(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* workspace, hipStream_t s) {
   const Sizes n = sizes_of(x);
-  TileParts* info = (TileParts*)workspace;
-  float *wide = (float*)((char*)workspace + n.wide_at), *narrow = (float*)((char*)workspace + n.narrow_at);
+  RowParts* info = (RowParts*)workspace;
+  float* parts = (float*)((char*)workspace + n.parts_at);
   // a scale of 0 leaves every score, masked ones apart, the same
   const float sc = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * LOG2E_F;
-  if (n.wide) prefix_wide_kernel<T, HD><<<WIDE_WGS, WIDE_THREADS, 0, s>>>(a, sc, info, wide, (int)n.wide);
-  if (n.narrow) prefix_narrow_kernel<T, HD><<<NARROW_WGS, NARROW_THREADS, 0, s>>>(a, sc, info, narrow, (int)n.narrow);
+  prefix_attn_kernel<T, HD><<<PA_WGS, PA_THREADS, 0, s>>>(a, sc, info, parts, PartsAt{(int)n.wide, (int)n.narrow});
   // few tokens: many threads each, whose parts are many
   const int G = a.heads / a.kv.kv_heads, threads = (int64_t)a.tokens * a.kv.kv_heads <= 1024 ? JOIN_MAX : 256;
   int R = 1;
   while (R < G && R < threads / (HD / 4)) R *= 2;
-  prefix_join_kernel<T, HD><<<dim3(a.tokens, a.kv.kv_heads), threads, 0, s>>>(a, info, wide, narrow, (int)n.wide,
-                                                                             (int)n.narrow, R);
+  prefix_join_kernel<T, HD><<<dim3(a.tokens, a.kv.kv_heads), threads, 0, s>>>(a, info, parts, (int)n.blocks(), R);
 }
 
 template <typename T>

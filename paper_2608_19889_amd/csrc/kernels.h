@@ -547,8 +547,9 @@ struct PrefixAttnShape {
   int seqs, groups, heads, kv_heads, hd;
   const int32_t *h_cu, *h_groups;
 };
-// upper bound of the units of work that rows of ``keys`` keys can make
-int64_t prefix_attn_units(const PrefixAttnShape& x, int64_t keys);
+// upper bound of the steps of work that rows of ``keys`` keys can make, and of the numbers
+// of its parts
+int64_t prefix_attn_steps(const PrefixAttnShape& x, int64_t keys);
 int64_t prefix_attn_workspace(const PrefixAttnShape& x);
 template <typename T>
 void launch_prefix_attn(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* workspace, hipStream_t s);

@@ -264,6 +264,49 @@ def test_attention_scores_far_apart(dtype):
     check_attention(p, scale=-0.7)
 
 
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attention_many_rows_with_scores_far_apart(hd, dtype):
+    """More than 128 rows of one key head, whose scores grow inside a tile of keys."""
+    p = Paged([(600, [(5 * i % 50, 1) for i in range(20)])], 8, 1, hd, dtype)
+    p.q *= 12
+    check_attention(p)
+    p = Paged([(70, [(3, 50), (0, 1)])], 12, 2, hd, dtype)
+    p.q *= 12
+    check_attention(p)
+
+
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("spread", [1, 12])
+@pytest.mark.parametrize("seqs,heads,hd", [(75, 16, 64), (18, 32, 128)])
+def test_attention_many_tiles_in_a_row(seqs, heads, hd, spread, dtype):
+    """A prefix so long that every workgroup goes through many tiles of keys."""
+    N, kv = 50011, 4
+    p = Paged([(N, [(0, 1)] * seqs)], heads, kv, hd, dtype, junk=False)
+    p.q *= spread
+    G, q = heads // kv, p.q.cpu().double()
+    prefix, own = p.prefix_table[0].cpu().long(), p.table[:, 0].cpu().long()
+    got, lse = (t.cpu().double() for t in ops.prefix_attention(
+        p.q, p.k_cache, p.v_cache, p.table, p.lens, want_lse=True, **p.attention_args()))
+    kc, vc = p.k_cache.cpu(), p.v_cache.cpu()
+    for h in range(kv):
+        k, v = (c[prefix, h].reshape(-1, hd)[:N].double() for c in (kc, vc))
+        k1, v1 = (c[own, h, 0].double().repeat_interleave(G, 0) for c in (kc, vc))
+        rows = q[:, h * G:(h + 1) * G].reshape(-1, hd)
+        s = torch.cat([rows @ k.T, (rows * k1).sum(1, keepdim=True)], 1) * hd ** -0.5
+        # the bound of Paged.attention
+        d = (hd + 2) * U * torch.maximum((rows.abs() @ k.abs().T).amax(1), (rows * k1).abs().sum(1)) * hd ** -0.5
+        x = s.amax(1, keepdim=True) - s
+        w = torch.softmax(s, 1)
+        eps = (2 * d + (w * (3 * x + 8)).amax(1) * U + (8 + N + 1) * U)[:, None]
+        out, size = w[:, :N] @ v + w[:, N:] * v1, w[:, :N] @ v.abs() + w[:, N:] * v1.abs()
+        bound = (2 * eps + (HALF[B] if dtype == B else 0)) * size
+        at = (slice(None), slice(h * G, (h + 1) * G))
+        check(got[at].reshape(-1, hd), out, bound + HALF[dtype] * (out.abs() + bound), ("out", h))
+        total = torch.logsumexp(s, 1)
+        check(lse[at].reshape(-1), total, eps[:, 0] + 4 * U * (1 + total.abs() + s.abs().amax(1)), ("lse", h))
+
+
 def test_attention_strides_and_in_place():
     for dtype in (F, B):
         p = Paged(CHUNKS["chunk"], 6, 2, 64, dtype)
