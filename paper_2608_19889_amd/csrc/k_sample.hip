@@ -109,7 +109,8 @@ AXON_DEV u64 wave_total(u64 v) {
 }
 
 // Over each thread's two entries, in the threads' order: the entry at which the running
-// sum (from ``from`` on) reaches target(total) >= 1; what is before it and in it.
+// sum (from ``from`` on) reaches target(total) >= 1; what is before it and in it.  -1:
+// none does, which is so only where a caller asks for more than there is.
 struct Found {
   int at;
   u64 before, in;
@@ -124,6 +125,7 @@ AXON_DEV Found find_entry(Shared& sh, const u64 (&v)[2], u64 from, F&& target, u
     if (lane >= d) upto += u;
   }
   if (lane == 63) sh.wave_sum[wave] = upto;
+  if (threadIdx.x == 0) sh.found = -1;
   __syncthreads();
   u64 before = from + upto - v[0] - v[1], sum = from;
 #pragma unroll
@@ -304,12 +306,24 @@ AXON_DEV int gather(Shared& sh, const R& row, P&& take, W&& weight) {
     if (n < FEW) sh.few[n] = Candidate{z, i, weight(z)};
   });
   __syncthreads();
-  return sh.count;
+  const int n = sh.count;
+  // (whole rounds of others())
+  if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < FEW) sh.few[n + threadIdx.x] = Candidate{-INFINITY, 0x7fffffff, 0};
+  __syncthreads();
+  return n;
 }
-// Four threads to a candidate (thread / 4): f(candidate) over a quarter each
+// Four threads to a candidate (thread / 4): f(candidate) over a quarter each, eight at a
+// time so that their reads are in flight together
 template <typename F>
 AXON_DEV void others(const Shared& sh, int n, F&& f) {
-  for (int j = threadIdx.x & 3; j < n; j += 4) f(sh.few[j]);
+  static_assert(FEW % 32 == 0, "rounds end inside few");
+  for (int j = threadIdx.x & 3; j < n; j += 32) {
+    Candidate c[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) c[k] = sh.few[j + 4 * k];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f(c[k]);
+  }
 }
 AXON_DEV u64 quad_sum(u64 v) {
   v += __shfl_xor(v, 1);
@@ -363,7 +377,7 @@ AXON_DEV Border find_border(Shared& sh, const Row<T>& row, uint32_t lo, uint32_t
         u64 w[2];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const int in = 2 * threadIdx.x + j, i = g.at * width + in;
+          const int in = 2 * threadIdx.x + j, i = max(g.at, 0) * width + in;
           w[j] = in < width && i < row.V && order_key<T>(sane(to_f32(row.z[i]))) == lo;
         }
         __syncthreads();
@@ -441,7 +455,7 @@ AXON_DEV int find_index(Shared& sh, const Row<T>& row, W&& weight, F&& target, u
   u64 w[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const int i = f.at * width + e + j;
+    const int i = max(f.at, 0) * width + e + j;
     const float z = i < row.V ? sane(to_f32(row.z[i])) : -INFINITY;
     w[j] = e + j < width && z >= row.cut ? weight(z, i) : 0;
   }
@@ -540,7 +554,7 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
       w[j] = m > -INFINITY && weight(m) ? (u64)rint(as_double(parts(m)) * in.chunk_sum[i] * unit) : 0;
     }
     const Found f = find_entry(sh, w, 0, [&](u64 sum) { return want = drawn(sum); }, &total);
-    const int first = f.at * CHUNK + 2 * tid;
+    const int first = max(f.at, 0) * CHUNK + 2 * tid;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const float v = first + j < V ? sane(to_f32(z[first + j])) : -INFINITY;
@@ -562,6 +576,7 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
       if ((tid & 63) == 0) sh.wave_sum[tid >> 6] = __double_as_longlong(sum);
       __syncthreads();
       sum = 0.;
+#pragma unroll
       for (int w = 0; w < S_THREADS / 64; ++w) sum += __longlong_as_double(sh.wave_sum[w]);
     }
     // Nothing below ``cut`` is kept (a top-k's weight, of which top-p takes its share,
@@ -663,6 +678,7 @@ __global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, voi
     }
   }
   if (tid == 0) {
+    token = min(max(token, 0), V - 1);  // (it is there; no address hangs on it)
     a.tokens[r] = token;
     const float v = sane(to_f32(z[token]));
     const double x = v == top ? 0. : ((double)v - top) / s.t;
