@@ -307,6 +307,22 @@ def test_attention_many_tiles_in_a_row(seqs, heads, hd, spread, dtype):
         check(lse[at].reshape(-1), total, eps[:, 0] + 4 * U * (1 + total.abs() + s.abs().amax(1)), ("lse", h))
 
 
+@pytest.mark.parametrize("dtype", [F, B])
+def test_attention_more_sequences_than_threads(dtype):
+    """Several segments to a thread of the plan; groups of none, sequences that take no part."""
+    g = torch.Generator().manual_seed(3)
+    some = lambda n: torch.randint(0, n, (1,), generator=g).item()  # noqa: E731
+    p = Paged([(some(40), [(some(20), 1)] * some(5)) for _ in range(330)] + [(9, [(3, 1)])], 2, 1, 64, dtype)
+    assert len(p.past) + len(p.prefix) > 2 * 420
+    p.lens[::7] = -1
+    p.lens[40:300] = -1  # a long run of segments without work
+    check_attention(p)
+    p = Paged([(some(30), [(some(9), some(3))] * (1 + some(3))) for _ in range(280)], 20, 1, 64, dtype)
+    assert len(p.past) + len(p.prefix) > 512
+    p.lens[::5] = -9
+    check_attention(p)
+
+
 def test_attention_strides_and_in_place():
     for dtype in (F, B):
         p = Paged(CHUNKS["chunk"], 6, 2, 64, dtype)

@@ -91,6 +91,13 @@ def test_flat_rows(kw, dtype):
     check(0.3 * z, u, **kw)
 
 
+@pytest.mark.parametrize("kw", FILTERS.values(), ids=FILTERS.keys())
+@pytest.mark.parametrize("V,dtype", [(262144, F), (262145, F), (300001, B), (1 << 22, F)])
+def test_largest_vocabularies(V, dtype, kw):
+    check(*logits(2, V, dtype, seed=V % 1000), **kw)
+    check(*logits(2, V, dtype, seed=V % 1000, peak=0.0), **kw)
+
+
 @pytest.mark.parametrize("dtype", [F, B])
 @pytest.mark.parametrize("V,ld", [(999, 1003), (50257, 50272), (4096, 4097)])
 def test_strides(V, ld, dtype):
