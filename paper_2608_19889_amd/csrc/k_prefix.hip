@@ -1086,7 +1086,7 @@ constexpr int JOIN_MAX = 1024;
 template <typename T, int HD>
 __global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T> a, const RowParts* info, const float* parts,
                                                                int blocks, int R) {
-  constexpr int LANES = HD / 4, AHEAD = 4;
+  constexpr int LANES = HD / 4, FIRST = 2, AHEAD = 4;
   __shared__ f32x4 sum_o[JOIN_MAX];
   __shared__ float sum_m[JOIN_MAX / LANES], sum_l[JOIN_MAX / LANES];
   const int t = blockIdx.x, kvh = blockIdx.y, KV = a.kv.kv_heads, G = a.heads / KV;
@@ -1103,45 +1103,67 @@ __global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T>
   };
   const int b = a.seqs.cu ? among(a.seqs.cu, a.seqs.seqs, t) : t;
   if (b >= a.seqs.seqs) return;  // behind the last sequence
-  const bool active = a.seqs.lens[b] >= 0;
   const int grp = a.shared.groups ? among(a.shared.cu, a.shared.groups, b) : 0;
-  const bool has[2] = {active && grp < a.shared.groups && a.shared.lens[min(grp, a.shared.groups - 1)] > 0, active};
+  const int own_len = a.seqs.lens[b], prefix_len = grp < a.shared.groups ? a.shared.lens[grp] : 0;
   for (int j0 = 0; j0 < G; j0 += R) {
     const int j = j0 + row;
     f32x4 o = {};
     float top = -INFINITY, l = 0.f;
+    // parts i0, i0 + groups, ... from ``part`` on (the last one where there are fewer)
+    auto read = [&](const float* part, int64_t step, int in, int count, int i0, auto& v, auto& m, auto& s) {
+#pragma unroll
+      for (int i = 0; i < (int)(sizeof(m) / sizeof(float)); ++i) {  // (loads without a condition stay in flight together)
+        const float* at = part + max(min(i0 + i * groups, count - 1), 0) * step;
+        m[i] = at[16 * HD + in];
+        s[i] = at[16 * HD + 16 + in];
+        v[i] = *(const f32x4*)(at + in * HD + 4 * d);
+      }
+    };
+    auto add = [&](int count, int i0, const auto& v, const auto& m, const auto& s) {
+      constexpr int N = sizeof(m) / sizeof(float);
+      float next = top;
+#pragma unroll
+      for (int i = 0; i < N; ++i) next = fmaxf(next, m[i]);
+      const float fall = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      l = fall > 0.f ? l * fall : l != l ? l : 0.f;
+      o = fall > 0.f ? o * fall : f32x4{};
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (i0 + i * groups >= count) continue;
+        const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
+        l += f > 0.f || s[i] != s[i] ? f * s[i] : 0.f;  // (scores that are all NaN: no maximum)
+        o += f > 0.f ? f * v[i] : f32x4{};
+      }
+    };
+    // The first parts of either segment are read before the lengths have come that say
+    // whether there are any (where not: some other place of the parts).
+    const float* part[2];
+    int64_t step[2];
+    int count[2], in[2];
+    f32x4 v[2][FIRST];
+    float m[2][FIRST], s[2][FIRST];
+#pragma unroll
     for (int k = 0; k < 2; ++k) {
-      if (!has[k] || j >= G) continue;
-      const RowParts p = j0 ? info[info_at(k, kvh, KV, (int64_t)a.tokens * G, (int64_t)t * G + j)] : where[k];
-      const int count = p.count >> 9, apart = p.count >> 4 & 31, in = p.count & 15;
-      if (p.block < 0 || count < 1 || (int64_t)p.block + (int64_t)(count - 1) * apart >= blocks) continue;
-      const int64_t step = (int64_t)apart * part_floats(HD);
-      const float* part = parts + (int64_t)p.block * part_floats(HD);
-      const float *po = part + in * HD + 4 * d, *pm = part + 16 * HD + in;
-      for (int i0 = group; i0 < count; i0 += AHEAD * groups) {
-        f32x4 v[AHEAD];
-        float m[AHEAD], s[AHEAD];
+      const RowParts p = j0 ? info[info_at(k, kvh, KV, (int64_t)a.tokens * G, (int64_t)t * G + min(j, G - 1))] : where[k];
+      const int apart = p.count >> 4 & 31;
+      count[k] = p.count >> 9;
+      const bool inside = p.block >= 0 && count[k] > 0 && (int64_t)p.block + (int64_t)(count[k] - 1) * apart < blocks;
+      count[k] = inside ? count[k] : 0;
+      in[k] = p.count & 15;
+      step[k] = (int64_t)apart * part_floats(HD);
+      part[k] = parts + (inside ? (int64_t)p.block : 0) * part_floats(HD);
+      read(part[k], step[k], in[k], count[k], group, v[k], m[k], s[k]);
+    }
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {  // (loads without a condition stay in flight together)
-          const int64_t at = min(i0 + i * groups, count - 1) * step;
-          m[i] = pm[at];
-          s[i] = pm[at + 16];
-          v[i] = *(const f32x4*)(po + at);
-        }
-        float next = top;
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) next = fmaxf(next, m[i]);
-        const float fall = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next);
-        top = next;
-        l = fall > 0.f ? l * fall : l != l ? l : 0.f;
-        o = fall > 0.f ? o * fall : f32x4{};
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-          if (i0 + i * groups >= count) continue;
-          const float f = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
-          l += f > 0.f || s[i] != s[i] ? f * s[i] : 0.f;  // (scores that are all NaN: no maximum)
-          o += f > 0.f ? f * v[i] : f32x4{};
-        }
+    for (int k = 0; k < 2; ++k) {
+      if (own_len < 0 || (k == 0 && prefix_len <= 0) || j >= G || group >= count[k]) continue;
+      add(count[k], group, v[k], m[k], s[k]);
+      for (int i0 = group + FIRST * groups; i0 < count[k]; i0 += AHEAD * groups) {
+        f32x4 w[AHEAD];
+        float wm[AHEAD], ws[AHEAD];
+        read(part[k], step[k], in[k], count[k], i0, w, wm, ws);
+        add(count[k], i0, w, wm, ws);
       }
     }
     if (groups > 1) {

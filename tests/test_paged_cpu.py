@@ -88,6 +88,7 @@ ATTEND_BAD = [
     ("call", dict(ldo=255), ax.AXON_E_INVALID, "stride of out"),
     ("call", dict(out=P, ldo=300), ax.AXON_E_INVALID, "q's buffer"),
     ("call", dict(lse=P + 2), ax.AXON_E_INVALID, "d_lse"),
+    ("batch", dict(table_stride=(1 << 30) // PAGES["page_size"]), ax.AXON_E_CAPACITY, "too many for one call"),
     ("prefix", dict(groups=-1), ax.AXON_E_INVALID, "groups"),
     ("prefix", dict(groups=4097), ax.AXON_E_INVALID, "groups"),
     ("prefix", dict(table_stride=0), ax.AXON_E_CAPACITY, "d_prefix_table"),
