@@ -1082,16 +1082,19 @@ __global__ void __launch_bounds__(PA_THREADS, 2) prefix_attn_kernel(PrefixAttnAr
 // A row's parts of both segments: out = sum f o / sum f l, f = 2^(m - max).  A workgroup
 // per (token, kv head): HD / 4 lanes for a part of a row, the parts shared out over as
 // many groups of them as it has for the R rows at a time, whose sums are joined in LDS.
+// Few tokens' rows have many parts: a large workgroup each, several loads ahead.  Many
+// tokens' have one or two of either segment: small ones, in few enough registers that 8
+// fit a CU's SIMDs (20 questions of 150 tokens: 150 MB, 37 us; 5 at a time 44).
 constexpr int JOIN_MAX = 1024;
-template <typename T, int HD>
-__global__ void __launch_bounds__(JOIN_MAX) prefix_join_kernel(PrefixAttnArgs<T> a, const RowParts* info, const float* parts,
+template <typename T, int HD, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == JOIN_MAX ? 4 : 8) prefix_join_kernel(PrefixAttnArgs<T> a, const RowParts* info, const float* parts,
                                                                int blocks, int R) {
-  constexpr int LANES = HD / 4, FIRST = 2, AHEAD = 4;
-  __shared__ f32x4 sum_o[JOIN_MAX];
-  __shared__ float sum_m[JOIN_MAX / LANES], sum_l[JOIN_MAX / LANES];
+  constexpr int LANES = HD / 4, FIRST = THREADS == JOIN_MAX ? 2 : 1, AHEAD = THREADS == JOIN_MAX ? 4 : 1;
+  __shared__ f32x4 sum_o[THREADS];
+  __shared__ float sum_m[THREADS / LANES], sum_l[THREADS / LANES];
   const int t = blockIdx.x, kvh = blockIdx.y, KV = a.kv.kv_heads, G = a.heads / KV;
   const int lane = threadIdx.x & 63, d = threadIdx.x % LANES, team = threadIdx.x / LANES, row = team % R;
-  const int groups = (int)blockDim.x / (LANES * R), group = team / R;  // of parts
+  const int groups = THREADS / (LANES * R), group = team / R;  // of parts
   // (read before it is known whether they are there, beside what says it)
   RowParts where[2];
 #pragma unroll
@@ -1243,10 +1246,15 @@ static void launch(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* w
   const float sc = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * LOG2E_F;
   prefix_attn_kernel<T, HD><<<PA_WGS, PA_THREADS, 0, s>>>(a, sc, info, parts, PartsAt{(int)n.wide, (int)n.narrow});
   // few tokens: many threads each, whose parts are many
-  const int G = a.heads / a.kv.kv_heads, threads = (int64_t)a.tokens * a.kv.kv_heads <= 1024 ? JOIN_MAX : 256;
-  int R = 1;
-  while (R < G && R < threads / (HD / 4)) R *= 2;
-  prefix_join_kernel<T, HD><<<dim3(a.tokens, a.kv.kv_heads), threads, 0, s>>>(a, info, parts, (int)n.blocks(), R);
+  auto join = [&](auto threads) {
+    constexpr int N = decltype(threads)::value;
+    const int G = a.heads / a.kv.kv_heads;
+    int R = 1;
+    while (R < G && R < N / (HD / 4)) R *= 2;
+    prefix_join_kernel<T, HD, N><<<dim3(a.tokens, a.kv.kv_heads), N, 0, s>>>(a, info, parts, (int)n.blocks(), R);
+  };
+  if ((int64_t)a.tokens * a.kv.kv_heads <= 1024) join(std::integral_constant<int, JOIN_MAX>{});
+  else join(std::integral_constant<int, 256>{});
 }
 
 template <typename T>
