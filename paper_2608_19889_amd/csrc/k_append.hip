@@ -54,7 +54,8 @@ template <typename T, bool RUNS>
 __global__ void __launch_bounds__(APPEND_THREADS) rope_append_kernel(AppendArgs<T> a) {
   __shared__ float cs[MAX_HALF], sn[MAX_HALF];
   constexpr int E = RUN<T>;
-  const int t = blockIdx.x, tid = threadIdx.x;
+  const int t = blockIdx.y * GRID_TOKENS + blockIdx.x, tid = threadIdx.x;
+  if (t >= a.tokens) return;
   const int b = a.seqs.cu ? find_sequence(a.seqs.cu, a.seqs.seqs, t) : t;
   if (b >= a.seqs.seqs) return;  // behind the last sequence
   const int len = a.seqs.lens[b];
@@ -157,9 +158,9 @@ template <typename T>
 void launch_rope_append(const AppendArgs<T>& a, hipStream_t s) {
   if (a.tokens <= 0) return;
   if (a.rot % (a.interleaved ? RUN<T> : 2 * RUN<T>) == 0)
-    rope_append_kernel<T, true><<<a.tokens, APPEND_THREADS, 0, s>>>(a);
+    rope_append_kernel<T, true><<<token_grid(a.tokens), APPEND_THREADS, 0, s>>>(a);
   else
-    rope_append_kernel<T, false><<<a.tokens, APPEND_THREADS, 0, s>>>(a);
+    rope_append_kernel<T, false><<<token_grid(a.tokens), APPEND_THREADS, 0, s>>>(a);
 }
 template void launch_rope_append<float>(const AppendArgs<float>&, hipStream_t);
 template void launch_rope_append<bf16>(const AppendArgs<bf16>&, hipStream_t);

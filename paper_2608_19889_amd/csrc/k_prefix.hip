@@ -1100,9 +1100,10 @@ __global__ void __launch_bounds__(THREADS, THREADS == JOIN_MAX ? 4 : 8) prefix_j
   constexpr int LANES = HD / 4, FIRST = THREADS == JOIN_MAX ? 2 : 1, AHEAD = THREADS == JOIN_MAX ? 4 : 1;
   __shared__ f32x4 sum_o[THREADS];
   __shared__ float sum_m[THREADS / LANES], sum_l[THREADS / LANES];
-  const int t = blockIdx.x, kvh = blockIdx.y, KV = a.kv.kv_heads, G = a.heads / KV;
+  const int t = blockIdx.y * GRID_TOKENS + blockIdx.x, kvh = blockIdx.z, KV = a.kv.kv_heads, G = a.heads / KV;
   const int lane = threadIdx.x & 63, d = threadIdx.x % LANES, team = threadIdx.x / LANES, row = team % R;
   const int groups = THREADS / (LANES * R), group = team / R;  // of parts
+  if (t >= a.tokens) return;
   // (read before it is known whether they are there, beside what says it)
   RowParts where[2];
 #pragma unroll
@@ -1250,8 +1251,8 @@ static void launch(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* w
   const Sizes n = sizes_of(x);
   RowParts* info = (RowParts*)workspace;
   float* parts = (float*)((char*)workspace + n.parts_at);
-  // a scale of 0 leaves every score, masked ones apart, the same
-  const float sc = a.scale == 0.f ? 1e-37f : fabsf(a.scale) * LOG2E_F;
+  // a scale of 0 leaves every score, masked ones apart, the same (-inf times 0 is NaN)
+  const float sc = std::max(fabsf(a.scale) * LOG2E_F, 1e-37f);
   prefix_attn_kernel<T, HD><<<PA_WGS, PA_THREADS, 0, s>>>(a, sc, info, parts, PartsAt{(int)n.wide, (int)n.narrow});
   // few tokens: many threads each, whose parts are many
   auto join = [&](auto threads) {
@@ -1259,7 +1260,9 @@ static void launch(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* w
     const int G = a.heads / a.kv.kv_heads;
     int R = 1;
     while (R < G && R < N / (HD / 4)) R *= 2;
-    prefix_join_kernel<T, HD, N><<<dim3(a.tokens, a.kv.kv_heads), N, 0, s>>>(a, info, parts, (int)n.blocks(), R);
+    dim3 grid = token_grid(a.tokens);
+    grid.z = a.kv.kv_heads;
+    prefix_join_kernel<T, HD, N><<<grid, N, 0, s>>>(a, info, parts, (int)n.blocks(), R);
   };
   if ((int64_t)a.tokens * a.kv.kv_heads <= 1024) join(std::integral_constant<int, JOIN_MAX>{});
   else join(std::integral_constant<int, 256>{});

@@ -528,6 +528,11 @@ struct AppendArgs {
 };
 template <typename T>
 void launch_rope_append(const AppendArgs<T>& a, hipStream_t s);
+// A workgroup per token, in a grid's x and y: 2^32 threads at most along one of them.
+constexpr int GRID_TOKENS = 1 << 20;
+inline dim3 token_grid(int tokens) {
+  return dim3(tokens < GRID_TOKENS ? tokens : GRID_TOKENS, (tokens + GRID_TOKENS - 1) / GRID_TOKENS);
+}
 
 template <typename T>
 struct PrefixAttnArgs {

@@ -261,6 +261,7 @@ def test_attention_scores_far_apart(dtype):
     p.q *= 12
     check_attention(p)
     check_attention(p, scale=0.0)
+    check_attention(p, scale=1e-42)
     check_attention(p, scale=-0.7)
 
 
@@ -352,6 +353,28 @@ def test_attention_more_sequences_than_groups_cover():
     p = Paged(DECODE["groups"], 8, 2, 64, B)
     p.cu_groups = [0, 2, 3, 5]  # the last four have no prefix
     check_attention(p)
+
+
+def test_more_tokens_than_a_grid_dimension_has_threads():
+    """2^24 tokens and some, most of them of a sequence that takes no part."""
+    n, hd = 1 << 24, 64
+    cu = [0, 100, n, n + 70]
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.empty((n + 70, 1, hd), dtype=B, device="cuda")
+    ends = torch.cat([torch.arange(100), n + torch.arange(70)]).cuda()
+    q[ends] = torch.randn((170, 1, hd), generator=g, device="cuda").to(B)
+    kc, vc = (torch.zeros((12, 1, 16, hd), dtype=B, device="cuda") for _ in range(2))
+    table = torch.full((3, 7), -1, dtype=torch.int32)
+    table[0], table[2, :5] = torch.arange(7), torch.arange(7, 12)
+    table, lens = table.cuda(), torch.tensor([0, -1, 0], dtype=torch.int32).cuda()
+    assert ops.rope_append(None, q, q, kc, vc, table, lens, cu_seqlens=cu) is None
+    for c in (kc, vc):
+        assert torch.equal(c[:7].view(112, hd)[:100], q[:100, 0]) and torch.equal(c[7:].view(80, hd)[:70], q[n:, 0])
+    out = torch.full_like(q, 5)
+    ops.prefix_attention(q, kc, vc, table, lens, cu_seqlens=cu, out=out)
+    few = ops.prefix_attention(q[ends].contiguous(), kc, vc, table[::2].contiguous(), lens[::2].contiguous(),
+                               cu_seqlens=[0, 100, 170])
+    assert torch.equal(out[ends], few) and not out[100:n].any()
 
 
 def test_same_bits_again():
