@@ -1090,13 +1090,14 @@ __global__ void __launch_bounds__(PA_THREADS, 2) prefix_attn_kernel(PrefixAttnAr
 // A row's parts of both segments: out = sum f o / sum f l, f = 2^(m - max).  A workgroup
 // per (token, kv head): HD / 4 lanes for a part of a row, the parts shared out over as
 // many groups of them as it has for the R rows at a time, whose sums are joined in LDS.
-// Few tokens' rows have many parts: a large workgroup each, several loads ahead.  Many
+// Few tokens' rows have many parts: a large workgroup each, several loads ahead (48
+// answers, 384 workgroups with 26 parts a row: 10.6 us; of 1024 threads 14.0).  Many
 // tokens' have one or two of either segment: small ones, in few enough registers that 8
 // fit a CU's SIMDs (20 questions of 150 tokens: 150 MB, 37 us; 5 at a time 44).
-constexpr int JOIN_MAX = 1024;
+constexpr int JOIN_MAX = 512;
 template <typename T, int HD, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == JOIN_MAX ? 4 : 8) prefix_join_kernel(PrefixAttnArgs<T> a, const RowParts* info, const float* parts,
-                                                               int blocks, int R) {
+__global__ void __launch_bounds__(THREADS, THREADS == JOIN_MAX ? 4 : 8)
+    prefix_join_kernel(PrefixAttnArgs<T> a, const RowParts* info, const float* parts, int blocks, int R) {
   constexpr int LANES = HD / 4, FIRST = THREADS == JOIN_MAX ? 2 : 1, AHEAD = THREADS == JOIN_MAX ? 4 : 1;
   __shared__ f32x4 sum_o[THREADS];
   __shared__ float sum_m[THREADS / LANES], sum_l[THREADS / LANES];
@@ -1264,7 +1265,8 @@ static void launch(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* w
     grid.z = a.kv.kv_heads;
     prefix_join_kernel<T, HD, N><<<grid, N, 0, s>>>(a, info, parts, (int)n.blocks(), R);
   };
-  if ((int64_t)a.tokens * a.kv.kv_heads <= 1024) join(std::integral_constant<int, JOIN_MAX>{});
+  // (512 large workgroups run at once; 384 of them 10.6 us, small ones 15, 2048 of them 19.3 and 8.6)
+  if ((int64_t)a.tokens * a.kv.kv_heads <= 512) join(std::integral_constant<int, JOIN_MAX>{});
   else join(std::integral_constant<int, 256>{});
 }
 
