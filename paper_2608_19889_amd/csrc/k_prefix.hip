@@ -20,10 +20,10 @@
 // of a tile in its run it leaves (max, sum, product).  What is added to what depends on
 // the lengths alone: the same bits every time.
 //
-// Measured (bf16 but for the first; us with the join): 4 answers to 300 keys 16, of which
+// Measured (bf16 but for the first; us with the join): 4 answers to 300 keys 14, of which
 // the two launches' chains of dependent loads are all; 64 of 28 heads over 4 to 4096 keys
 // and 600 of their own 38 (83 MB); 256 of 32 over 8 to 16 prompts of 1100 66 (195 MB, 2.9
-// TB/s); 48 of 40 over 8 to 50011 keys 111 (376 MB and 50 GFLOP: 3.4 TB/s, 450 TFLOP/s);
+// TB/s); 48 of 40 over 8 to 50011 keys 108 (376 MB and 50 GFLOP: 3.5 TB/s, 463 TFLOP/s);
 // 20 questions of 150 tokens of 28 over 4 behind 2500 keys 227 (110 GFLOP; 190 of tiles, a
 // unit of 256 rows and 64 keys 2.2 against 0.9 of matrix instructions alone, and 130 MB of
 // parts written and read again).

@@ -21,8 +21,8 @@
 // of itself), which its few passes find in the L2; without a filter the sums lead it to
 // the token's chunk.
 //
-// Measured: 384 rows of 128256 float32, each with its own settings, 70 us (scan 44, 4.5
-// TB/s; the rest 26); 64 of 152064 with a nucleus 38 (scan 16: the float64 weights, some
+// Measured: 384 rows of 128256 float32, each with its own settings, 63 us (scan 44, 4.5
+// TB/s; the rest 20); 64 of 152064 with a nucleus 38 (scan 16: the float64 weights, some
 // 100 cycles each to a wavefront, stand beside 8 of reading; the rest 22: a chain of some
 // ten exchanges through LDS, 12 for most rows, 22 for one whose candidates are more than
 // can be compared); 8 of 32000 with top-k and top-p 17 (4 + 13, latency).  A scan of fewer
@@ -33,8 +33,7 @@
 namespace axon {
 
 typedef unsigned long long u64;
-constexpr int S_THREADS = 1024;
-constexpr int BINS = 2 * S_THREADS;
+constexpr int BINS = 2048;
 
 // 2^x for x <= 0 as v 2^n, v in [0.7, 1.42]: 2^f on [-1/2, 1/2] as the polynomial of
 // degree 10 through 2^f at Chebyshev's nodes, 4e-16 of itself off and exactly 1 at 0.
@@ -92,67 +91,10 @@ struct Candidate {
 };
 constexpr int FEW = 256;  // candidates that are compared each with each
 
-struct Shared {
-  u64 bins[BINS];
-  Candidate few[FEW];
-  u64 wave_sum[S_THREADS / 64];
-  u64 before, in;
-  int found, count;
-  u64 sum[2];
-  float red[S_THREADS / 64];
-};
-
-AXON_DEV void clear_bins(Shared& sh) {
-  __syncthreads();
-  for (int i = threadIdx.x; i < BINS; i += S_THREADS) sh.bins[i] = 0;
-  if (threadIdx.x == 0) sh.found = -1;
-  __syncthreads();
-}
-
 AXON_DEV u64 wave_total(u64 v) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
   return v;
-}
-
-// Over each thread's two entries, in the threads' order: the entry at which the running
-// sum (from ``from`` on) reaches target(total) >= 1; what is before it and in it.  -1:
-// none does, which is so only where a caller asks for more than there is.
-struct Found {
-  int at;
-  u64 before, in;
-};
-template <typename F>
-AXON_DEV Found find_entry(Shared& sh, const u64 (&v)[2], u64 from, F&& target, u64* total = nullptr) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  u64 upto = v[0] + v[1];
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 u = __shfl_up(upto, d);
-    if (lane >= d) upto += u;
-  }
-  if (lane == 63) sh.wave_sum[wave] = upto;
-  if (threadIdx.x == 0) sh.found = -1;
-  __syncthreads();
-  u64 before = from + upto - v[0] - v[1], sum = from;
-#pragma unroll
-  for (int w = 0; w < S_THREADS / 64; ++w) {
-    before += w < wave ? sh.wave_sum[w] : 0;
-    sum += sh.wave_sum[w];
-  }
-  const u64 want = target(sum);
-  if (total) *total = sum;
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    if (before < want && want <= before + v[j]) {
-      sh.found = 2 * threadIdx.x + j;
-      sh.before = before;
-      sh.in = v[j];
-    }
-    before += v[j];
-  }
-  __syncthreads();
-  return Found{sh.found, sh.before, sh.in};
 }
 
 // ---------------------------------------------------------------- one reading of the logits
@@ -270,426 +212,507 @@ __global__ void __launch_bounds__(SCAN_THREADS) sample_scan_kernel(SampleArgs a,
 constexpr int LIST = 2048;        // blocks that are listed; more: all of the row
 constexpr int MAX_BLOCKS = 8192;  // maxima that fit into LDS (262144 logits)
 
-// The values of a row that can matter: those of the listed blocks, or (n < 0) of all.
-// What is below ``cut`` is passed over.
-template <typename T>
-struct Row {
-  static constexpr int N = RUN<T>, LANES = BLOCK / N;
-  const T* z;
-  int V;
-  float cut;
-  int n;
-  const int32_t* list;
-  AXON_DEV int items() const { return n < 0 ? (V + N - 1) / N : n * LANES; }
-  AXON_DEV int first(int e) const { return n < 0 ? e * N : list[e / LANES] * BLOCK + e % LANES * N; }
-  template <typename F>
-  AXON_DEV void each(F&& f) const {
-    float v[N], next[N];
-    const int end = items();
-    if ((int)threadIdx.x < end) load_run(z, first(threadIdx.x), V, v);
-#pragma unroll 1
-    for (int e = threadIdx.x; e < end; e += S_THREADS) {
-      const int at = first(e);
-      if (e + S_THREADS < end) load_run(z, first(e + S_THREADS), V, next);
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (v[i] >= cut) f(v[i], at + i);
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] = next[i];
-    }
-  }
-};
+// What a workgroup of S_THREADS does for its row
+template <int S_THREADS>
+struct RowOf {
+  static constexpr int EACH = BINS / S_THREADS;  // of BINS entries, a thread's
+  static constexpr int SHARE = S_THREADS / FEW;  // threads of a candidate
 
-// up to FEW values of the row that ``take`` takes, in sh.few in any order; their number
-// (more than FEW: not all of them are there)
-template <typename R, typename P, typename W>
-AXON_DEV int gather(Shared& sh, const R& row, P&& take, W&& weight) {
-  __syncthreads();
-  if (threadIdx.x == 0) sh.count = 0;
-  __syncthreads();
-  row.each([&](float z, int i) {
-    if (!take(z)) return;
-    const int n = atomicAdd(&sh.count, 1);
-    if (n < FEW) sh.few[n] = Candidate{z, i, weight(z)};
-  });
-  __syncthreads();
-  const int n = sh.count;
-  // (whole rounds of others())
-  if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < FEW) sh.few[n + threadIdx.x] = Candidate{-INFINITY, 0x7fffffff, 0};
-  __syncthreads();
-  return n;
-}
-// Four threads to a candidate (thread / 4): f(candidate) over a quarter each, eight at a
-// time so that their reads are in flight together
-template <typename F>
-AXON_DEV void others(const Shared& sh, int n, F&& f) {
-  static_assert(FEW % 32 == 0, "rounds end inside few");
-  for (int j = threadIdx.x & 3; j < n; j += 32) {
-    Candidate c[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) c[k] = sh.few[j + 4 * k];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) f(c[k]);
-  }
-}
-AXON_DEV u64 quad_sum(u64 v) {
-  v += __shfl_xor(v, 1);
-  return v + __shfl_xor(v, 2);
-}
-// whether a comes before b in descending order
-AXON_DEV bool ahead(const Candidate& a, const Candidate& b) { return a.z > b.z || (a.z == b.z && a.i < b.i); }
-
-// The border in descending order: values above key are kept, of those on it the indices
-// up to last.  COUNT: ``want`` values are kept, else as many as it takes for their weights
-// to reach ``want``; all there are if that is not reached.
-struct Border {
-  uint32_t key;
-  int last;
-};
-template <bool COUNT, typename T, typename W>
-AXON_DEV Border find_border(Shared& sh, const Row<T>& row, uint32_t lo, uint32_t hi, W&& weight, u64 want) {
-  u64 above = 0;  // (number or weight) of what is above hi
-  for (;;) {
-    int shift = 0;
-    while ((hi - lo) >> shift >= BINS) ++shift;
-    clear_bins(sh);
-    row.each([&](float z, int) {
-      const uint32_t k = order_key<T>(z);
-      if (k < lo || k > hi) return;
-      const u64 w = COUNT ? 1 : weight(z);
-      if (w) atomicAdd(&sh.bins[(k - lo) >> shift], w);
-    });
-    __syncthreads();
-    const int e = BINS - 1 - 2 * threadIdx.x;
-    const u64 v[2] = {sh.bins[e], sh.bins[e - 1]};
-    const Found f = find_entry(sh, v, above, [&](u64 total) { return want = min(want, total); });
-    const uint32_t bin = BINS - 1 - f.at;
-    lo += bin << shift;
-    hi = min(hi, lo + ((1u << shift) - 1));
-    above = f.before;
-    if (lo == hi) {
-      // all have one value: as many of them as are wanted, the lowest indices
-      const u64 each = COUNT ? 1 : weight(key_value<T>(lo)), most = f.in / each, take = (want - above + each - 1) / each;
-      int last = row.V;
-      if (take < most) {
-        const int width = (row.V + BINS - 1) / BINS;  // <= BINS
-        clear_bins(sh);
-        row.each([&](float z, int i) {
-          if (order_key<T>(z) == lo) atomicAdd(&sh.bins[i / width], (u64)1);
-        });
-        __syncthreads();
-        const u64 b[2] = {sh.bins[2 * threadIdx.x], sh.bins[2 * threadIdx.x + 1]};
-        const Found g = find_entry(sh, b, 0, [&](u64) { return take; });
-        u64 w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int in = 2 * threadIdx.x + j, i = max(g.at, 0) * width + in;
-          w[j] = in < width && i < row.V && order_key<T>(sane(to_f32(row.z[i]))) == lo;
-        }
-        __syncthreads();
-        last = g.at * width + find_entry(sh, w, g.before, [&](u64) { return take; }).at;
-      }
-      return Border{lo, last};
-    }
-    const int n = gather(sh, row, [&](float z) { const uint32_t k = order_key<T>(z); return lo <= k && k <= hi; },
-                         [&](float z) { return COUNT ? (u64)1 : weight(z); });
-    if (n <= FEW) {  // few enough to compare
-      const int i = threadIdx.x >> 2;
-      if (i < n) {
-        const Candidate me = sh.few[i];
-        u64 before = 0;
-        others(sh, n, [&](const Candidate& c) { before += ahead(c, me) ? c.w : 0; });
-        before = above + quad_sum(before);
-        if ((threadIdx.x & 3) == 0 && before < want && want <= before + me.w) sh.found = i;
-      }
-      __syncthreads();
-      const Candidate me = sh.few[min(sh.found, n - 1)];
-      return Border{order_key<T>(me.z), me.i};
-    }
-  }
-}
-
-// the workgroup's sum of f over the row's values
-template <typename R, typename F>
-AXON_DEV u64 row_sum(Shared& sh, const R& row, F&& f) {
-  u64 sum = 0;
-  row.each([&](float z, int i) { sum += f(z, i); });
-  sum = wave_total(sum);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.wave_sum[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  sum = 0;
-#pragma unroll
-  for (int w = 0; w < S_THREADS / 64; ++w) sum += sh.wave_sum[w];
-  return sum;
-}
-
-// The index at which the running sum of weight(z, i) reaches target(total), which is set.
-// weight is 0 below the row's cut.
-template <typename T, typename W, typename F>
-AXON_DEV int find_index(Shared& sh, const Row<T>& row, W&& weight, F&& target, u64* total) {
-  int width = (row.V + BINS - 1) / BINS;  // of a bin, <= BINS
-  clear_bins(sh);
-  if (row.n >= 0) {
-    row.each([&](float z, int i) {
-      const u64 w = weight(z, i);
-      if (w) atomicAdd(&sh.bins[i / width], w);
-    });
-  } else {
-    // all of the row: a wavefront adds up a chunk
-    width = CHUNK;
-    for (int c = threadIdx.x >> 6; c < chunks_of(row.V); c += S_THREADS / 64) {
-      u64 sum = 0;
-#pragma unroll 2
-      for (int j = 0; j < CHUNK / (64 * RUN<T>); ++j) {
-        float v[RUN<T>];
-        const int first = c * CHUNK + (j * 64 + (threadIdx.x & 63)) * RUN<T>;
-        load_run(row.z, first, row.V, v);
-#pragma unroll
-        for (int i = 0; i < RUN<T>; ++i)
-          if (v[i] >= row.cut) sum += weight(v[i], first + i);
-      }
-      sum = wave_total(sum);
-      if ((threadIdx.x & 63) == 0) sh.bins[c] = sum;
-    }
-  }
-  __syncthreads();
-  u64 want = 0;
-  const int e = 2 * threadIdx.x;
-  const u64 v[2] = {sh.bins[e], sh.bins[e + 1]};
-  const Found f = find_entry(sh, v, 0, [&](u64 t) { return want = target(t); }, total);
-  u64 w[2];
-#pragma unroll
-  for (int j = 0; j < 2; ++j) {
-    const int i = max(f.at, 0) * width + e + j;
-    const float z = i < row.V ? sane(to_f32(row.z[i])) : -INFINITY;
-    w[j] = e + j < width && z >= row.cut ? weight(z, i) : 0;
-  }
-  __syncthreads();
-  return f.at * width + find_entry(sh, w, f.before, [&](u64) { return want; }).at;
-}
-
-// the workgroup's maximum
-AXON_DEV float block_top(Shared& sh, float v) {
-  v = wave_max(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = v;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < S_THREADS / 64; ++w) v = fmaxf(v, sh.red[w]);
-  return v;
-}
-
-template <typename T>
-__global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, void* ws) {
-  __shared__ Shared sh;
-  __shared__ alignas(16) float maxima[MAX_BLOCKS];
-  __shared__ int32_t list[LIST];
-  constexpr float LOWEST = -3.402823466e38f;
-  const int r = blockIdx.x, V = a.vocab, chunks = chunks_of(V), blocks = chunks * CHUNK_BLOCKS, tid = threadIdx.x;
-  const T* z = (const T*)a.logits + r * a.ld;
-  const RowSums in = row_sums(ws, r, V);
-  const Settings s = settings_of(a, r);
-  const float uniform = a.uniform[r];
-  const bool filtered = !s.greedy && (s.by_rank || s.p < 1.f || s.low > 0.f), fits = blocks <= MAX_BLOCKS;
-  // (loads of everything that is needed, in flight together)
-  const float chunk_max = tid < chunks ? in.chunk_max[tid] : -INFINITY;
-  const bool summed = needs_sum(s);
-  const double chunk_sum = summed && tid < chunks ? in.chunk_sum[tid] : 0.;
-  float top = chunk_max, lowest = INFINITY;  // of the maxima that are numbers
-  for (int i = tid + S_THREADS; i < chunks; i += S_THREADS) top = fmaxf(top, in.chunk_max[i]);
-  if (filtered && fits) {
-    f32x4 m[MAX_BLOCKS / (4 * S_THREADS)];
-#pragma unroll
-    for (int j = 0; j < MAX_BLOCKS / (4 * S_THREADS); ++j) {
-      const int i = 4 * (j * S_THREADS + tid);
-      m[j] = i < blocks ? *(const f32x4*)(in.block_max + i) : f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-    }
-#pragma unroll
-    for (int j = 0; j < MAX_BLOCKS / (4 * S_THREADS); ++j) {
-      const int i = 4 * (j * S_THREADS + tid);
-      if (i < blocks) *(f32x4*)(maxima + i) = m[j];
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (m[j][k] > -INFINITY) lowest = fminf(lowest, m[j][k]);
-    }
-  }
-  top = block_top(sh, top);
-  if (top == -INFINITY) {
-    if (tid == 0) {
-      a.tokens[r] = -1;
-      a.logps[r] = 0.f;
-    }
-    return;
-  }
-  if (s.greedy) {  // the first block with the maximum, the first there
-    if (tid == 0) sh.found = blocks;
-    __syncthreads();
-    for (int i = tid; i < blocks; i += S_THREADS)
-      if (in.block_max[i] == top) {
-        atomicMin(&sh.found, i);
-        break;
-      }
-    __syncthreads();
-    if (tid >= 64) return;
-    const int i = sh.found * BLOCK + tid;
-    const uint64_t has = __ballot(tid < BLOCK && i < V && sane(to_f32(z[min(i, V - 1)])) == top);
-    if (tid == 0) {
-      a.tokens[r] = sh.found * BLOCK + __ffsll((long long)has) - 1;
-      a.logps[r] = 0.f;
-    }
-    return;
-  }
-  const int scale = 62 - (V > 1 ? 32 - __clz(V - 1) : 0);
-  const double c = per_unit(s), unit = ldexp(1., scale);
-  auto parts = [&](float v) { return exp2_neg(v == top ? 0. : ((double)v - top) * c); };
-  auto weight = [&](float v) { return as_fixed(parts(v), scale); };
-  // the place in the kept weights' running sum, 1 .. sum
-  auto drawn = [&](u64 sum) {
-    return min((u64)((double)fminf(fmaxf(uniform, 0.f), 1.f) * (double)sum), sum - 1) + 1;
+  struct Shared {
+    u64 bins[BINS];
+    Candidate few[FEW];
+    u64 wave_sum[S_THREADS / 64];
+    u64 before, in;
+    int found, count;
+    u64 sum[2];
+    float red[S_THREADS / 64];
   };
-  u64 total = 0;
-  int token;
-  if (!filtered) {
-    u64 w[2], want = 0;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int i = 2 * tid + j;
-      const float m = i < chunks ? in.chunk_max[i] : -INFINITY;
-      // (a chunk whose weights are all 0 is not one to look in)
-      w[j] = m > -INFINITY && weight(m) ? (u64)rint(as_double(parts(m)) * in.chunk_sum[i] * unit) : 0;
+
+  static AXON_DEV void clear_bins(Shared& sh) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < BINS; i += S_THREADS) sh.bins[i] = 0;
+    if (threadIdx.x == 0) sh.found = -1;
+    __syncthreads();
+  }
+
+  // Over each thread's EACH entries, in the threads' order: the entry at which the running
+  // sum (from ``from`` on) reaches target(total) >= 1; what is before it and in it.  -1:
+  // none does, which is so only where a caller asks for more than there is.
+  struct Found {
+    int at;
+    u64 before, in;
+  };
+  template <typename F>
+  static AXON_DEV Found find_entry(Shared& sh, const u64 (&v)[EACH], u64 from, F&& target, u64* total = nullptr) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    u64 mine = 0;
+  #pragma unroll
+    for (int j = 0; j < EACH; ++j) mine += v[j];
+    u64 upto = mine;
+  #pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const u64 u = __shfl_up(upto, d);
+      if (lane >= d) upto += u;
     }
-    const Found f = find_entry(sh, w, 0, [&](u64 sum) { return want = drawn(sum); }, &total);
-    const int first = max(f.at, 0) * CHUNK + 2 * tid;
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const float v = first + j < V ? sane(to_f32(z[first + j])) : -INFINITY;
-      w[j] = v > -INFINITY ? weight(v) : 0;
+    if (lane == 63) sh.wave_sum[wave] = upto;
+    if (threadIdx.x == 0) sh.found = -1;
+    __syncthreads();
+    u64 before = from + upto - mine, sum = from;
+  #pragma unroll
+    for (int w = 0; w < S_THREADS / 64; ++w) {
+      before += w < wave ? sh.wave_sum[w] : 0;
+      sum += sh.wave_sum[w];
+    }
+    const u64 want = target(sum);
+    if (total) *total = sum;
+  #pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      if (before < want && want <= before + v[j]) {
+        sh.found = EACH * threadIdx.x + j;
+        sh.before = before;
+        sh.in = v[j];
+      }
+      before += v[j];
     }
     __syncthreads();
-    token = f.at * CHUNK + find_entry(sh, w, 0, [&](u64 sum) { return min(want - f.before, sum); }).at;
-  } else {
-    const double share = (double)fmaxf(s.p, 0.f), least = s.low > 0.f ? (double)fminf(s.low, 1.f) : -1.;
-    double sum = 0.;  // of all weights
-    if (summed) {
-      if (chunk_max > -INFINITY) sum = as_double(parts(chunk_max)) * chunk_sum;
-      for (int i = tid + S_THREADS; i < chunks; i += S_THREADS) {
-        const float m = in.chunk_max[i];
-        if (m > -INFINITY) sum += as_double(parts(m)) * in.chunk_sum[i];
+    return Found{sh.found, sh.before, sh.in};
+  }
+
+  // The values of a row that can matter: those of the listed blocks, or (n < 0) of all.
+  // What is below ``cut`` is passed over.
+  template <typename T>
+  struct Row {
+    static constexpr int N = RUN<T>, LANES = BLOCK / N;
+    const T* z;
+    int V;
+    float cut;
+    int n;
+    const int32_t* list;
+    AXON_DEV int items() const { return n < 0 ? (V + N - 1) / N : n * LANES; }
+    AXON_DEV int first(int e) const { return n < 0 ? e * N : list[e / LANES] * BLOCK + e % LANES * N; }
+    template <typename F>
+    AXON_DEV void each(F&& f) const {
+      float v[N], next[N];
+      const int end = items();
+      if ((int)threadIdx.x < end) load_run(z, first(threadIdx.x), V, v);
+  #pragma unroll 1
+      for (int e = threadIdx.x; e < end; e += S_THREADS) {
+        const int at = first(e);
+        if (e + S_THREADS < end) load_run(z, first(e + S_THREADS), V, next);
+  #pragma unroll
+        for (int i = 0; i < N; ++i)
+          if (v[i] >= cut) f(v[i], at + i);
+  #pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = next[i];
       }
-#pragma unroll
-      for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
-      if ((tid & 63) == 0) sh.wave_sum[tid >> 6] = __double_as_longlong(sum);
-      __syncthreads();
-      sum = 0.;
-#pragma unroll
-      for (int w = 0; w < S_THREADS / 64; ++w) sum += __longlong_as_double(sh.wave_sum[w]);
     }
-    // Nothing below ``cut`` is kept (a top-k's weight, of which top-p takes its share,
-    // has to be there in full).
-    float cut = LOWEST;
-    if (s.low > 0.f && !(s.by_rank && s.p < 1.f)) cut = (float)(top + log2(least) / c);
-    if (s.by_rank || s.p < 1.f) {
-      lowest = -block_top(sh, -lowest);
-      const float per_bin = (BINS - 1) / (top - lowest);
-      if (fits && per_bin > 0.f && per_bin < INFINITY) {
-        clear_bins(sh);
-        // (the share, a little more: these weights are rounded differently)
-        const u64 want = s.by_rank ? (u64)s.k : (u64)(share * sum * (1ll << 32) * 1.0001) + 1;
-        const float c32 = (float)c;
-        for (int i = tid; i < blocks; i += S_THREADS) {
-          const float m = maxima[i];
-          if (m > -INFINITY)
-            atomicAdd(&sh.bins[min((int)((top - m) * per_bin), BINS - 1)],
-                      s.by_rank ? (u64)1 : (u64)(__builtin_amdgcn_exp2f((m - top) * c32) * 4294967296.f));
+  };
+
+  // up to FEW values of the row that ``take`` takes, in sh.few in any order; their number
+  // (more than FEW: not all of them are there)
+  template <typename R, typename P, typename W>
+  static AXON_DEV int gather(Shared& sh, const R& row, P&& take, W&& weight) {
+    __syncthreads();
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+    row.each([&](float z, int i) {
+      if (!take(z)) return;
+      const int n = atomicAdd(&sh.count, 1);
+      if (n < FEW) sh.few[n] = Candidate{z, i, weight(z)};
+    });
+    __syncthreads();
+    const int n = sh.count;
+    // (whole rounds of others())
+    if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < FEW) sh.few[n + threadIdx.x] = Candidate{-INFINITY, 0x7fffffff, 0};
+    __syncthreads();
+    return n;
+  }
+  // SHARE threads to a candidate (thread / SHARE): f(candidate) over a part each, eight at a
+  // time so that their reads are in flight together
+  template <typename F>
+  static AXON_DEV void others(const Shared& sh, int n, F&& f) {
+    static_assert(FEW % 32 == 0 && 32 % (8 * SHARE) == 0, "rounds end inside few");
+    for (int j = threadIdx.x % SHARE; j < n; j += 8 * SHARE) {
+      Candidate c[8];
+  #pragma unroll
+      for (int k = 0; k < 8; ++k) c[k] = sh.few[j + SHARE * k];
+  #pragma unroll
+      for (int k = 0; k < 8; ++k) f(c[k]);
+    }
+  }
+  static AXON_DEV u64 share_sum(u64 v) {
+  #pragma unroll
+    for (int d = 1; d < SHARE; d <<= 1) v += __shfl_xor(v, d);
+    return v;
+  }
+  // whether a comes before b in descending order
+  static AXON_DEV bool ahead(const Candidate& a, const Candidate& b) { return a.z > b.z || (a.z == b.z && a.i < b.i); }
+
+  // The border in descending order: values above key are kept, of those on it the indices
+  // up to last.  COUNT: ``want`` values are kept, else as many as it takes for their weights
+  // to reach ``want``; all there are if that is not reached.
+  struct Border {
+    uint32_t key;
+    int last;
+  };
+  template <bool COUNT, typename T, typename W>
+  static AXON_DEV Border find_border(Shared& sh, const Row<T>& row, uint32_t lo, uint32_t hi, W&& weight, u64 want) {
+    u64 above = 0;  // (number or weight) of what is above hi
+    for (;;) {
+      int shift = 0;
+      while ((hi - lo) >> shift >= BINS) ++shift;
+      clear_bins(sh);
+      row.each([&](float z, int) {
+        const uint32_t k = order_key<T>(z);
+        if (k < lo || k > hi) return;
+        const u64 w = COUNT ? 1 : weight(z);
+        if (w) atomicAdd(&sh.bins[(k - lo) >> shift], w);
+      });
+      __syncthreads();
+      u64 v[EACH];
+  #pragma unroll
+      for (int j = 0; j < EACH; ++j) v[j] = sh.bins[BINS - 1 - EACH * threadIdx.x - j];
+      const Found f = find_entry(sh, v, above, [&](u64 total) { return want = min(want, total); });
+      const uint32_t bin = BINS - 1 - f.at;
+      lo += bin << shift;
+      hi = min(hi, lo + ((1u << shift) - 1));
+      above = f.before;
+      if (lo == hi) {
+        // all have one value: as many of them as are wanted, the lowest indices
+        const u64 each = COUNT ? 1 : weight(key_value<T>(lo)), most = f.in / each, take = (want - above + each - 1) / each;
+        int last = row.V;
+        if (take < most) {
+          const int width = (row.V + BINS - 1) / BINS;  // <= BINS
+          clear_bins(sh);
+          row.each([&](float z, int i) {
+            if (order_key<T>(z) == lo) atomicAdd(&sh.bins[i / width], (u64)1);
+          });
+          __syncthreads();
+          u64 b[EACH];
+  #pragma unroll
+          for (int j = 0; j < EACH; ++j) b[j] = sh.bins[EACH * threadIdx.x + j];
+          const Found g = find_entry(sh, b, 0, [&](u64) { return take; });
+          u64 w[EACH];
+  #pragma unroll
+          for (int j = 0; j < EACH; ++j) {
+            const int in = EACH * threadIdx.x + j, i = max(g.at, 0) * width + in;
+            w[j] = in < width && i < row.V && order_key<T>(sane(to_f32(row.z[i]))) == lo;
+          }
+          __syncthreads();
+          last = g.at * width + find_entry(sh, w, g.before, [&](u64) { return take; }).at;
+        }
+        return Border{lo, last};
+      }
+      const int n = gather(sh, row, [&](float z) { const uint32_t k = order_key<T>(z); return lo <= k && k <= hi; },
+                           [&](float z) { return COUNT ? (u64)1 : weight(z); });
+      if (n <= FEW) {  // few enough to compare
+        const int i = threadIdx.x / SHARE;
+        if (i < n) {
+          const Candidate me = sh.few[i];
+          u64 before = 0;
+          others(sh, n, [&](const Candidate& c) { before += ahead(c, me) ? c.w : 0; });
+          before = above + share_sum(before);
+          if (threadIdx.x % SHARE == 0 && before < want && want <= before + me.w) sh.found = i;
         }
         __syncthreads();
-        const u64 v[2] = {sh.bins[2 * tid], sh.bins[2 * tid + 1]};
-        const Found f = find_entry(sh, v, 0, [&](u64) { return want; });
-        // every value of bins 0 .. f.at, with the roundings of a bin's number
-        if (f.at >= 0) cut = fmaxf(cut, top - (f.at + 1) / per_bin * 1.000001f);
+        const Candidate me = sh.few[min(sh.found, n - 1)];
+        return Border{order_key<T>(me.z), me.i};
       }
     }
-    cut = fmaxf(cut - fabsf(cut) * 1e-6f, LOWEST);
-    Row<T> row{z, V, cut, -1, list};
-    if (fits) {
-      __syncthreads();
-      if (tid == 0) sh.found = 0;
+  }
+
+  // the workgroup's sum of f over the row's values
+  template <typename R, typename F>
+  static AXON_DEV u64 row_sum(Shared& sh, const R& row, F&& f) {
+    u64 sum = 0;
+    row.each([&](float z, int i) { sum += f(z, i); });
+    sum = wave_total(sum);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.wave_sum[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    sum = 0;
+  #pragma unroll
+    for (int w = 0; w < S_THREADS / 64; ++w) sum += sh.wave_sum[w];
+    return sum;
+  }
+
+  // The index at which the running sum of weight(z, i) reaches target(total), which is set.
+  // weight is 0 below the row's cut.
+  template <typename T, typename W, typename F>
+  static AXON_DEV int find_index(Shared& sh, const Row<T>& row, W&& weight, F&& target, u64* total) {
+    int width = (row.V + BINS - 1) / BINS;  // of a bin, <= BINS
+    clear_bins(sh);
+    if (row.n >= 0) {
+      row.each([&](float z, int i) {
+        const u64 w = weight(z, i);
+        if (w) atomicAdd(&sh.bins[i / width], w);
+      });
+    } else {
+      // all of the row: a wavefront adds up a chunk
+      width = CHUNK;
+      for (int c = threadIdx.x >> 6; c < chunks_of(row.V); c += S_THREADS / 64) {
+        u64 sum = 0;
+  #pragma unroll 2
+        for (int j = 0; j < CHUNK / (64 * RUN<T>); ++j) {
+          float v[RUN<T>];
+          const int first = c * CHUNK + (j * 64 + (threadIdx.x & 63)) * RUN<T>;
+          load_run(row.z, first, row.V, v);
+  #pragma unroll
+          for (int i = 0; i < RUN<T>; ++i)
+            if (v[i] >= row.cut) sum += weight(v[i], first + i);
+        }
+        sum = wave_total(sum);
+        if ((threadIdx.x & 63) == 0) sh.bins[c] = sum;
+      }
+    }
+    __syncthreads();
+    u64 want = 0;
+    const int e = EACH * threadIdx.x;
+    u64 v[EACH];
+  #pragma unroll
+    for (int j = 0; j < EACH; ++j) v[j] = sh.bins[e + j];
+    const Found f = find_entry(sh, v, 0, [&](u64 t) { return want = target(t); }, total);
+    u64 w[EACH];
+  #pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int i = max(f.at, 0) * width + e + j;
+      const float z = i < row.V ? sane(to_f32(row.z[i])) : -INFINITY;
+      w[j] = e + j < width && z >= row.cut ? weight(z, i) : 0;
+    }
+    __syncthreads();
+    return f.at * width + find_entry(sh, w, f.before, [&](u64) { return want; }).at;
+  }
+
+  // the workgroup's maximum
+  static AXON_DEV float block_top(Shared& sh, float v) {
+    v = wave_max(v);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) sh.red[threadIdx.x >> 6] = v;
+    __syncthreads();
+  #pragma unroll
+    for (int w = 0; w < S_THREADS / 64; ++w) v = fmaxf(v, sh.red[w]);
+    return v;
+  }
+
+  template <typename T>
+  static AXON_DEV void run(const SampleArgs& a, void* ws, Shared& sh, float* maxima, int32_t* list) {
+    constexpr float LOWEST = -3.402823466e38f;
+    const int r = blockIdx.x, V = a.vocab, chunks = chunks_of(V), blocks = chunks * CHUNK_BLOCKS, tid = threadIdx.x;
+    const T* z = (const T*)a.logits + r * a.ld;
+    const RowSums in = row_sums(ws, r, V);
+    const Settings s = settings_of(a, r);
+    const float uniform = a.uniform[r];
+    const bool filtered = !s.greedy && (s.by_rank || s.p < 1.f || s.low > 0.f), fits = blocks <= MAX_BLOCKS;
+    // (loads of everything that is needed, in flight together)
+    const float chunk_max = tid < chunks ? in.chunk_max[tid] : -INFINITY;
+    const bool summed = needs_sum(s);
+    const double chunk_sum = summed && tid < chunks ? in.chunk_sum[tid] : 0.;
+    float top = chunk_max, lowest = INFINITY;  // of the maxima that are numbers
+    for (int i = tid + S_THREADS; i < chunks; i += S_THREADS) top = fmaxf(top, in.chunk_max[i]);
+    if (filtered && fits) {
+      f32x4 m[MAX_BLOCKS / (4 * S_THREADS)];
+  #pragma unroll
+      for (int j = 0; j < MAX_BLOCKS / (4 * S_THREADS); ++j) {
+        const int i = 4 * (j * S_THREADS + tid);
+        m[j] = i < blocks ? *(const f32x4*)(in.block_max + i) : f32x4{-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      }
+  #pragma unroll
+      for (int j = 0; j < MAX_BLOCKS / (4 * S_THREADS); ++j) {
+        const int i = 4 * (j * S_THREADS + tid);
+        if (i < blocks) *(f32x4*)(maxima + i) = m[j];
+  #pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (m[j][k] > -INFINITY) lowest = fminf(lowest, m[j][k]);
+      }
+    }
+    top = block_top(sh, top);
+    if (top == -INFINITY) {
+      if (tid == 0) {
+        a.tokens[r] = -1;
+        a.logps[r] = 0.f;
+      }
+      return;
+    }
+    if (s.greedy) {  // the first block with the maximum, the first there
+      if (tid == 0) sh.found = blocks;
       __syncthreads();
       for (int i = tid; i < blocks; i += S_THREADS)
-        if (maxima[i] >= cut) {
-          const int n = atomicAdd(&sh.found, 1);
-          if (n < LIST) list[n] = i;
+        if (in.block_max[i] == top) {
+          atomicMin(&sh.found, i);
+          break;
         }
       __syncthreads();
-      if (sh.found <= LIST) row.n = sh.found;
-    }
-    const int n = row.n < 0 ? FEW + 1 : gather(sh, row, [](float) { return true; }, weight);
-    if (n <= FEW) {
-      // few: each compared with each, by rank and weight, then by index
-      if (tid == 0) sh.sum[0] = sh.sum[1] = 0;
-      if (tid == 0) sh.found = 0;
-      __syncthreads();
-      const int me = tid >> 2;
-      const bool leads = me < n && (tid & 3) == 0;
-      const Candidate x = sh.few[min(me, n - 1)];
-      u64 rank = 0, before = 0;
-      others(sh, n, [&](const Candidate& o) {
-        const bool is = ahead(o, x);
-        rank += is;
-        before += is ? o.w : 0;
-      });
-      rank = quad_sum(rank);
-      before = quad_sum(before);
-      const bool first = !s.by_rank || rank < (u64)s.k;
-      if (s.by_rank && s.p < 1.f) {
-        if (leads && first) atomicAdd(&sh.sum[0], x.w);
-        __syncthreads();
+      if (tid >= 64) return;
+      const int i = sh.found * BLOCK + tid;
+      const uint64_t has = __ballot(tid < BLOCK && i < V && sane(to_f32(z[min(i, V - 1)])) == top);
+      if (tid == 0) {
+        a.tokens[r] = sh.found * BLOCK + __ffsll((long long)has) - 1;
+        a.logps[r] = 0.f;
       }
-      const double of = s.by_rank ? (double)sh.sum[0] : sum * unit;
-      bool kept = first && x.w > 0 && (double)x.w >= least * unit;
-      if (s.p < 1.f) kept = kept && before < max((u64)ceil(share * of), (u64)1);
-      if (leads && kept) atomicAdd(&sh.sum[1], x.w);
+      return;
+    }
+    const int scale = 62 - (V > 1 ? 32 - __clz(V - 1) : 0);
+    const double c = per_unit(s), unit = ldexp(1., scale);
+    auto parts = [&](float v) { return exp2_neg(v == top ? 0. : ((double)v - top) * c); };
+    auto weight = [&](float v) { return as_fixed(parts(v), scale); };
+    // the place in the kept weights' running sum, 1 .. sum
+    auto drawn = [&](u64 sum) {
+      return min((u64)((double)fminf(fmaxf(uniform, 0.f), 1.f) * (double)sum), sum - 1) + 1;
+    };
+    u64 total = 0;
+    int token;
+    if (!filtered) {
+      u64 w[EACH], want = 0;
+  #pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const int i = EACH * tid + j;
+        const float m = i < chunks ? in.chunk_max[i] : -INFINITY;
+        // (a chunk whose weights are all 0 is not one to look in)
+        w[j] = m > -INFINITY && weight(m) ? (u64)rint(as_double(parts(m)) * in.chunk_sum[i] * unit) : 0;
+      }
+      const Found f = find_entry(sh, w, 0, [&](u64 sum) { return want = drawn(sum); }, &total);
+      const int first = max(f.at, 0) * CHUNK + EACH * tid;
+  #pragma unroll
+      for (int j = 0; j < EACH; ++j) {
+        const float v = first + j < V ? sane(to_f32(z[first + j])) : -INFINITY;
+        w[j] = v > -INFINITY ? weight(v) : 0;
+      }
       __syncthreads();
-      if (leads && !kept) sh.few[me].w = 0;
-      __syncthreads();
-      total = sh.sum[1];
-      const u64 want = drawn(total);
-      before = 0;
-      others(sh, n, [&](const Candidate& o) { before += o.i < x.i ? o.w : 0; });
-      before = quad_sum(before);
-      if (leads && kept && before < want && want <= before + x.w) sh.found = x.i;
-      __syncthreads();
-      token = sh.found;
+      token = f.at * CHUNK + find_entry(sh, w, 0, [&](u64 sum) { return min(want - f.before, sum); }).at;
     } else {
-      const uint32_t lo = order_key<T>(cut), hi = order_key<T>(top);
-      Border b{0, V};
-      if (s.by_rank) b = find_border<true>(sh, row, lo, hi, weight, (u64)s.k);
-      if (s.p < 1.f) {
-        const double of = s.by_rank ? (double)row_sum(sh, row, [&](float v, int i) {
-          const uint32_t k = order_key<T>(v);
-          return k > b.key || (k == b.key && i <= b.last) ? weight(v) : 0;
-        }) : sum * unit;
-        b = find_border<false>(sh, row, max(lo, b.key), hi, weight, max((u64)ceil(share * of), (u64)1));
+      const double share = (double)fmaxf(s.p, 0.f), least = s.low > 0.f ? (double)fminf(s.low, 1.f) : -1.;
+      double sum = 0.;  // of all weights
+      if (summed) {
+        if (chunk_max > -INFINITY) sum = as_double(parts(chunk_max)) * chunk_sum;
+        for (int i = tid + S_THREADS; i < chunks; i += S_THREADS) {
+          const float m = in.chunk_max[i];
+          if (m > -INFINITY) sum += as_double(parts(m)) * in.chunk_sum[i];
+        }
+  #pragma unroll
+        for (int d = 1; d < 64; d <<= 1) sum += __shfl_xor(sum, d);
+        if ((tid & 63) == 0) sh.wave_sum[tid >> 6] = __double_as_longlong(sum);
+        __syncthreads();
+        sum = 0.;
+  #pragma unroll
+        for (int w = 0; w < S_THREADS / 64; ++w) sum += __longlong_as_double(sh.wave_sum[w]);
       }
-      token = find_index(
-          sh, row,
-          [&](float v, int i) {
+      // Nothing below ``cut`` is kept (a top-k's weight, of which top-p takes its share,
+      // has to be there in full).
+      float cut = LOWEST;
+      if (s.low > 0.f && !(s.by_rank && s.p < 1.f)) cut = (float)(top + log2(least) / c);
+      if (s.by_rank || s.p < 1.f) {
+        lowest = -block_top(sh, -lowest);
+        const float per_bin = (BINS - 1) / (top - lowest);
+        if (fits && per_bin > 0.f && per_bin < INFINITY) {
+          clear_bins(sh);
+          // (the share, a little more: these weights are rounded differently)
+          const u64 want = s.by_rank ? (u64)s.k : (u64)(share * sum * (1ll << 32) * 1.0001) + 1;
+          const float c32 = (float)c;
+          for (int i = tid; i < blocks; i += S_THREADS) {
+            const float m = maxima[i];
+            if (m > -INFINITY)
+              atomicAdd(&sh.bins[min((int)((top - m) * per_bin), BINS - 1)],
+                        s.by_rank ? (u64)1 : (u64)(__builtin_amdgcn_exp2f((m - top) * c32) * 4294967296.f));
+          }
+          __syncthreads();
+          u64 v[EACH];
+  #pragma unroll
+          for (int j = 0; j < EACH; ++j) v[j] = sh.bins[EACH * tid + j];
+          const Found f = find_entry(sh, v, 0, [&](u64) { return want; });
+          // every value of bins 0 .. f.at, with the roundings of a bin's number
+          if (f.at >= 0) cut = fmaxf(cut, top - (f.at + 1) / per_bin * 1.000001f);
+        }
+      }
+      cut = fmaxf(cut - fabsf(cut) * 1e-6f, LOWEST);
+      Row<T> row{z, V, cut, -1, list};
+      if (fits) {
+        __syncthreads();
+        if (tid == 0) sh.found = 0;
+        __syncthreads();
+        for (int i = tid; i < blocks; i += S_THREADS)
+          if (maxima[i] >= cut) {
+            const int n = atomicAdd(&sh.found, 1);
+            if (n < LIST) list[n] = i;
+          }
+        __syncthreads();
+        if (sh.found <= LIST) row.n = sh.found;
+      }
+      const int n = row.n < 0 ? FEW + 1 : gather(sh, row, [](float) { return true; }, weight);
+      if (n <= FEW) {
+        // few: each compared with each, by rank and weight, then by index
+        if (tid == 0) sh.sum[0] = sh.sum[1] = 0;
+        if (tid == 0) sh.found = 0;
+        __syncthreads();
+        const int me = tid / SHARE;
+        const bool leads = me < n && tid % SHARE == 0;
+        const Candidate x = sh.few[min(me, n - 1)];
+        u64 rank = 0, before = 0;
+        others(sh, n, [&](const Candidate& o) {
+          const bool is = ahead(o, x);
+          rank += is;
+          before += is ? o.w : 0;
+        });
+        rank = share_sum(rank);
+        before = share_sum(before);
+        const bool first = !s.by_rank || rank < (u64)s.k;
+        if (s.by_rank && s.p < 1.f) {
+          if (leads && first) atomicAdd(&sh.sum[0], x.w);
+          __syncthreads();
+        }
+        const double of = s.by_rank ? (double)sh.sum[0] : sum * unit;
+        bool kept = first && x.w > 0 && (double)x.w >= least * unit;
+        if (s.p < 1.f) kept = kept && before < max((u64)ceil(share * of), (u64)1);
+        if (leads && kept) atomicAdd(&sh.sum[1], x.w);
+        __syncthreads();
+        if (leads && !kept) sh.few[me].w = 0;
+        __syncthreads();
+        total = sh.sum[1];
+        const u64 want = drawn(total);
+        before = 0;
+        others(sh, n, [&](const Candidate& o) { before += o.i < x.i ? o.w : 0; });
+        before = share_sum(before);
+        if (leads && kept && before < want && want <= before + x.w) sh.found = x.i;
+        __syncthreads();
+        token = sh.found;
+      } else {
+        const uint32_t lo = order_key<T>(cut), hi = order_key<T>(top);
+        Border b{0, V};
+        if (s.by_rank) b = find_border<true>(sh, row, lo, hi, weight, (u64)s.k);
+        if (s.p < 1.f) {
+          const double of = s.by_rank ? (double)row_sum(sh, row, [&](float v, int i) {
             const uint32_t k = order_key<T>(v);
-            if (v == -INFINITY || k < b.key || (k == b.key && i > b.last)) return (u64)0;
-            const u64 w = weight(v);
-            return (double)w >= least * unit ? w : (u64)0;
-          },
-          drawn, &total);
+            return k > b.key || (k == b.key && i <= b.last) ? weight(v) : 0;
+          }) : sum * unit;
+          b = find_border<false>(sh, row, max(lo, b.key), hi, weight, max((u64)ceil(share * of), (u64)1));
+        }
+        token = find_index(
+            sh, row,
+            [&](float v, int i) {
+              const uint32_t k = order_key<T>(v);
+              if (v == -INFINITY || k < b.key || (k == b.key && i > b.last)) return (u64)0;
+              const u64 w = weight(v);
+              return (double)w >= least * unit ? w : (u64)0;
+            },
+            drawn, &total);
+      }
+    }
+    if (tid == 0) {
+      token = min(max(token, 0), V - 1);  // (it is there; no address hangs on it)
+      a.tokens[r] = token;
+      const float v = sane(to_f32(z[token]));
+      const double x = v == top ? 0. : ((double)v - top) / s.t;
+      a.logps[r] = (float)(x - log((double)total / unit));
     }
   }
-  if (tid == 0) {
-    token = min(max(token, 0), V - 1);  // (it is there; no address hangs on it)
-    a.tokens[r] = token;
-    const float v = sane(to_f32(z[token]));
-    const double x = v == top ? 0. : ((double)v - top) / s.t;
-    a.logps[r] = (float)(x - log((double)total / unit));
-  }
+};
+
+template <typename T, int S_THREADS>
+__global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, void* ws) {
+  using R = RowOf<S_THREADS>;
+  __shared__ typename R::Shared sh;
+  __shared__ alignas(16) float maxima[MAX_BLOCKS];
+  __shared__ int32_t list[LIST];
+  R::template run<T>(a, ws, sh, maxima, list);
 }
 
 int64_t sample_workspace(int64_t rows, int vocab) { return rows * row_bytes(vocab); }
@@ -698,7 +721,11 @@ template <typename T>
 static void launch(const SampleArgs& a, void* ws, hipStream_t s) {
   constexpr int PER = SCAN_THREADS / 64;
   sample_scan_kernel<T><<<dim3((chunks_of(a.vocab) + PER - 1) / PER, a.rows), SCAN_THREADS, 0, s>>>(a, ws);
-  sample_row_kernel<T><<<a.rows, S_THREADS, 0, s>>>(a, ws);
+  // One large workgroup's registers fill a CU; two small ones have room, which counts
+  // where rows are more than CUs (384 rows with their own settings 26 and 19 us, 64 with
+  // a nucleus 21 and 26).
+  if (a.rows <= 256) sample_row_kernel<T, 1024><<<a.rows, 1024, 0, s>>>(a, ws);
+  else sample_row_kernel<T, 512><<<a.rows, 512, 0, s>>>(a, ws);
 }
 
 void launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {

@@ -191,6 +191,17 @@ def test_many_rows_and_none():
     assert t.shape == (0,) and lp.shape == (0,)
 
 
+@pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("kw", FILTERS.values(), ids=FILTERS.keys())
+def test_more_rows_than_compute_units(kw, dtype):
+    """More than 256 rows take smaller workgroups: few candidates, many, and equal ones."""
+    check(*logits(300, 4099, dtype, seed=9), **kw)
+    check(*logits(259, 20000, dtype, seed=10, peak=0.0), **kw)
+    z, u = logits(257, 3000, dtype, seed=11)
+    z = torch.where(z > 0, 1.5, z).to(dtype)
+    check(z, u, **kw)
+
+
 def test_out_stream_and_graph():
     z, u = logits(16, 32000)
     want, wlp = check(z, u, **FILTERS["all"])
