@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(SCAN_THREADS) sample_scan_kernel(SampleArgs a,
 
 constexpr int LIST = 2048;        // blocks that are listed; more: all of the row
 constexpr int MAX_BLOCKS = 8192;  // maxima that fit into LDS (262144 logits)
+constexpr int KEPT = MAX_BLOCKS * 4 / sizeof(Candidate);  // candidates that fit into their place
 
 // What a workgroup of S_THREADS does for its row
 template <int S_THREADS>
@@ -288,10 +289,16 @@ struct RowOf {
     float cut;
     int n;
     const int32_t* list;
+    const Candidate* kept;  // the values not below ``cut``, if they are here already (n_kept >= 0)
+    int n_kept;
     AXON_DEV int items() const { return n < 0 ? (V + N - 1) / N : n * LANES; }
     AXON_DEV int first(int e) const { return n < 0 ? e * N : list[e / LANES] * BLOCK + e % LANES * N; }
     template <typename F>
     AXON_DEV void each(F&& f) const {
+      if (n_kept >= 0) {
+        for (int e = threadIdx.x; e < n_kept; e += S_THREADS) f(kept[e].z, kept[e].i);
+        return;
+      }
       float v[N], next[N];
       const int end = items();
       if ((int)threadIdx.x < end) load_run(z, first(threadIdx.x), V, v);
@@ -308,34 +315,34 @@ struct RowOf {
     }
   };
 
-  // up to FEW values of the row that ``take`` takes, in sh.few in any order; their number
-  // (more than FEW: not all of them are there)
+  // up to ``most`` values of the row that ``take`` takes, in ``to`` in any order; their number
+  // (more than ``most``: not all of them are there)
   template <typename R, typename P, typename W>
-  static AXON_DEV int gather(Shared& sh, const R& row, P&& take, W&& weight) {
+  static AXON_DEV int gather(Shared& sh, Candidate* to, int most, const R& row, P&& take, W&& weight) {
     __syncthreads();
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
     row.each([&](float z, int i) {
       if (!take(z)) return;
       const int n = atomicAdd(&sh.count, 1);
-      if (n < FEW) sh.few[n] = Candidate{z, i, weight(z)};
+      if (n < most) to[n] = Candidate{z, i, weight(z)};
     });
     __syncthreads();
     const int n = sh.count;
     // (whole rounds of others())
-    if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < FEW) sh.few[n + threadIdx.x] = Candidate{-INFINITY, 0x7fffffff, 0};
+    if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < most) to[n + threadIdx.x] = Candidate{-INFINITY, 0x7fffffff, 0};
     __syncthreads();
     return n;
   }
   // SHARE threads to a candidate (thread / SHARE): f(candidate) over a part each, eight at a
   // time so that their reads are in flight together
   template <typename F>
-  static AXON_DEV void others(const Shared& sh, int n, F&& f) {
+  static AXON_DEV void others(const Candidate* all, int n, F&& f) {
     static_assert(FEW % 32 == 0 && 32 % (8 * SHARE) == 0, "rounds end inside few");
     for (int j = threadIdx.x % SHARE; j < n; j += 8 * SHARE) {
       Candidate c[8];
   #pragma unroll
-      for (int k = 0; k < 8; ++k) c[k] = sh.few[j + SHARE * k];
+      for (int k = 0; k < 8; ++k) c[k] = all[j + SHARE * k];
   #pragma unroll
       for (int k = 0; k < 8; ++k) f(c[k]);
     }
@@ -403,14 +410,14 @@ struct RowOf {
         }
         return Border{lo, last};
       }
-      const int n = gather(sh, row, [&](float z) { const uint32_t k = order_key<T>(z); return lo <= k && k <= hi; },
+      const int n = gather(sh, sh.few, FEW, row, [&](float z) { const uint32_t k = order_key<T>(z); return lo <= k && k <= hi; },
                            [&](float z) { return COUNT ? (u64)1 : weight(z); });
       if (n <= FEW) {  // few enough to compare
         const int i = threadIdx.x / SHARE;
         if (i < n) {
           const Candidate me = sh.few[i];
           u64 before = 0;
-          others(sh, n, [&](const Candidate& c) { before += ahead(c, me) ? c.w : 0; });
+          others(sh.few, n, [&](const Candidate& c) { before += ahead(c, me) ? c.w : 0; });
           before = above + share_sum(before);
           if (threadIdx.x % SHARE == 0 && before < want && want <= before + me.w) sh.found = i;
         }
@@ -624,7 +631,7 @@ struct RowOf {
         }
       }
       cut = fmaxf(cut - fabsf(cut) * 1e-6f, LOWEST);
-      Row<T> row{z, V, cut, -1, list};
+      Row<T> row{z, V, cut, -1, list, nullptr, -1};
       if (fits) {
         __syncthreads();
         if (tid == 0) sh.found = 0;
@@ -637,7 +644,9 @@ struct RowOf {
         __syncthreads();
         if (sh.found <= LIST) row.n = sh.found;
       }
-      const int n = row.n < 0 ? FEW + 1 : gather(sh, row, [](float) { return true; }, weight);
+      // (the maxima are not needed any more)
+      Candidate* kept = (Candidate*)maxima;
+      const int n = row.n < 0 ? KEPT + 1 : gather(sh, kept, KEPT, row, [](float) { return true; }, weight);
       if (n <= FEW) {
         // few: each compared with each, by rank and weight, then by index
         if (tid == 0) sh.sum[0] = sh.sum[1] = 0;
@@ -645,9 +654,9 @@ struct RowOf {
         __syncthreads();
         const int me = tid / SHARE;
         const bool leads = me < n && tid % SHARE == 0;
-        const Candidate x = sh.few[min(me, n - 1)];
+        const Candidate x = kept[min(me, n - 1)];
         u64 rank = 0, before = 0;
-        others(sh, n, [&](const Candidate& o) {
+        others(kept, n, [&](const Candidate& o) {
           const bool is = ahead(o, x);
           rank += is;
           before += is ? o.w : 0;
@@ -660,21 +669,25 @@ struct RowOf {
           __syncthreads();
         }
         const double of = s.by_rank ? (double)sh.sum[0] : sum * unit;
-        bool kept = first && x.w > 0 && (double)x.w >= least * unit;
-        if (s.p < 1.f) kept = kept && before < max((u64)ceil(share * of), (u64)1);
-        if (leads && kept) atomicAdd(&sh.sum[1], x.w);
+        bool stays = first && x.w > 0 && (double)x.w >= least * unit;
+        if (s.p < 1.f) stays = stays && before < max((u64)ceil(share * of), (u64)1);
+        if (leads && stays) atomicAdd(&sh.sum[1], x.w);
         __syncthreads();
-        if (leads && !kept) sh.few[me].w = 0;
+        if (leads && !stays) kept[me].w = 0;
         __syncthreads();
         total = sh.sum[1];
         const u64 want = drawn(total);
         before = 0;
-        others(sh, n, [&](const Candidate& o) { before += o.i < x.i ? o.w : 0; });
+        others(kept, n, [&](const Candidate& o) { before += o.i < x.i ? o.w : 0; });
         before = share_sum(before);
-        if (leads && kept && before < want && want <= before + x.w) sh.found = x.i;
+        if (leads && stays && before < want && want <= before + x.w) sh.found = x.i;
         __syncthreads();
         token = sh.found;
       } else {
+        if (n <= KEPT) {
+          row.kept = kept;
+          row.n_kept = n;
+        }
         const uint32_t lo = order_key<T>(cut), hi = order_key<T>(top);
         Border b{0, V};
         if (s.by_rank) b = find_border<true>(sh, row, lo, hi, weight, (u64)s.k);
