@@ -21,12 +21,12 @@
 // of itself), which its few passes find in the L2; without a filter the sums lead it to
 // the token's chunk.
 //
-// Measured: 384 rows of 128256 float32, each with its own settings, 63 us (scan 44, 4.5
-// TB/s; the rest 20); 64 of 152064 with a nucleus 38 (scan 16: the float64 weights, some
-// 100 cycles each to a wavefront, stand beside 8 of reading; the rest 22: a chain of some
-// ten exchanges through LDS, 12 for most rows, 22 for one whose candidates are more than
-// can be compared); 8 of 32000 with top-k and top-p 17 (4 + 13, latency).  A scan of fewer
-// wavefronts that load a chunk ahead is slower: 20 and 56 us with 4096.
+// Measured: 384 rows of 128256 float32, each with its own settings, 62 us (scan 44, 4.5
+// TB/s; the rest 17); 64 of 152064 with a nucleus 35 (scan 16: the float64 weights, some
+// 100 cycles each to a wavefront, stand beside 8 of reading; the rest 19: a chain of some
+// ten exchanges through LDS, 11 for most rows, 19 where 200 candidates are compared); 8 of
+// 32000 with top-k and top-p 17 (4 + 12, latency).  A scan of fewer wavefronts that load a
+// chunk ahead is slower: 20 and 56 us with 4096.
 #include "common.h"
 #include "kernels.h"
 
@@ -83,12 +83,14 @@ AXON_DEV float key_value(uint32_t k) {
   return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu));
 }
 
-// A value that a filter can keep
+// A value that a filter can keep.  Descending order is that of ``key``, one comparison: the
+// value's bits in ascending order above those of -1 - index.
 struct Candidate {
-  float z;
-  int i;
-  u64 w;
+  u64 key, w;
+  AXON_DEV float z() const { return key_value<float>((uint32_t)(key >> 32)); }
+  AXON_DEV int i() const { return (int)~(uint32_t)key; }
 };
+AXON_DEV Candidate candidate(float z, int i, u64 w) { return Candidate{(u64)order_key<float>(z) << 32 | ~(uint32_t)i, w}; }
 constexpr int FEW = 256;  // candidates that are compared each with each
 
 AXON_DEV u64 wave_total(u64 v) {
@@ -296,7 +298,7 @@ struct RowOf {
     template <typename F>
     AXON_DEV void each(F&& f) const {
       if (n_kept >= 0) {
-        for (int e = threadIdx.x; e < n_kept; e += S_THREADS) f(kept[e].z, kept[e].i);
+        for (int e = threadIdx.x; e < n_kept; e += S_THREADS) f(kept[e].z(), kept[e].i());
         return;
       }
       float v[N], next[N];
@@ -325,12 +327,12 @@ struct RowOf {
     row.each([&](float z, int i) {
       if (!take(z)) return;
       const int n = atomicAdd(&sh.count, 1);
-      if (n < most) to[n] = Candidate{z, i, weight(z)};
+      if (n < most) to[n] = candidate(z, i, weight(z));
     });
     __syncthreads();
     const int n = sh.count;
     // (whole rounds of others())
-    if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < most) to[n + threadIdx.x] = Candidate{-INFINITY, 0x7fffffff, 0};
+    if ((int)threadIdx.x < 32 && n + (int)threadIdx.x < most) to[n + threadIdx.x] = Candidate{0, 0};
     __syncthreads();
     return n;
   }
@@ -347,13 +349,12 @@ struct RowOf {
       for (int k = 0; k < 8; ++k) f(c[k]);
     }
   }
-  static AXON_DEV u64 share_sum(u64 v) {
+  template <typename V>
+  static AXON_DEV V share_sum(V v) {
   #pragma unroll
     for (int d = 1; d < SHARE; d <<= 1) v += __shfl_xor(v, d);
     return v;
   }
-  // whether a comes before b in descending order
-  static AXON_DEV bool ahead(const Candidate& a, const Candidate& b) { return a.z > b.z || (a.z == b.z && a.i < b.i); }
 
   // The border in descending order: values above key are kept, of those on it the indices
   // up to last.  COUNT: ``want`` values are kept, else as many as it takes for their weights
@@ -417,13 +418,13 @@ struct RowOf {
         if (i < n) {
           const Candidate me = sh.few[i];
           u64 before = 0;
-          others(sh.few, n, [&](const Candidate& c) { before += ahead(c, me) ? c.w : 0; });
+          others(sh.few, n, [&](const Candidate& c) { before += c.key > me.key ? c.w : 0; });
           before = above + share_sum(before);
           if (threadIdx.x % SHARE == 0 && before < want && want <= before + me.w) sh.found = i;
         }
         __syncthreads();
         const Candidate me = sh.few[min(sh.found, n - 1)];
-        return Border{order_key<T>(me.z), me.i};
+        return Border{order_key<T>(me.z()), me.i()};
       }
     }
   }
@@ -655,15 +656,16 @@ struct RowOf {
         const int me = tid / SHARE;
         const bool leads = me < n && tid % SHARE == 0;
         const Candidate x = kept[min(me, n - 1)];
-        u64 rank = 0, before = 0;
+        u64 before = 0;
+        uint32_t rank = 0;
         others(kept, n, [&](const Candidate& o) {
-          const bool is = ahead(o, x);
+          const bool is = o.key > x.key;
           rank += is;
           before += is ? o.w : 0;
         });
         rank = share_sum(rank);
         before = share_sum(before);
-        const bool first = !s.by_rank || rank < (u64)s.k;
+        const bool first = !s.by_rank || rank < (uint32_t)s.k;
         if (s.by_rank && s.p < 1.f) {
           if (leads && first) atomicAdd(&sh.sum[0], x.w);
           __syncthreads();
@@ -678,9 +680,9 @@ struct RowOf {
         total = sh.sum[1];
         const u64 want = drawn(total);
         before = 0;
-        others(kept, n, [&](const Candidate& o) { before += o.i < x.i ? o.w : 0; });
+        others(kept, n, [&](const Candidate& o) { before += (uint32_t)o.key > (uint32_t)x.key ? o.w : 0; });
         before = share_sum(before);
-        if (leads && stays && before < want && want <= before + x.w) sh.found = x.i;
+        if (leads && stays && before < want && want <= before + x.w) sh.found = x.i();
         __syncthreads();
         token = sh.found;
       } else {
@@ -720,7 +722,7 @@ struct RowOf {
 };
 
 template <typename T, int S_THREADS>
-__global__ void __launch_bounds__(S_THREADS) sample_row_kernel(SampleArgs a, void* ws) {
+__global__ void __launch_bounds__(S_THREADS, 4) sample_row_kernel(SampleArgs a, void* ws) {
   using R = RowOf<S_THREADS>;
   __shared__ typename R::Shared sh;
   __shared__ alignas(16) float maxima[MAX_BLOCKS];
@@ -735,8 +737,8 @@ static void launch(const SampleArgs& a, void* ws, hipStream_t s) {
   constexpr int PER = SCAN_THREADS / 64;
   sample_scan_kernel<T><<<dim3((chunks_of(a.vocab) + PER - 1) / PER, a.rows), SCAN_THREADS, 0, s>>>(a, ws);
   // One large workgroup's registers fill a CU; two small ones have room, which counts
-  // where rows are more than CUs (384 rows with their own settings 26 and 19 us, 64 with
-  // a nucleus 21 and 26).
+  // where rows are more than CUs (384 rows with their own settings 26 and 20 us, 64 with
+  // a nucleus 21 and 26, measured before candidates had one key to compare).
   if (a.rows <= 256) sample_row_kernel<T, 1024><<<a.rows, 1024, 0, s>>>(a, ws);
   else sample_row_kernel<T, 512><<<a.rows, 512, 0, s>>>(a, ws);
 }
