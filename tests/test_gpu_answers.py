@@ -140,6 +140,27 @@ def test_two_captured_decode_loops_in_turn():
             d.u.copy_(d.uniform[min(i + 2, STEPS)])
 
 
+def test_two_loops_on_two_streams_at_once():
+    loops = [Decoder(B, 11), Decoder(B, 12)]
+    want = [d.answers(d.step) for d in loops]
+    streams = [torch.cuda.Stream() for _ in loops]
+    got = [[], []]
+    for d in loops:
+        d.start()
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i in range(STEPS):
+        for j, d in enumerate(loops):
+            with torch.cuda.stream(streams[j]):
+                _, out, lp = d.step()
+                got[j].append((d.tokens.clone(), lp, out))
+                d.u.copy_(d.uniform[min(i + 2, STEPS)])
+    torch.cuda.synchronize()
+    for j in range(2):
+        for i in range(STEPS):
+            assert all(torch.equal(a, b) for a, b in zip(got[j][i], want[j][i])), (i, j)
+
+
 def test_sampling_from_a_model_and_its_policy_loss():
     """Tokens drawn from a model's logits, prompt and decode steps; the log-probabilities
     that were drawn from are the old ones of the policy loss over the same answers."""
