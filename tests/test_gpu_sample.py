@@ -202,6 +202,16 @@ def test_more_rows_than_compute_units(kw, dtype):
     check(z, u, **kw)
 
 
+@pytest.mark.parametrize("V", [5000, 300001, 1 << 22])
+def test_a_row_alone_and_among_many(V):
+    """Larger and smaller workgroups give a row the same bits."""
+    z = logits(3, V, B, seed=12)[0].repeat(100, 1)
+    u = torch.rand((300,), generator=torch.Generator().manual_seed(13)).cuda()
+    for kw in FILTERS.values():
+        many, few = ops.sample_tokens(z, u, **kw), ops.sample_tokens(z[150:190], u[150:190], **kw)
+        assert all(torch.equal(m[150:190], f) for m, f in zip(many, few)), kw
+
+
 def test_out_stream_and_graph():
     z, u = logits(16, 32000)
     want, wlp = check(z, u, **FILTERS["all"])
