@@ -29,11 +29,11 @@
 // chunk ahead is slower: 20 and 56 us with 4096.
 #include "common.h"
 #include "kernels.h"
+#include "search_range.h"
 
 namespace axon {
 
 typedef unsigned long long u64;
-constexpr int BINS = 2048;
 
 // 2^x for x <= 0 as v 2^n, v in [0.7, 1.42]: 2^f on [-1/2, 1/2] as the polynomial of
 // degree 10 through 2^f at Chebyshev's nodes, 4e-16 of itself off and exactly 1 at 0.
@@ -322,7 +322,10 @@ struct RowOf {
   template <typename R, typename P, typename W>
   static AXON_DEV int gather(Shared& sh, Candidate* to, int most, const R& row, P&& take, W&& weight) {
     __syncthreads();
-    if (threadIdx.x == 0) sh.count = 0;
+    if (threadIdx.x == 0) {
+      sh.count = 0;
+      sh.found = -1;
+    }
     __syncthreads();
     row.each([&](float z, int i) {
       if (!take(z)) return;
@@ -358,7 +361,8 @@ struct RowOf {
 
   // The border in descending order: values above key are kept, of those on it the indices
   // up to last.  COUNT: ``want`` values are kept, else as many as it takes for their weights
-  // to reach ``want``; all there are if that is not reached.
+  // to reach ``want``; all there are if that is not reached.  A search that finds nothing
+  // (none does) ends it with all of the range.
   struct Border {
     uint32_t key;
     int last;
@@ -366,9 +370,11 @@ struct RowOf {
   template <bool COUNT, typename T, typename W>
   static AXON_DEV Border find_border(Shared& sh, const Row<T>& row, uint32_t lo, uint32_t hi, W&& weight, u64 want) {
     u64 above = 0;  // (number or weight) of what is above hi
+    KeyRange range{lo, hi};
     for (;;) {
-      int shift = 0;
-      while ((hi - lo) >> shift >= BINS) ++shift;
+      lo = range.lo;
+      hi = range.hi;
+      const int shift = range.shift();
       clear_bins(sh);
       row.each([&](float z, int) {
         const uint32_t k = order_key<T>(z);
@@ -381,9 +387,9 @@ struct RowOf {
   #pragma unroll
       for (int j = 0; j < EACH; ++j) v[j] = sh.bins[BINS - 1 - EACH * threadIdx.x - j];
       const Found f = find_entry(sh, v, above, [&](u64 total) { return want = min(want, total); });
-      const uint32_t bin = BINS - 1 - f.at;
-      lo += bin << shift;
-      hi = min(hi, lo + ((1u << shift) - 1));
+      if (!range.narrow(f.at)) return Border{lo, row.V};
+      lo = range.lo;
+      hi = range.hi;
       above = f.before;
       if (lo == hi) {
         // all have one value: as many of them as are wanted, the lowest indices
@@ -423,7 +429,8 @@ struct RowOf {
           if (threadIdx.x % SHARE == 0 && before < want && want <= before + me.w) sh.found = i;
         }
         __syncthreads();
-        const Candidate me = sh.few[min(sh.found, n - 1)];
+        if (sh.found < 0) return Border{lo, row.V};
+        const Candidate me = sh.few[sh.found];
         return Border{order_key<T>(me.z()), me.i()};
       }
     }
