@@ -3,7 +3,6 @@
 // Argument checks only; the kernels are in k_append.hip, k_prefix.hip and k_sample.hip.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <cmath>
 
 #include "kernels.h"
@@ -82,19 +81,25 @@ PagedSeqs seqs_of(const axon_kv_batch& b) {
   return PagedSeqs{b.seqs, b.d_cu_seqlens, b.d_lens, b.d_block_table, b.table_stride};
 }
 
-int check_attention(const axon_kv_pages* pages, const axon_kv_batch* batch, const axon_kv_prefix* prefix,
-                    int64_t tokens, int32_t heads) {
-  if (int r = check_pages(pages)) return r;
-  if (int r = check_batch(batch, tokens, pages->page_size)) return r;
-  if (int r = check_prefix(prefix, batch->seqs, pages->page_size)) return r;
-  return check_heads(heads, pages->kv_heads);
-}
-
 PrefixAttnShape shape_of(const axon_kv_pages& pages, const axon_kv_batch& batch, const axon_kv_prefix* prefix,
                          int64_t tokens, int32_t heads) {
   const int groups = prefix ? prefix->groups : 0;
   return PrefixAttnShape{tokens, batch.seqs, groups, heads, pages.kv_heads, pages.head_dim, batch.h_cu_seqlens,
                          groups ? prefix->h_cu_groups : nullptr};
+}
+
+int check_attention(const axon_kv_pages* pages, const axon_kv_batch* batch, const axon_kv_prefix* prefix,
+                    int64_t tokens, int32_t heads) {
+  if (int r = check_pages(pages)) return r;
+  if (int r = check_batch(batch, tokens, pages->page_size)) return r;
+  if (int r = check_prefix(prefix, batch->seqs, pages->page_size)) return r;
+  if (int r = check_heads(heads, pages->kv_heads)) return r;
+  const PrefixAttnShape shape = shape_of(*pages, *batch, prefix, tokens, heads);
+  const int64_t ps = pages->page_size, own = batch->table_stride, shared = shape.groups ? prefix->table_stride : 0;
+  if (!prefix_attn_fits(shape, own * ps, shared * ps))
+    return fail(AXON_E_CAPACITY, num(tokens) + " tokens of " + num(heads) + " heads over tables of " + num(own) + " and " +
+                                     num(shared) + " pages are too many for one call");
+  return AXON_OK;
 }
 
 }  // namespace
@@ -161,12 +166,7 @@ extern "C" int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_b
     if (d_lse)
       if (int r = check_array("d_lse", d_lse, 4)) return r;
     const PrefixAttnShape shape = shape_of(*pages, *batch, prefix, tokens, heads);
-    const int64_t longest = std::max(batch->table_stride, shape.groups ? prefix->table_stride : 0);
-    const int64_t need = prefix_attn_workspace(shape);
-    if (prefix_attn_steps(shape, longest * pages->page_size) >= (int64_t)1 << 31 || need >= (int64_t)1 << 40)
-      return fail(AXON_E_CAPACITY, num(tokens) + " tokens of " + num(heads) + " heads over tables of " + num(longest) +
-                                       " pages are too many for one call");
-    if (int r = check_workspace(workspace, workspace_bytes, need)) return r;
+    if (int r = check_workspace(workspace, workspace_bytes, prefix_attn_workspace(shape))) return r;
     const SharedPrefix shared = prefix ? SharedPrefix{prefix->groups, prefix->d_cu_groups, prefix->d_prefix_lens,
                                                       prefix->d_prefix_table, prefix->table_stride}
                                        : SharedPrefix{};

@@ -38,6 +38,7 @@ namespace axon {
 constexpr float LOG2E_F = 1.4426950408889634f;
 constexpr int PA_WGS = 256, PA_THREADS = 512, PA_WAVES = 8;
 constexpr int WIDE_KEYS = 64, WIDE_ROWS = 256, NARROW_KEYS = 16, NARROW_ROWS = 16;
+constexpr int WIDE_START = 6, NARROW_START = 4;  // steps of a tile's beginning
 constexpr int SLOT_BLOCKS = WIDE_ROWS / 16;  // 16-row blocks of a wide part
 
 // ---------------------------------------------------------------- plan
@@ -91,18 +92,18 @@ AXON_DEV int row_keys(const Segment& g, int G, int r) {
   return (int)min(g.own ? g.len + r / G + 1 : g.len, (int64_t)g.room);
 }
 
-// The tiles of one kind, their units, and their steps: STEP for each unit, and START more
+// The tiles of one kind, their units, and their steps: one for each unit, and START more
 // at its beginning that stand for what a tile costs by itself (looking up pages, loading
-// queries, filling the pipeline).  Workers share the steps.  A narrow unit is one step; a
-// wide one takes a workgroup as long as 9 (128 dimensions) or 14 (64) narrow ones take its
-// 8 wavefronts.  Measured, with START six units (us, attention of 64 answers to 4096 tokens,
-// 256 to 16 prompts of 64 dimensions, 48 to 50011): STEP 4 and START 12 44, 115, 135;
-// 8 and 48 36, 77, 114; 12 and 72 35, 68, 123.
+// queries, filling the pipeline).  Workers share the steps of a kind, workgroups are shared
+// out over the kinds by WEIGHT: a wide unit takes a workgroup as long as 9 (128 dimensions)
+// or 14 (64) narrow ones take its 8 wavefronts.  Measured (us, attention of 64 answers to
+// 4096 tokens, 256 to 16 prompts of 64 dimensions, 48 to 50011): WEIGHT 4 and START 3 44,
+// 115, 135; 8 and 6 36, 77, 114; 12 and 6 35, 68, 123.
 template <bool WIDE, int HD>
 struct Tiles {
   static constexpr int ROWS = WIDE ? WIDE_ROWS : NARROW_ROWS, KEYS = WIDE ? WIDE_KEYS : NARROW_KEYS;
-  static constexpr int STEP = !WIDE ? 1 : HD == 128 ? 9 : 14, START = WIDE ? 6 * STEP : 4;
-  static constexpr int LEAST = WIDE ? 4 * STEP : 2;  // steps that are worth a worker
+  static constexpr int WEIGHT = !WIDE ? 1 : HD == 128 ? 9 : 14, START = WIDE ? WIDE_START : NARROW_START;
+  static constexpr int LEAST = WIDE ? 4 : 2;  // steps that are worth a worker
   static AXON_DEV int of(const Segment& g, int G) {  // of a kv head
     const int rows = g.tokens * G;
     return rows > NARROW_ROWS ? (WIDE ? (rows + ROWS - 1) / ROWS : 0) : (WIDE || rows <= 0 ? 0 : 1);
@@ -112,7 +113,7 @@ struct Tiles {
   }
   static AXON_DEV int steps(const Segment& g, int G, int rt) {
     const int u = units(g, G, rt);
-    return u ? STEP * u + START : 0;
+    return u ? u + START : 0;
   }
   // (steps, tiles) of a kv head
   static AXON_DEV int2 sizes(const Segment& g, int G) {
@@ -291,14 +292,13 @@ template <bool WIDE, int HD>
 AXON_DEV Work work_of(const Segment& g, const Place& p, int G, int at, int end, const Shares& shares, int me) {
   using X = Tiles<WIDE, HD>;
   const int steps = X::steps(g, G, p.rt);
-  // a unit belongs to who has its first step
-  auto unit_at = [](int step) { return max(step - X::START + X::STEP - 1, 0) / X::STEP; };
+  auto unit_at = [](int step) { return max(step - X::START, 0); };
   Work w;
   w.take = min(steps - p.step, end - at);
   w.first = unit_at(p.step);
   w.last = unit_at(p.step + w.take);
   w.leads = w.first == 0 && w.last > 0;
-  w.parts = w.leads ? shares.of(at - p.step + steps - X::STEP) - me + 1 : 0;
+  w.parts = w.leads ? shares.of(at - p.step + steps - 1) - me + 1 : 0;
   return w;
 }
 
@@ -1016,11 +1016,12 @@ __global__ void __launch_bounds__(PA_THREADS, 2) prefix_attn_kernel(PrefixAttnAr
   Plan<T, HD> plan(a, plan_sh);
   const int G = plan.G, KV = plan.KV, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t all_rows = (int64_t)a.tokens * G;
-  // The workgroups of an XCD (blockIdx % 8) are shared out over the kinds as the steps
-  // are; consecutive runs go to one XCD, whose L2 holds what they share.
+  // The workgroups of an XCD (blockIdx % 8) are shared out over the kinds as the steps and
+  // their weight are; consecutive runs go to one XCD, whose L2 holds what they share.
   constexpr int PER = PA_WGS / 8;
   const int total_n = __builtin_amdgcn_readfirstlane(plan.total[0]), total_w = __builtin_amdgcn_readfirstlane(plan.total[1]);
-  const int wide_wgs = !total_w ? 0 : !total_n ? PER : min(max((int)((float)PER * total_w / ((float)total_w + total_n) + 0.5f), 1), PER - 1);
+  const float cost_w = (float)Tiles<true, HD>::WEIGHT * total_w;
+  const int wide_wgs = !total_w ? 0 : !total_n ? PER : min(max((int)(PER * cost_w / (cost_w + total_n) + 0.5f), 1), PER - 1);
   const int xcd = blockIdx.x % 8, nth = blockIdx.x / 8;
   if (nth < wide_wgs) {
     const Shares shares(min(8 * wide_wgs, max(total_w / Tiles<true, HD>::LEAST, 1)), total_w);
@@ -1213,7 +1214,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == JOIN_MAX ? 4 : 8)
 
 namespace {
 
+struct Tally {  // tiles of a kind: of own keys, of prefixes
+  int64_t own = 0, shared = 0;
+  int64_t all() const { return own + shared; }
+};
 struct Sizes {
+  Tally wide_tiles, narrow_tiles;
   int64_t wide, narrow;  // slots of each kind (0: no such tile)
   int64_t parts_at, bytes;
   int64_t blocks() const { return wide * SLOT_BLOCKS + narrow; }
@@ -1221,17 +1227,16 @@ struct Sizes {
 Sizes sizes_of(const PrefixAttnShape& x) {
   const int64_t G = x.heads / x.kv_heads;
   auto token = [&](int b) -> int64_t { return x.h_cu ? x.h_cu[b] : b; };
-  int64_t wide = 0, narrow = 0;
-  auto add = [&](int64_t tokens) {
-    const int64_t rows = tokens * G;
-    if (rows > NARROW_ROWS) wide += (rows + WIDE_ROWS - 1) / WIDE_ROWS;
-    else if (rows > 0) ++narrow;
-  };
-  for (int g = 0; g < x.groups; ++g) add(token(x.h_groups[g + 1]) - token(x.h_groups[g]));
-  for (int b = 0; b < x.seqs; ++b) add(x.h_cu ? x.h_cu[b + 1] - x.h_cu[b] : 1);
   Sizes s;
-  s.wide = wide ? wide * x.kv_heads + PA_WGS : 0;
-  s.narrow = narrow ? narrow * x.kv_heads + PA_WGS * PA_WAVES : 0;
+  auto add = [&](int64_t Tally::*of, int64_t tokens) {
+    const int64_t rows = tokens * G;
+    if (rows > NARROW_ROWS) s.wide_tiles.*of += (rows + WIDE_ROWS - 1) / WIDE_ROWS * x.kv_heads;
+    else if (rows > 0) s.narrow_tiles.*of += x.kv_heads;
+  };
+  for (int g = 0; g < x.groups; ++g) add(&Tally::shared, token(x.h_groups[g + 1]) - token(x.h_groups[g]));
+  for (int b = 0; b < x.seqs; ++b) add(&Tally::own, x.h_cu ? x.h_cu[b + 1] - x.h_cu[b] : 1);
+  s.wide = s.wide_tiles.all() ? s.wide_tiles.all() + PA_WGS : 0;
+  s.narrow = s.narrow_tiles.all() ? s.narrow_tiles.all() + PA_WGS * PA_WAVES : 0;
   s.parts_at = (2 * x.tokens * x.heads * (int64_t)sizeof(RowParts) + 15) / 16 * 16;
   s.bytes = s.parts_at + s.blocks() * part_floats(x.hd) * 4;
   return s;
@@ -1241,10 +1246,19 @@ Sizes sizes_of(const PrefixAttnShape& x) {
 
 int64_t prefix_attn_workspace(const PrefixAttnShape& x) { return sizes_of(x).bytes; }
 
-int64_t prefix_attn_steps(const PrefixAttnShape& x, int64_t keys) {
+bool prefix_attn_fits(const PrefixAttnShape& x, int64_t own_keys, int64_t prefix_keys) {
   const Sizes s = sizes_of(x);
-  return std::max({s.wide * 14 * ((keys + WIDE_KEYS - 1) / WIDE_KEYS + 6), s.narrow * ((keys + NARROW_KEYS - 1) / NARROW_KEYS + 4),
-                   s.blocks()});  // (14: the largest step)
+  // A tile's steps are those of the longest row of its table.  The slots past the tiles',
+  // one a worker, count as tiles of the longest: of tables up to some 2^24 keys that is
+  // little, and longer ones it leaves to few calls.
+  auto steps = [&](const Tally& n, int64_t slots, int64_t keys, int64_t start) {
+    auto of = [&](int64_t k) { return (k + keys - 1) / keys + start; };
+    return n.own * of(own_keys) + n.shared * of(prefix_keys) + (slots - n.all()) * of(std::max(own_keys, prefix_keys));
+  };
+  constexpr int64_t MOST = ((int64_t)1 << 31) - 1;
+  return steps(s.wide_tiles, s.wide, WIDE_KEYS, WIDE_START) <= MOST &&
+         steps(s.narrow_tiles, s.narrow, NARROW_KEYS, NARROW_START) <= MOST && s.blocks() <= MOST &&
+         s.bytes < (int64_t)1 << 39;  // (no card has that; 264 bytes a row and more leave rows 32 bits)
 }
 
 template <typename T, int HD>

@@ -552,9 +552,9 @@ struct PrefixAttnShape {
   int seqs, groups, heads, kv_heads, hd;
   const int32_t *h_cu, *h_groups;
 };
-// upper bound of the steps of work that rows of ``keys`` keys can make, and of the numbers
-// of its parts
-int64_t prefix_attn_steps(const PrefixAttnShape& x, int64_t keys);
+// whether 32 bits number the steps of work of tables whose rows list that many keys, and its
+// parts
+bool prefix_attn_fits(const PrefixAttnShape& x, int64_t own_keys, int64_t prefix_keys);
 int64_t prefix_attn_workspace(const PrefixAttnShape& x);
 template <typename T>
 void launch_prefix_attn(const PrefixAttnArgs<T>& a, const PrefixAttnShape& x, void* workspace, hipStream_t s);

@@ -377,6 +377,31 @@ def test_more_tokens_than_a_grid_dimension_has_threads():
     assert torch.equal(out[ends], few) and not out[100:n].any()
 
 
+def test_as_many_sequences_as_are_taken_with_long_tables():
+    """4096 tokens of 40 heads a kv head, tables of 2^18 keys that list few, against the same
+    64 at a time.  Each is off by (2 eps + 2 u) max |v| at most, eps as in Paged.attention."""
+    n, kv, G, hd, columns = 4096, 8, 40, 64, (1 << 18) // 16
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q = torch.randn((n, kv * G, hd), generator=g, device="cuda")
+    kc, vc = (torch.randn((n + 9, kv, 16, hd), generator=g, device="cuda") for _ in range(2))
+    lens = torch.randint(0, 16, (n,), generator=g, device="cuda", dtype=torch.int32)
+    table = torch.full((n, columns), -1, dtype=torch.int32, device="cuda")
+    table[:, 0] = torch.arange(9, n + 9, device="cuda")
+    prefix = torch.full((1, columns), -1, dtype=torch.int32, device="cuda")
+    prefix[0, :9] = torch.arange(9, device="cuda")
+    plens = torch.tensor([135], dtype=torch.int32, device="cuda")
+    got = ops.prefix_attention(q, kc, vc, table, lens, prefix_table=prefix, prefix_lens=plens)
+    keys = torch.cat([kc[:9].abs().amax((0, 2)), kc[9:].abs().amax((0, 2))]).amax(0)  # [hd]
+    score = float((q.abs() * keys).sum(2).max()) * hd ** -0.5
+    eps = 2 * (hd + 2) * U * score + (3 * 2 * score + 8) * U + (8 + 151) * U
+    bound = 2 * (2 * eps + 2 * U) * float(vc.abs().max())
+    for i in range(0, n, 64):
+        part = slice(i, i + 64)
+        want = ops.prefix_attention(q[part], kc, vc, table[part, :1].contiguous(), lens[part],
+                                    prefix_table=prefix[:, :9].contiguous(), prefix_lens=plens)
+        assert float((got[part] - want).abs().max()) <= bound, i
+
+
 def test_same_bits_again():
     for dtype in (F, B):
         p = Paged([(2000, [(300, 1), (3, 1)]), (70, [(9, 20)])], 8, 2, 128, dtype)

@@ -170,6 +170,49 @@ def test_sample_refusals(change, code, text):
     refused(ax.lib().axon_sample_tokens(*{**SAMPLE, **change}.values()), code, text)
 
 
+def large_call(tokens, heads, kv, hd, keys, groups=0, cu=None, page=16, prefix_keys=None):
+    """(workspace, the refusal of a call with no workspace): ``groups`` even groups of the sequences"""
+    seqs = tokens if cu is None else len(cu) - 1
+    host = None if cu is None else ints(*cu)
+    pages = ax.AxonKvPages(P, 2 * P, B, kv, hd, page, 1 << 20)
+    batch = ax.AxonKvBatch(seqs, -(-keys // page), None if cu is None else P, host, P, P)
+    sums = ints(*(i * seqs // max(groups, 1) for i in range(groups + 1)))
+    shared = ax.AxonKvPrefix(groups, -(-(prefix_keys or keys) // page), P, sums, P, P) if groups else None
+    L = ax.lib()
+    need = L.axon_prefix_attention_workspace(pages, batch, shared, tokens, heads)
+    with pytest.raises(ax.AxonError) as e:
+        ax._check(L.axon_prefix_attention(pages, batch, shared, tokens, heads, P, heads * hd, 1.0, P, heads * hd, None,
+                                          None, BIG, None))
+    return need, e.value
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads", [8, 128, 256, 320, 512, 4096])
+@pytest.mark.parametrize("groups", [0, 1, 100, 4096])
+def test_the_documented_sizes_are_taken(groups, heads, hd):
+    """4096 single tokens of any heads over 8 kv heads and tables of 2^18 keys."""
+    need, e = large_call(4096, heads, 8, hd, 1 << 18, groups)
+    assert 0 < need < 1 << 39 and e.code == ax.AXON_E_INVALID and "workspace is NULL" in str(e)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("groups", [0, 1])
+def test_a_long_prompt_is_taken(groups, hd):
+    need, e = large_call(200000, 64, 8, hd, 200000, groups, cu=[0, 200000], prefix_keys=1 << 20)
+    assert 0 < need < 1 << 39 and e.code == ax.AXON_E_INVALID and "workspace is NULL" in str(e)
+    # many rows over short tables, few over a long one
+    need, e = large_call(4096, 64, 8, hd, 64, 1, prefix_keys=1 << 23)
+    assert need > 0 and e.code == ax.AXON_E_INVALID and "workspace is NULL" in str(e)
+
+
+def test_a_call_too_large_is_refused_before_its_workspace():
+    for call in (dict(tokens=6, heads=4, kv=2, hd=64, keys=1 << 30, cu=[0, 2, 2, 6]),
+                 dict(tokens=4096, heads=1024, kv=1024, hd=64, keys=1 << 20),
+                 dict(tokens=1 << 30, heads=4096, kv=1024, hd=128, keys=1 << 16, cu=[0, 1 << 30])):
+        need, e = large_call(**call)
+        assert need == 0 and e.code == ax.AXON_E_CAPACITY and "too many for one call" in str(e), call
+
+
 def test_binding_refuses_what_it_cannot_hand_over():
     x = torch.zeros(4, 8)
     i = torch.zeros(4, 1, dtype=torch.int32)
