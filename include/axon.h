@@ -477,11 +477,12 @@ int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch* batch, int
  * head h reads kv head h / (heads / kv_heads).  Each prefix is read once for all of its
  * sequences.  A token with no key has out 0.  d_lse: float [tokens][heads], the logarithm
  * of the sum of exp(scale q k) (-inf: no key), or NULL.  What the cache holds at masked
- * places (behind the last key, later tokens) is not used, whatever it is.  prefix may be
- * NULL.  AXON_E_CAPACITY where 32 bits do not number the rows' blocks of keys that their
- * tables could list: not for 4096 single tokens of any heads over 8 kv heads and tables of
- * 2^18 keys, in any groups, nor for a prompt of 200000 tokens of 64 heads over 8 whose
- * table lists them.  The workspace of a call that is refused is 0. */
+ * places (behind the last key, later tokens) is not used, whatever it is.  Weights of 1 at
+ * most times values are summed in float32: |v| up to 3e38 / keys does not overflow.  prefix
+ * may be NULL.  AXON_E_CAPACITY where 32 bits do not number the rows' blocks of keys that
+ * their tables could list: not for 4096 single tokens of any heads over 8 kv heads and
+ * tables of 2^18 keys, in any groups, nor for a prompt of 200000 tokens of 64 heads over 8
+ * whose table lists them.  The workspace of a call that is refused is 0. */
 int64_t axon_prefix_attention_workspace(const axon_kv_pages* pages, const axon_kv_batch* batch,
                                         const axon_kv_prefix* prefix, int64_t tokens, int32_t heads);
 int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_batch* batch, const axon_kv_prefix* prefix,

@@ -502,13 +502,14 @@ AXON_DEV const T* q_row(const PrefixAttnArgs<T>& a, const Segment& g, int G, int
   return a.q + (int64_t)(g.tok0 + r / G) * a.ldq + (int64_t)(kvh * G + r % G) * HD;
 }
 
-// The reference m of a row's weights 2^(score - m): the running maximum (in base 2, times
-// the scale), or up to 8 less, so that the sum and the products are hardly rescaled after
-// the first keys (a weight is 256 at most).
+// The reference m of a row's weights 2^(score - m): where the maximum (in base 2, times the
+// scale) passes it, it goes 8 above it, so that the sum and the products are hardly rescaled
+// after the first keys.  A weight is 1 at most: what is summed leaves float32's range no
+// earlier than with the maximum itself for a reference.
 template <int N, typename V>
 AXON_DEV void raise(float& m, float top, float& l, V (&o)[N]) {
-  if (!__any(top > m + 8.f)) return;
-  const float m_new = fmaxf(m, top);
+  if (!__any(top > m)) return;
+  const float m_new = top > m ? top + 8.f : m;
   const float fall = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - m_new);
   m = m_new;
   l *= fall;

@@ -309,6 +309,33 @@ def test_attention_many_tiles_in_a_row(seqs, heads, hd, spread, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F, B])
+@pytest.mark.parametrize("size", [2e36, 2.0 ** -122])
+@pytest.mark.parametrize("growth", [7.9, 0.0])
+@pytest.mark.parametrize("groups,heads,kv,hd", [
+    ([(150, [(20, 1)] * 5)], 8, 2, 64),           # 20 rows
+    ([(150, [(3, 1)] * 40)], 8, 1, 128),          # 320
+    ([(0, [(99, 1), (140, 1)])], 8, 2, 128),      # 4, a wavefront's
+    ([(0, [(99, 1), (140, 1)])], 8, 2, 64),
+    ([(70, [(90, 60), (5, 1)])], 4, 2, 64),       # many new tokens
+])
+def test_attention_values_near_the_ends_of_the_range(groups, heads, kv, hd, growth, size, dtype):
+    """Large and small finite values, and scores that grow along the keys by less than 8 (in
+    base 2) or not at all: sums of weights and values stay in range where weights of 1 at most
+    do."""
+    p = Paged(groups, heads, kv, hd, dtype)
+    p.q.zero_()
+    p.q[..., 0] = 1
+    for table, lens in ((p.table, [a + b for a, b in zip(p.past, p.new)]), (p.prefix_table, p.prefix)):
+        for row, n in zip(table.cpu().tolist(), lens):
+            for j in range(n):
+                at = (row[j // p.page], slice(None), j % p.page)
+                p.k_cache[at] = 0
+                p.k_cache[(*at, 0)] = growth * j / n
+                p.v_cache[at] = size * (1 + torch.rand((kv, hd), generator=torch.Generator().manual_seed(j))).to(dtype).cuda()
+    check_attention(p, scale=math.log(2))
+
+
+@pytest.mark.parametrize("dtype", [F, B])
 def test_attention_more_sequences_than_threads(dtype):
     """Several segments to a thread of the plan; groups of none, sequences that take no part."""
     g = torch.Generator().manual_seed(3)
