@@ -461,8 +461,8 @@ typedef struct {
  * [tokens][kv_heads][head_dim], of the cache's type; q_out as q (it may be q).  Key j of
  * sequence b is at position p = d_offsets[b] + j (NULL: j; with a shared prefix, its
  * length).  The pair (x, y) of dimension i becomes
- *   scale (x cos a - y sin a, y cos a + x sin a),  a = p d_inv_freq[i] (float64, product
- * and reduction as well), i < rot / 2; a pair is the dimensions (i, rot / 2 + i), or
+ *   scale (x cos a - y sin a, y cos a + x sin a),  a = p d_inv_freq[i] (rounded to float64,
+ * reduced without a further loss), i < rot / 2; a pair is the dimensions (i, rot / 2 + i), or
  * (2 i, 2 i + 1) with interleaved == 1; those from ``rot`` (even, 0..head_dim) on stay
  * as they are.  Any long-context scaling is a choice of d_inv_freq and scale.  No two
  * tokens may go to one place in the cache. */

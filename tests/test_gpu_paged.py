@@ -1,6 +1,7 @@
 """Rotating and appending to a paged cache, and attention over it with shared
 prefixes, on the GPU against float64."""
 import math
+from fractions import Fraction
 
 import pytest
 import torch
@@ -101,6 +102,31 @@ def test_append(groups, heads, kv, hd, rot, interleaved, dtype):
 def test_append_far_positions_pages_and_scale(page, dtype):
     p = Paged(RAGGED, 8, 2, 64, dtype, page=page)
     check_append(p, 64, scale=1.3, offsets=[0, 1 << 20, 2000000000, 999999, 2147483647, 5], theta=500000.0, fused=True)
+
+
+@pytest.mark.parametrize("rot", [2, 64])
+def test_append_reduces_far_angles(rot):
+    """Far positions that are close to whole turns (numerators of 2 pi's continued fraction, and
+    their neighbours): the small angle that is left has all its digits.  The bound is that of
+    check_append, of the cosine and the sine each by itself (one of the two products is 0)."""
+    pi = Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899")
+    near = [710, 103993, 312689, 4272943, 10838702, 80143857, 411557987, 2137933792, 2147483647]
+    near = near + [n - 1 for n in near] + [3 * 411557987, 26 * 80143857]
+    left = []
+    for n in near:
+        turns = Fraction(n) / (2 * pi)
+        left.append(float((turns - round(turns)) * 2 * pi))
+    n = len(near)
+    k = torch.zeros((n, 1, 64), device="cuda")
+    k[..., :rot // 2] = 1
+    kc, vc = (torch.zeros((n, 1, 16, 64), device="cuda") for _ in range(2))
+    table, lens = torch.arange(n, dtype=torch.int32, device="cuda")[:, None], torch.zeros(n, dtype=torch.int32, device="cuda")
+    inv = torch.ones(rot // 2, dtype=torch.float64, device="cuda")
+    ops.rope_append(None, k, k, kc, vc, table, lens, inv, offsets=torch.tensor(near, dtype=torch.int32, device="cuda"))
+    left = torch.tensor(left, dtype=torch.float64)[:, None].expand(-1, rot // 2)
+    for i, f in ((0, torch.cos), (rot // 2, torch.sin)):
+        want = f(left)
+        check(kc[:, 0, 0, i:i + rot // 2], want, 11 * U * want.abs(), f.__name__)
 
 
 def test_append_strides_in_place_and_without_queries():
