@@ -598,9 +598,9 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
     (axon_prefix_attention).  Cache, block_table, lens and cu_seqlens as the
     :func:`rope_append` before it took them.  prefix_table int32 [groups, pages] and
     prefix_lens int32 [groups]; cu_groups a host list of prefix sums of the groups'
-    sequences (None: one group of all; groups_device its device copy).  scale: 1 /
-    sqrt(head dim) by default; ``out`` may be q.  Returns out, with want_lse (out,
-    logarithms of the sums, float32 [tokens, heads])."""
+    sequences (None: one group of all; groups_device its device copy, which a captured call
+    with cu_groups needs).  scale: 1 / sqrt(head dim) by default; ``out`` may be q.  Returns
+    out, with want_lse (out, logarithms of the sums, float32 [tokens, heads])."""
     pages = _pages_arg(k_cache, v_cache)
     hd, dtype = pages.head_dim, k_cache.dtype
     qv, ldq = _head_rows(q, None, hd, dtype, "q")
@@ -615,6 +615,8 @@ def prefix_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tens
             if groups != 1:
                 raise ValueError("several groups need cu_groups")
             cu_groups = [0, batch.seqs]
+            if groups_device is None and batch.seqs:  # (filled on the device: no capture takes a copy from the host)
+                groups_device = torch.arange(0, batch.seqs + 1, batch.seqs, dtype=torch.int32, device=q.device)
         host, cu = _sums(cu_groups, groups_device, groups, "cu_groups", q)
         prefix = AxonKvPrefix(groups, columns, cu.data_ptr(), host, plens.data_ptr(), table.data_ptr())
         keep = (keep, table, plens, cu)

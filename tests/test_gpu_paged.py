@@ -518,6 +518,28 @@ def test_captured_decode_step_follows_its_lengths():
         lens += 1
 
 
+def test_captured_call_of_one_group_without_its_sums():
+    p = Paged([(70, [(13, 1), (0, 1), (31, 1)])], 8, 2, 64, B)
+    kw = dict(prefix_table=p.prefix_table, prefix_lens=p.prefix_lens)
+    step = lambda: ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, **kw)  # noqa: E731
+    assert torch.equal(step(), ops.prefix_attention(p.q, p.k_cache, p.v_cache, p.table, p.lens, cu_groups=[0, 3], **kw))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(4):
+        p.q.copy_(torch.randn_like(p.q, dtype=F))
+        p.prefix_lens.fill_(70 - 9 * i)
+        graph.replay()
+        want = step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want), i
+
+
 def test_a_buffer_counts_as_modified():
     p = Paged(ONE, 4, 2, 64, F)
     versions = [t._version for t in (p.k_cache, p.v_cache, p.q)]
