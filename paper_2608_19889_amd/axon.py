@@ -637,6 +637,8 @@ def _setting(value, rows: int, dtype, name: str):
     """(an array over the rows or None, the number for all of them)"""
     if isinstance(value, torch.Tensor):
         return _vector(value, rows, dtype, name), 0
+    if dtype == torch.int32:  # (of a longer number ctypes would hand over the low 32 bits)
+        value = max(-(1 << 31), min(value, (1 << 31) - 1))
     return None, value
 
 

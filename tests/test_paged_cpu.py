@@ -260,6 +260,17 @@ def test_binding_layouts(monkeypatch):
         ax._setting(torch.zeros(4), 4, torch.int32, "top_k")
 
 
+@pytest.mark.parametrize("k,taken", [(0, 0), (7, 7), ((1 << 31) - 1, (1 << 31) - 1), (1 << 31, (1 << 31) - 1),
+                                     ((1 << 32) + 5, (1 << 31) - 1), ((1 << 63) - 1, (1 << 31) - 1),
+                                     (-1, -1), (-(1 << 32), -(1 << 31)), (5 - (1 << 32), -(1 << 31))])
+def test_top_k_past_32_bits_keeps_its_meaning(k, taken):
+    """All are kept, or the call refused: not the number that the low 32 bits make."""
+    assert ax._setting(k, 4, torch.int32, "top_k") == (None, taken)
+    if k < 0:
+        call = {**SAMPLE, "k": ax._setting(k, 4, torch.int32, "top_k")[1]}
+        refused(ax.lib().axon_sample_tokens(*call.values()), ax.AXON_E_INVALID, "top_k must be >= 0")
+
+
 def test_structures_match_the_c_compiler(tmp_path):
     names = {"axon_kv_pages": ax.AxonKvPages, "axon_kv_batch": ax.AxonKvBatch, "axon_kv_prefix": ax.AxonKvPrefix}
     lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "axon.h"', "int main(void) {"]
