@@ -474,8 +474,8 @@ int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch* batch, int
 /* Attention of the new tokens (their keys and values are in the cache): out [tokens]
  * [heads][head_dim] (of the cache's type; it may be q) is the softmax of scale q k over
  * the group's prefix and the sequence's own keys up to the token itself, times v; query
- * head h reads kv head h / (heads / kv_heads).  Each prefix is read once for all of its
- * sequences.  A token with no key has out 0.  d_lse: float [tokens][heads], the logarithm
+ * head h reads kv head h / (heads / kv_heads).  A prefix is read once for 256 rows (tokens
+ * times heads / kv_heads) of its sequences.  A token with no key has out 0.  d_lse: float [tokens][heads], the logarithm
  * of the sum of exp(scale q k) (-inf: no key), or NULL.  What the cache holds at masked
  * places (behind the last key, later tokens) is not used, whatever it is.  Weights of 1 at
  * most times values are summed in float32: |v| up to 3e38 / keys does not overflow.  prefix

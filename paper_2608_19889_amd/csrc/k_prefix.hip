@@ -5,7 +5,7 @@
 // A *segment* is a list of keys and the tokens that read it: a group's prefix with the
 // tokens of all of its sequences, or a sequence's own keys with its own tokens.  The
 // rows of a segment and kv head are its tokens' query heads of that kv head, so a
-// prefix is multiplied with everything that shares it.  Rows go in tiles: a segment of
+// prefix is read once for 256 rows of what shares it.  Rows go in tiles: a segment of
 // at most 16 rows is one *narrow* tile (a single token's own keys), any other is cut
 // into *wide* ones of 256 rows.  A workgroup works on tiles of one kind:
 //   wide    its 8 wavefronts take 32 rows each, over keys that all of them read from LDS
@@ -20,13 +20,15 @@
 // of a tile in its run it leaves (max, sum, product).  What is added to what depends on
 // the lengths alone: the same bits every time.
 //
-// Measured (bf16 but for the first; us with the join): 4 answers to 300 keys 14, of which
-// the two launches' chains of dependent loads are all; 64 of 28 heads over 4 to 4096 keys
-// and 600 of their own 38 (83 MB); 256 of 32 over 8 to 16 prompts of 1100 66 (195 MB, 2.9
-// TB/s); 48 of 40 over 8 to 50011 keys 108 (376 MB and 50 GFLOP: 3.5 TB/s, 463 TFLOP/s);
-// 20 questions of 150 tokens of 28 over 4 behind 2500 keys 227 (110 GFLOP; 190 of tiles, a
-// unit of 256 rows and 64 keys 2.2 against 0.9 of matrix instructions alone, and 130 MB of
-// parts written and read again).
+// Measured (bf16 but for the first; us a call, back to back, with the join): 4 answers to
+// 300 keys 16, of which the two launches' chains of dependent loads are 14; 64 of 28 heads
+// over 4 to 4096 keys and 600 of their own 36 (83 MB); 256 of 32 over 8 to 16 prompts of
+// 1100 66 (195 MB, 3.0 TB/s); 48 of 40 over 8 to 50011 keys 107 (376 MB and 50 GFLOP: 3.5
+// TB/s, 470 TFLOP/s); 20 questions of 150 tokens of 28 over 4 behind 2500 keys 201 (110
+// GFLOP; a unit of 256 rows and 64 keys 2.2 against 0.9 of matrix instructions alone, and 130
+// MB of parts written and read again; under the profiler the two kernels add up to 228).
+// In float32 a wide unit's matrix instructions take 16 times as long, and WEIGHT below is
+// bf16's: 64 answers of 9 over 3 to 4096 keys 49, of 28 over 4 of 128 dimensions 192.
 #include <algorithm>
 #include <type_traits>
 
