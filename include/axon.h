@@ -427,14 +427,14 @@ typedef struct {
 
 /* The sequences of a call, 1..4096.  Sequence b's new tokens are rows cu_seqlens[b] ..
  * cu_seqlens[b + 1] - 1 of the call's tensors (prefix sums from 0, [seqs + 1]; the host
- * copy is what is checked), or row b when both are NULL.  Rows behind the last
- * sequence's (a batch padded to a fixed size) are neither read nor written.  d_lens[b]
- * keys of the sequence were in the cache before the call; the new ones follow as its
- * keys d_lens[b], d_lens[b] + 1, ...  d_lens[b] < 0: the sequence takes no part
- * (nothing of it is stored, its attention is 0).  Key j is in page d_block_table[b]
- * [j / page_size]; an entry outside [0, num_pages), and what is past the row's
- * table_stride pages, is no page: what would go there is not stored, and keys there are
- * masked out. */
+ * copy is what is checked, the device's holds the same numbers, at a captured call's
+ * replays too), or row b when both are NULL.  Rows behind the last sequence's (a batch
+ * padded to a fixed size) are neither read nor written.  d_lens[b] keys of the sequence
+ * were in the cache before the call; the new ones follow as its keys d_lens[b],
+ * d_lens[b] + 1, ...  d_lens[b] < 0: the sequence takes no part (nothing of it is stored,
+ * its attention is 0).  Key j is in page d_block_table[b][j / page_size]; an entry outside
+ * [0, num_pages), and what is past the row's table_stride pages, is no page: what would go
+ * there is not stored, and keys there are masked out. */
 typedef struct {
   int32_t seqs;
   int32_t table_stride;
@@ -445,8 +445,9 @@ typedef struct {
 } axon_kv_batch;
 
 /* Shared prefixes, 0..4096: the sequences cu_groups[g] .. cu_groups[g + 1] - 1 (prefix
- * sums from 0, [groups + 1], up to seqs) all have the first d_prefix_lens[g] keys of the
- * pages d_prefix_table[g] before their own.  Sequences past the last group have none. */
+ * sums from 0, [groups + 1], up to seqs, the same numbers on both sides) all have the first
+ * d_prefix_lens[g] keys of the pages d_prefix_table[g] before their own.  Sequences past the
+ * last group have none. */
 typedef struct {
   int32_t groups;
   int32_t table_stride;
