@@ -463,9 +463,9 @@ typedef struct {
  * sequence b is at position p = d_offsets[b] + j (NULL: j; with a shared prefix, its
  * length).  The pair (x, y) of dimension i becomes
  *   scale (x cos a - y sin a, y cos a + x sin a),  a = p d_inv_freq[i] (rounded to float64,
- * reduced without a further loss), i < rot / 2; a pair is the dimensions (i, rot / 2 + i), or
- * (2 i, 2 i + 1) with interleaved == 1; those from ``rot`` (even, 0..head_dim) on stay
- * as they are.  Any long-context scaling is a choice of d_inv_freq and scale.  No two
+ * reduced without a further loss), i < rot / 2; a pair is the dimensions (i, rot / 2 + i),
+ * or (2 i, 2 i + 1) with interleaved == 1; those from ``rot`` (even, 0..head_dim) on stay as
+ * they are.  Any long-context scaling is a choice of d_inv_freq and scale.  No two
  * tokens may go to one place in the cache. */
 int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch* batch, int64_t tokens, int32_t heads,
                      const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, void* q_out,
@@ -476,14 +476,15 @@ int axon_rope_append(const axon_kv_pages* pages, const axon_kv_batch* batch, int
  * [heads][head_dim] (of the cache's type; it may be q) is the softmax of scale q k over
  * the group's prefix and the sequence's own keys up to the token itself, times v; query
  * head h reads kv head h / (heads / kv_heads).  A prefix is read once for 256 rows (tokens
- * times heads / kv_heads) of its sequences.  A token with no key has out 0.  d_lse: float [tokens][heads], the logarithm
- * of the sum of exp(scale q k) (-inf: no key), or NULL.  What the cache holds at masked
- * places (behind the last key, later tokens) is not used, whatever it is.  Weights of 1 at
- * most times values are summed in float32: |v| up to 3e38 / keys does not overflow.  prefix
- * may be NULL.  AXON_E_CAPACITY where 32 bits do not number the rows' blocks of keys that
- * their tables could list: not for 4096 single tokens of any heads over 8 kv heads and
- * tables of 2^18 keys, in any groups, nor for a prompt of 200000 tokens of 64 heads over 8
- * whose table lists them.  The workspace of a call that is refused is 0. */
+ * times heads / kv_heads) of its sequences.  A token with no key has out 0.  d_lse: float
+ * [tokens][heads], the logarithm of the sum of exp(scale q k) (-inf: no key), or NULL.
+ * What the cache holds at masked places (behind the last key, later tokens) is not used,
+ * whatever it is.  Weights of 1 at most times values are summed in float32: |v| up to 3e38 /
+ * keys does not overflow.  prefix may be NULL.  AXON_E_CAPACITY where 32 bits do not number
+ * the rows' blocks of keys that their tables could list: not for 4096 single tokens of any
+ * heads over 8 kv heads and tables of 2^18 keys, in any groups, nor for a prompt of 200000
+ * tokens of 64 heads over 8 whose table lists them.  The workspace of a call that is refused
+ * is 0. */
 int64_t axon_prefix_attention_workspace(const axon_kv_pages* pages, const axon_kv_batch* batch,
                                         const axon_kv_prefix* prefix, int64_t tokens, int32_t heads);
 int axon_prefix_attention(const axon_kv_pages* pages, const axon_kv_batch* batch, const axon_kv_prefix* prefix,
